@@ -226,6 +226,93 @@ KEYDIFF_API int keydiff_prefill_block_layers_rope(keydiff_cache_t *const *caches
                                       const float *cos_table, const float *sin_table, int64_t table_rows,
                                       void *const *out, void *stream);
 
+/* The block step of a model that norms its queries and keys for each head before the rotation (step (1) of Fig. 1 again): the
+ * same launch ahead of the step's own norms and rotates, in one pass over the block.
+ *   u_i = x_i w_i / sqrt(mean_j x_j^2 + norm_eps)      over the head_dim values of a row; then the rotation above on u, all in
+ *                                                      float, every product and sum rounded on its own, the result once to bf16
+ *   q_weight, k_weight        device, bf16 [head_dim] for all heads (stride 0) or [heads][head_dim] with a stride in elements, a
+ *                             multiple of 8; 16-byte aligned.  Both null: no norm
+ *   cos_table, sin_table      as above.  Both null: no rotation (table_rows is not used then)
+ * A step needs one of the two at least.  `_layers`: `form` is an array, one entry per layer.                         */
+typedef struct {
+    const void *q_weight, *k_weight;
+    int64_t q_weight_stride, k_weight_stride;
+    float norm_eps;
+    const float *cos_table, *sin_table;
+    int64_t table_rows;
+} keydiff_row_form_t;
+KEYDIFF_API int keydiff_prefill_block_norm_rope(keydiff_cache_t *cache, const void *q, const void *k_new, const void *v_new,
+                               int32_t Bt, int64_t pos0, const keydiff_row_form_t *form, void *out, float *scores_out,
+                               void *stream);
+KEYDIFF_API int keydiff_prefill_block_layers_norm_rope(keydiff_cache_t *const *caches, int32_t n_layers, const void *const *q,
+                                      const void *const *k_new, const void *const *v_new, int32_t Bt, int64_t pos0,
+                                      const keydiff_row_form_t *form, void *const *out, void *stream);
+
+/* Rows of bf16 tensors as a projection leaves them: the row of (sequence, head, token) is the head_dim contiguous values at
+ * data + sequence * seq_stride + head * head_stride + token * token_stride (elements; data 16-byte aligned, strides multiples
+ * of 8 and not negative).  Views into one fused projection's output are such rows.                                      */
+typedef struct {
+    const void *data;
+    int64_t seq_stride, head_stride, token_stride;
+} keydiff_rows_t;
+
+/* Norms and rotation alone: the rows of q (n_q_heads) and k (n_kv_heads) of Bt tokens of `batch` sequences, to q_out
+ * [batch][n_q_heads][Bt][head_dim] and k_out [batch][n_kv_heads][Bt][head_dim].  Token j of a sequence is at position pos0 + j
+ * or, where `positions` (device int32 [batch][Bt]) is not null, at its entry there; a token whose entry lies outside the tables
+ * is left out, its rows in q_out and k_out stay as they are.  The outputs must not overlap the inputs.                    */
+KEYDIFF_API int keydiff_norm_rope(const keydiff_rows_t *q, const keydiff_rows_t *k, int32_t batch, int32_t n_q_heads,
+                      int32_t n_kv_heads, int32_t head_dim, int32_t Bt, int64_t pos0, const int32_t *positions,
+                      const keydiff_row_form_t *form, void *q_out, void *k_out, void *stream);
+
+/* Several continuations of one prompt (samples, beams, drafts).  Every sequence that continues a prompt has rows of its own in
+ * pages of a pool; the prompt's rows, those of a KeyDiff cache, are shared and not copied.
+ *   k_pages, v_pages  device, bf16 [n_pages][n_kv_heads][page_rows][head_dim]; page_rows a power of two, 8 to 1024
+ *   table             device int32 [n_seqs][table_width]: row r of sequence s lies in row r % page_rows of page
+ *                     table[s][r / page_rows].  Sequences may share pages that none of them appends to
+ *   lens              device int32 [n_seqs]: rows the sequence holds before this step; negative: the sequence is not in use, and
+ *                     nothing of it is read or written
+ *   n_new             device int32 [n_seqs], nullable: how many of the Bt tokens of a step the sequence takes (null: all); rows of
+ *                     outputs behind them stay as they are
+ * table, lens and n_new are read by the kernels, so a captured step may be replayed with other contents.  What a kernel
+ * finds there is checked: a page outside the pool, or a row outside the table, is neither read nor written, and
+ * its keys count as absent.                                                                                               */
+typedef struct {
+    void *k_pages, *v_pages;
+    const int32_t *table, *lens, *n_new;
+    int32_t n_seqs, n_q_heads, n_kv_heads, head_dim;
+    int32_t page_rows, n_pages, table_width;
+} keydiff_branches_t;
+
+/* Append (Eq. 5 for the continuations): token j of sequence s becomes row lens[s] + j of the sequence, at position
+ * pos0[s] + lens[s] + j (pos0: device int32 [n_seqs], null: zeros; the position of a sequence's first own row: the length
+ * of its prompt).  `form` (nullable: rows are taken as they are) norms and rotates queries and keys on the way;
+ * the queries are written to q_out [n_seqs][n_q_heads][Bt][head_dim] for keydiff_branch_attention (q and q_out null:
+ * keys and values only).  lens is not changed: all layers of a step read the same lengths, and the caller advances them
+ * behind the last one.  A token at a position outside the tables is left out.                                         */
+KEYDIFF_API int keydiff_branch_append(const keydiff_branches_t *b, const keydiff_rows_t *q, const keydiff_rows_t *k,
+                          const keydiff_rows_t *v, int32_t Bt, const int32_t *pos0, const keydiff_row_form_t *form,
+                          void *q_out, void *stream);
+
+/* Attention of the appended tokens (Eq. 2): the query of token j of sequence s sees the prefix_len rows of prompt
+ * s / (n_seqs / n_prefixes) and the sequence's own rows 0 .. lens[s] + j.
+ *   k_prefix, v_prefix  device, bf16 [n_prefixes][n_kv_heads][prefix_cap][head_dim]; null with n_prefixes 0: own rows alone
+ *   n_prefixes          must divide n_seqs; sequences of one prompt follow one another
+ *   softmax_scale       <= 0 selects 1/sqrt(head_dim)
+ *   out                 [n_seqs][n_q_heads][Bt][head_dim]; a query that sees no key (every page absent) gets zeros
+ *   workspace           device, 256-byte aligned, of at least keydiff_branch_workspace_bytes; carries nothing between calls.
+ *                       Calls that may overlap need workspaces of their own
+ * The prompt's rows are read once for all sequences that share them.  Sums and softmax statistics are kept in float.
+ * Inputs must be finite (those of rows that a query sees, and those of rows seen by another token of the same step).   */
+KEYDIFF_API int keydiff_branch_workspace_bytes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, size_t *bytes);
+KEYDIFF_API int keydiff_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt,
+                             const void *k_prefix, const void *v_prefix, int32_t n_prefixes, int32_t prefix_len,
+                             int64_t prefix_cap, float softmax_scale, void *out, void *workspace, size_t workspace_bytes,
+                             void *stream);
+/* ... with the rows and the softmax scale of a KeyDiff cache: prompt i is sequence i of the cache's batch, and the rows are those it
+ * holds when the call is made (a pending eviction is enqueued first).  The cache is not changed.                         */
+KEYDIFF_API int keydiff_cache_branch_attention(keydiff_cache_t *prompt, const keydiff_branches_t *b, const keydiff_rows_t *q,
+                                   int32_t Bt, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Enqueue the pending eviction of `cache` on `stream`, if it has one (else a no-op). */
 KEYDIFF_API int keydiff_finish(keydiff_cache_t *cache, void *stream);
 

@@ -13,6 +13,10 @@ from .binding import (  # noqa: F401
     KeyDiffCache,
     KeyDiffConfig,
     KeyDiffError,
+    branch_append,
+    branch_attention,
+    branch_workspace_bytes,
     load_library,
+    norm_rope,
     prefill_block_layers,
 )

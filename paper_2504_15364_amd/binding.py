@@ -6,6 +6,7 @@ as the owner of device memory and streams.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 
@@ -21,6 +22,8 @@ EXPORTS = (
     "keydiff_workspace_bytes", "keydiff_init_cache", "keydiff_prefill_block", "keydiff_prefill_block_static",
     "keydiff_prefill_block_deferred",
     "keydiff_prefill_block_layers", "keydiff_prefill_block_rope", "keydiff_prefill_block_layers_rope", "keydiff_finish", "keydiff_decode_step",
+    "keydiff_prefill_block_norm_rope", "keydiff_prefill_block_layers_norm_rope", "keydiff_norm_rope", "keydiff_branch_append",
+    "keydiff_branch_workspace_bytes", "keydiff_branch_attention", "keydiff_cache_branch_attention",
     "keydiff_scores", "keydiff_cache_len", "keydiff_cache_plan", "keydiff_cache_positions", "keydiff_cache_load",
     "keydiff_cache_status", "keydiff_profile_enable", "keydiff_profile_read", "keydiff_destroy_cache",
     "keydiff_last_error", "keydiff_version",
@@ -37,6 +40,21 @@ class _Config(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "budget_N", "block_B",
                                          "anchor_mode", "window_W", "layout")] + \
                [("eps", C.c_float), ("softmax_scale", C.c_float)]
+
+
+class _RowForm(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("q_weight_stride", C.c_int64),
+                ("k_weight_stride", C.c_int64), ("norm_eps", C.c_float), ("cos_table", C.c_void_p),
+                ("sin_table", C.c_void_p), ("table_rows", C.c_int64)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("seq_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64)]
+
+
+class _Branches(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_pages", "v_pages", "table", "lens", "n_new")] + \
+               [(n, C.c_int32) for n in ("n_seqs", "n_q_heads", "n_kv_heads", "head_dim", "page_rows", "n_pages", "table_width")]
 
 
 @dataclass
@@ -81,6 +99,14 @@ def load_library() -> C.CDLL:
     L.keydiff_prefill_block_layers.argtypes = [pp, i32, pp, pp, pp, i32, i64, pp, vp]
     L.keydiff_prefill_block_rope.argtypes = [vp, vp, vp, vp, i32, i64, vp, vp, i64, vp, vp, vp]
     L.keydiff_prefill_block_layers_rope.argtypes = [pp, i32, pp, pp, pp, i32, i64, vp, vp, i64, pp, vp]
+    fp, rp, bp = C.POINTER(_RowForm), C.POINTER(_Rows), C.POINTER(_Branches)
+    L.keydiff_prefill_block_norm_rope.argtypes = [vp, vp, vp, vp, i32, i64, fp, vp, vp, vp]
+    L.keydiff_prefill_block_layers_norm_rope.argtypes = [pp, i32, pp, pp, pp, i32, i64, fp, pp, vp]
+    L.keydiff_norm_rope.argtypes = [rp, rp, i32, i32, i32, i32, i32, i64, vp, fp, vp, vp, vp]
+    L.keydiff_branch_append.argtypes = [bp, rp, rp, rp, i32, vp, fp, vp, vp]
+    L.keydiff_branch_workspace_bytes.argtypes = [bp, i32, i32, szp]
+    L.keydiff_branch_attention.argtypes = [bp, rp, i32, vp, vp, i32, i32, i64, C.c_float, vp, vp, C.c_size_t, vp]
+    L.keydiff_cache_branch_attention.argtypes = [vp, bp, rp, i32, vp, vp, C.c_size_t, vp]
     L.keydiff_finish.argtypes = [vp, vp]
     L.keydiff_decode_step.argtypes = [vp, vp, vp, vp, i64, vp, vp]
     L.keydiff_scores.argtypes = [vp, vp, vp]
@@ -169,12 +195,14 @@ def check_rope_tables(cfg, cos, sin):
         raise ValueError("cos and sin tables differ in shape")
 
 
-def prefill_block_layers(caches, q, k_new, v_new, pos0: int, out=None, stream=None, rope=None):
+def prefill_block_layers(caches, q, k_new, v_new, pos0: int, out=None, stream=None, rope=None, norm=None):
     """One block through the layers of a model: `caches`, `q`, `k_new`, `v_new` (and `out`) are
     sequences with one entry per layer.  Layers shaped alike share their launches; else every layer's eviction
     rides in the next layer's launch.
     rope = (cos, sin): float32 device tables [positions][head_dim / 2]; q and k_new are then rotated
-    inside the call (keydiff_prefill_block_layers_rope)."""
+    inside the call (keydiff_prefill_block_layers_rope).
+    norm = (q_weights, k_weights, eps): one bf16 weight tensor per layer each, [head_dim] or [heads][head_dim]; q and k_new are
+    then normed for each head inside the call, ahead of the rotation if there is one (keydiff_prefill_block_layers_norm_rope)."""
     import torch
     n = len(caches)
     assert n >= 1 and len(q) == len(k_new) == len(v_new) == n
@@ -191,6 +219,18 @@ def prefill_block_layers(caches, q, k_new, v_new, pos0: int, out=None, stream=No
         check_block_shapes(c.cfg, None, None, None, out=to, Bt=Bt)
     arr = lambda ptrs: (C.c_void_p * n)(*ptrs)
     L = caches[0]._L
+    if norm is not None:
+        q_weights, k_weights, eps = norm
+        if not len(q_weights) == len(k_weights) == n:
+            raise ValueError(f"norm needs one weight tensor per layer, got {len(q_weights)} and {len(k_weights)} for {n} layers")
+        cos, sin = rope if rope is not None else (None, None)
+        forms = (_RowForm * n)(*(_form(c.cfg.n_q_heads, c.cfg.n_kv_heads, c.cfg.head_dim, cos, sin, wq, wk, eps, c.device)
+                                 for c, wq, wk in zip(caches, q_weights, k_weights)))
+        _check(L.keydiff_prefill_block_layers_norm_rope(arr([c._h.value for c in caches]), n,
+                                                        arr([t.data_ptr() for t in q]), arr([t.data_ptr() for t in k_new]),
+                                                        arr([t.data_ptr() for t in v_new]), Bt, int(pos0), forms,
+                                                        arr([t.data_ptr() for t in out]), _stream_ptr(stream)))
+        return out
     if rope is not None:
         cos, sin = rope
         check_rope_tables(caches[0].cfg, cos, sin)
@@ -204,6 +244,235 @@ def prefill_block_layers(caches, q, k_new, v_new, pos0: int, out=None, stream=No
                                           arr([t.data_ptr() for t in q]), arr([t.data_ptr() for t in k_new]),
                                           arr([t.data_ptr() for t in v_new]), Bt, int(pos0),
                                           arr([t.data_ptr() for t in out]), _stream_ptr(stream)))
+    return out
+
+
+# ------------------------------------------------------------------ norms and rotation alone; continuations of a prompt
+def check_rows(name, t, shape):
+    """A tensor of rows [sequences][heads][tokens][head_dim]: bf16, the innermost dimension contiguous, other strides free (views into
+    a fused projection's output are fine)."""
+    import torch
+    if t.dtype is not torch.bfloat16 or t.shape != shape or t.stride(3) != 1:
+        raise ValueError(f"{name} must be a bf16 tensor of shape {tuple(shape)} with a contiguous last dimension, "
+                         f"got {tuple(t.shape)} {t.dtype}, strides {t.stride()}")
+
+
+def check_contiguous(name, t, shape, dtype):
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {tuple(t.shape)} {t.dtype}")
+
+
+def _check_devices(device, *tensors):
+    if device.type != "cuda":
+        raise ValueError(f"the tensors must live on a GPU, got {device}")
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"the tensors must live on one device, got {device} and {t.device}")
+
+
+def _rows(t):
+    n, h, b, _ = t.shape
+    s = t.stride()
+    return _Rows(t.data_ptr(), s[0] if n > 1 else 0, s[1] if h > 1 else 0, s[2] if b > 1 else 0)
+
+
+def _form(hq, hkv, d, cos, sin, q_weight, k_weight, eps, device=None):
+    """keydiff_row_form_t of norm weights ([d] or [heads][d] bf16, or None) and rotary tables (float32 [positions][d / 2], or None)."""
+    import torch
+    f = _RowForm(norm_eps=eps)
+    if (q_weight is None) != (k_weight is None) or (cos is None) != (sin is None):
+        raise ValueError("q_weight and k_weight, and cos and sin, are given together or not at all")
+    if q_weight is not None:
+        for name, w, heads in (("q_weight", q_weight, hq), ("k_weight", k_weight, hkv)):
+            if w.dtype is not torch.bfloat16 or w.shape not in ((d,), (heads, d)) or w.stride(-1) != 1:
+                raise ValueError(f"{name} must be a bf16 tensor of shape ({d},) or ({heads}, {d}), got {tuple(w.shape)} {w.dtype}")
+            if device is not None and w.device != device:
+                raise ValueError(f"{name} must live on {device}, got {w.device}")
+        f.q_weight, f.k_weight = q_weight.data_ptr(), k_weight.data_ptr()
+        f.q_weight_stride = q_weight.stride(0) if q_weight.dim() == 2 and hq > 1 else 0
+        f.k_weight_stride = k_weight.stride(0) if k_weight.dim() == 2 and hkv > 1 else 0
+    if cos is not None:
+        for name, t in (("cos", cos), ("sin", sin)):
+            if t.dtype is not torch.float32 or t.dim() != 2 or t.shape[1] != d // 2 or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous float32 table [positions][{d // 2}], got {tuple(t.shape)} {t.dtype}")
+            if device is not None and t.device != device:
+                raise ValueError(f"{name} must live on {device}, got {t.device}")
+        if cos.shape != sin.shape:
+            raise ValueError("cos and sin tables differ in shape")
+        f.cos_table, f.sin_table, f.table_rows = cos.data_ptr(), sin.data_ptr(), cos.shape[0]
+    return f
+
+
+def _enqueue(device, stream, call, *args):
+    """The call on `stream` (None: torch's current one) of the tensors' device, whichever device is current."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        _check(call(*args, _stream_ptr(stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, _stream_ptr(stream)))
+
+
+def norm_rope(q, k, cos=None, sin=None, pos0: int = 0, positions=None, q_weight=None, k_weight=None, norm_eps: float = 1e-6,
+              q_out=None, k_out=None, stream=None):
+    """Root mean square norms of the queries and keys of each head (bf16 weights [d] or [heads][d]; None: no norm) and the rotary
+    position embedding (float32 tables [positions][d / 2]; None: no rotation) in one pass.
+    q [batch][Hq][T][d], k [batch][Hkv][T][d] bf16, any strides with a contiguous last dimension; token j is at position pos0 + j or
+    at positions[b][j] (int32 [batch][T]; a token outside the tables is left out).  Returns contiguous (q_out, k_out)."""
+    import torch
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError(f"q and k are [batch][heads][tokens][head_dim], got {tuple(q.shape)} and {tuple(k.shape)}")
+    b, hq, T, d = q.shape
+    hkv = k.shape[1]
+    check_rows("q", q, (b, hq, T, d))
+    check_rows("k", k, (b, hkv, T, d))
+    if positions is not None:
+        check_contiguous("positions", positions, (b, T), torch.int32)
+    if q_out is not None:
+        check_contiguous("q_out", q_out, q.shape, torch.bfloat16)
+    if k_out is not None:
+        check_contiguous("k_out", k_out, k.shape, torch.bfloat16)
+    device = q.device
+    form = _form(hq, hkv, d, cos, sin, q_weight, k_weight, norm_eps, device)
+    _check_devices(device, k, positions, q_out, k_out)
+    if q_out is None:
+        q_out = torch.empty((b, hq, T, d), dtype=torch.bfloat16, device=device)
+    if k_out is None:
+        k_out = torch.empty((b, hkv, T, d), dtype=torch.bfloat16, device=device)
+    rq, rk = _rows(q), _rows(k)
+    _enqueue(device, stream, load_library().keydiff_norm_rope, C.byref(rq), C.byref(rk), b, hq, hkv, d, T, int(pos0),
+             positions.data_ptr() if positions is not None else None, C.byref(form), q_out.data_ptr(), k_out.data_ptr())
+    return q_out, k_out
+
+
+def check_branches(n_seqs, d, hkv, k_pages, v_pages, table, lens, n_new):
+    """The pages of n_seqs sequences: pools [pages][hkv][page_rows][d] bf16, table [n_seqs][width], lens and n_new [n_seqs] int32."""
+    import torch
+    if k_pages.dim() != 4 or k_pages.shape[1] != hkv or k_pages.shape[3] != d:
+        raise ValueError(f"k_pages must be [pages][{hkv}][page_rows][{d}], got {tuple(k_pages.shape)}")
+    check_contiguous("k_pages", k_pages, k_pages.shape, torch.bfloat16)
+    check_contiguous("v_pages", v_pages, k_pages.shape, torch.bfloat16)
+    if table.dim() != 2:
+        raise ValueError(f"table must be [{n_seqs}][width], got {tuple(table.shape)}")
+    check_contiguous("table", table, (n_seqs, table.shape[1]), torch.int32)
+    check_contiguous("lens", lens, (n_seqs,), torch.int32)
+    if n_new is not None:
+        check_contiguous("n_new", n_new, (n_seqs,), torch.int32)
+
+
+def _branches(n_seqs, hq, hkv, d, k_pages, v_pages, table, lens, n_new):
+    return _Branches(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), lens.data_ptr(),
+                     n_new.data_ptr() if n_new is not None else None, n_seqs, hq, hkv, d, k_pages.shape[2], k_pages.shape[0],
+                     table.shape[1])
+
+
+def branch_append(q, k_new, v_new, k_pages, v_pages, table, lens, n_new=None, pos0=None, cos=None, sin=None, q_weight=None,
+                  k_weight=None, norm_eps: float = 1e-6, q_out=None, stream=None):
+    """New tokens of sequences that continue prompts: norms and rotation of q and k_new as in norm_rope, keys and values into the
+    sequences' pages behind the lens[s] rows they hold, at positions pos0[s] + lens[s] + j (pos0: int32 [n_seqs], the length of the
+    sequence's prompt; None: zeros).  lens is not changed.
+    q [n_seqs][Hq][Bt][d] (None: keys and values only), k_new, v_new [n_seqs][Hkv][Bt][d]; k_pages, v_pages
+    [pages][Hkv][page_rows][d]; table int32 [n_seqs][width]; n_new int32 [n_seqs] (None: all Bt).  Returns the contiguous queries
+    for branch_attention; tokens that are left out (behind a sequence's n_new, lens < 0) keep their rows of q_out, which
+    hold anything if it is None."""
+    import torch
+    if k_new.dim() != 4 or (q is not None and q.dim() != 4):
+        raise ValueError("q, k_new and v_new are [sequences][heads][tokens][head_dim]")
+    n, hkv, Bt, d = k_new.shape
+    hq = q.shape[1] if q is not None else hkv
+    check_rows("k_new", k_new, (n, hkv, Bt, d))
+    check_rows("v_new", v_new, (n, hkv, Bt, d))
+    check_branches(n, d, hkv, k_pages, v_pages, table, lens, n_new)
+    if q is not None:
+        check_rows("q", q, (n, hq, Bt, d))
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if q_out is not None:
+        check_contiguous("q_out", q_out, q.shape, torch.bfloat16)
+    if pos0 is not None:
+        check_contiguous("pos0", pos0, (n,), torch.int32)
+    device = k_new.device
+    form = _form(hq, hkv, d, cos, sin, q_weight, k_weight, norm_eps, device)
+    _check_devices(device, q, v_new, k_pages, v_pages, table, lens, n_new, pos0, q_out)
+    if q is not None and q_out is None:
+        q_out = torch.empty((n, hq, Bt, d), dtype=torch.bfloat16, device=device)
+    b = _branches(n, hq, hkv, d, k_pages, v_pages, table, lens, n_new)
+    rk, rv = _rows(k_new), _rows(v_new)
+    rq = _rows(q) if q is not None else None
+    _enqueue(device, stream, load_library().keydiff_branch_append, C.byref(b), C.byref(rq) if rq is not None else None, C.byref(rk),
+             C.byref(rv), Bt, pos0.data_ptr() if pos0 is not None else None, C.byref(form),
+             q_out.data_ptr() if q_out is not None else None)
+    return q_out
+
+
+@functools.lru_cache(maxsize=256)
+def _branch_workspace_bytes(n_seqs, hq, hkv, d, Bt, n_prefixes, device_index):
+    b = _Branches(n_seqs=n_seqs, n_q_heads=hq, n_kv_heads=hkv, head_dim=d)
+    size = C.c_size_t()
+    _check(load_library().keydiff_branch_workspace_bytes(C.byref(b), Bt, n_prefixes, C.byref(size)))
+    return size.value
+
+
+def branch_workspace_bytes(n_seqs, n_q_heads, n_kv_heads, head_dim, Bt=1, n_prefixes=0):
+    """Bytes of the workspace that branch_attention needs for calls of these sizes on the current device."""
+    return _branch_workspace_bytes(n_seqs, n_q_heads, n_kv_heads, head_dim, Bt, n_prefixes, None)
+
+
+def branch_attention(q, k_pages, v_pages, table, lens, prefix=None, n_new=None, softmax_scale: float = 0.0, out=None, workspace=None,
+                     stream=None):
+    """Attention of the tokens that branch_append has appended: token j of sequence s sees all rows of its prompt and its sequence's
+    own rows 0 .. lens[s] + j (lens, table, n_new, pools: as given to branch_append).
+    q [n_seqs][Hq][Bt][d] bf16 (any strides with a contiguous last dimension).
+    prefix: the prompts' rows, shared by the sequences that continue them: a KeyDiffCache whose batch holds the prompts, or
+    (k, v, rows) with k, v bf16 [prompts][Hkv][at least rows][d]; sequence s continues prompt s / (n_seqs / prompts).  None: own rows
+    alone.  softmax_scale <= 0: 1/sqrt(d), or the cache's.
+    workspace: a uint8 tensor of at least branch_workspace_bytes that no other call in flight uses (None: allocated for the call).
+    Returns out [n_seqs][Hq][Bt][d]; rows behind a sequence's n_new, and those of a sequence with lens < 0, are left as they were
+    (they hold anything where out is None)."""
+    import torch
+    if q.dim() != 4 or k_pages.dim() != 4:
+        raise ValueError("q is [sequences][heads][tokens][head_dim] and pools are [pages][heads][page_rows][head_dim]")
+    n, hq, Bt, d = q.shape
+    hkv = k_pages.shape[1]
+    check_rows("q", q, (n, hq, Bt, d))
+    check_branches(n, d, hkv, k_pages, v_pages, table, lens, n_new)
+    if out is not None:
+        check_contiguous("out", out, q.shape, torch.bfloat16)
+    cache = prefix if isinstance(prefix, KeyDiffCache) else None
+    kp = vp = None
+    prompts = rows = cap = 0
+    device = q.device
+    if cache is not None:
+        prompts = cache.cfg.batch
+        if softmax_scale > 0:
+            raise ValueError("softmax_scale is the cache's")
+        if cache.device != device:
+            raise ValueError(f"the cache lives on {cache.device}, the queries on {device}")
+    elif prefix is not None:
+        kp, vp, rows = prefix
+        prompts, cap = kp.shape[0], kp.shape[2]
+        check_contiguous("prefix keys", kp, (prompts, hkv, cap, d), torch.bfloat16)
+        check_contiguous("prefix values", vp, kp.shape, torch.bfloat16)
+        if not 0 <= rows <= cap:
+            raise ValueError(f"the prefix has {cap} rows a head, {rows} are to be read")
+    _check_devices(device, k_pages, v_pages, table, lens, n_new, out, workspace, kp, vp)
+    need = _branch_workspace_bytes(n, hq, hkv, d, Bt, prompts, device.index)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        if stream is not None:   # torch must not hand the memory out again before the work on that stream is done
+            workspace.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device))
+    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need:
+        raise ValueError(f"workspace must be a contiguous uint8 tensor of at least {need} elements")
+    if out is None:
+        out = torch.empty((n, hq, Bt, d), dtype=torch.bfloat16, device=device)
+    b, rq = _branches(n, hq, hkv, d, k_pages, v_pages, table, lens, n_new), _rows(q)
+    if cache is not None:
+        _enqueue(device, stream, cache._L.keydiff_cache_branch_attention, cache._h, C.byref(b), C.byref(rq), Bt, out.data_ptr(),
+                 workspace.data_ptr(), workspace.numel())
+    else:
+        _enqueue(device, stream, load_library().keydiff_branch_attention, C.byref(b), C.byref(rq), Bt,
+                 kp.data_ptr() if kp is not None else None, vp.data_ptr() if vp is not None else None, prompts, int(rows), cap,
+                 softmax_scale, out.data_ptr(), workspace.data_ptr(), workspace.numel())
     return out
 
 
@@ -274,6 +543,20 @@ class KeyDiffCache:
                                                   int(pos0), cos.data_ptr(), sin.data_ptr(), cos.shape[0], out.data_ptr(),
                                                   scores_out.data_ptr() if scores_out is not None else None,
                                                   _stream_ptr(stream)))
+        return out
+
+    def prefill_block_norm_rope(self, q, k_new, v_new, pos0: int, cos, sin, q_weight, k_weight, norm_eps: float = 1e-6, out=None,
+                                scores_out=None, stream=None):
+        """prefill_block on a block whose q and k_new are neither normed nor rotated yet: bf16 weights [head_dim] or
+        [heads][head_dim] of the root mean square norm of each head's rows, tables as for prefill_block_rope.  Weights None: no
+        norm; tables None: no rotation."""
+        Bt, out = self._block_args(q, k_new, v_new, out, scores_out)
+        cfg = self.cfg
+        form = _form(cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, cos, sin, q_weight, k_weight, norm_eps, self.device)
+        _check(self._L.keydiff_prefill_block_norm_rope(self._h, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), Bt,
+                                                       int(pos0), C.byref(form), out.data_ptr(),
+                                                       scores_out.data_ptr() if scores_out is not None else None,
+                                                       _stream_ptr(stream)))
         return out
 
     def prefill_block_static(self, q, k_new, v_new, pos0: int, out, scores_out=None, stream=None):

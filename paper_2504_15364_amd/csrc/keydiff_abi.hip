@@ -11,6 +11,7 @@
 #include <new>
 #include <vector>
 
+#include "kd_branch.h"
 #include "kd_kernels.h"
 
 namespace {
@@ -521,10 +522,82 @@ void step_enqueued(keydiff_cache *c, const kd::StepParams &p, int64_t pos0, bool
 // Every check and every planning decision comes before the first launch, so an argument, shape or
 // state error leaves nothing enqueued.
 // The caller's rotary tables: float [rows][head_dim / 2] each; both null = q and k_new arrive rotated.
+// With `form`: norms and rotation by the entry of the layer (cos_t, sin_t and rows are its own).
 struct Rope {
     const float *cos_t, *sin_t;
     int64_t rows;
+    const keydiff_row_form_t *form = nullptr;
 };
+
+// A norm of nothing or a rotation of nothing is left out: both weights, or both tables, are null.
+int check_form(const keydiff_row_form_t *f, int head_dim, bool needed)
+{
+    if (!f) return fail(KEYDIFF_EINVAL, "null pointer");
+    const bool norm = f->q_weight || f->k_weight, rope = f->cos_table || f->sin_table;
+    if (needed && !norm && !rope) return fail(KEYDIFF_EINVAL, "neither norm weights nor rotary tables");
+    if (norm) {
+        if (!f->q_weight || !f->k_weight) return fail(KEYDIFF_EINVAL, "null norm weight");
+        if (misaligned(f->q_weight) || misaligned(f->k_weight)) return fail(KEYDIFF_EINVAL, "norm weights must be 16-byte aligned");
+        for (const int64_t st : {f->q_weight_stride, f->k_weight_stride})
+            if (st < 0 || st % 8 || (st != 0 && st < head_dim) || st > 0x7fffffff)
+                return fail(KEYDIFF_ESHAPE, "the stride of norm weights must be 0 or a multiple of 8 of at least head_dim, got %lld", (long long)st);
+        if (!(f->norm_eps >= 0.f)) return fail(KEYDIFF_EINVAL, "norm_eps must not be negative");
+    }
+    if (rope) {
+        if (!f->cos_table || !f->sin_table) return fail(KEYDIFF_EINVAL, "null rotary table");
+        if (misaligned(f->cos_table) || misaligned(f->sin_table)) return fail(KEYDIFF_EINVAL, "rotary tables must be 16-byte aligned");
+        if (f->table_rows < 1) return fail(KEYDIFF_ESHAPE, "the rotary tables hold no position");
+    }
+    return KEYDIFF_OK;
+}
+
+kd::RowForm row_form(const keydiff_row_form_t *f)
+{
+    kd::RowForm r{};
+    if (!f) return r;
+    r.q_w = static_cast<const uint16_t *>(f->q_weight);
+    r.k_w = static_cast<const uint16_t *>(f->k_weight);
+    r.q_w_head = (int32_t)f->q_weight_stride;
+    r.k_w_head = (int32_t)f->k_weight_stride;
+    r.cos_t = f->cos_table;
+    r.sin_t = f->sin_table;
+    r.table_rows = f->table_rows;
+    r.eps = f->norm_eps;
+    return r;
+}
+
+// The tables of a step's rotation, or the norm and rotation of its layer
+int check_rope(const Rope &r, int head_dim, int64_t pos0, int32_t Bt)
+{
+    if (r.form) {
+        if (int rc = check_form(r.form, head_dim, true)) return rc;
+        if (!r.cos_t) return KEYDIFF_OK;
+    }
+    if (!r.cos_t || !r.sin_t) return fail(KEYDIFF_EINVAL, "null rotary table");
+    if (misaligned(r.cos_t) || misaligned(r.sin_t)) return fail(KEYDIFF_EINVAL, "rotary tables must be 16-byte aligned");
+    if (pos0 + Bt > r.rows) return fail(KEYDIFF_ESHAPE, "the rotary tables hold %lld positions; the block ends at %lld",
+                                        (long long)r.rows, (long long)(pos0 + Bt));
+    return KEYDIFF_OK;
+}
+
+// The blocks of b.layers layers shaped by `cf` formed in one launch; `forms`: the layers' norms and rotations, or null: rotated by the tables
+hipError_t launch_forms(const kd::RopeBatch &b, const Rope &rope, const keydiff_row_form_t *forms, const keydiff_config_t &cf, int32_t Bt,
+                        int64_t pos0, hipStream_t s)
+{
+    if (!forms)
+        return kd::launch_rope(b, rope.cos_t, rope.sin_t, cf.batch * cf.n_q_heads * Bt, cf.batch * cf.n_kv_heads * Bt, Bt, cf.head_dim,
+                               (int32_t)pos0, s);
+    kd::NormRopeLayers n{};
+    n.layers = b.layers;
+    n.batch = cf.batch;
+    n.hq = cf.n_q_heads;
+    n.hkv = cf.n_kv_heads;
+    n.Bt = Bt;
+    n.D = cf.head_dim;
+    n.pos0 = pos0;
+    for (int i = 0; i < b.layers; ++i) n.layer[i] = {b.q[i], b.k[i], b.q_rot[i], b.k_rot[i], row_form(&forms[i])};
+    return kd::launch_norm_rope_layers(n, s);
+}
 
 int block_step(keydiff_cache *c, const void *q, const void *k_new, const void *v_new, int32_t Bt, int64_t pos0,
                void *out, float *scores_out, bool defer, keydiff_cache *carry, unsigned char *work, hipStream_t s,
@@ -539,12 +612,8 @@ int block_step(keydiff_cache *c, const void *q, const void *k_new, const void *v
     if (Bt < 1 || Bt > c->cfg.block_B) return fail(KEYDIFF_ESHAPE, "Bt must lie in [1, block_B], got %d", Bt);
     if (pos0 < 0 || pos0 + Bt > 0x7fffffffLL) return fail(KEYDIFF_ESHAPE, "positions must fit in int32");
     if (carry == c) return fail(KEYDIFF_EINVAL, "a cache cannot carry its own eviction");
-    if (rope) {
-        if (!rope->cos_t || !rope->sin_t) return fail(KEYDIFF_EINVAL, "null rotary table");
-        if (misaligned(rope->cos_t) || misaligned(rope->sin_t)) return fail(KEYDIFF_EINVAL, "rotary tables must be 16-byte aligned");
-        if (pos0 + Bt > rope->rows) return fail(KEYDIFF_ESHAPE, "the rotary tables hold %lld positions; the block ends at %lld",
-                                                (long long)rope->rows, (long long)(pos0 + Bt));
-    }
+    if (rope)
+        if (int rc = check_rope(*rope, c->cfg.head_dim, pos0, Bt)) return rc;
     const keydiff_config_t &cf = c->cfg;
     const int n = c->len + Bt, N = cf.budget_N;
     const bool contiguous = continues(c, pos0);
@@ -593,9 +662,7 @@ int block_step(keydiff_cache *c, const void *q, const void *k_new, const void *v
         b.k[0] = p.k_new;
         b.q_rot[0] = q_rot;
         b.k_rot[0] = k_rot;
-        KD_LAUNCH(kd::launch_rope(b, rope->cos_t, rope->sin_t, cf.batch * cf.n_q_heads * Bt, cf.batch * cf.n_kv_heads * Bt,
-                                  Bt, cf.head_dim, (int32_t)pos0, s),
-                  "rotary embedding kernel");
+        KD_LAUNCH(launch_forms(b, *rope, rope->form, cf, Bt, pos0, s), "rotary embedding kernel");
         p.q = q_rot;
         p.k_new = k_rot;
     }
@@ -1028,8 +1095,10 @@ int keydiff_prefill_block_deferred(keydiff_cache_t *c, const void *q, const void
 }
 
 static int block_layers(keydiff_cache_t *const *caches, int32_t n_layers, const void *const *q, const void *const *k_new,
-                        const void *const *v_new, int32_t Bt, int64_t pos0, void *const *out, void *stream, const Rope *rope)
+                        const void *const *v_new, int32_t Bt, int64_t pos0, void *const *out, void *stream, const Rope *rope,
+                        const keydiff_row_form_t *forms = nullptr)
 {
+    // rope: the tables of all layers; forms: norms and rotation of every layer
     if (!caches || !q || !k_new || !v_new || !out) return fail(KEYDIFF_EINVAL, "null pointer");
     if (n_layers < 1) return fail(KEYDIFF_ESHAPE, "n_layers must be positive, got %d", n_layers);
     for (int l = 0; l < n_layers; ++l) {
@@ -1039,12 +1108,16 @@ static int block_layers(keydiff_cache_t *const *caches, int32_t n_layers, const 
             if (caches[m] == caches[l]) return fail(KEYDIFF_EINVAL, "layers %d and %d share a cache", m, l);
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
+    auto rope_of = [&](int l) { return forms ? Rope{forms[l].cos_table, forms[l].sin_table, forms[l].table_rows, &forms[l]} : *rope; };
+    for (int l = 0; forms && l < n_layers; ++l)
+        if (int rc = check_rope(rope_of(l), caches[l]->cfg.head_dim, pos0, Bt)) return rc;
     // The blocks of all layers rotated ahead, up to 32 layers a launch, into the layers' own scratch regions (which nothing
     // but the step of the same layer reads).  Only where every layer would pass the checks of its step that the
     // rotation depends on and the layers are shaped alike; else each step rotates its own block, so that what
     // is enqueued before an error is found is the same as ever.
-    bool rotated = rope && n_layers > 1 && rope->cos_t && rope->sin_t && !misaligned(rope->cos_t) && !misaligned(rope->sin_t) &&
-                   Bt >= 1 && pos0 >= 0 && pos0 + Bt <= 0x7fffffffLL && pos0 + Bt <= rope->rows;
+    bool rotated = (forms || (rope && rope->cos_t && rope->sin_t && !misaligned(rope->cos_t) && !misaligned(rope->sin_t) &&
+                              pos0 + Bt <= rope->rows)) &&
+                   n_layers > 1 && Bt >= 1 && pos0 >= 0 && pos0 + Bt <= 0x7fffffffLL;
     for (int l = 0; l < n_layers && rotated; ++l) {
         const keydiff_config_t &cf = caches[l]->cfg, &c0 = caches[0]->cfg;
         rotated = cf.batch == c0.batch && cf.n_q_heads == c0.n_q_heads && cf.n_kv_heads == c0.n_kv_heads &&
@@ -1068,15 +1141,16 @@ static int block_layers(keydiff_cache_t *const *caches, int32_t n_layers, const 
             b.k_rot[i] = reinterpret_cast<uint16_t *>(c->scratch + c->L.off_k_rot);
         }
         ProfScope ps(caches[l0], KEYDIFF_K_AUX, s);
-        KD_LAUNCH(kd::launch_rope(b, rope->cos_t, rope->sin_t, cf.batch * cf.n_q_heads * Bt, cf.batch * cf.n_kv_heads * Bt,
-                                  Bt, cf.head_dim, (int32_t)pos0, s),
-                  "rotary embedding kernel");
+        KD_LAUNCH(launch_forms(b, rope_of(l0), forms ? forms + l0 : nullptr, cf, Bt, pos0, s), "rotary embedding kernel");
     }
     auto q_of = [&](int l) { return rotated ? (const void *)(caches[l]->scratch + caches[l]->L.off_q_rot) : q[l]; };
     auto k_of = [&](int l) { return rotated ? (const void *)(caches[l]->scratch + caches[l]->L.off_k_rot) : k_new[l]; };
-    if (n_layers == 1)   // nothing to share a launch with, and nothing that could carry the eviction
-        return block_step(caches[0], q[0], k_new[0], v_new[0], Bt, pos0, out[0], nullptr, false, nullptr, caches[0]->scratch, s, rope);
-    if ((!rope || rotated) && layers_alike(caches, n_layers, q, k_new, v_new, Bt, pos0, out, rotated)) {
+    const bool raw = rope || forms;   // the blocks arrive as the projections left them
+    if (n_layers == 1) {   // nothing to share a launch with, and nothing that could carry the eviction
+        const Rope one = raw ? rope_of(0) : Rope{};
+        return block_step(caches[0], q[0], k_new[0], v_new[0], Bt, pos0, out[0], nullptr, false, nullptr, caches[0]->scratch, s, raw ? &one : nullptr);
+    }
+    if ((!raw || rotated) && layers_alike(caches, n_layers, q, k_new, v_new, Bt, pos0, out, rotated)) {
         kd::StepParams one = step_params(caches[0], q[0], k_new[0], v_new[0], Bt, pos0, out[0], nullptr, caches[0]->scratch);
         const int groups = layer_groups(caches[0], one, n_layers);
         for (int l = 0, i = 0; i < groups; ++i) {
@@ -1103,8 +1177,10 @@ static int block_layers(keydiff_cache_t *const *caches, int32_t n_layers, const 
         // ... and, ORDERED layout, the row shift of the layer before that one, whose selection rode in the
         // launch of the layer between them
         keydiff_cache *shifted = n_layers > 2 ? caches[(l + n_layers - 2) % n_layers] : nullptr;
+        const bool here = raw && !rotated;
+        const Rope own = here ? rope_of(l) : Rope{};
         if (int rc = block_step(caches[l], q_of(l), k_of(l), v_new[l], Bt, pos0, out[l], nullptr, true, carry,
-                                caches[l]->scratch, s, rotated ? nullptr : rope, shifted, n_layers > 2))
+                                caches[l]->scratch, s, here ? &own : nullptr, shifted, n_layers > 2))
             return rc;
     }
     return KEYDIFF_OK;
@@ -1124,6 +1200,269 @@ int keydiff_prefill_block_layers_rope(keydiff_cache_t *const *caches, int32_t n_
 {
     const Rope rope{cos_table, sin_table, table_rows};
     return block_layers(caches, n_layers, q, k_new, v_new, Bt, pos0, out, stream, &rope);
+}
+
+int keydiff_prefill_block_norm_rope(keydiff_cache_t *c, const void *q, const void *k_new, const void *v_new, int32_t Bt,
+                                    int64_t pos0, const keydiff_row_form_t *form, void *out, float *scores_out, void *stream)
+{
+    if (!c || !form) return fail(KEYDIFF_EINVAL, "null pointer");
+    const Rope rope{form->cos_table, form->sin_table, form->table_rows, form};
+    return block_step(c, q, k_new, v_new, Bt, pos0, out, scores_out, false, nullptr, c->scratch,
+                      static_cast<hipStream_t>(stream), &rope);
+}
+
+int keydiff_prefill_block_layers_norm_rope(keydiff_cache_t *const *caches, int32_t n_layers, const void *const *q,
+                                           const void *const *k_new, const void *const *v_new, int32_t Bt, int64_t pos0,
+                                           const keydiff_row_form_t *form, void *const *out, void *stream)
+{
+    if (!form) return fail(KEYDIFF_EINVAL, "null pointer");
+    return block_layers(caches, n_layers, q, k_new, v_new, Bt, pos0, out, stream, nullptr, form);
+}
+
+// ------------------------------------------------------------------ norms and rotation alone; continuations of a prompt
+namespace {
+
+constexpr int kMaxHeads = 4096;   // query heads, and KV heads, of the operators below
+
+int check_heads(int32_t n_seqs, int32_t hq, int32_t hkv, int32_t head_dim, int32_t Bt)
+{
+    if (n_seqs < 1 || hq < 1 || hkv < 1 || Bt < 1) return fail(KEYDIFF_ESHAPE, "sequences, head counts and Bt must be positive");
+    if (hq % hkv) return fail(KEYDIFF_ESHAPE, "n_q_heads must be a multiple of n_kv_heads");
+    if (head_dim != 64 && head_dim != 128) return fail(KEYDIFF_ESHAPE, "head_dim must be 64 or 128");
+    if (hq > kMaxHeads) return fail(KEYDIFF_ESHAPE, "n_q_heads must not exceed %d", kMaxHeads);
+    if ((int64_t)n_seqs * Bt * hq > 0x7fffffff) return fail(KEYDIFF_ESHAPE, "sequences * Bt * n_q_heads must fit in int32");
+    return KEYDIFF_OK;
+}
+
+// elements that rows of `heads` heads reach, from data on
+size_t span(const keydiff_rows_t &r, int32_t n_seqs, int32_t heads, int32_t Bt, int32_t head_dim)
+{
+    return (size_t)(n_seqs - 1) * r.seq_stride + (size_t)(heads - 1) * r.head_stride + (size_t)(Bt - 1) * r.token_stride + head_dim;
+}
+
+int check_rows(const keydiff_rows_t *r, const char *name)
+{
+    if (!r || !r->data) return fail(KEYDIFF_EINVAL, "null pointer: %s", name);
+    if (misaligned(r->data)) return fail(KEYDIFF_EINVAL, "%s must be 16-byte aligned", name);
+    for (const int64_t st : {r->seq_stride, r->head_stride, r->token_stride})
+        if (st < 0 || st % 8 || st > ((int64_t)1 << 40))
+            return fail(KEYDIFF_ESHAPE, "the strides of %s must be multiples of 8 elements and not negative, got %lld", name, (long long)st);
+    return KEYDIFF_OK;
+}
+
+kd::Rows rows_of(const keydiff_rows_t &r) { return {static_cast<const uint16_t *>(r.data), r.seq_stride, r.head_stride, r.token_stride}; }
+
+int check_branches(const keydiff_branches_t *b, int32_t Bt)
+{
+    if (!b || !b->k_pages || !b->v_pages || !b->table || !b->lens) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (int rc = check_heads(b->n_seqs, b->n_q_heads, b->n_kv_heads, b->head_dim, Bt)) return rc;
+    if (misaligned(b->k_pages) || misaligned(b->v_pages)) return fail(KEYDIFF_EINVAL, "pages must be 16-byte aligned");
+    if (b->page_rows < 8 || b->page_rows > 1024 || (b->page_rows & (b->page_rows - 1)))
+        return fail(KEYDIFF_ESHAPE, "page_rows must be a power of two from 8 to 1024, got %d", b->page_rows);
+    if (b->n_pages < 1 || b->table_width < 1) return fail(KEYDIFF_ESHAPE, "n_pages and table_width must be positive");
+    if ((int64_t)b->table_width * b->page_rows > 0x3fffffff) return fail(KEYDIFF_ESHAPE, "table_width * page_rows must not exceed 2^30");
+    return KEYDIFF_OK;
+}
+
+kd::Pages pages_of(const keydiff_branches_t *b)
+{
+    kd::Pages p{};
+    p.k = static_cast<uint16_t *>(b->k_pages);
+    p.v = static_cast<uint16_t *>(b->v_pages);
+    p.table = b->table;
+    p.lens = b->lens;
+    p.n_new = b->n_new;
+    while ((1 << p.page_shift) < b->page_rows) ++p.page_shift;
+    p.n_pages = b->n_pages;
+    p.width = b->table_width;
+    return p;
+}
+
+// n_prefixes prompts, 0 without a prefix; the sizes with which a launch counts its tiles stay inside int32
+int check_prefixes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, int32_t prefix_len)
+{
+    if (n_prefixes < 0 || (n_prefixes > 0 && b->n_seqs % n_prefixes))
+        return fail(KEYDIFF_ESHAPE, "n_prefixes must divide the %d sequences, got %d", b->n_seqs, n_prefixes);
+    if (prefix_len < 0 || prefix_len > 0x3fffffff) return fail(KEYDIFF_ESHAPE, "prefix_len must lie in [0, 2^30), got %d", prefix_len);
+    const int64_t Mt = (int64_t)b->n_q_heads / b->n_kv_heads * Bt, fan = n_prefixes > 0 ? b->n_seqs / n_prefixes : 0;
+    const double shared = (double)n_prefixes * b->n_kv_heads * (fan * Mt / 16 + 1) * (prefix_len / 32 + 1);
+    const double own = (double)b->n_seqs * b->n_kv_heads * (Mt / 16 + 1) * ((int64_t)b->table_width * b->page_rows / 32 + 1);
+    if (shared > 2e9 || own > 2e9) return fail(KEYDIFF_ESHAPE, "too many rows for one call: the tiles of 32 keys and 16 query rows must fit in int32");
+    return KEYDIFF_OK;
+}
+
+int branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix,
+                     int32_t n_prefixes, int32_t prefix_len, int64_t prefix_cap, float scale_log2e, void *out, void *workspace,
+                     size_t workspace_bytes, hipStream_t s)
+{
+    kd::BranchParams p{};
+    p.q = rows_of(*q);
+    p.out = static_cast<uint16_t *>(out);
+    p.k_prefix = static_cast<const uint16_t *>(k_prefix);
+    p.v_prefix = static_cast<const uint16_t *>(v_prefix);
+    p.pages = pages_of(b);
+    p.n_seqs = b->n_seqs;
+    p.n_prefixes = n_prefixes;
+    p.fan = n_prefixes > 0 ? b->n_seqs / n_prefixes : 0;
+    p.hkv = b->n_kv_heads;
+    p.G = b->n_q_heads / b->n_kv_heads;
+    p.Bt = Bt;
+    p.D = b->head_dim;
+    p.prefix_len = n_prefixes > 0 ? prefix_len : 0;
+    p.prefix_cap = prefix_cap;
+    p.cus = std::max(compute_units(), 2);
+    p.scale_log2e = scale_log2e;
+    size_t off_ml = 0, off_plan = 0;
+    const size_t need = kd::branch_workspace(p.n_seqs, n_prefixes, p.hkv, p.G, Bt, p.D, p.cus, &off_ml, &off_plan);
+    if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
+    unsigned char *w = static_cast<unsigned char *>(workspace);
+    p.part_o = reinterpret_cast<float *>(w);
+    p.part_ml = reinterpret_cast<float2 *>(w + off_ml);
+    p.plan = reinterpret_cast<int32_t *>(w + off_plan);
+    KD_LAUNCH(kd::launch_branch_attention(p, s), "branch attention kernels");
+    return KEYDIFF_OK;
+}
+
+int check_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *out, const void *workspace)
+{
+    if (int rc = check_branches(b, Bt)) return rc;
+    if (int rc = check_rows(q, "q")) return rc;
+    if (!out || !workspace) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (misaligned(out)) return fail(KEYDIFF_EINVAL, "out must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(KEYDIFF_EINVAL, "the workspace must be 256-byte aligned");
+    return KEYDIFF_OK;
+}
+
+}  // namespace
+
+int keydiff_norm_rope(const keydiff_rows_t *q, const keydiff_rows_t *k, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
+                      int32_t head_dim, int32_t Bt, int64_t pos0, const int32_t *positions, const keydiff_row_form_t *form,
+                      void *q_out, void *k_out, void *stream)
+{
+    if (int rc = check_heads(batch, n_q_heads, n_kv_heads, head_dim, Bt)) return rc;
+    if (int rc = check_rows(q, "q")) return rc;
+    if (int rc = check_rows(k, "k")) return rc;
+    if (!q_out || !k_out) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (misaligned(q_out) || misaligned(k_out)) return fail(KEYDIFF_EINVAL, "tensors must be 16-byte aligned");
+    if (int rc = check_form(form, head_dim, true)) return rc;
+    if (pos0 < 0 || pos0 + Bt > 0x7fffffffLL) return fail(KEYDIFF_ESHAPE, "positions must fit in int32");
+    if (form->cos_table && !positions && pos0 + Bt > form->table_rows)
+        return fail(KEYDIFF_ESHAPE, "the rotary tables hold %lld positions; the block ends at %lld", (long long)form->table_rows,
+                    (long long)(pos0 + Bt));
+    const size_t q_in = 2 * span(*q, batch, n_q_heads, Bt, head_dim), k_in = 2 * span(*k, batch, n_kv_heads, Bt, head_dim);
+    const size_t token = (size_t)batch * Bt * head_dim * 2, q_bytes = token * n_q_heads, k_bytes = token * n_kv_heads;
+    if (overlap(q_out, q_bytes, q->data, q_in) || overlap(q_out, q_bytes, k->data, k_in) || overlap(k_out, k_bytes, q->data, q_in) ||
+        overlap(k_out, k_bytes, k->data, k_in) || overlap(q_out, q_bytes, k_out, k_bytes))
+        return fail(KEYDIFF_EINVAL, "the outputs must not overlap the inputs or one another");
+    kd::NormRopeParams p{};
+    p.q = rows_of(*q);
+    p.k = rows_of(*k);
+    p.q_out = static_cast<uint16_t *>(q_out);
+    p.k_out = static_cast<uint16_t *>(k_out);
+    p.form = row_form(form);
+    p.positions = positions;
+    p.pos0 = pos0;
+    p.n_seqs = batch;
+    p.hq = n_q_heads;
+    p.hkv = n_kv_heads;
+    p.Bt = Bt;
+    p.D = head_dim;
+    KD_LAUNCH(kd::launch_norm_rope(p, static_cast<hipStream_t>(stream)), "norm and rotation kernel");
+    return KEYDIFF_OK;
+}
+
+int keydiff_branch_append(const keydiff_branches_t *b, const keydiff_rows_t *q, const keydiff_rows_t *k, const keydiff_rows_t *v,
+                          int32_t Bt, const int32_t *pos0, const keydiff_row_form_t *form, void *q_out, void *stream)
+{
+    if (int rc = check_branches(b, Bt)) return rc;
+    const bool queries = (q && q->data) || q_out;
+    if (queries) {
+        if (int rc = check_rows(q, "q")) return rc;
+        if (!q_out) return fail(KEYDIFF_EINVAL, "null pointer: q_out");
+        if (misaligned(q_out)) return fail(KEYDIFF_EINVAL, "q_out must be 16-byte aligned");
+    }
+    if (int rc = check_rows(k, "k")) return rc;
+    if (int rc = check_rows(v, "v")) return rc;
+    if (form)
+        if (int rc = check_form(form, b->head_dim, false)) return rc;
+    const size_t q_bytes = (size_t)b->n_seqs * Bt * b->n_q_heads * b->head_dim * 2;
+    const size_t pool = (size_t)b->n_pages * b->n_kv_heads * b->page_rows * b->head_dim * 2;
+    struct {
+        const keydiff_rows_t *r;
+        int32_t heads;
+    } in[3] = {{k, b->n_kv_heads}, {v, b->n_kv_heads}, {q, b->n_q_heads}};
+    for (int i = 0; i < (queries ? 3 : 2); ++i) {
+        const size_t bytes = 2 * span(*in[i].r, b->n_seqs, in[i].heads, Bt, b->head_dim);
+        if ((queries && overlap(q_out, q_bytes, in[i].r->data, bytes)) || overlap(b->k_pages, pool, in[i].r->data, bytes) ||
+            overlap(b->v_pages, pool, in[i].r->data, bytes))
+            return fail(KEYDIFF_EINVAL, "q_out and the pages must not overlap the inputs");
+    }
+    if (overlap(b->k_pages, pool, b->v_pages, pool) ||
+        (queries && (overlap(q_out, q_bytes, b->k_pages, pool) || overlap(q_out, q_bytes, b->v_pages, pool))))
+        return fail(KEYDIFF_EINVAL, "q_out, k_pages and v_pages must not overlap one another");
+    kd::NormRopeParams p{};
+    if (queries) p.q = rows_of(*q);
+    p.k = rows_of(*k);
+    p.v = rows_of(*v);
+    p.q_out = static_cast<uint16_t *>(q_out);
+    p.form = row_form(form);
+    p.positions = pos0;
+    p.pages = pages_of(b);
+    p.n_seqs = b->n_seqs;
+    p.hq = queries ? b->n_q_heads : 0;
+    p.hkv = b->n_kv_heads;
+    p.Bt = Bt;
+    p.D = b->head_dim;
+    KD_LAUNCH(kd::launch_branch_append(p, static_cast<hipStream_t>(stream)), "branch append kernel");
+    return KEYDIFF_OK;
+}
+
+int keydiff_branch_workspace_bytes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, size_t *bytes)
+{
+    if (!b || !bytes) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (int rc = check_heads(b->n_seqs, b->n_q_heads, b->n_kv_heads, b->head_dim, Bt)) return rc;
+    if (n_prefixes < 0 || (n_prefixes > 0 && b->n_seqs % n_prefixes))
+        return fail(KEYDIFF_ESHAPE, "n_prefixes must divide the %d sequences, got %d", b->n_seqs, n_prefixes);
+    size_t off_ml = 0, off_plan = 0;
+    *bytes = kd::branch_workspace(b->n_seqs, n_prefixes, b->n_kv_heads, b->n_q_heads / b->n_kv_heads, Bt, b->head_dim,
+                                  std::max(compute_units(), 2), &off_ml, &off_plan);
+    return KEYDIFF_OK;
+}
+
+int keydiff_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix,
+                             int32_t n_prefixes, int32_t prefix_len, int64_t prefix_cap, float softmax_scale, void *out,
+                             void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_branch_attention(b, q, Bt, out, workspace)) return rc;
+    if (int rc = check_prefixes(b, Bt, n_prefixes, prefix_len)) return rc;
+    if (n_prefixes > 0 && prefix_len > 0) {
+        if (!k_prefix || !v_prefix) return fail(KEYDIFF_EINVAL, "null pointer: prefix rows");
+        if (misaligned(k_prefix) || misaligned(v_prefix)) return fail(KEYDIFF_EINVAL, "tensors must be 16-byte aligned");
+        if (prefix_cap < prefix_len) return fail(KEYDIFF_ESHAPE, "prefix_cap must be at least prefix_len");
+    }
+    const double scale = softmax_scale > 0.f ? (double)softmax_scale : 1.0 / std::sqrt((double)b->head_dim);
+    return branch_attention(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, (float)(scale * 1.4426950408889634), out,
+                            workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+int keydiff_cache_branch_attention(keydiff_cache_t *c, const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, void *out,
+                                   void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!c) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (int rc = check_branch_attention(b, q, Bt, out, workspace)) return rc;
+    if (b->n_q_heads != c->cfg.n_q_heads || b->n_kv_heads != c->cfg.n_kv_heads || b->head_dim != c->cfg.head_dim)
+        return fail(KEYDIFF_ESHAPE, "the cache holds %d / %d heads of %d, the continuations have %d / %d of %d", c->cfg.n_q_heads,
+                    c->cfg.n_kv_heads, c->cfg.head_dim, b->n_q_heads, b->n_kv_heads, b->head_dim);
+    // (a pending eviction leaves the budget's rows)
+    const int32_t rows = c->len;
+    if (int rc = check_prefixes(b, Bt, c->cfg.batch, rows)) return rc;
+    size_t off_ml = 0, off_plan = 0;
+    const size_t need = kd::branch_workspace(b->n_seqs, c->cfg.batch, b->n_kv_heads, b->n_q_heads / b->n_kv_heads, Bt, b->head_dim,
+                                             std::max(compute_units(), 2), &off_ml, &off_plan);
+    if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (int rc = finish_pending(c, s)) return rc;
+    return branch_attention(b, q, Bt, c->k, c->v, c->cfg.batch, c->len, c->L.cap, c->scale_log2e, out, workspace, workspace_bytes, s);
 }
 
 int keydiff_finish(keydiff_cache_t *c, void *stream)
