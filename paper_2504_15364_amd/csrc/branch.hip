@@ -348,14 +348,20 @@ __device__ void own_part(const BranchParams &p, const Plan &plan, int own_wave, 
         }
         u32x4 kr[2][NC], vr[NV];
         uint32_t absent = 0;   // bit i: rows 8 i .. of the tile in registers lie on a page that does not exist
-        // A tile's rows lie in groups of eight on one page each (pages have a multiple of eight rows).  Rows past the last repeat it.
+        // A tile's rows lie in groups of eight on one page each (pages have a multiple of eight rows).  The numbers of its pages are
+        // requested a tile ahead of its rows.  Rows past the last repeat it.
+        int pages[4];
+        auto look_up = [&](int t) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pages[i] = table[min(t * TK + 8 * i, n - 1) >> shift];
+        };
         auto load = [&](int t) {
             const uint16_t *kg8[4], *vg8[4];   // first row of each group, head h
             absent = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int row = min(t * TK + 8 * i, (n - 1) & ~7);
-                int page = __builtin_amdgcn_readfirstlane(table[row >> shift]);
+                int page = __builtin_amdgcn_readfirstlane(pages[i]);
                 if ((uint32_t)page >= (uint32_t)p.pages.n_pages) {
                     absent |= 1u << i;
                     page = 0;
@@ -383,13 +389,18 @@ __device__ void own_part(const BranchParams &p, const Plan &plan, int own_wave, 
                     if (absent >> (i * RPL / 8) & 1) vr[i] = u32x4{0u, 0u, 0u, 0u};
             }
         };
+        look_up(t0);
         load(t0);
+        look_up(t0 + 1);
         for (int t = t0; t < t1; ++t) {
             const uint32_t hidden = absent;
             tile_step<D, CB>(
                 st, kr, vr, vt, p.scale_log2e, lane,
                 [&]() {
-                    if (t + 1 < t1) load(t + 1);
+                    if (t + 1 < t1) {
+                        load(t + 1);
+                        look_up(t + 2);
+                    }
                 },
                 [&](f32x4 (&sc)[CB][2]) {
                     if ((t + 1) * TK > min(len, n) || hidden) {   // uniform: rows that not every query sees
@@ -479,54 +490,90 @@ __global__ __launch_bounds__(64 * NW) void branch_main_kernel(BranchParams p)
     }
 }
 
-// The join of a row's pieces: D / 4 threads a row
+// The join of a row's pieces: `groups` groups of D / 4 threads take a row's pieces in turn, four at a time, and join what they have
+// in LDS.  (Groups: where there are few rows and many pieces, the pieces requested one behind another were all the time this took: one
+// sequence, 8192 shared rows, 17.7 us with one group a row.)
 template <int D, int CBS, int CBO>
-__global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int wgs)
+__global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int wgs, int groups)
 {
-    constexpr int TPR = D / 4, RS = 16 * CBS, RO = 16 * CBO;
+    constexpr int TPR = D / 4, RS = 16 * CBS, RO = 16 * CBO, BATCH = 4;
+    __shared__ f32x4 acc_s[256];
+    __shared__ float2 ml_s[256 / TPR];
     const int Mt = p.G * p.Bt;
-    const int64_t row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    const int unit = (int)threadIdx.x / TPR, group = unit % groups;
+    const int64_t row = (int64_t)blockIdx.x * (256 / TPR / groups) + unit / groups;
     const int d0 = (int)threadIdx.x % TPR * 4;
-    if (row >= (int64_t)p.n_seqs * p.hkv * Mt) return;
-    const int sh = (int)(row / Mt), m = (int)(row - (int64_t)sh * Mt), s = sh / p.hkv, h = sh - s * p.hkv;
-    if (m % p.Bt >= new_of(p, s)) return;   // left as it was
-    // the pieces: slots [a0, a1) of the shared part, [b0, b1) of the own part
-    int a0 = 0, a1 = 0, b0 = 0, b1 = 0, am = 0, bm = 0;
-    if (p.prefix_len > 0) {
-        const int c = s / p.fan, mm = (s - c * p.fan) * Mt + m, blocks = (p.fan * Mt + RS - 1) / RS, nt = (p.prefix_len + TK - 1) / TK;
-        const int seg = (c * p.hkv + h) * blocks + mm / RS, chunk = p.plan[0];
-        am = mm % RS;
-        a0 = seg * nt / chunk + seg;
-        a1 = ((seg + 1) * nt - 1) / chunk + seg + 1;
-    }
-    const int n = own_rows(p, s);
-    if (n > 0) {
-        const int blocks = (Mt + RO - 1) / RO, nt = (n + TK - 1) / TK, chunk = p.plan[1];
-        const int local = h * blocks + m / RO, first = p.plan[BRANCH_PLAN_WORDS + s] * p.hkv * blocks + local * nt;
-        const int seg = s * p.hkv * blocks + local;
-        bm = m % RO;
-        b0 = first / chunk + seg;
-        b1 = (first + nt - 1) / chunk + seg + 1;
+    const bool exists = row < (int64_t)p.n_seqs * p.hkv * Mt;
+    const int sh = exists ? (int)(row / Mt) : 0, m = exists ? (int)(row - (int64_t)sh * Mt) : 0, s = sh / p.hkv, h = sh - s * p.hkv;
+    const bool wanted = exists && m % p.Bt < new_of(p, s);   // else left as it was
+    // the pieces: slots a0 .. of the shared part, b0 .. of the own part
+    int a0 = 0, na = 0, b0 = 0, nb = 0, am = 0, bm = 0;
+    if (wanted) {
+        if (p.prefix_len > 0) {
+            const int c = s / p.fan, mm = (s - c * p.fan) * Mt + m, blocks = (p.fan * Mt + RS - 1) / RS, nt = (p.prefix_len + TK - 1) / TK;
+            const int seg = (c * p.hkv + h) * blocks + mm / RS, chunk = p.plan[0];
+            am = mm % RS;
+            a0 = seg * nt / chunk;
+            na = ((seg + 1) * nt - 1) / chunk + 1 - a0;
+            a0 += seg;
+        }
+        const int n = own_rows(p, s);
+        if (n > 0) {
+            const int blocks = (Mt + RO - 1) / RO, nt = (n + TK - 1) / TK, chunk = p.plan[1];
+            const int local = h * blocks + m / RO, first = p.plan[BRANCH_PLAN_WORDS + s] * p.hkv * blocks + local * nt;
+            const int seg = s * p.hkv * blocks + local;
+            bm = m % RO;
+            b0 = first / chunk;
+            nb = (first + nt - 1) / chunk + 1 - b0;
+            b0 += seg;
+        }
     }
     const size_t rows = shared_slots(p.n_prefixes, p.fan, p.hkv, Mt, RS, wgs) * RS;
-    const float2 *ml_a = p.part_ml + am, *ml_b = p.part_ml + rows + bm;
-    const float *o_a = p.part_o + (size_t)am * D + d0, *o_b = p.part_o + (rows + bm) * D + d0;
-    float mx = -INFINITY;
-    for (int i = a0; i < a1; ++i) mx = fmaxf(mx, ml_a[(size_t)i * RS].x);
-    for (int i = b0; i < b1; ++i) mx = fmaxf(mx, ml_b[(size_t)i * RO].x);
+    float mx = -INFINITY, L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float L = 0.f;
-    auto add = [&](float2 ml, const float *o) {
-        const float f = ml.x == -INFINITY ? 0.f : ml.y * __builtin_amdgcn_exp2f(ml.x - mx);
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(o);
+    for (int i0 = group; i0 < na + nb; i0 += groups * BATCH) {
+        float2 ml[BATCH];
+        f32x4 o[BATCH];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] += f * v[i];
-        L += f;
-    };
-#pragma unroll 4
-    for (int i = a0; i < a1; ++i) add(ml_a[(size_t)i * RS], o_a + (size_t)i * RS * D);
-#pragma unroll 4
-    for (int i = b0; i < b1; ++i) add(ml_b[(size_t)i * RO], o_b + (size_t)i * RO * D);
+        for (int k = 0; k < BATCH; ++k) {
+            const int i = min(i0 + k * groups, na + nb - 1);
+            const size_t at = i < na ? (size_t)(a0 + i) * RS + am : rows + (size_t)(b0 + i - na) * RO + bm;
+            ml[k] = p.part_ml[at];
+            o[k] = *reinterpret_cast<const f32x4 *>(p.part_o + at * D + d0);
+            if (i0 + k * groups >= na + nb) ml[k] = make_float2(-INFINITY, 0.f);
+        }
+        float top = mx;
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) top = fmaxf(top, ml[k].x);
+        if (top == -INFINITY) continue;
+        const float old = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - top);
+        L *= old;
+        acc *= old;
+        mx = top;
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const float f = ml[k].x == -INFINITY ? 0.f : ml[k].y * __builtin_amdgcn_exp2f(ml[k].x - mx);
+            acc += f * o[k];
+            L += f;
+        }
+    }
+    if (groups > 1) {   // uniform
+        acc_s[threadIdx.x] = acc;
+        if (d0 == 0) ml_s[unit] = make_float2(mx, L);
+        __syncthreads();
+        if (group != 0) return;
+        float top = -INFINITY;
+        for (int k = 0; k < groups; ++k) top = fmaxf(top, ml_s[unit + k].x);
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        L = 0.f;
+        for (int k = 0; k < groups; ++k) {
+            const float2 ml = ml_s[unit + k];
+            const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+            acc += f * acc_s[threadIdx.x + k * TPR];
+            L += f * ml.y;
+        }
+    }
+    if (!wanted) return;
     const float inv = L > 0.f ? 1.f / L : 0.f;   // a row that sees no key is zero
     bf16x4 o;
 #pragma unroll
@@ -559,14 +606,17 @@ hipError_t launch_branch_attention(const BranchParams &p, hipStream_t s)
     const int Mt = p.G * p.Bt, cbs = p.prefix_len > 0 ? col_blocks(p.fan * Mt) : 1, cbo = col_blocks(Mt);
     const int wgs = p.cus;
     const int64_t rows = (int64_t)p.n_seqs * p.hkv * Mt;
-    const int per = 256 / (p.D / 4);
+    const int units = 256 / (p.D / 4);
+    int groups = 1;   // as many as the chip's threads hold at once, and no more than a workgroup
+    while (groups < units && rows * (p.D / 4) * groups * 2 <= (int64_t)p.cus * 2048) groups *= 2;
+    const int per = units / groups;
     const dim3 merge_grid((unsigned)((rows + per - 1) / per));
 #define KD_GO(D, S, O)                                                                                        \
     {                                                                                                         \
         hipLaunchKernelGGL((branch_main_kernel<D, S, O>), dim3(wgs), dim3(64 * NW), 0, s, p);                 \
         const hipError_t e = hipGetLastError();                                                               \
         if (e != hipSuccess) return e;                                                                        \
-        hipLaunchKernelGGL((branch_merge_kernel<D, S, O>), merge_grid, dim3(256), 0, s, p, wgs);              \
+        hipLaunchKernelGGL((branch_merge_kernel<D, S, O>), merge_grid, dim3(256), 0, s, p, wgs, groups);              \
         return hipGetLastError();                                                                             \
     }
 #define KD_GO_D(D)                                    \
