@@ -73,9 +73,9 @@ __device__ __forceinline__ int own_rows(const BranchParams &p, int s)
 
 // How the work is cut (uniform; the merge reads it from BranchParams::plan)
 struct Plan {
-    int shared_wgs, shared_chunk;   // workgroups of the shared part, tiles each takes
-    int own_chunk;                  // tiles a wave of the own part takes
-    int shared_tiles, own_tiles;
+    int shared_wgs;                // workgroups of the shared part; task t of its list is done by workgroup t % shared_wgs
+    int shared_segs, splits;       // (prompt, head, block of rows) segments, and pieces of each: piece k of segment g is task k segs + g
+    int own_tiles, own_chunk;      // tiles of the own part; how many of them a wave takes
 };
 
 // One wave's state of a block of 16 x CB query rows: column c16 of block cb is query row 16 cb + c16
@@ -97,83 +97,132 @@ struct State {
     }
 };
 
-// 16-byte units of a V row in LDS are permuted so that what a transposing read gathers lies in different banks
+// 16-byte units of a V row in LDS are permuted so that what a transposing read gathers lies in different banks, those of a K row so
+// that the 16 rows of an operand read do
 template <int D>
 __device__ __forceinline__ int v_swizzle(int row)
 {
     constexpr int UPR = D / 8, VSW = UPR / 4;
     return UPR == 16 ? (VSW * (row & 3)) ^ (2 * ((row >> 2) & 1)) : VSW * (row & 3);
 }
-
-// One tile: kr, vr hold its rows (V's are moved to the wave's piece of LDS first; `refill` then requests the next tile's).
-// Logits S^T = K Q^T: element i of s[cb][kg] is key 16 kg + 4 g + i of query row 16 cb + c16; `mask(s)` sets those that are not
-// seen to -inf.  Outputs O^T += V^T P^T: the keys are enumerated in accumulator order, and two transposing reads fetch exactly those.
-// The weights go into the second product as two bf16 numbers, rounded value and rest (16 bits in all): rounded to one, their error
-// alone would be as large as the output's own rounding, and these products do not bound the kernel.
-template <int D, int CB, class Refill, class Mask>
-__device__ __forceinline__ void tile_step(State<D, CB> &st, u32x4 (&kr)[2][D / 32], u32x4 (&vr)[TK * D / 512], unsigned char *vt, float scale_log2e,
-                                          int lane, Refill refill, Mask mask)
+template <int D>
+__device__ __forceinline__ int k_swizzle(int row)
 {
-    constexpr int NC = D / 32, NDB = D / 16, UPR = D / 8, ROWB = D * 2, RPL = 64 / UPR, NV = TK / RPL;
+    return D == 128 ? row & 15 : (row >> 1) & 7;
+}
+
+// A tile of 32 keys in three steps.
+// Logits S^T = K Q^T: element i of s[cb][kg] is key 16 kg + 4 g + i of query row 16 cb + c16; key(kg, c) gives chunk c (32 columns) of the
+// lane's row of key group kg as an operand.
+template <int D, int CB, class Key>
+__device__ __forceinline__ void tile_logits(const State<D, CB> &st, f32x4 (&s)[CB][2], Key key)
+{
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) s[cb][0] = s[cb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int kg = 0; kg < 2; ++kg) {
+            const bf16x8 k = key(kg, c);
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) s[cb][kg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, st.q[cb][c], s[cb][kg], 0, 0, 0);
+        }
+}
+
+__device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // (fmaxf would quiet both first)
+
+// Weights 2^(s - m) of one block of rows.  They go into the second product as two bf16 numbers, the upper half of the float and the
+// rest (16 bits in all): rounded to one, their error alone would be as large as the output's own rounding.
+template <int D, int CB>
+__device__ __forceinline__ void tile_weights(State<D, CB> &st, const f32x4 (&s)[2], int cb, float scale_log2e, bf16x8 &ph, bf16x8 &pl)
+{
+    const float top = max2(max2(max2(s[0][0], s[0][1]), max2(s[0][2], s[0][3])), max2(max2(s[1][0], s[1][1]), max2(s[1][2], s[1][3])));
+    if (__builtin_amdgcn_ballot_w64(top * scale_log2e > st.m[cb] + RESCALE_SLACK) != 0) {   // rare: the reference moves
+        const float mx = max_over_rows(top) * scale_log2e;
+        const bool need = mx > st.m[cb] + RESCALE_SLACK;
+        const float alpha = need ? __builtin_amdgcn_exp2f(st.m[cb] - mx) : 1.f;
+        st.m[cb] = need ? mx : st.m[cb];
+        st.l[cb] *= alpha;
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st.o[cb][db][i] *= alpha;
+    }
+    const float nm = st.m[cb] == -INFINITY ? 0.f : -st.m[cb];
+    uint32_t w[8];
+    u32x4 hi;
+    float l[4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(__builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], scale_log2e, nm)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        l[i] = __uint_as_float(w[2 * i]) + __uint_as_float(w[2 * i + 1]);
+        hi[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302);   // upper halves of both
+        pl[2 * i] = (__bf16)(__uint_as_float(w[2 * i]) - __uint_as_float(w[2 * i] & 0xFFFF0000u));
+        pl[2 * i + 1] = (__bf16)(__uint_as_float(w[2 * i + 1]) - __uint_as_float(w[2 * i + 1] & 0xFFFF0000u));
+    }
+    ph = __builtin_bit_cast(bf16x8, hi);
+    st.l[cb] += (l[0] + l[1]) + (l[2] + l[3]);
+}
+
+// Outputs O^T += V^T P^T: the keys are enumerated in accumulator order (k-slot 8 g + i is key 4 g + i for i < 4 and 16 + 4 g + i - 4
+// otherwise), and two transposing reads fetch exactly those.
+template <int D>
+__device__ __forceinline__ bf16x8 value_operand(const unsigned char *vt, int lane, int db)
+{
     const int c16 = lane & 15, g = lane >> 4;
+    const int rd_row = 4 * g + (c16 >> 2), rd_unit = ((c16 & 3) >> 1) ^ v_swizzle<D>(rd_row);   // (rows + 16 have the same swizzle)
+    const unsigned char *ap = vt + rd_row * (2 * D) + (c16 & 1) * 8 + (((2 * db) ^ rd_unit) * 16);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)(ap));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)(ap + 16 * (2 * D)));
+    return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+template <int D, int CB>
+__device__ __forceinline__ void tile_outputs(State<D, CB> &st, int db, bf16x8 va, const bf16x8 (&ph)[CB], const bf16x8 (&pl)[CB])
+{
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) st.o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, ph[cb], st.o[cb][db], 0, 0, 0);
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) st.o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl[cb], st.o[cb][db], 0, 0, 0);
+}
+
+// The three in turn; `between` runs once the keys have been used, `mask(s)` sets logits that are not seen to -inf.
+template <int D, int CB, class Key, class Between, class Mask>
+__device__ __forceinline__ void tile_step(State<D, CB> &st, const unsigned char *vt, float scale_log2e, int lane, Key key, Between between, Mask mask)
+{
+    f32x4 s[CB][2];
+    tile_logits<D, CB>(st, s, key);
+    between();
+    mask(s);
+    bf16x8 ph[CB], pl[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) tile_weights<D, CB>(st, s[cb], cb, scale_log2e, ph[cb], pl[cb]);
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) tile_outputs<D, CB>(st, db, value_operand<D>(vt, lane, db), ph, pl);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// Logits of keys from `seen` on (counted from the tile's first) to -inf
+template <int CB>
+__device__ __forceinline__ void hide_from(f32x4 (&s)[CB][2], int seen, int g)
+{
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[cb][kg][i] = 16 * kg + 4 * g + i < seen ? s[cb][kg][i] : -INFINITY;
+}
+
+// A V tile from registers to the wave's own piece of LDS
+template <int D>
+__device__ __forceinline__ void store_v(unsigned char *vt, const u32x4 (&vr)[TK * D / 512], int lane)
+{
+    constexpr int UPR = D / 8, ROWB = D * 2, RPL = 64 / UPR, NV = TK / RPL;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int row = lane / UPR + RPL * i;
         *reinterpret_cast<u32x4 *>(vt + row * ROWB + (((lane % UPR) ^ v_swizzle<D>(row)) * 16)) = vr[i];
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    f32x4 s[CB][2];
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) s[cb][0] = s[cb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int kg = 0; kg < 2; ++kg)
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb)
-                s[cb][kg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[kg][c]), st.q[cb][c], s[cb][kg], 0, 0, 0);
-    refill();
-    mask(s);
-    bf16x8 ph[CB], pl[CB];
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        float mx = fmaxf(fmaxf(fmaxf(s[cb][0][0], s[cb][0][1]), fmaxf(s[cb][0][2], s[cb][0][3])),
-                         fmaxf(fmaxf(s[cb][1][0], s[cb][1][1]), fmaxf(s[cb][1][2], s[cb][1][3])));
-        mx = max_over_rows(mx) * scale_log2e;
-        const bool need = mx > st.m[cb] + RESCALE_SLACK;
-        if (__builtin_amdgcn_ballot_w64(need) != 0) {
-            const float alpha = need ? __builtin_amdgcn_exp2f(st.m[cb] - mx) : 1.f;
-            st.m[cb] = need ? mx : st.m[cb];
-            st.l[cb] *= alpha;
-#pragma unroll
-            for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) st.o[cb][db][i] *= alpha;
-        }
-        const float nm = st.m[cb] == -INFINITY ? 0.f : -st.m[cb];
-#pragma unroll
-        for (int kg = 0; kg < 2; ++kg)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[cb][kg][i], scale_log2e, nm));
-                st.l[cb] += w;
-                const __bf16 hi = (__bf16)w;
-                ph[cb][4 * kg + i] = hi;
-                pl[cb][4 * kg + i] = (__bf16)(w - (float)hi);
-            }
-    }
-    const int rd_row = 4 * g + (c16 >> 2), rd_unit = ((c16 & 3) >> 1) ^ v_swizzle<D>(rd_row);   // (rows + 16 have the same swizzle)
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) {
-        const unsigned char *ap = vt + rd_row * ROWB + (c16 & 1) * 8 + (((2 * db) ^ rd_unit) * 16);
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)(ap));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)(ap + 16 * ROWB));
-        const bf16x8 va = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            st.o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, ph[cb], st.o[cb][db], 0, 0, 0);
-            st.o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl[cb], st.o[cb][db], 0, 0, 0);
-        }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
@@ -184,23 +233,43 @@ __device__ __forceinline__ const uint16_t *query_row(const BranchParams &p, int 
     return p.q.p + (int64_t)s * p.q.seq + (int64_t)(h * p.G + m / p.Bt) * p.q.head + (int64_t)(m % p.Bt) * p.q.token;
 }
 
-// The shared part: one workgroup, its piece of the list
+// A task of the shared part: piece k of segment (prompt c, head h, block mb of rows).  Blocks of the same rows of the cache lie n_prefixes
+// hkv tasks apart: with eight KV heads on the same XCD, whose L2 then serves all but one of them.
+struct Segment {
+    int ch, mb, c, h, k;
+};
+__device__ __forceinline__ Segment segment_of(const BranchParams &p, int task, int segs)
+{
+    Segment s;
+    const int heads = p.n_prefixes * p.hkv;
+    s.k = task / segs;
+    const int g = task - s.k * segs;
+    s.mb = g / heads;
+    s.ch = g - s.mb * heads;
+    s.c = s.ch / p.hkv;
+    s.h = s.ch - s.c * p.hkv;
+    return s;
+}
+
+// Floats from one row of a wave's outputs in LDS to the next: four more than the row, so that the 16 rows that a store touches lie in
+// different banks (without them such a store took sixteen turns, and the join of the eight waves 5.6 us)
+template <int D>
+constexpr int OUT_PITCH = D + 4;
+
+// The shared part with at most 32 query rows: one workgroup, its piece of the list, every wave tiles of its own
 template <int D, int CB>
-__device__ void shared_part(const BranchParams &p, const Plan &plan, unsigned char *smem)
+__device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned char *smem)
 {
     constexpr int NC = D / 32, NDB = D / 16, UPR = D / 8, ROWB = D * 2, RPL = 64 / UPR, NV = TK / RPL, R = 16 * CB;
     __shared__ float2 ml_s[NW][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c16 = lane & 15, g = lane >> 4;
-    const int Mt = p.G * p.Bt, M = p.fan * Mt, blocks = (M + R - 1) / R, nt = (p.prefix_len + TK - 1) / TK;
-    int at = (int)blockIdx.x * plan.shared_chunk;
-    const int end = min(at + plan.shared_chunk, plan.shared_tiles);
+    const int Mt = p.G * p.Bt, M = p.fan * Mt, nt = (p.prefix_len + TK - 1) / TK;
     unsigned char *vt = smem + (size_t)wave * TK * ROWB;
     float *outs = reinterpret_cast<float *>(smem);   // the waves' outputs of one block of 16 rows, where their V tiles were
-    while (at < end) {
-        const int seg = at / nt, t0 = at - seg * nt, t1 = min(nt, t0 + end - at);
-        at += t1 - t0;
-        const int ch = seg / blocks, mb = seg - ch * blocks, c = ch / p.hkv, h = ch - c * p.hkv;
+    for (int task = blockIdx.x; task < plan.shared_segs * plan.splits; task += plan.shared_wgs) {
+        const Segment sg = segment_of(p, task, plan.shared_segs);
+        const int ch = sg.ch, mb = sg.mb, c = sg.c, h = sg.h, stride = plan.splits * NW;
         const uint16_t *kh = p.k_prefix + (size_t)ch * p.prefix_cap * D, *vh = p.v_prefix + (size_t)ch * p.prefix_cap * D;
         State<D, CB> st;
         st.reset();
@@ -219,8 +288,8 @@ __device__ void shared_part(const BranchParams &p, const Plan &plan, unsigned ch
             for (int i = 0; i < NV; ++i)
                 vr[i] = *reinterpret_cast<const u32x4 *>(vh + (size_t)min(t * TK + i * RPL + lane / UPR, p.prefix_len - 1) * D + (lane % UPR) * 8);
         };
-        int t = t0 + wave;
-        if (t < t1) {
+        int t = sg.k * NW + wave;
+        if (t < nt) {
             load_k(t);
             load_v(t);
         }
@@ -231,36 +300,29 @@ __device__ void shared_part(const BranchParams &p, const Plan &plan, unsigned ch
 #pragma unroll
             for (int cc = 0; cc < NC; ++cc) st.q[cb][cc] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qr + cc * 32));
         }
-        for (; t < t1; t += NW) {
+        for (; t < nt; t += stride) {
+            store_v<D>(vt, vr, lane);
             tile_step<D, CB>(
-                st, kr, vr, vt, p.scale_log2e, lane,
+                st, vt, p.scale_log2e, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); },
                 [&]() {
-                    if (t + NW < t1) {
-                        load_k(t + NW);
-                        load_v(t + NW);
+                    if (t + stride < nt) {
+                        load_k(t + stride);
+                        load_v(t + stride);
                     }
                 },
                 [&](f32x4 (&s)[CB][2]) {
-                    if ((t + 1) * TK > p.prefix_len) {   // uniform
-                        const int lim = p.prefix_len - t * TK - 4 * g;
-#pragma unroll
-                        for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-                            for (int kg = 0; kg < 2; ++kg)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) s[cb][kg][i] = 16 * kg + i < lim ? s[cb][kg][i] : -INFINITY;
-                    }
+                    if ((t + 1) * TK > p.prefix_len) hide_from<CB>(s, p.prefix_len - t * TK, g);   // uniform
                 });
         }
         // the eight results become one, a block of 16 rows at a time
-        const size_t slot = (size_t)blockIdx.x + seg;
+        const size_t slot = task;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             const float l = sum_over_rows(st.l[cb]);
             __syncthreads();
-            float *ow = outs + (size_t)wave * 16 * D;
+            float *ow = outs + (size_t)wave * 16 * OUT_PITCH<D>;
 #pragma unroll
-            for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(ow + c16 * D + 16 * db + 4 * g) = st.o[cb][db];
+            for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(ow + c16 * OUT_PITCH<D> + 16 * db + 4 * g) = st.o[cb][db];
             if (g == 0) ml_s[wave][c16] = make_float2(st.m[cb], l);
             __syncthreads();
             const int rows = min(16, M - mb * R - 16 * cb);
@@ -275,7 +337,7 @@ __device__ void shared_part(const BranchParams &p, const Plan &plan, unsigned ch
                 for (int w = 0; w < NW; ++w) {
                     const float2 ml = ml_s[w][m];
                     const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - mx);
-                    const f32x4 o = *reinterpret_cast<const f32x4 *>(outs + ((size_t)w * 16 + m) * D + d0);
+                    const f32x4 o = *reinterpret_cast<const f32x4 *>(outs + ((size_t)w * 16 + m) * OUT_PITCH<D> + d0);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[i] += f * o[i];
                     L += f * ml.y;
@@ -288,6 +350,228 @@ __device__ void shared_part(const BranchParams &p, const Plan &plan, unsigned ch
             }
         }
         __syncthreads();   // the outputs are read before the next segment's V tiles overwrite them
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void wait_copies()   // at most N of this wave's copies still in flight
+{
+    static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+}
+
+// LDS of the shared part with many query rows: a ring of stages, each a tile of K and V for every group of waves
+template <int D, int RW>
+constexpr int stage_bytes() { return NW / RW * 2 * TK * D * 2; }
+constexpr int stages_of(int RW) { return RW; }
+
+// The shared part with 32 RW query rows (RW 2, 4 or 8) a workgroup: RW waves of 32 rows each work on the same tile, NW / RW groups of
+// them on different tiles.  The tiles come into LDS once for all waves, by asynchronous copies (no registers) that run ahead of
+// their use through a ring.  Where every wave read its own keys, 256 sequences of three query heads to a KV
+// head read the shared rows 24 times, and of that traffic, 5.7 TB/s past the L2s, came all the time: 120 us.
+// RW 4 and 8: the two waves of a SIMD take turns.  One is on the matrix pipe (outputs of the tile before, logits of this one) while the
+// other forms its weights on the vector ALU, and barriers keep them half a step apart: in step with one another both want the same
+// pipe at the same time, and a tile took 1.6 us where the longer of the two pipes needs 0.7.
+template <int D, int RW>
+__device__ void shared_many(const BranchParams &p, const Plan &plan, unsigned char *smem)
+{
+    constexpr int NC = D / 32, NDB = D / 16, UPR = D / 8, ROWB = D * 2, R = 32 * RW, KW = NW / RW, CB = 2;
+    constexpr int TILEB = TK * ROWB, STAGEB = stage_bytes<D, RW>(), NS = stages_of(RW);
+    constexpr int RPC = 1024 / ROWB, CPT = TILEB / 1024;   // rows of a copy (64 lanes x 16 bytes), copies of a tile
+    constexpr int CPW = KW * 2 * CPT / NW;                 // copies of a stage a wave issues
+    static_assert(KW * 2 * CPT % NW == 0 && CPW >= 1, "the copies of a stage are dealt evenly");
+    __shared__ float2 ml_s[NW][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c16 = lane & 15, g = lane >> 4, rw = wave % RW, kw = wave / RW;
+    const int Mt = p.G * p.Bt, M = p.fan * Mt, nt = (p.prefix_len + TK - 1) / TK, units = (nt + KW - 1) / KW;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
+    for (int task = blockIdx.x; task < plan.shared_segs * plan.splits; task += plan.shared_wgs) {
+        const Segment sg = segment_of(p, task, plan.shared_segs);
+        const int ch = sg.ch, mb = sg.mb, c = sg.c, h = sg.h;
+        const uint16_t *kh = p.k_prefix + (size_t)ch * p.prefix_cap * D, *vh = p.v_prefix + (size_t)ch * p.prefix_cap * D;
+        const int m0 = mb * R + 32 * rw;   // the wave's first query row
+        const bool active = m0 < M;        // uniform in the wave: else it only copies
+        const int steps = (units - sg.k + plan.splits - 1) / plan.splits;
+        // stage `it` of the piece (one behind its end repeats rows that exist: what a wave waits for stays the same number of copies)
+        auto issue = [&](int it) {
+#pragma unroll
+            for (int i = 0; i < CPW; ++i) {
+                const int id = wave + NW * i, grp = id / (2 * CPT), part = id % (2 * CPT), isv = part >= CPT, r0 = part % CPT * RPC;
+                const int row = r0 + lane / UPR, unit = lane % UPR;
+                const int key = min(((sg.k + it * plan.splits) * KW + grp) * TK + row, p.prefix_len - 1);
+                const uint16_t *src = (isv ? vh : kh) + (size_t)key * D + (unit ^ (isv ? v_swizzle<D>(row) : k_swizzle<D>(row))) * 8;
+                lds_copy16(lds0 + (uint32_t)((it % NS) * STAGEB + grp * 2 * TILEB + isv * TILEB + r0 * ROWB), src);
+            }
+        };
+        // The query rows are requested behind the first copies, and waited for here: where the compiler finds them used (in the loop) it
+        // would wait in every step, and with them for all copies, which it does not count.
+        constexpr int FIRST = NS > 3 ? 2 : 1;
+#pragma unroll
+        for (int it = 0; it < FIRST; ++it) issue(it);
+        State<D, CB> st;
+        st.reset();
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            const int m = min(m0 + 16 * cb + c16, M - 1);
+            const uint16_t *qr = query_row(p, c * p.fan + m / Mt, h, m % Mt) + 8 * g;
+#pragma unroll
+            for (int cc = 0; cc < NC; ++cc) st.q[cb][cc] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qr + cc * 32));
+        }
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int cc = 0; cc < NC; ++cc) asm volatile("" : "+v"(st.q[cb][cc]));
+        auto key_operand = [&](const unsigned char *kt, int kg, int cc) {
+            const int row = 16 * kg + c16;
+            return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(kt + row * ROWB + (((4 * cc + g) ^ k_swizzle<D>(row)) * 16)));
+        };
+        auto tile_of = [&](int it) { return (sg.k + it * plan.splits) * KW + kw; };
+        auto lds_of = [&](int it) { return smem + (it % NS) * STAGEB + kw * 2 * TILEB; };
+        if constexpr (RW == 2) {
+#pragma unroll
+            for (int it = FIRST; it < NS - 1; ++it) issue(it);
+            for (int it = 0; it < steps; ++it) {
+                wait_copies<CPW *(NS - 2)>();   // this wave's part of stage `it` has landed
+                __syncthreads();                // ... and every wave's, and nobody reads the stage before it any more
+                issue(it + NS - 1);
+                const int t = tile_of(it);
+                if (!active || t >= nt) continue;   // uniform in the wave
+                const unsigned char *kt = lds_of(it);
+                tile_step<D, CB>(
+                    st, kt + TILEB, p.scale_log2e, lane, [&](int kg, int cc) { return key_operand(kt, kg, cc); }, [&]() {},
+                    [&](f32x4 (&s)[CB][2]) {
+                        if ((t + 1) * TK > p.prefix_len) hide_from<CB>(s, p.prefix_len - t * TK, g);   // uniform
+                    });
+            }
+        } else {
+            // Half steps, a barrier behind each: in 2 it the first four waves multiply for step `it` and the others weigh step it - 1, in
+            // 2 it + 1 the other way round.  Multiplying for step `it` reads K of stage `it` and V of stage it - 1, so stage it - 2 is free
+            // once the others are through with step it - 1: behind half step 2 it - 1.
+            static_assert(NS >= 4, "two stages in use, one landing");
+            const bool late = wave >= 4;
+            f32x4 s[CB][2];
+            bf16x8 ph[CB], pl[CB];
+            // (the order is pinned: operands are requested a group of products ahead of the one that uses them)
+            bf16x8 va[NDB], ka[2][2];
+            auto request_keys = [&](const unsigned char *kt, int cc) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int kg = 0; kg < 2; ++kg) ka[i][kg] = key_operand(kt, kg, cc + i);
+            };
+            auto multiply = [&](int it) {
+                issue(it + NS - 2);
+                if (!active) return;
+                const unsigned char *kt = lds_of(it), *vt = lds_of(it - 1 + NS) + TILEB;
+                if (it > 0) {
+#pragma unroll
+                    for (int db = 0; db < NDB; ++db) va[db] = value_operand<D>(vt, lane, db);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int db = 0; db < NDB / 2; ++db) tile_outputs<D, CB>(st, db, va[db], ph, pl);
+                    request_keys(kt, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int db = NDB / 2; db < NDB; ++db) tile_outputs<D, CB>(st, db, va[db], ph, pl);
+                } else {
+                    request_keys(kt, 0);
+                }
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) s[cb][0] = s[cb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int cc = 0; cc < NC; cc += 2) {
+                    bf16x8 now[2][2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int kg = 0; kg < 2; ++kg) now[i][kg] = ka[i][kg];
+                    if (cc + 2 < NC) request_keys(kt, cc + 2);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+                            for (int cb = 0; cb < CB; ++cb)
+                                s[cb][kg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now[i][kg], st.q[cb][cc + i], s[cb][kg], 0, 0, 0);
+                }
+            };
+            auto weigh = [&](int it) {
+                if (active) {
+                    const int t = tile_of(it);
+                    if ((t + 1) * TK > p.prefix_len) hide_from<CB>(s, p.prefix_len - t * TK, g);   // uniform; a tile behind the last: all of it
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb) tile_weights<D, CB>(st, s[cb], cb, p.scale_log2e, ph[cb], pl[cb]);
+                }
+            };
+#pragma unroll
+            for (int it = FIRST; it < NS - 2; ++it) issue(it);
+            wait_copies<CPW *(NS - 3)>();   // this wave's part of stage 0 has landed
+            __syncthreads();
+            if (late) __syncthreads();
+            for (int it = 0; it < steps; ++it) {
+                multiply(it);
+                if (late) wait_copies<CPW *(NS - 3)>();   // ... of stage it + 1
+                __syncthreads();
+                weigh(it);
+                if (!late) wait_copies<CPW *(NS - 3)>();
+                __syncthreads();
+            }
+            if (!late) __syncthreads();
+            if (active) {
+                const unsigned char *vt = lds_of(steps - 1) + TILEB;
+#pragma unroll
+                for (int db = 0; db < NDB; ++db) tile_outputs<D, CB>(st, db, value_operand<D>(vt, lane, db), ph, pl);
+            }
+        }
+        wait_copies<0>();   // (of stages behind the end)
+        const size_t slot = task;
+        if constexpr (KW == 1) {
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                const float L = sum_over_rows(st.l[cb]), inv = L > 0.f ? 1.f / L : 0.f;
+                if (m0 + 16 * cb + c16 < M) {
+                    const size_t r = slot * R + 32 * rw + 16 * cb + c16;
+#pragma unroll
+                    for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(p.part_o + r * D + 16 * db + 4 * g) = st.o[cb][db] * inv;
+                    if (g == 0) p.part_ml[r] = make_float2(st.m[cb], L);
+                }
+            }
+            __syncthreads();   // every wave's copies have landed and its reads are done: the ring is free
+        } else {
+            // the results of the groups become one, a block of 16 rows of every row wave at a time
+            float *outs = reinterpret_cast<float *>(smem);
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                const float l = sum_over_rows(st.l[cb]);
+                __syncthreads();
+                float *ow = outs + (size_t)wave * 16 * OUT_PITCH<D>;
+#pragma unroll
+                for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(ow + c16 * OUT_PITCH<D> + 16 * db + 4 * g) = st.o[cb][db];
+                if (g == 0) ml_s[wave][c16] = make_float2(st.m[cb], l);
+                __syncthreads();
+                for (int it = tid; it < RW * 16 * (D / 4); it += 64 * NW) {
+                    const int w0 = it / (16 * (D / 4)), m = it / (D / 4) % 16, d0 = it % (D / 4) * 4;
+                    if (mb * R + 32 * w0 + 16 * cb + m >= M) continue;
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int k = 0; k < KW; ++k) mx = fmaxf(mx, ml_s[w0 + k * RW][m].x);
+                    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+                    float L = 0.f;
+#pragma unroll
+                    for (int k = 0; k < KW; ++k) {
+                        const float2 ml = ml_s[w0 + k * RW][m];
+                        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - mx);
+                        acc += f * *reinterpret_cast<const f32x4 *>(outs + ((size_t)(w0 + k * RW) * 16 + m) * OUT_PITCH<D> + d0);
+                        L += f * ml.y;
+                    }
+                    const size_t r = slot * R + 32 * w0 + 16 * cb + m;
+                    *reinterpret_cast<f32x4 *>(p.part_o + r * D + d0) = acc * (L > 0.f ? 1.f / L : 0.f);
+                    if (d0 == 0) p.part_ml[r] = make_float2(mx, L);
+                }
+            }
+            __syncthreads();   // the outputs are read before the next segment's tiles overwrite them
+        }
     }
 }
 
@@ -394,8 +678,9 @@ __device__ void own_part(const BranchParams &p, const Plan &plan, int own_wave, 
         look_up(t0 + 1);
         for (int t = t0; t < t1; ++t) {
             const uint32_t hidden = absent;
+            store_v<D>(vt, vr, lane);
             tile_step<D, CB>(
-                st, kr, vr, vt, p.scale_log2e, lane,
+                st, vt, p.scale_log2e, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); },
                 [&]() {
                     if (t + 1 < t1) {
                         load(t + 1);
@@ -431,16 +716,30 @@ __device__ void own_part(const BranchParams &p, const Plan &plan, int own_wave, 
     }
 }
 
-// Slots of the shared part at most: one per workgroup and segment end
+// Slots of the shared part at most: one per task
 __host__ __device__ inline size_t shared_slots(int n_prefixes, int fan, int hkv, int Mt, int R, int wgs)
 {
-    return (size_t)n_prefixes * hkv * ((fan * Mt + R - 1) / R) + wgs;
+    const size_t segs = (size_t)n_prefixes * hkv * ((fan * Mt + R - 1) / R);
+    return 2 * segs > (size_t)wgs ? 2 * segs : wgs;
 }
 
-template <int D, int CBS, int CBO>
+// RS, RO: query rows of a block of the shared and of the own part
+template <int D, int RS>
+constexpr int lds_bytes()
+{
+    constexpr int waves = NW * 16 * OUT_PITCH<D> * 4;   // the outputs of the waves' 16 rows; a piece of V for every wave is a little less
+    static_assert(waves >= NW * TK * D * 2, "");
+    if constexpr (RS > 32) {
+        constexpr int ring = stages_of(RS / 32) * stage_bytes<D, RS / 32>();
+        return ring > waves ? ring : waves;
+    }
+    return waves;
+}
+
+template <int D, int RS, int RO>
 __global__ __launch_bounds__(64 * NW) void branch_main_kernel(BranchParams p)
 {
-    __shared__ __attribute__((aligned(16))) unsigned char smem[NW * TK * D * 2];
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[lds_bytes<D, RS>()];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int Mt = p.G * p.Bt, M = p.fan * Mt;
     const int wgs = (int)gridDim.x;
@@ -448,23 +747,46 @@ __global__ __launch_bounds__(64 * NW) void branch_main_kernel(BranchParams p)
     Plan plan;
     int own = 0;
     for (int base = 0; base < p.n_seqs; base += 64) own += base + lane < p.n_seqs ? (own_rows(p, base + lane) + TK - 1) / TK : 0;
-    plan.own_tiles = __builtin_amdgcn_readfirstlane(wave_sum(own)) * p.hkv * ((Mt + 16 * CBO - 1) / (16 * CBO));
-    plan.shared_tiles = (p.prefix_len + TK - 1) / TK * p.n_prefixes * p.hkv * ((M + 16 * CBS - 1) / (16 * CBS));
+    plan.own_tiles = __builtin_amdgcn_readfirstlane(wave_sum(own)) * p.hkv * ((Mt + RO - 1) / RO);
     {
-        const float s = (float)plan.shared_tiles, o = (float)plan.own_tiles;
-        int w = s > 0.f ? (int)(wgs * (s / (s + o)) + 0.5f) : 0;
-        if (plan.shared_tiles > 0) w = max(w, 1);
-        if (plan.own_tiles > 0) w = min(w, wgs - 1);
-        plan.shared_chunk = w > 0 ? (plan.shared_tiles + w - 1) / w : 1;
-        plan.shared_wgs = (plan.shared_tiles + plan.shared_chunk - 1) / plan.shared_chunk;
+        constexpr int KW = RS > 32 ? NW / (RS / 32) : NW;   // tiles that a workgroup of the shared part works on at a time
+        const int nt = (p.prefix_len + TK - 1) / TK, units = (nt + KW - 1) / KW;
+        plan.shared_segs = nt > 0 ? p.n_prefixes * p.hkv * ((M + RS - 1) / RS) : 0;
+        // No piece leaves its segment: the start and the end of a segment cost a workgroup several tiles' time.  Every lane prices one way to
+        // deal the workgroups -- `splits` pieces of each segment, or with more segments than workgroups a share of the workgroups for
+        // whole or halved segments -- and the cheapest is taken.  Prices in us, of a tile step that is not held up by the others' traffic
+        // (STEP: measured; OWN_STEP likewise, of a wave); where traffic is the limit the shares hardly matter.
+        constexpr float STEP = RS == 256 ? 0.8f : RS == 128 ? 1.3f : RS == 64 ? 2.2f : 2.5f, SHARED_FIXED = 6.f, OWN_STEP = 2.5f;
+        const int segs = plan.shared_segs, most = plan.own_tiles > 0 ? wgs - 1 : wgs;
+        int w = 0, splits = 1;
+        float price = INFINITY;
+        if (segs > 0 && segs <= most) {
+            const int top = min(most / segs, units);
+            splits = min((lane + 1) * ((top + 63) / 64), top);
+            w = segs * splits;
+            price = (float)((units + splits - 1) / splits) * STEP;
+        } else if (segs > 0) {
+            w = max(most * (lane + 1) / 64, 1);
+            const float whole = (float)((segs + w - 1) / w) * ((float)units * STEP + SHARED_FIXED);
+            const float half = (float)((2 * segs + w - 1) / w) * ((float)((units + 1) / 2) * STEP + SHARED_FIXED);
+            splits = units > 1 && half < whole ? 2 : 1;
+            price = fminf(whole, half);
+        }
+        const int others = (wgs - w) * NW;
+        price = fmaxf(price, (float)((plan.own_tiles + others - 1) / max(others, 1)) * OWN_STEP);
+        float best = price;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) best = fminf(best, __shfl_xor(best, d));
+        const int from = __builtin_ctzll(__builtin_amdgcn_ballot_w64(price == best) | 1ull << 63);
+        plan.splits = __builtin_amdgcn_readlane(splits, from);
+        plan.shared_wgs = segs > 0 ? __builtin_amdgcn_readlane(w, from) : 0;
         const int waves = max((wgs - plan.shared_wgs) * NW, 1);
         plan.own_chunk = max((plan.own_tiles + waves - 1) / waves, 1);
     }
     if (blockIdx.x == 0) {   // ... for the merge
         if (tid == 0) {
-            p.plan[0] = plan.shared_chunk;
+            p.plan[0] = plan.splits;
             p.plan[1] = plan.own_chunk;
-            p.plan[2] = plan.own_tiles;
         }
         if (wave == 0) {
             int first = 0;
@@ -482,10 +804,11 @@ __global__ __launch_bounds__(64 * NW) void branch_main_kernel(BranchParams p)
         }
     }
     if ((int)blockIdx.x < plan.shared_wgs) {
-        shared_part<D, CBS>(p, plan, smem);
+        if constexpr (RS > 32) shared_many<D, RS / 32>(p, plan, smem);
+        else shared_few<D, RS / 16>(p, plan, smem);
     } else {
-        const size_t rows = shared_slots(p.n_prefixes, p.fan, p.hkv, Mt, 16 * CBS, wgs) * (16 * CBS);
-        own_part<D, CBO>(p, plan, ((int)blockIdx.x - plan.shared_wgs) * NW + wave, p.part_o + rows * D, p.part_ml + rows,
+        const size_t rows = shared_slots(p.n_prefixes, p.fan, p.hkv, Mt, RS, wgs) * RS;
+        own_part<D, RO / 16>(p, plan, ((int)blockIdx.x - plan.shared_wgs) * NW + wave, p.part_o + rows * D, p.part_ml + rows,
                          smem + (size_t)wave * TK * D * 2);
     }
 }
@@ -493,10 +816,10 @@ __global__ __launch_bounds__(64 * NW) void branch_main_kernel(BranchParams p)
 // The join of a row's pieces: `groups` groups of D / 4 threads take a row's pieces in turn, four at a time, and join what they have
 // in LDS.  (Groups: where there are few rows and many pieces, the pieces requested one behind another were all the time this took: one
 // sequence, 8192 shared rows, 17.7 us with one group a row.)
-template <int D, int CBS, int CBO>
+template <int D, int RS, int RO>
 __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int wgs, int groups)
 {
-    constexpr int TPR = D / 4, RS = 16 * CBS, RO = 16 * CBO, BATCH = 4;
+    constexpr int TPR = D / 4, BATCH = 4;
     __shared__ f32x4 acc_s[256];
     __shared__ float2 ml_s[256 / TPR];
     const int Mt = p.G * p.Bt;
@@ -506,16 +829,15 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
     const bool exists = row < (int64_t)p.n_seqs * p.hkv * Mt;
     const int sh = exists ? (int)(row / Mt) : 0, m = exists ? (int)(row - (int64_t)sh * Mt) : 0, s = sh / p.hkv, h = sh - s * p.hkv;
     const bool wanted = exists && m % p.Bt < new_of(p, s);   // else left as it was
-    // the pieces: slots a0 .. of the shared part, b0 .. of the own part
-    int a0 = 0, na = 0, b0 = 0, nb = 0, am = 0, bm = 0;
+    // the pieces: na slots of the shared part, nb slots from b0 on of the own part
+    int a0 = 0, na = 0, segs = 0, b0 = 0, nb = 0, am = 0, bm = 0;
     if (wanted) {
         if (p.prefix_len > 0) {
-            const int c = s / p.fan, mm = (s - c * p.fan) * Mt + m, blocks = (p.fan * Mt + RS - 1) / RS, nt = (p.prefix_len + TK - 1) / TK;
-            const int seg = (c * p.hkv + h) * blocks + mm / RS, chunk = p.plan[0];
+            const int c = s / p.fan, mm = (s - c * p.fan) * Mt + m;
             am = mm % RS;
-            a0 = seg * nt / chunk;
-            na = ((seg + 1) * nt - 1) / chunk + 1 - a0;
-            a0 += seg;
+            a0 = mm / RS * p.n_prefixes * p.hkv + c * p.hkv + h;   // piece i in slot a0 + i segs
+            segs = p.n_prefixes * p.hkv * ((p.fan * Mt + RS - 1) / RS);
+            na = p.plan[0];
         }
         const int n = own_rows(p, s);
         if (n > 0) {
@@ -537,7 +859,7 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
             const int i = min(i0 + k * groups, na + nb - 1);
-            const size_t at = i < na ? (size_t)(a0 + i) * RS + am : rows + (size_t)(b0 + i - na) * RO + bm;
+            const size_t at = i < na ? ((size_t)a0 + (size_t)i * segs) * RS + am : rows + (size_t)(b0 + i - na) * RO + bm;
             ml[k] = p.part_ml[at];
             o[k] = *reinterpret_cast<const f32x4 *>(p.part_o + at * D + d0);
             if (i0 + k * groups >= na + nb) ml[k] = make_float2(-INFINITY, 0.f);
@@ -581,15 +903,23 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
     *reinterpret_cast<bf16x4 *>(p.out + (((size_t)s * p.hkv + h) * Mt + m) * D + d0) = o;
 }
 
-// Blocks of 16 query rows a wave takes: two where there are more than 16 rows
-int col_blocks(int rows) { return rows > 16 ? 2 : 1; }
+// Query rows of a block: of the own part 16, or 32 where a sequence has more; of the shared part as many waves of 32 rows as there
+// are rows for, up to eight.  Above four waves' rows, blocks of four or of eight waves, whichever leaves fewer waves without rows.
+int own_block(int64_t rows) { return rows > 16 ? 32 : 16; }
+int shared_block(int64_t rows)
+{
+    if (rows <= 32) return rows > 16 ? 32 : 16;
+    if (rows <= 64) return 64;
+    if (rows <= 128) return 128;
+    return (rows + 255) / 256 * 2 <= (rows + 127) / 128 ? 256 : 128;
+}
 
 }  // namespace
 
 size_t branch_workspace(int n_seqs, int n_prefixes, int hkv, int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_plan)
 {
-    const size_t Mt = (size_t)G * Bt, fan = n_prefixes > 0 ? (size_t)n_seqs / n_prefixes : 0;
-    const size_t RS = 16 * (size_t)col_blocks((int)(fan * Mt < 64 ? fan * Mt : 64)), RO = 16 * (size_t)col_blocks((int)(Mt < 64 ? Mt : 64));
+    const int64_t Mt = (int64_t)G * Bt, fan = n_prefixes > 0 ? n_seqs / n_prefixes : 0;
+    const size_t RS = shared_block(fan * Mt), RO = own_block(Mt);
     const size_t shared = shared_slots(n_prefixes, (int)fan, hkv, (int)Mt, (int)RS, cus) * RS;
     const size_t own = ((size_t)n_seqs * hkv * ((Mt + RO - 1) / RO) + (size_t)cus * NW) * RO;
     size_t off = (shared + own) * D * 4;
@@ -601,33 +931,43 @@ size_t branch_workspace(int n_seqs, int n_prefixes, int hkv, int G, int Bt, int 
     return off;
 }
 
+namespace {
+
+template <int D, int RS, int RO>
+hipError_t launch(const BranchParams &p, hipStream_t s)
+{
+    const int64_t rows = (int64_t)p.n_seqs * p.hkv * p.G * p.Bt;
+    const int units = 256 / (D / 4);
+    int groups = 1;   // as many as the chip's threads hold at once, and no more than a workgroup
+    while (groups < units && rows * (D / 4) * groups * 2 <= (int64_t)p.cus * 2048) groups *= 2;
+    const int per = units / groups, wgs = p.cus;
+    hipLaunchKernelGGL((branch_main_kernel<D, RS, RO>), dim3(wgs), dim3(64 * NW), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((branch_merge_kernel<D, RS, RO>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, s, p, wgs, groups);
+    return hipGetLastError();
+}
+
+template <int D, int RO>
+hipError_t launch(const BranchParams &p, int RS, hipStream_t s)
+{
+    switch (RS) {
+    case 16: return launch<D, 16, RO>(p, s);
+    case 32: return launch<D, 32, RO>(p, s);
+    case 64: return launch<D, 64, RO>(p, s);
+    case 128: return launch<D, 128, RO>(p, s);
+    default: return launch<D, 256, RO>(p, s);
+    }
+}
+
+}  // namespace
+
 hipError_t launch_branch_attention(const BranchParams &p, hipStream_t s)
 {
-    const int Mt = p.G * p.Bt, cbs = p.prefix_len > 0 ? col_blocks(p.fan * Mt) : 1, cbo = col_blocks(Mt);
-    const int wgs = p.cus;
-    const int64_t rows = (int64_t)p.n_seqs * p.hkv * Mt;
-    const int units = 256 / (p.D / 4);
-    int groups = 1;   // as many as the chip's threads hold at once, and no more than a workgroup
-    while (groups < units && rows * (p.D / 4) * groups * 2 <= (int64_t)p.cus * 2048) groups *= 2;
-    const int per = units / groups;
-    const dim3 merge_grid((unsigned)((rows + per - 1) / per));
-#define KD_GO(D, S, O)                                                                                        \
-    {                                                                                                         \
-        hipLaunchKernelGGL((branch_main_kernel<D, S, O>), dim3(wgs), dim3(64 * NW), 0, s, p);                 \
-        const hipError_t e = hipGetLastError();                                                               \
-        if (e != hipSuccess) return e;                                                                        \
-        hipLaunchKernelGGL((branch_merge_kernel<D, S, O>), merge_grid, dim3(256), 0, s, p, wgs, groups);              \
-        return hipGetLastError();                                                                             \
-    }
-#define KD_GO_D(D)                                    \
-    if (cbs == 1 && cbo == 1) KD_GO(D, 1, 1)          \
-    if (cbs == 2 && cbo == 1) KD_GO(D, 2, 1)          \
-    if (cbs == 1 && cbo == 2) KD_GO(D, 1, 2)          \
-    KD_GO(D, 2, 2)
-    if (p.D == 128) { KD_GO_D(128) }
-    if (p.D == 64) { KD_GO_D(64) }
-#undef KD_GO_D
-#undef KD_GO
+    const int64_t Mt = (int64_t)p.G * p.Bt;
+    const int RS = shared_block(p.fan * Mt), RO = own_block(Mt);
+    if (p.D == 128) return RO == 16 ? launch<128, 16>(p, RS, s) : launch<128, 32>(p, RS, s);
+    if (p.D == 64) return RO == 16 ? launch<64, 16>(p, RS, s) : launch<64, 32>(p, RS, s);
     return hipErrorInvalidValue;
 }
 

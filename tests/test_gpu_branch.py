@@ -296,6 +296,13 @@ CASES = [
     (64, 1, 64, 1, 2, 130, 8, 1, [40, 9], None),                                # 64 query heads to one KV head
     (16, 16, 64, 2, 1, 65, 1024, 2, [0, 1500], None),                           # a KV head for every query head
     (24, 8, 128, 1, 90, 300, 16, 1, [i % 40 for i in range(90)], None),
+    # 64, 240, 256 and 500 rows of one KV head over a prompt: two to eight waves share its tiles, in one block or two
+    (8, 2, 128, 1, 16, 1500, 16, 1, [3 * i for i in range(16)], None),
+    (6, 2, 128, 2, 80, 1000, 16, 1, [i % 7 for i in range(160)], None),
+    (8, 2, 64, 1, 64, 97, 32, 1, [i for i in range(64)], None),
+    (8, 2, 64, 1, 125, 777, 8, 1, [i % 50 - 1 for i in range(125)], None),
+    (8, 2, 64, 1, 16, 3000, 8, 1, [1] * 16, None),
+    (16, 4, 128, 1, 30, 2049, 8, 1, [1] * 30, None),
 ]
 
 
