@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+import struct
 from dataclasses import dataclass
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -99,7 +100,7 @@ def load_library() -> C.CDLL:
     L.keydiff_prefill_block_layers.argtypes = [pp, i32, pp, pp, pp, i32, i64, pp, vp]
     L.keydiff_prefill_block_rope.argtypes = [vp, vp, vp, vp, i32, i64, vp, vp, i64, vp, vp, vp]
     L.keydiff_prefill_block_layers_rope.argtypes = [pp, i32, pp, pp, pp, i32, i64, vp, vp, i64, pp, vp]
-    fp, rp, bp = C.POINTER(_RowForm), C.POINTER(_Rows), C.POINTER(_Branches)
+    fp = rp = bp = vp   # keydiff_row_form_t, keydiff_rows_t, keydiff_branches_t: a structure by reference, or its bytes
     L.keydiff_prefill_block_norm_rope.argtypes = [vp, vp, vp, vp, i32, i64, fp, vp, vp, vp]
     L.keydiff_prefill_block_layers_norm_rope.argtypes = [pp, i32, pp, pp, pp, i32, i64, fp, pp, vp]
     L.keydiff_norm_rope.argtypes = [rp, rp, i32, i32, i32, i32, i32, i64, vp, fp, vp, vp, vp]
@@ -224,8 +225,8 @@ def prefill_block_layers(caches, q, k_new, v_new, pos0: int, out=None, stream=No
         if not len(q_weights) == len(k_weights) == n:
             raise ValueError(f"norm needs one weight tensor per layer, got {len(q_weights)} and {len(k_weights)} for {n} layers")
         cos, sin = rope if rope is not None else (None, None)
-        forms = (_RowForm * n)(*(_form(c.cfg.n_q_heads, c.cfg.n_kv_heads, c.cfg.head_dim, cos, sin, wq, wk, eps, c.device)
-                                 for c, wq, wk in zip(caches, q_weights, k_weights)))
+        forms = b"".join(_pack_form(c.cfg.n_q_heads, c.cfg.n_kv_heads, c.cfg.head_dim, cos, sin, wq, wk, eps, c.device)
+                         for c, wq, wk in zip(caches, q_weights, k_weights))
         _check(L.keydiff_prefill_block_layers_norm_rope(arr([c._h.value for c in caches]), n,
                                                         arr([t.data_ptr() for t in q]), arr([t.data_ptr() for t in k_new]),
                                                         arr([t.data_ptr() for t in v_new]), Bt, int(pos0), forms,
@@ -248,69 +249,82 @@ def prefill_block_layers(caches, q, k_new, v_new, pos0: int, out=None, stream=No
 
 
 # ------------------------------------------------------------------ norms and rotation alone; continuations of a prompt
-def check_rows(name, t, shape):
-    """A tensor of rows [sequences][heads][tokens][head_dim]: bf16, the innermost dimension contiguous, other strides free (views into
-    a fused projection's output are fine)."""
-    import torch
-    if t.dtype is not torch.bfloat16 or t.shape != shape or t.stride(3) != 1:
-        raise ValueError(f"{name} must be a bf16 tensor of shape {tuple(shape)} with a contiguous last dimension, "
-                         f"got {tuple(t.shape)} {t.dtype}, strides {t.stride()}")
+# The structures of these calls are packed into bytes: a tenth of the time that filling a ctypes structure takes (of 14 us a call on
+# the host, where the kernels of a generation step take 3 to 5).
+_ROWS = struct.Struct("Pqqq")               # keydiff_rows_t
+_ROW_FORM = struct.Struct("PPqqfPPq")       # keydiff_row_form_t
+_BRANCHES = struct.Struct("PPPPP7i4x")      # keydiff_branches_t
+assert (_ROWS.size, _ROW_FORM.size, _BRANCHES.size) == (C.sizeof(_Rows), C.sizeof(_RowForm), C.sizeof(_Branches))
 
 
-def check_contiguous(name, t, shape, dtype):
+def _pack_rows(name, t, n, heads, tokens, d, bf16, device):
+    """keydiff_rows_t of a tensor of rows [sequences][heads][tokens][head_dim]: bf16, the innermost dimension contiguous, other strides
+    free (views into a fused projection's output are fine)."""
+    s = t.stride()
+    if t.dtype is not bf16 or t.shape != (n, heads, tokens, d) or s[3] != 1:
+        raise ValueError(f"{name} must be a bf16 tensor of shape {(n, heads, tokens, d)} with a contiguous last dimension, "
+                         f"got {tuple(t.shape)} {t.dtype}, strides {s}")
+    if t.device != device:
+        raise ValueError(f"the tensors must live on one device, got {device} and {t.device} for {name}")
+    return _ROWS.pack(t.data_ptr(), s[0] if n > 1 else 0, s[1] if heads > 1 else 0, s[2] if tokens > 1 else 0)
+
+
+def _dense(name, t, shape, dtype, device):
+    """The address of a contiguous tensor of this shape and type."""
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {tuple(t.shape)} {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"the tensors must live on one device, got {device} and {t.device} for {name}")
+    return t.data_ptr()
 
 
-def _check_devices(device, *tensors):
-    if device.type != "cuda":
-        raise ValueError(f"the tensors must live on a GPU, got {device}")
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"the tensors must live on one device, got {device} and {t.device}")
+def _weight(name, w, heads, d, bf16, device):
+    """The address and the stride from head to head of norm weights [d] or [heads][d]."""
+    shape, strides = w.shape, w.stride()
+    one = len(shape) == 1
+    if w.dtype is not bf16 or (shape != (d,) if one else shape != (heads, d)) or strides[-1] != 1:
+        raise ValueError(f"{name} must be a bf16 tensor of shape ({d},) or ({heads}, {d}), got {tuple(shape)} {w.dtype}")
+    if w.device != device:
+        raise ValueError(f"{name} must live on {device}, got {w.device}")
+    return w.data_ptr(), 0 if one or heads == 1 else strides[0]
 
 
-def _rows(t):
-    n, h, b, _ = t.shape
-    s = t.stride()
-    return _Rows(t.data_ptr(), s[0] if n > 1 else 0, s[1] if h > 1 else 0, s[2] if b > 1 else 0)
-
-
-def _form(hq, hkv, d, cos, sin, q_weight, k_weight, eps, device=None):
+def _pack_form(hq, hkv, d, cos, sin, q_weight, k_weight, eps, device):
     """keydiff_row_form_t of norm weights ([d] or [heads][d] bf16, or None) and rotary tables (float32 [positions][d / 2], or None)."""
     import torch
-    f = _RowForm(norm_eps=eps)
-    if (q_weight is None) != (k_weight is None) or (cos is None) != (sin is None):
-        raise ValueError("q_weight and k_weight, and cos and sin, are given together or not at all")
-    if q_weight is not None:
-        for name, w, heads in (("q_weight", q_weight, hq), ("k_weight", k_weight, hkv)):
-            if w.dtype is not torch.bfloat16 or w.shape not in ((d,), (heads, d)) or w.stride(-1) != 1:
-                raise ValueError(f"{name} must be a bf16 tensor of shape ({d},) or ({heads}, {d}), got {tuple(w.shape)} {w.dtype}")
-            if device is not None and w.device != device:
-                raise ValueError(f"{name} must live on {device}, got {w.device}")
-        f.q_weight, f.k_weight = q_weight.data_ptr(), k_weight.data_ptr()
-        f.q_weight_stride = q_weight.stride(0) if q_weight.dim() == 2 and hq > 1 else 0
-        f.k_weight_stride = k_weight.stride(0) if k_weight.dim() == 2 and hkv > 1 else 0
-    if cos is not None:
-        for name, t in (("cos", cos), ("sin", sin)):
-            if t.dtype is not torch.float32 or t.dim() != 2 or t.shape[1] != d // 2 or not t.is_contiguous():
-                raise ValueError(f"{name} must be a contiguous float32 table [positions][{d // 2}], got {tuple(t.shape)} {t.dtype}")
-            if device is not None and t.device != device:
-                raise ValueError(f"{name} must live on {device}, got {t.device}")
-        if cos.shape != sin.shape:
-            raise ValueError("cos and sin tables differ in shape")
-        f.cos_table, f.sin_table, f.table_rows = cos.data_ptr(), sin.data_ptr(), cos.shape[0]
-    return f
+    qw = kw = qs = ks = c = s = rows = 0
+    if q_weight is not None and k_weight is not None:
+        qw, qs = _weight("q_weight", q_weight, hq, d, torch.bfloat16, device)
+        kw, ks = _weight("k_weight", k_weight, hkv, d, torch.bfloat16, device)
+    elif q_weight is not k_weight:
+        raise ValueError("q_weight and k_weight are given together or not at all")
+    if cos is not None and sin is not None:
+        if cos.dim() != 2:
+            raise ValueError(f"cos must be a float32 table [positions][{d // 2}], got {tuple(cos.shape)}")
+        rows = cos.shape[0]
+        c, s = _dense("cos", cos, (rows, d // 2), torch.float32, device), _dense("sin", sin, (rows, d // 2), torch.float32, device)
+    elif cos is not sin:
+        raise ValueError("cos and sin are given together or not at all")
+    return _ROW_FORM.pack(qw, kw, qs, ks, eps, c, s, rows)
 
 
 def _enqueue(device, stream, call, *args):
     """The call on `stream` (None: torch's current one) of the tensors' device, whichever device is current."""
-    import torch
-    if torch.cuda.current_device() == device.index:
-        _check(call(*args, _stream_ptr(stream)))
+    from torch import _C
+    current, raw = getattr(_C, "_cuda_getDevice", None), getattr(_C, "_cuda_getCurrentRawStream", None)   # (see _stream_ptr)
+    if current is not None and raw is not None and current() == device.index:
+        rc = call(*args, raw(device.index) if stream is None else getattr(stream, "cuda_stream", stream))
     else:
+        import torch
         with torch.cuda.device(device):
-            _check(call(*args, _stream_ptr(stream)))
+            rc = call(*args, _stream_ptr(stream))
+    if rc != OK:
+        _check(rc)
+
+
+def _need_gpu(device):
+    if device.type != "cuda":
+        raise ValueError(f"the tensors must live on a GPU, got {device}")
 
 
 def norm_rope(q, k, cos=None, sin=None, pos0: int = 0, positions=None, q_weight=None, k_weight=None, norm_eps: float = 1e-6,
@@ -323,47 +337,36 @@ def norm_rope(q, k, cos=None, sin=None, pos0: int = 0, positions=None, q_weight=
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError(f"q and k are [batch][heads][tokens][head_dim], got {tuple(q.shape)} and {tuple(k.shape)}")
     b, hq, T, d = q.shape
-    hkv = k.shape[1]
-    check_rows("q", q, (b, hq, T, d))
-    check_rows("k", k, (b, hkv, T, d))
-    if positions is not None:
-        check_contiguous("positions", positions, (b, T), torch.int32)
+    hkv, device, bf16 = k.shape[1], q.device, torch.bfloat16
+    rq, rk = _pack_rows("q", q, b, hq, T, d, bf16, device), _pack_rows("k", k, b, hkv, T, d, bf16, device)
+    at = _dense("positions", positions, (b, T), torch.int32, device) if positions is not None else None
+    form = _pack_form(hq, hkv, d, cos, sin, q_weight, k_weight, norm_eps, device)
     if q_out is not None:
-        check_contiguous("q_out", q_out, q.shape, torch.bfloat16)
+        _dense("q_out", q_out, (b, hq, T, d), bf16, device)
     if k_out is not None:
-        check_contiguous("k_out", k_out, k.shape, torch.bfloat16)
-    device = q.device
-    form = _form(hq, hkv, d, cos, sin, q_weight, k_weight, norm_eps, device)
-    _check_devices(device, k, positions, q_out, k_out)
+        _dense("k_out", k_out, (b, hkv, T, d), bf16, device)
+    _need_gpu(device)
     if q_out is None:
-        q_out = torch.empty((b, hq, T, d), dtype=torch.bfloat16, device=device)
+        q_out = torch.empty((b, hq, T, d), dtype=bf16, device=device)
     if k_out is None:
-        k_out = torch.empty((b, hkv, T, d), dtype=torch.bfloat16, device=device)
-    rq, rk = _rows(q), _rows(k)
-    _enqueue(device, stream, load_library().keydiff_norm_rope, C.byref(rq), C.byref(rk), b, hq, hkv, d, T, int(pos0),
-             positions.data_ptr() if positions is not None else None, C.byref(form), q_out.data_ptr(), k_out.data_ptr())
+        k_out = torch.empty((b, hkv, T, d), dtype=bf16, device=device)
+    _enqueue(device, stream, load_library().keydiff_norm_rope, rq, rk, b, hq, hkv, d, T, int(pos0), at, form, q_out.data_ptr(),
+             k_out.data_ptr())
     return q_out, k_out
 
 
-def check_branches(n_seqs, d, hkv, k_pages, v_pages, table, lens, n_new):
-    """The pages of n_seqs sequences: pools [pages][hkv][page_rows][d] bf16, table [n_seqs][width], lens and n_new [n_seqs] int32."""
-    import torch
-    if k_pages.dim() != 4 or k_pages.shape[1] != hkv or k_pages.shape[3] != d:
-        raise ValueError(f"k_pages must be [pages][{hkv}][page_rows][{d}], got {tuple(k_pages.shape)}")
-    check_contiguous("k_pages", k_pages, k_pages.shape, torch.bfloat16)
-    check_contiguous("v_pages", v_pages, k_pages.shape, torch.bfloat16)
+def _pack_branches(n, hq, hkv, d, k_pages, v_pages, table, lens, n_new, bf16, i32, device):
+    """keydiff_branches_t: pools [pages][hkv][page_rows][d] bf16, table [n_seqs][width], lens and n_new [n_seqs] int32."""
+    shape = k_pages.shape
+    if len(shape) != 4 or shape[1] != hkv or shape[3] != d:
+        raise ValueError(f"k_pages must be [pages][{hkv}][page_rows][{d}], got {tuple(shape)}")
     if table.dim() != 2:
-        raise ValueError(f"table must be [{n_seqs}][width], got {tuple(table.shape)}")
-    check_contiguous("table", table, (n_seqs, table.shape[1]), torch.int32)
-    check_contiguous("lens", lens, (n_seqs,), torch.int32)
-    if n_new is not None:
-        check_contiguous("n_new", n_new, (n_seqs,), torch.int32)
-
-
-def _branches(n_seqs, hq, hkv, d, k_pages, v_pages, table, lens, n_new):
-    return _Branches(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), lens.data_ptr(),
-                     n_new.data_ptr() if n_new is not None else None, n_seqs, hq, hkv, d, k_pages.shape[2], k_pages.shape[0],
-                     table.shape[1])
+        raise ValueError(f"table must be [{n}][width], got {tuple(table.shape)}")
+    width = table.shape[1]
+    return _BRANCHES.pack(_dense("k_pages", k_pages, shape, bf16, device), _dense("v_pages", v_pages, shape, bf16, device),
+                          _dense("table", table, (n, width), i32, device), _dense("lens", lens, (n,), i32, device),
+                          _dense("n_new", n_new, (n,), i32, device) if n_new is not None else 0,
+                          n, hq, hkv, d, shape[2], shape[0], width)
 
 
 def branch_append(q, k_new, v_new, k_pages, v_pages, table, lens, n_new=None, pos0=None, cos=None, sin=None, q_weight=None,
@@ -380,28 +383,23 @@ def branch_append(q, k_new, v_new, k_pages, v_pages, table, lens, n_new=None, po
         raise ValueError("q, k_new and v_new are [sequences][heads][tokens][head_dim]")
     n, hkv, Bt, d = k_new.shape
     hq = q.shape[1] if q is not None else hkv
-    check_rows("k_new", k_new, (n, hkv, Bt, d))
-    check_rows("v_new", v_new, (n, hkv, Bt, d))
-    check_branches(n, d, hkv, k_pages, v_pages, table, lens, n_new)
+    device, bf16, i32 = k_new.device, torch.bfloat16, torch.int32
+    rk, rv = _pack_rows("k_new", k_new, n, hkv, Bt, d, bf16, device), _pack_rows("v_new", v_new, n, hkv, Bt, d, bf16, device)
+    b = _pack_branches(n, hq, hkv, d, k_pages, v_pages, table, lens, n_new, bf16, i32, device)
+    rq = out = None
     if q is not None:
-        check_rows("q", q, (n, hq, Bt, d))
+        rq = _pack_rows("q", q, n, hq, Bt, d, bf16, device)
     elif q_out is not None:
         raise ValueError("q_out without q")
     if q_out is not None:
-        check_contiguous("q_out", q_out, q.shape, torch.bfloat16)
-    if pos0 is not None:
-        check_contiguous("pos0", pos0, (n,), torch.int32)
-    device = k_new.device
-    form = _form(hq, hkv, d, cos, sin, q_weight, k_weight, norm_eps, device)
-    _check_devices(device, q, v_new, k_pages, v_pages, table, lens, n_new, pos0, q_out)
+        out = _dense("q_out", q_out, (n, hq, Bt, d), bf16, device)
+    first = _dense("pos0", pos0, (n,), i32, device) if pos0 is not None else None
+    form = _pack_form(hq, hkv, d, cos, sin, q_weight, k_weight, norm_eps, device)
+    _need_gpu(device)
     if q is not None and q_out is None:
-        q_out = torch.empty((n, hq, Bt, d), dtype=torch.bfloat16, device=device)
-    b = _branches(n, hq, hkv, d, k_pages, v_pages, table, lens, n_new)
-    rk, rv = _rows(k_new), _rows(v_new)
-    rq = _rows(q) if q is not None else None
-    _enqueue(device, stream, load_library().keydiff_branch_append, C.byref(b), C.byref(rq) if rq is not None else None, C.byref(rk),
-             C.byref(rv), Bt, pos0.data_ptr() if pos0 is not None else None, C.byref(form),
-             q_out.data_ptr() if q_out is not None else None)
+        q_out = torch.empty((n, hq, Bt, d), dtype=bf16, device=device)
+        out = q_out.data_ptr()
+    _enqueue(device, stream, load_library().keydiff_branch_append, b, rq, rk, rv, Bt, first, form, out)
     return q_out
 
 
@@ -434,45 +432,46 @@ def branch_attention(q, k_pages, v_pages, table, lens, prefix=None, n_new=None, 
         raise ValueError("q is [sequences][heads][tokens][head_dim] and pools are [pages][heads][page_rows][head_dim]")
     n, hq, Bt, d = q.shape
     hkv = k_pages.shape[1]
-    check_rows("q", q, (n, hq, Bt, d))
-    check_branches(n, d, hkv, k_pages, v_pages, table, lens, n_new)
-    if out is not None:
-        check_contiguous("out", out, q.shape, torch.bfloat16)
-    cache = prefix if isinstance(prefix, KeyDiffCache) else None
-    kp = vp = None
+    device, bf16 = q.device, torch.bfloat16
+    rq = _pack_rows("q", q, n, hq, Bt, d, bf16, device)
+    b = _pack_branches(n, hq, hkv, d, k_pages, v_pages, table, lens, n_new, bf16, torch.int32, device)
+    to = _dense("out", out, (n, hq, Bt, d), bf16, device) if out is not None else None
+    cache = kp = vp = None
     prompts = rows = cap = 0
-    device = q.device
-    if cache is not None:
+    if prefix is None:
+        pass
+    elif isinstance(prefix, KeyDiffCache):
+        cache = prefix
         prompts = cache.cfg.batch
         if softmax_scale > 0:
             raise ValueError("softmax_scale is the cache's")
         if cache.device != device:
             raise ValueError(f"the cache lives on {cache.device}, the queries on {device}")
-    elif prefix is not None:
+    else:
         kp, vp, rows = prefix
+        if kp.dim() != 4:
+            raise ValueError(f"prefix keys are [prompts][{hkv}][rows][{d}], got {tuple(kp.shape)}")
         prompts, cap = kp.shape[0], kp.shape[2]
-        check_contiguous("prefix keys", kp, (prompts, hkv, cap, d), torch.bfloat16)
-        check_contiguous("prefix values", vp, kp.shape, torch.bfloat16)
         if not 0 <= rows <= cap:
             raise ValueError(f"the prefix has {cap} rows a head, {rows} are to be read")
-    _check_devices(device, k_pages, v_pages, table, lens, n_new, out, workspace, kp, vp)
+        kp = _dense("prefix keys", kp, (prompts, hkv, cap, d), bf16, device)
+        vp = _dense("prefix values", vp, (prompts, hkv, cap, d), bf16, device)
+    _need_gpu(device)
     need = _branch_workspace_bytes(n, hq, hkv, d, Bt, prompts, device.index)
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
         if stream is not None:   # torch must not hand the memory out again before the work on that stream is done
             workspace.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device))
-    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need:
-        raise ValueError(f"workspace must be a contiguous uint8 tensor of at least {need} elements")
+    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need or workspace.device != device:
+        raise ValueError(f"workspace must be a contiguous uint8 tensor of at least {need} elements on {device}")
     if out is None:
-        out = torch.empty((n, hq, Bt, d), dtype=torch.bfloat16, device=device)
-    b, rq = _branches(n, hq, hkv, d, k_pages, v_pages, table, lens, n_new), _rows(q)
+        out = torch.empty((n, hq, Bt, d), dtype=bf16, device=device)
+        to = out.data_ptr()
     if cache is not None:
-        _enqueue(device, stream, cache._L.keydiff_cache_branch_attention, cache._h, C.byref(b), C.byref(rq), Bt, out.data_ptr(),
-                 workspace.data_ptr(), workspace.numel())
+        _enqueue(device, stream, cache._L.keydiff_cache_branch_attention, cache._h, b, rq, Bt, to, workspace.data_ptr(), workspace.numel())
     else:
-        _enqueue(device, stream, load_library().keydiff_branch_attention, C.byref(b), C.byref(rq), Bt,
-                 kp.data_ptr() if kp is not None else None, vp.data_ptr() if vp is not None else None, prompts, int(rows), cap,
-                 softmax_scale, out.data_ptr(), workspace.data_ptr(), workspace.numel())
+        _enqueue(device, stream, load_library().keydiff_branch_attention, b, rq, Bt, kp, vp, prompts, int(rows), cap, softmax_scale, to,
+                 workspace.data_ptr(), workspace.numel())
     return out
 
 
@@ -552,9 +551,9 @@ class KeyDiffCache:
         norm; tables None: no rotation."""
         Bt, out = self._block_args(q, k_new, v_new, out, scores_out)
         cfg = self.cfg
-        form = _form(cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, cos, sin, q_weight, k_weight, norm_eps, self.device)
+        form = _pack_form(cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, cos, sin, q_weight, k_weight, norm_eps, self.device)
         _check(self._L.keydiff_prefill_block_norm_rope(self._h, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), Bt,
-                                                       int(pos0), C.byref(form), out.data_ptr(),
+                                                       int(pos0), form, out.data_ptr(),
                                                        scores_out.data_ptr() if scores_out is not None else None,
                                                        _stream_ptr(stream)))
         return out

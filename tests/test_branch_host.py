@@ -141,7 +141,7 @@ def test_workspace_covers_what_the_launch_addresses():
     a = kd.branch_workspace_bytes(1, 32, 8, 128, 1, 1)
     assert a >= (256 + 8) * 16 * 128 * 4
     assert kd.branch_workspace_bytes(64, 32, 8, 128, 1, 1) > kd.branch_workspace_bytes(16, 32, 8, 128, 1, 1) > a
-    assert kd.branch_workspace_bytes(64, 32, 8, 128, 4, 1) > kd.branch_workspace_bytes(64, 32, 8, 128, 1, 1)
+    assert kd.branch_workspace_bytes(64, 32, 8, 128, 8, 1) > kd.branch_workspace_bytes(64, 32, 8, 128, 1, 1)
     with pytest.raises(kd.KeyDiffError):
         kd.branch_workspace_bytes(5, 32, 8, 128, 1, 2)
 
@@ -168,7 +168,7 @@ def test_wrapper_refuses_tensors_that_do_not_fit():
         kd.norm_rope(q, k, cos, cos, q_weight=z(7, 64), k_weight=w)
     with pytest.raises(ValueError, match="sin"):
         kd.norm_rope(q, k, cos, z(50, 64, dt=torch.float32))
-    with pytest.raises(ValueError, match="differ"):
+    with pytest.raises(ValueError, match="sin"):
         kd.norm_rope(q, k, cos, cos[:40].contiguous())
     with pytest.raises(ValueError, match="v_new"):
         kd.branch_append(q, k, k[:, :1], pages, pages, table, lens)
