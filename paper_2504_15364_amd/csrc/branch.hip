@@ -19,6 +19,7 @@
 // The lists follow from the lengths on the device: the launch itself does not depend on them and may be replayed from a graph.
 #include "kd_branch.h"
 #include "kd_device.h"
+#include "kd_select.h"
 
 namespace kd {
 
@@ -50,31 +51,22 @@ __device__ __forceinline__ float sum_over_rows(float x)
     const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
-__device__ __forceinline__ int wave_sum(int x)
+// New tokens of a sequence that holds `len` rows, and rows that are keys of theirs (its own and the new ones); 0 where it has nothing to do
+__device__ __forceinline__ int new_of(const BranchParams &p, int len, int asked) { return len < 0 ? 0 : max(0, min(asked, p.Bt)); }
+__device__ __forceinline__ int own_rows(const BranchParams &p, int len, int asked)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-    return x;
-}
-
-// Rows that are keys of a sequence's new tokens (its own rows and the new ones), 0 where it has nothing to do
-__device__ __forceinline__ int new_of(const BranchParams &p, int s)
-{
-    if (p.pages.lens[s] < 0) return 0;
-    return p.pages.n_new ? max(0, min(p.pages.n_new[s], p.Bt)) : p.Bt;
-}
-__device__ __forceinline__ int own_rows(const BranchParams &p, int s)
-{
-    const int fresh = new_of(p, s);
+    const int fresh = new_of(p, len, asked);
     if (fresh == 0) return 0;
-    const int64_t n = (int64_t)p.pages.lens[s] + fresh, most = (int64_t)p.pages.width << p.pages.page_shift;
+    const int64_t n = (int64_t)len + fresh, most = (int64_t)p.pages.width << p.pages.page_shift;
     return (int)(n < most ? n : most);
 }
+__device__ __forceinline__ int asked_of(const BranchParams &p, int s) { return p.pages.n_new ? p.pages.n_new[s] : p.Bt; }
+__device__ __forceinline__ int own_rows(const BranchParams &p, int s) { return own_rows(p, p.pages.lens[s], asked_of(p, s)); }
 
 // How the work is cut (uniform; the merge reads it from BranchParams::plan)
 struct Plan {
     int shared_wgs;                // workgroups of the shared part; task t of its list is done by workgroup t % shared_wgs
-    int shared_segs, splits;       // (prompt, head, block of rows) segments, and pieces of each: piece k of segment g is task k segs + g
+    int splits;                    // pieces of each of its segments (prompt, head, block of rows): piece k of segment g is task k segs + g
     int own_tiles, own_chunk;      // tiles of the own part; how many of them a wave takes
 };
 
@@ -230,7 +222,8 @@ __device__ __forceinline__ void store_v(unsigned char *vt, const u32x4 (&vr)[TK 
 // Address of query row m (order g, j) of sequence s and KV head h
 __device__ __forceinline__ const uint16_t *query_row(const BranchParams &p, int s, int h, int m)
 {
-    return p.q.p + (int64_t)s * p.q.seq + (int64_t)(h * p.G + m / p.Bt) * p.q.head + (int64_t)(m % p.Bt) * p.q.token;
+    const int g = p.by_Bt.divide(m), j = m - g * p.Bt;
+    return p.q.p + (int64_t)s * p.q.seq + (int64_t)(h * p.G + g) * p.q.head + (int64_t)j * p.q.token;
 }
 
 // A task of the shared part: piece k of segment (prompt c, head h, block mb of rows).  Blocks of the same rows of the cache lie n_prefixes
@@ -238,15 +231,14 @@ __device__ __forceinline__ const uint16_t *query_row(const BranchParams &p, int 
 struct Segment {
     int ch, mb, c, h, k;
 };
-__device__ __forceinline__ Segment segment_of(const BranchParams &p, int task, int segs)
+__device__ __forceinline__ Segment segment_of(const BranchParams &p, int task)
 {
     Segment s;
-    const int heads = p.n_prefixes * p.hkv;
-    s.k = task / segs;
-    const int g = task - s.k * segs;
-    s.mb = g / heads;
-    s.ch = g - s.mb * heads;
-    s.c = s.ch / p.hkv;
+    s.k = p.by_segs.divide(task);
+    const int g = task - s.k * p.shared_segs;
+    s.mb = p.by_heads.divide(g);
+    s.ch = g - s.mb * p.n_prefixes * p.hkv;
+    s.c = p.by_hkv.divide(s.ch);
     s.h = s.ch - s.c * p.hkv;
     return s;
 }
@@ -256,7 +248,7 @@ __device__ __forceinline__ Segment segment_of(const BranchParams &p, int task, i
 template <int D>
 constexpr int OUT_PITCH = D + 4;
 
-// The shared part with at most 32 query rows: one workgroup, its piece of the list, every wave tiles of its own
+// The shared part with at most 16 query rows: one workgroup, its piece of the list, every wave tiles of its own
 template <int D, int CB>
 __device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned char *smem)
 {
@@ -267,36 +259,37 @@ __device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned cha
     const int Mt = p.G * p.Bt, M = p.fan * Mt, nt = (p.prefix_len + TK - 1) / TK;
     unsigned char *vt = smem + (size_t)wave * TK * ROWB;
     float *outs = reinterpret_cast<float *>(smem);   // the waves' outputs of one block of 16 rows, where their V tiles were
-    for (int task = blockIdx.x; task < plan.shared_segs * plan.splits; task += plan.shared_wgs) {
-        const Segment sg = segment_of(p, task, plan.shared_segs);
+    for (int task = blockIdx.x; task < p.shared_segs * plan.splits; task += plan.shared_wgs) {
+        const Segment sg = segment_of(p, task);
         const int ch = sg.ch, mb = sg.mb, c = sg.c, h = sg.h, stride = plan.splits * NW;
         const uint16_t *kh = p.k_prefix + (size_t)ch * p.prefix_cap * D, *vh = p.v_prefix + (size_t)ch * p.prefix_cap * D;
         State<D, CB> st;
         st.reset();
         u32x4 kr[2][NC], vr[NV];
-        // rows past the last repeat it: finite data whose weights are masked to zero
+        // rows past the last repeat it: finite data whose weights are masked to zero.  (Offsets of 32 bits from the head's first row.)
         auto load_k = [&](int t) {
 #pragma unroll
             for (int kg = 0; kg < 2; ++kg) {
-                const uint16_t *kb = kh + (size_t)min(t * TK + 16 * kg + c16, p.prefix_len - 1) * D + 8 * g;
+                const uint32_t off = (uint32_t)min(t * TK + 16 * kg + c16, p.prefix_len - 1) * ROWB + 16 * g;
 #pragma unroll
-                for (int cc = 0; cc < NC; ++cc) kr[kg][cc] = *reinterpret_cast<const u32x4 *>(kb + cc * 32);
+                for (int cc = 0; cc < NC; ++cc) kr[kg][cc] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(kh) + off + cc * 64);
             }
         };
         auto load_v = [&](int t) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                vr[i] = *reinterpret_cast<const u32x4 *>(vh + (size_t)min(t * TK + i * RPL + lane / UPR, p.prefix_len - 1) * D + (lane % UPR) * 8);
+            for (int i = 0; i < NV; ++i) {
+                const uint32_t off = (uint32_t)min(t * TK + i * RPL + lane / UPR, p.prefix_len - 1) * ROWB + lane % UPR * 16;
+                vr[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(vh) + off);
+            }
         };
         int t = sg.k * NW + wave;
-        if (t < nt) {
-            load_k(t);
-            load_v(t);
-        }
+        load_k(t);   // (a tile behind the last repeats rows that exist)
+        load_v(t);
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             const int m = min(mb * R + 16 * cb + c16, M - 1);
-            const uint16_t *qr = query_row(p, c * p.fan + m / Mt, h, m % Mt) + 8 * g;
+            const int f = p.by_Mt.divide(m);
+            const uint16_t *qr = query_row(p, c * p.fan + f, h, m - f * Mt) + 8 * g;
 #pragma unroll
             for (int cc = 0; cc < NC; ++cc) st.q[cb][cc] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qr + cc * 32));
         }
@@ -385,13 +378,12 @@ __device__ void shared_many(const BranchParams &p, const Plan &plan, unsigned ch
     const int c16 = lane & 15, g = lane >> 4, rw = wave % RW, kw = wave / RW;
     const int Mt = p.G * p.Bt, M = p.fan * Mt, nt = (p.prefix_len + TK - 1) / TK, units = (nt + KW - 1) / KW;
     const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
-    for (int task = blockIdx.x; task < plan.shared_segs * plan.splits; task += plan.shared_wgs) {
-        const Segment sg = segment_of(p, task, plan.shared_segs);
+    for (int task = blockIdx.x; task < p.shared_segs * plan.splits; task += plan.shared_wgs) {
+        const Segment sg = segment_of(p, task);
         const int ch = sg.ch, mb = sg.mb, c = sg.c, h = sg.h;
         const uint16_t *kh = p.k_prefix + (size_t)ch * p.prefix_cap * D, *vh = p.v_prefix + (size_t)ch * p.prefix_cap * D;
         const int m0 = mb * R + 32 * rw;   // the wave's first query row
         const bool active = m0 < M;        // uniform in the wave: else it only copies
-        const int steps = (units - sg.k + plan.splits - 1) / plan.splits;
         // stage `it` of the piece (one behind its end repeats rows that exist: what a wave waits for stays the same number of copies)
         auto issue = [&](int it) {
 #pragma unroll
@@ -399,24 +391,24 @@ __device__ void shared_many(const BranchParams &p, const Plan &plan, unsigned ch
                 const int id = wave + NW * i, grp = id / (2 * CPT), part = id % (2 * CPT), isv = part >= CPT, r0 = part % CPT * RPC;
                 const int row = r0 + lane / UPR, unit = lane % UPR;
                 const int key = min(((sg.k + it * plan.splits) * KW + grp) * TK + row, p.prefix_len - 1);
-                const uint16_t *src = (isv ? vh : kh) + (size_t)key * D + (unit ^ (isv ? v_swizzle<D>(row) : k_swizzle<D>(row))) * 8;
-                lds_copy16(lds0 + (uint32_t)((it % NS) * STAGEB + grp * 2 * TILEB + isv * TILEB + r0 * ROWB), src);
+                const uint32_t off = (uint32_t)key * ROWB + (uint32_t)(unit ^ (isv ? v_swizzle<D>(row) : k_swizzle<D>(row))) * 16;
+                lds_copy16(lds0 + (uint32_t)((it % NS) * STAGEB + grp * 2 * TILEB + isv * TILEB + r0 * ROWB), isv ? vh : kh, off);
             }
         };
-        // The query rows are requested behind the first copies, and waited for here: where the compiler finds them used (in the loop) it
+        // The query rows are requested ahead of the first copies, and waited for ahead of the loop: where the compiler finds them used it
         // would wait in every step, and with them for all copies, which it does not count.
-        constexpr int FIRST = NS > 3 ? 2 : 1;
-#pragma unroll
-        for (int it = 0; it < FIRST; ++it) issue(it);
         State<D, CB> st;
         st.reset();
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             const int m = min(m0 + 16 * cb + c16, M - 1);
-            const uint16_t *qr = query_row(p, c * p.fan + m / Mt, h, m % Mt) + 8 * g;
+            const int f = p.by_Mt.divide(m);
+            const uint16_t *qr = query_row(p, c * p.fan + f, h, m - f * Mt) + 8 * g;
 #pragma unroll
             for (int cc = 0; cc < NC; ++cc) st.q[cb][cc] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qr + cc * 32));
         }
+        issue(0);
+        const int steps = (units - sg.k + plan.splits - 1) / plan.splits;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -429,7 +421,7 @@ __device__ void shared_many(const BranchParams &p, const Plan &plan, unsigned ch
         auto lds_of = [&](int it) { return smem + (it % NS) * STAGEB + kw * 2 * TILEB; };
         if constexpr (RW == 2) {
 #pragma unroll
-            for (int it = FIRST; it < NS - 1; ++it) issue(it);
+            for (int it = 1; it < NS - 1; ++it) issue(it);
             for (int it = 0; it < steps; ++it) {
                 wait_copies<CPW *(NS - 2)>();   // this wave's part of stage `it` has landed
                 __syncthreads();                // ... and every wave's, and nobody reads the stage before it any more
@@ -505,7 +497,7 @@ __device__ void shared_many(const BranchParams &p, const Plan &plan, unsigned ch
                 }
             };
 #pragma unroll
-            for (int it = FIRST; it < NS - 2; ++it) issue(it);
+            for (int it = 1; it < NS - 2; ++it) issue(it);
             wait_copies<CPW *(NS - 3)>();   // this wave's part of stage 0 has landed
             __syncthreads();
             if (late) __syncthreads();
@@ -575,144 +567,165 @@ __device__ void shared_many(const BranchParams &p, const Plan &plan, unsigned ch
     }
 }
 
-// The own part: one wave, its piece of the list.  `slots`: slots and rows of the shared part, behind which the own part's lie.
+// The own part: one wave, its piece of the list.  len0, rows0: length and own rows of sequence `lane`.
+// Three tiles are under way at a time, across the ends of segments: of one the page numbers are looked up, of one the rows (and, where it
+// opens a segment, the queries: the products have just used the last ones) are on their way, one is worked on.  Where every segment began
+// with its own chain of look-ups, 256 sequences that had just begun took 4 us a tile.
 template <int D, int CB>
-__device__ void own_part(const BranchParams &p, const Plan &plan, int own_wave, float *part_o, float2 *part_ml, unsigned char *vt)
+__device__ void own_part(const BranchParams &p, const Plan &plan, int own_wave, int len0, int rows0, float *part_o, float2 *part_ml, unsigned char *vt)
 {
     constexpr int NC = D / 32, NDB = D / 16, UPR = D / 8, RPL = 64 / UPR, NV = TK / RPL, R = 16 * CB;
     const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
-    const int Mt = p.G * p.Bt, blocks = (Mt + R - 1) / R, shift = p.pages.page_shift;
-    int at = own_wave * plan.own_chunk;
-    const int end = min(at + plan.own_chunk, plan.own_tiles);
-    if (at >= end) return;
-    // the sequence whose tiles hold tile `at`: `first` its first tile in the list
-    int s = 0, first = 0, seg_of_s = 0;
-    for (int base = 0; base < p.n_seqs; base += 64) {
-        const int mine = base + lane < p.n_seqs ? (own_rows(p, base + lane) + TK - 1) / TK * p.hkv * blocks : 0;
-        int upto = mine;   // inclusive sum over the lanes
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
+    const int Mt = p.G * p.Bt, blocks = (Mt + R - 1) / R, per_seq = p.hkv * blocks, shift = p.pages.page_shift;
+    const int begin = own_wave * plan.own_chunk, end = min(begin + plan.own_chunk, plan.own_tiles);
+    if (begin >= end) return;
+    // where a tile lies: sequence s (n own rows, `len` of them old), segment `local` of it, tile t of that
+    struct Place {
+        int s, local, t, n, nt, len;
+    };
+    auto enter = [&](Place &w, int s) {
+        w.s = s;
+        w.n = s < 64 ? __builtin_amdgcn_readlane(rows0, s & 63) : __builtin_amdgcn_readfirstlane(own_rows(p, s));
+        w.len = s < 64 ? __builtin_amdgcn_readlane(len0, s & 63) : __builtin_amdgcn_readfirstlane(p.pages.lens[s]);
+        w.nt = (w.n + TK - 1) / TK;
+    };
+    auto advance = [&](Place &w) {   // (there is a next tile)
+        if (++w.t < w.nt) return;
+        w.t = 0;
+        if (++w.local < per_seq) return;
+        w.local = 0;
+        do enter(w, w.s + 1);
+        while (w.n == 0);
+    };
+    Place cur;
+    {
+        int first = 0, s = 0;
+        for (int base = 0; base < p.n_seqs; base += 64) {
+            const int mine = (base == 0 ? rows0 + TK - 1 : base + lane < p.n_seqs ? own_rows(p, base + lane) + TK - 1 : 0) / TK * per_seq;
+            const int upto = (int)wave_inclusive_scan((uint32_t)mine), all = __builtin_amdgcn_readlane(upto, 63);
+            if (first + all > begin) {
+                const int k = __builtin_ctzll(__builtin_amdgcn_ballot_w64(first + upto > begin));
+                s = base + k;
+                first += __builtin_amdgcn_readlane(upto, k) - __builtin_amdgcn_readlane(mine, k);
+                break;
+            }
+            first += all;
         }
-        const int all = __builtin_amdgcn_readlane(upto, 63);
-        if (first + all > at) {
-            const uint64_t past = __builtin_amdgcn_ballot_w64(first + upto > at);
-            const int k = __builtin_ctzll(past);
-            s = base + k;
-            first += __builtin_amdgcn_readlane(upto, k) - __builtin_amdgcn_readlane(mine, k);
-            break;
-        }
-        first += all;
+        enter(cur, s);
+        cur.local = (begin - first) / cur.nt;
+        cur.t = begin - first - cur.local * cur.nt;
     }
-    seg_of_s = s * p.hkv * blocks;
-    while (at < end) {
-        const int n = own_rows(p, s), nt = (n + TK - 1) / TK;   // uniform
-        if (at >= first + nt * p.hkv * blocks) {
-            first += nt * p.hkv * blocks;
-            ++s;
-            seg_of_s += p.hkv * blocks;
-            continue;
+    State<D, CB> st;
+    st.reset();
+    u32x4 kr[2][NC], vr[NV];
+    uint32_t absent = 0;   // bit i: rows 8 i .. of the tile in registers lie on a page that does not exist
+    int pages[4];
+    // A tile's rows lie in groups of eight on one page each (pages have a multiple of eight rows).  Rows past the last repeat it.
+    auto look_up = [&](const Place &w) {
+        const int32_t *table = p.pages.table + (size_t)w.s * p.pages.width;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pages[i] = table[min(w.t * TK + 8 * i, w.n - 1) >> shift];
+    };
+    auto load = [&](const Place &w) {
+        const int h = p.by_own_blocks.divide(w.local), last = w.n - 1;
+        const uint16_t *kg8[4], *vg8[4];   // first row of each group, head h
+        absent = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = min(w.t * TK + 8 * i, last & ~7);
+            int page = __builtin_amdgcn_readfirstlane(pages[i]);
+            if ((uint32_t)page >= (uint32_t)p.pages.n_pages) {
+                absent |= 1u << i;
+                page = 0;
+            }
+            const size_t off = ((((size_t)page * p.hkv + h) << shift) + (size_t)(row & ((1 << shift) - 1))) * D;
+            kg8[i] = p.pages.k + off;
+            vg8[i] = p.pages.v + off;
         }
-        const int local = (at - first) / nt, t0 = at - first - local * nt, t1 = min(nt, t0 + end - at);
-        at += t1 - t0;
-        const int h = local / blocks, mb = local - h * blocks;
-        const int len = p.pages.lens[s];
-        const int32_t *table = p.pages.table + (size_t)s * p.pages.width;
-        State<D, CB> st;
-        st.reset();
-        int vis[CB];   // rows [0, vis) are seen by the lane's query
+#pragma unroll
+        for (int kg = 0; kg < 2; ++kg) {
+            const int row = w.t * TK + 16 * kg + c16, in8 = min(row, last) & 7;
+            const uint16_t *kb = (c16 < 8 ? kg8[2 * kg] : kg8[2 * kg + 1]) + in8 * D + 8 * g;
+#pragma unroll
+            for (int cc = 0; cc < NC; ++cc) kr[kg][cc] = *reinterpret_cast<const u32x4 *>(kb + cc * 32);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int row = w.t * TK + i * RPL + lane / UPR, in8 = min(row, last) & 7;
+            vr[i] = *reinterpret_cast<const u32x4 *>(vg8[i * RPL / 8] + in8 * D + (lane % UPR) * 8);
+        }
+        if (absent) {   // (values of such rows may be anything: their weight is zero, and so are they)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (absent >> (i * RPL / 8) & 1) vr[i] = u32x4{0u, 0u, 0u, 0u};
+        }
+    };
+    auto row_of = [&](const Place &w, int cb) { return min((w.local - p.by_own_blocks.divide(w.local) * blocks) * R + 16 * cb + c16, Mt - 1); };
+    auto load_queries = [&](const Place &w) {
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-            const int m = min(mb * R + 16 * cb + c16, Mt - 1);
-            vis[cb] = min(len + m % p.Bt + 1, n);
-            const uint16_t *qr = query_row(p, s, h, m) + 8 * g;
+            const uint16_t *qr = query_row(p, w.s, p.by_own_blocks.divide(w.local), row_of(w, cb)) + 8 * g;
 #pragma unroll
             for (int cc = 0; cc < NC; ++cc) st.q[cb][cc] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qr + cc * 32));
         }
-        u32x4 kr[2][NC], vr[NV];
-        uint32_t absent = 0;   // bit i: rows 8 i .. of the tile in registers lie on a page that does not exist
-        // A tile's rows lie in groups of eight on one page each (pages have a multiple of eight rows).  The numbers of its pages are
-        // requested a tile ahead of its rows.  Rows past the last repeat it.
-        int pages[4];
-        auto look_up = [&](int t) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pages[i] = table[min(t * TK + 8 * i, n - 1) >> shift];
-        };
-        auto load = [&](int t) {
-            const uint16_t *kg8[4], *vg8[4];   // first row of each group, head h
-            absent = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = min(t * TK + 8 * i, (n - 1) & ~7);
-                int page = __builtin_amdgcn_readfirstlane(pages[i]);
-                if ((uint32_t)page >= (uint32_t)p.pages.n_pages) {
-                    absent |= 1u << i;
-                    page = 0;
-                }
-                const size_t off = ((((size_t)page * p.hkv + h) << shift) + (size_t)(row & ((1 << shift) - 1))) * D;
-                kg8[i] = p.pages.k + off;
-                vg8[i] = p.pages.v + off;
-            }
-            const int last = n - 1;
-#pragma unroll
-            for (int kg = 0; kg < 2; ++kg) {
-                const int row = t * TK + 16 * kg + c16, in8 = min(row, last) & 7;
-                const uint16_t *kb = (c16 < 8 ? kg8[2 * kg] : kg8[2 * kg + 1]) + in8 * D + 8 * g;
-#pragma unroll
-                for (int cc = 0; cc < NC; ++cc) kr[kg][cc] = *reinterpret_cast<const u32x4 *>(kb + cc * 32);
-            }
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int row = t * TK + i * RPL + lane / UPR, in8 = min(row, last) & 7;
-                vr[i] = *reinterpret_cast<const u32x4 *>(vg8[i * RPL / 8] + in8 * D + (lane % UPR) * 8);
-            }
-            if (absent) {   // (values of such rows may be anything: their weight is zero, and so are they)
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (absent >> (i * RPL / 8) & 1) vr[i] = u32x4{0u, 0u, 0u, 0u};
-            }
-        };
-        look_up(t0);
-        load(t0);
-        look_up(t0 + 1);
-        for (int t = t0; t < t1; ++t) {
-            const uint32_t hidden = absent;
-            store_v<D>(vt, vr, lane);
-            tile_step<D, CB>(
-                st, vt, p.scale_log2e, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); },
-                [&]() {
-                    if (t + 1 < t1) {
-                        load(t + 1);
-                        look_up(t + 2);
+    };
+    Place nxt = cur, far = cur;
+    look_up(cur);
+    load_queries(cur);
+    load(cur);
+    if (begin + 1 < end) {
+        advance(nxt);
+        look_up(nxt);
+    }
+    for (int at = begin; at < end; ++at) {
+        const uint32_t hidden = absent;
+        const bool ends = at + 1 == end || nxt.t == 0;   // the wave's last tile of the segment
+        store_v<D>(vt, vr, lane);
+        tile_step<D, CB>(
+            st, vt, p.scale_log2e, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); },
+            [&]() {
+                if (at + 1 < end) {
+                    load(nxt);
+                    if (nxt.t == 0) load_queries(nxt);
+                    far = nxt;
+                    if (at + 2 < end) {
+                        advance(far);
+                        look_up(far);
                     }
-                },
-                [&](f32x4 (&sc)[CB][2]) {
-                    if ((t + 1) * TK > min(len, n) || hidden) {   // uniform: rows that not every query sees
+                }
+            },
+            [&](f32x4 (&sc)[CB][2]) {
+                if ((cur.t + 1) * TK > min(cur.len, cur.n) || hidden) {   // uniform: rows that not every query sees
 #pragma unroll
-                        for (int cb = 0; cb < CB; ++cb) {
-                            const int lim = vis[cb] - t * TK - 4 * g;
+                    for (int cb = 0; cb < CB; ++cb) {
+                        const int m = row_of(cur, cb), vis = min(cur.len + m - p.by_Bt.divide(m) * p.Bt + 1, cur.n);
+                        const int lim = vis - cur.t * TK - 4 * g;
 #pragma unroll
-                            for (int kg = 0; kg < 2; ++kg) {
-                                const bool gone = hidden >> (2 * kg + (g >> 1)) & 1;
+                        for (int kg = 0; kg < 2; ++kg) {
+                            const bool gone = hidden >> (2 * kg + (g >> 1)) & 1;
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) sc[cb][kg][i] = 16 * kg + i < lim && !gone ? sc[cb][kg][i] : -INFINITY;
-                            }
+                            for (int i = 0; i < 4; ++i) sc[cb][kg][i] = 16 * kg + i < lim && !gone ? sc[cb][kg][i] : -INFINITY;
                         }
                     }
-                });
-        }
-        const size_t slot = (size_t)own_wave + seg_of_s + local;
+                }
+            });
+        if (ends) {
+            const size_t slot = (size_t)own_wave + (size_t)cur.s * per_seq + cur.local;
+            const int first_row = (cur.local - p.by_own_blocks.divide(cur.local) * blocks) * R;
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            const float L = sum_over_rows(st.l[cb]), inv = L > 0.f ? 1.f / L : 0.f;
-            if (mb * R + 16 * cb + c16 < Mt) {
-                float *ow = part_o + (slot * R + 16 * cb + c16) * D;
+            for (int cb = 0; cb < CB; ++cb) {
+                const float L = sum_over_rows(st.l[cb]), inv = L > 0.f ? 1.f / L : 0.f;
+                if (first_row + 16 * cb + c16 < Mt) {
+                    float *ow = part_o + (slot * R + 16 * cb + c16) * D;
 #pragma unroll
-                for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(ow + 16 * db + 4 * g) = st.o[cb][db] * inv;
-                if (g == 0) part_ml[slot * R + 16 * cb + c16] = make_float2(st.m[cb], L);
+                    for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(ow + 16 * db + 4 * g) = st.o[cb][db] * inv;
+                    if (g == 0) part_ml[slot * R + 16 * cb + c16] = make_float2(st.m[cb], L);
+                }
             }
+            st.reset();
         }
+        cur = nxt;
+        nxt = far;
     }
 }
 
@@ -736,71 +749,78 @@ constexpr int lds_bytes()
     return waves;
 }
 
+// How the work is cut: the same on every wave.  rows0: own rows of sequence `lane`.
+// No piece leaves its segment: the start and the end of a segment cost a workgroup several tiles' time.  Every lane prices one way to
+// deal the workgroups -- `splits` pieces of each segment, or with more segments than workgroups a share of the workgroups for
+// whole or halved segments -- and the cheapest is taken.  Prices in us, of a tile step that is not held up by the others' traffic
+// (STEP: measured; OWN_STEP likewise, of a wave); where traffic is the limit the shares hardly matter.
+template <int RS, int RO>
+__device__ __forceinline__ Plan make_plan(const BranchParams &p, int units, int wgs, int rows0, int lane)
+{
+    constexpr float STEP = RS == 256 ? 1.35f : RS == 128 ? 1.5f : RS == 64 ? 2.2f : 2.5f, SHARED_FIXED = 6.f, OWN_STEP = 2.5f;
+    auto up = [](float x, float y) { return __builtin_ceilf(x * __builtin_amdgcn_rcpf(y)); };   // (a price may be off by the quotient's last bit)
+    Plan plan;
+    int own = (rows0 + TK - 1) / TK;
+    for (int base = 64; base < p.n_seqs; base += 64) own += base + lane < p.n_seqs ? (own_rows(p, base + lane) + TK - 1) / TK : 0;
+    plan.own_tiles = __builtin_amdgcn_readlane((int)wave_inclusive_scan((uint32_t)own), 63) * p.hkv * ((p.G * p.Bt + RO - 1) / RO);
+    const int segs = p.shared_segs, most = plan.own_tiles > 0 ? wgs - 1 : wgs;
+    int w = 0, splits = 1;
+    float price = INFINITY;
+    if (segs > 0 && segs <= most) {
+        const int top = min(p.by_segs.divide(most), units);
+        splits = min((lane + 1) * ((top + 63) / 64), top);
+        w = segs * splits;
+        price = up((float)units, (float)splits) * STEP;
+    } else if (segs > 0) {
+        w = max(most * (lane + 1) / 64, 1);
+        const float whole = up((float)segs, (float)w) * ((float)units * STEP + SHARED_FIXED);
+        const float half = up(2.f * (float)segs, (float)w) * ((float)((units + 1) / 2) * STEP + SHARED_FIXED);
+        splits = units > 1 && half < whole ? 2 : 1;
+        price = fminf(whole, half);
+    }
+    const int others = (wgs - w) * NW;
+    if (plan.own_tiles > 0) price = fmaxf(price, up((float)plan.own_tiles, (float)others) * OWN_STEP);
+    const uint32_t cheap = ~__float_as_uint(price);   // (prices are not negative: the cheapest has the largest complement)
+    uint32_t best = cheap;
+    best = max(best, dpp_fetch<0x111, 0xF>(best));
+    best = max(best, dpp_fetch<0x112, 0xF>(best));
+    best = max(best, dpp_fetch<0x114, 0xF>(best));
+    best = max(best, dpp_fetch<0x118, 0xF>(best));
+    best = max(best, dpp_fetch<0x142, 0xA>(best));
+    best = max(best, dpp_fetch<0x143, 0xC>(best));
+    best = (uint32_t)__builtin_amdgcn_readlane((int)best, 63);
+    const int from = __builtin_ctzll(__builtin_amdgcn_ballot_w64(cheap == best));   // (of equal ones that with the fewest pieces)
+    plan.splits = __builtin_amdgcn_readlane(splits, from);
+    plan.shared_wgs = segs > 0 ? __builtin_amdgcn_readlane(w, from) : 0;
+    const int waves = max((wgs - plan.shared_wgs) * NW, 1);
+    plan.own_chunk = max((int)((float)plan.own_tiles * __builtin_amdgcn_rcpf((float)waves)), 1);
+    while ((int64_t)plan.own_chunk * waves < plan.own_tiles) ++plan.own_chunk;
+    return plan;
+}
+
 template <int D, int RS, int RO>
 __global__ __launch_bounds__(64 * NW) void branch_main_kernel(BranchParams p)
 {
+    warm_arguments<sizeof(BranchParams)>();
     __shared__ __attribute__((aligned(1024))) unsigned char smem[lds_bytes<D, RS>()];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int Mt = p.G * p.Bt, M = p.fan * Mt;
-    const int wgs = (int)gridDim.x;
-    // ---- the lists and how they are dealt: the same on every wave
-    Plan plan;
-    int own = 0;
-    for (int base = 0; base < p.n_seqs; base += 64) own += base + lane < p.n_seqs ? (own_rows(p, base + lane) + TK - 1) / TK : 0;
-    plan.own_tiles = __builtin_amdgcn_readfirstlane(wave_sum(own)) * p.hkv * ((Mt + RO - 1) / RO);
-    {
-        constexpr int KW = RS > 32 ? NW / (RS / 32) : NW;   // tiles that a workgroup of the shared part works on at a time
-        const int nt = (p.prefix_len + TK - 1) / TK, units = (nt + KW - 1) / KW;
-        plan.shared_segs = nt > 0 ? p.n_prefixes * p.hkv * ((M + RS - 1) / RS) : 0;
-        // No piece leaves its segment: the start and the end of a segment cost a workgroup several tiles' time.  Every lane prices one way to
-        // deal the workgroups -- `splits` pieces of each segment, or with more segments than workgroups a share of the workgroups for
-        // whole or halved segments -- and the cheapest is taken.  Prices in us, of a tile step that is not held up by the others' traffic
-        // (STEP: measured; OWN_STEP likewise, of a wave); where traffic is the limit the shares hardly matter.
-        constexpr float STEP = RS == 256 ? 0.8f : RS == 128 ? 1.3f : RS == 64 ? 2.2f : 2.5f, SHARED_FIXED = 6.f, OWN_STEP = 2.5f;
-        const int segs = plan.shared_segs, most = plan.own_tiles > 0 ? wgs - 1 : wgs;
-        int w = 0, splits = 1;
-        float price = INFINITY;
-        if (segs > 0 && segs <= most) {
-            const int top = min(most / segs, units);
-            splits = min((lane + 1) * ((top + 63) / 64), top);
-            w = segs * splits;
-            price = (float)((units + splits - 1) / splits) * STEP;
-        } else if (segs > 0) {
-            w = max(most * (lane + 1) / 64, 1);
-            const float whole = (float)((segs + w - 1) / w) * ((float)units * STEP + SHARED_FIXED);
-            const float half = (float)((2 * segs + w - 1) / w) * ((float)((units + 1) / 2) * STEP + SHARED_FIXED);
-            splits = units > 1 && half < whole ? 2 : 1;
-            price = fminf(whole, half);
-        }
-        const int others = (wgs - w) * NW;
-        price = fmaxf(price, (float)((plan.own_tiles + others - 1) / max(others, 1)) * OWN_STEP);
-        float best = price;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) best = fminf(best, __shfl_xor(best, d));
-        const int from = __builtin_ctzll(__builtin_amdgcn_ballot_w64(price == best) | 1ull << 63);
-        plan.splits = __builtin_amdgcn_readlane(splits, from);
-        plan.shared_wgs = segs > 0 ? __builtin_amdgcn_readlane(w, from) : 0;
-        const int waves = max((wgs - plan.shared_wgs) * NW, 1);
-        plan.own_chunk = max((plan.own_tiles + waves - 1) / waves, 1);
-    }
-    if (blockIdx.x == 0) {   // ... for the merge
-        if (tid == 0) {
+    const int Mt = p.G * p.Bt, wgs = (int)gridDim.x;
+    const int len0 = p.pages.lens[min(lane, p.n_seqs - 1)], asked0 = asked_of(p, min(lane, p.n_seqs - 1));
+    constexpr int KW = RS > 32 ? NW / (RS / 32) : NW;   // tiles that a workgroup of the shared part works on at a time
+    const int units = ((p.prefix_len + TK - 1) / TK + KW - 1) / KW;
+    const int rows0 = lane < p.n_seqs ? own_rows(p, len0, asked0) : 0;
+    const Plan plan = make_plan<RS, RO>(p, units, wgs, rows0, lane);
+    if (blockIdx.x == 0 && wave == 0) {   // ... for the join
+        if (lane == 0) {
             p.plan[0] = plan.splits;
             p.plan[1] = plan.own_chunk;
         }
-        if (wave == 0) {
-            int first = 0;
-            for (int base = 0; base < p.n_seqs; base += 64) {
-                const int mine = base + lane < p.n_seqs ? (own_rows(p, base + lane) + TK - 1) / TK : 0;
-                int upto = mine;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int o = __shfl_up(upto, d);
-                    if (lane >= d) upto += o;
-                }
-                if (base + lane < p.n_seqs) p.plan[BRANCH_PLAN_WORDS + base + lane] = first + upto - mine;
-                first += __builtin_amdgcn_readlane(upto, 63);
-            }
+        int first = 0;
+        for (int base = 0; base < p.n_seqs; base += 64) {
+            const int mine = (base == 0 ? rows0 + TK - 1 : base + lane < p.n_seqs ? own_rows(p, base + lane) + TK - 1 : 0) / TK;
+            const int upto = (int)wave_inclusive_scan((uint32_t)mine);
+            if (base + lane < p.n_seqs) p.plan[BRANCH_PLAN_WORDS + base + lane] = first + upto - mine;
+            first += __builtin_amdgcn_readlane(upto, 63);
         }
     }
     if ((int)blockIdx.x < plan.shared_wgs) {
@@ -808,8 +828,8 @@ __global__ __launch_bounds__(64 * NW) void branch_main_kernel(BranchParams p)
         else shared_few<D, RS / 16>(p, plan, smem);
     } else {
         const size_t rows = shared_slots(p.n_prefixes, p.fan, p.hkv, Mt, RS, wgs) * RS;
-        own_part<D, RO / 16>(p, plan, ((int)blockIdx.x - plan.shared_wgs) * NW + wave, p.part_o + rows * D, p.part_ml + rows,
-                         smem + (size_t)wave * TK * D * 2);
+        own_part<D, RO / 16>(p, plan, ((int)blockIdx.x - plan.shared_wgs) * NW + wave, len0, rows0, p.part_o + rows * D, p.part_ml + rows,
+                             smem + (size_t)wave * TK * D * 2);
     }
 }
 
@@ -827,22 +847,24 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
     const int64_t row = (int64_t)blockIdx.x * (256 / TPR / groups) + unit / groups;
     const int d0 = (int)threadIdx.x % TPR * 4;
     const bool exists = row < (int64_t)p.n_seqs * p.hkv * Mt;
-    const int sh = exists ? (int)(row / Mt) : 0, m = exists ? (int)(row - (int64_t)sh * Mt) : 0, s = sh / p.hkv, h = sh - s * p.hkv;
-    const bool wanted = exists && m % p.Bt < new_of(p, s);   // else left as it was
+    const int sh = exists ? p.by_Mt.divide((int)row) : 0, m = exists ? (int)row - sh * Mt : 0, s = p.by_hkv.divide(sh), h = sh - s * p.hkv;
+    // (all that says where the pieces are is requested at once)
+    const int len = p.pages.lens[s], asked = asked_of(p, s), splits = p.plan[0], chunk = p.plan[1], tiles_before = p.plan[BRANCH_PLAN_WORDS + s];
+    const bool wanted = exists && m - p.by_Bt.divide(m) * p.Bt < new_of(p, len, asked);   // else left as it was
     // the pieces: na slots of the shared part, nb slots from b0 on of the own part
     int a0 = 0, na = 0, segs = 0, b0 = 0, nb = 0, am = 0, bm = 0;
     if (wanted) {
         if (p.prefix_len > 0) {
-            const int c = s / p.fan, mm = (s - c * p.fan) * Mt + m;
+            const int c = p.by_fan.divide(s), mm = (s - c * p.fan) * Mt + m;
             am = mm % RS;
             a0 = mm / RS * p.n_prefixes * p.hkv + c * p.hkv + h;   // piece i in slot a0 + i segs
-            segs = p.n_prefixes * p.hkv * ((p.fan * Mt + RS - 1) / RS);
-            na = p.plan[0];
+            segs = p.shared_segs;
+            na = splits;
         }
-        const int n = own_rows(p, s);
+        const int n = own_rows(p, len, asked);
         if (n > 0) {
-            const int blocks = (Mt + RO - 1) / RO, nt = (n + TK - 1) / TK, chunk = p.plan[1];
-            const int local = h * blocks + m / RO, first = p.plan[BRANCH_PLAN_WORDS + s] * p.hkv * blocks + local * nt;
+            const int blocks = (Mt + RO - 1) / RO, nt = (n + TK - 1) / TK;
+            const int local = h * blocks + m / RO, first = tiles_before * p.hkv * blocks + local * nt;
             const int seg = s * p.hkv * blocks + local;
             bm = m % RO;
             b0 = first / chunk;
@@ -903,12 +925,12 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
     *reinterpret_cast<bf16x4 *>(p.out + (((size_t)s * p.hkv + h) * Mt + m) * D + d0) = o;
 }
 
-// Query rows of a block: of the own part 16, or 32 where a sequence has more; of the shared part as many waves of 32 rows as there
-// are rows for, up to eight.  Above four waves' rows, blocks of four or of eight waves, whichever leaves fewer waves without rows.
+// Query rows of a block: of the own part 16, or 32 where a sequence has more; of the shared part 16, or two, four or eight waves of 32
+// rows.  Above four waves' rows, blocks of four or of eight waves, whichever leaves fewer waves without rows.
 int own_block(int64_t rows) { return rows > 16 ? 32 : 16; }
 int shared_block(int64_t rows)
 {
-    if (rows <= 32) return rows > 16 ? 32 : 16;
+    if (rows <= 16) return 16;
     if (rows <= 64) return 64;
     if (rows <= 128) return 128;
     return (rows + 255) / 256 * 2 <= (rows + 127) / 128 ? 256 : 128;
@@ -953,7 +975,6 @@ hipError_t launch(const BranchParams &p, int RS, hipStream_t s)
 {
     switch (RS) {
     case 16: return launch<D, 16, RO>(p, s);
-    case 32: return launch<D, 32, RO>(p, s);
     case 64: return launch<D, 64, RO>(p, s);
     case 128: return launch<D, 128, RO>(p, s);
     default: return launch<D, 256, RO>(p, s);
@@ -962,10 +983,18 @@ hipError_t launch(const BranchParams &p, int RS, hipStream_t s)
 
 }  // namespace
 
-hipError_t launch_branch_attention(const BranchParams &p, hipStream_t s)
+hipError_t launch_branch_attention(BranchParams p, hipStream_t s)
 {
     const int64_t Mt = (int64_t)p.G * p.Bt;
     const int RS = shared_block(p.fan * Mt), RO = own_block(Mt);
+    p.shared_segs = p.prefix_len > 0 ? (int32_t)(p.n_prefixes * p.hkv * ((p.fan * Mt + RS - 1) / RS)) : 0;
+    p.by_segs.set(p.shared_segs > 0 ? p.shared_segs : 1);
+    p.by_heads.set(p.n_prefixes > 0 ? p.n_prefixes * p.hkv : 1);
+    p.by_hkv.set(p.hkv);
+    p.by_Mt.set((uint32_t)Mt);
+    p.by_Bt.set(p.Bt);
+    p.by_fan.set(p.fan > 0 ? p.fan : 1);
+    p.by_own_blocks.set((uint32_t)((Mt + RO - 1) / RO));
     if (p.D == 128) return RO == 16 ? launch<128, 16>(p, RS, s) : launch<128, 32>(p, RS, s);
     if (p.D == 64) return RO == 16 ? launch<64, 16>(p, RS, s) : launch<64, 32>(p, RS, s);
     return hipErrorInvalidValue;

@@ -55,6 +55,23 @@ struct NormRopeLayers {
 hipError_t launch_norm_rope_layers(const NormRopeLayers &p, hipStream_t s);
 
 // ------------------------------------------------------------------ attention of sequences that share a prompt's cache
+// Quotients of numbers below 2^31 by a number that the host knows (three instructions; the compiler's division, some forty that wait for one
+// another, eleven of them ahead of a launch's first loads, took 1.5 us).  With s the bits of d - 1 and mul = 2^32 (2^s - d) / d + 1 rounded down,
+// n / d = (n mul / 2^32 + n) / 2^s.
+struct Divisor {
+    uint32_t mul, shift;
+    void set(uint32_t d)
+    {
+        shift = 0;
+        while ((1ull << shift) < d) ++shift;
+        mul = (uint32_t)((((1ull << shift) - d) << 32) / d + 1);
+    }
+#ifdef __HIP_DEVICE_COMPILE__
+    __device__ __forceinline__ int divide(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+#else
+    int divide(int n) const { return (int)((uint32_t)(((uint64_t)(uint32_t)n * mul) >> 32) + (uint32_t)n) >> shift; }
+#endif
+};
 struct BranchParams {
     Rows q;
     uint16_t *out;                        // [n_seqs][hq][Bt][D]
@@ -68,10 +85,11 @@ struct BranchParams {
     int64_t prefix_cap;
     int32_t cus;
     float scale_log2e;
+    int32_t shared_segs;                  // (prompt, head, block of rows) segments of the shared part; 0: there is none
+    Divisor by_segs, by_heads, by_hkv, by_Mt, by_Bt, by_fan, by_own_blocks;   // heads: n_prefixes hkv; Mt: G Bt
 };
 constexpr int BRANCH_PLAN_WORDS = 8;
 size_t branch_workspace(int n_seqs, int n_prefixes, int hkv, int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_plan);
-hipError_t configure_branch_kernels();
-hipError_t launch_branch_attention(const BranchParams &p, hipStream_t s);
+hipError_t launch_branch_attention(BranchParams p, hipStream_t s);   // (segments and divisors are filled in here)
 
 }  // namespace kd

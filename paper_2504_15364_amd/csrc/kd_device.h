@@ -79,6 +79,16 @@ __device__ __forceinline__ void lds_copy16(uint32_t lds_base, const void *gaddr)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(base), "v"(gaddr) : "memory");
 }
 
+// ... from a uniform address and an offset of 32 bits per lane
+__device__ __forceinline__ void lds_copy16(uint32_t lds_base, const void *gbase, uint32_t byte_off)
+{
+    const uint32_t base = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_base);
+    const uint64_t g = (uint64_t)(uintptr_t)gbase;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)g), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(g >> 32));
+    const uint64_t gu = ((uint64_t)hi << 32) | (uint64_t)lo;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(base), "v"(byte_off), "s"(gu) : "memory");
+}
+
 __device__ __forceinline__ double bf16_lo(uint32_t w) { return (double)__uint_as_float(w << 16); }
 __device__ __forceinline__ double bf16_hi(uint32_t w) { return (double)__uint_as_float(w & 0xFFFF0000u); }
 

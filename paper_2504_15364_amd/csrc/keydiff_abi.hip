@@ -1283,7 +1283,7 @@ int check_prefixes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, 
 {
     if (n_prefixes < 0 || (n_prefixes > 0 && b->n_seqs % n_prefixes))
         return fail(KEYDIFF_ESHAPE, "n_prefixes must divide the %d sequences, got %d", b->n_seqs, n_prefixes);
-    if (prefix_len < 0 || prefix_len > 0x3fffffff) return fail(KEYDIFF_ESHAPE, "prefix_len must lie in [0, 2^30), got %d", prefix_len);
+    if (prefix_len < 0 || prefix_len > (1 << 23)) return fail(KEYDIFF_ESHAPE, "prefix_len must lie in [0, 2^23], got %d", prefix_len);
     const int64_t Mt = (int64_t)b->n_q_heads / b->n_kv_heads * Bt, fan = n_prefixes > 0 ? b->n_seqs / n_prefixes : 0;
     const double shared = (double)n_prefixes * b->n_kv_heads * (fan * Mt / 16 + 1) * (prefix_len / 32 + 1);
     const double own = (double)b->n_seqs * b->n_kv_heads * (Mt / 16 + 1) * ((int64_t)b->table_width * b->page_rows / 32 + 1);
