@@ -680,6 +680,12 @@ __device__ void own_part(const BranchParams &p, const Plan &plan, int own_wave, 
     for (int at = begin; at < end; ++at) {
         const uint32_t hidden = absent;
         const bool ends = at + 1 == end || nxt.t == 0;   // the wave's last tile of the segment
+        // Of the two waves of a SIMD the older one goes first whenever both could: with equal shares of a long list it was done after
+        // 89 us, the younger one after 108.  The younger one goes first every other tile.
+        if (threadIdx.x >= 64 * NW / 2) {
+            if ((at - begin) & 1) __builtin_amdgcn_s_setprio(0);
+            else __builtin_amdgcn_s_setprio(1);
+        }
         store_v<D>(vt, vr, lane);
         tile_step<D, CB>(
             st, vt, p.scale_log2e, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); },
@@ -749,15 +755,26 @@ constexpr int lds_bytes()
     return waves;
 }
 
+// Prices in us, measured by stamps of the clock inside the kernel where neither part waits for the other's traffic: a step of the shared part
+// (every group of waves a tile) and what a task takes besides; a tile of a wave of the own part and what a wave takes besides; and what a
+// tile of own rows takes at the rate that memory gives all workgroups together, which no share of them changes.
+template <int D, int RS, int RO>
+struct Prices {
+    static constexpr bool wide = D == 128;
+    static constexpr float step = RS == 256 ? (wide ? 1.3f : 1.0f) : RS == 128 ? (wide ? 1.45f : 1.1f) : RS == 64 ? (wide ? 2.35f : 1.1f) : (wide ? 2.5f : 1.5f);
+    static constexpr float task = RS == 256 ? (wide ? 9.f : 7.f) : RS == 128 ? (wide ? 9.5f : 6.5f) : RS == 64 ? (wide ? 8.8f : 5.5f) : (wide ? 4.5f : 4.f);
+    static constexpr float own_tile = RO == 16 ? (wide ? 2.7f : 1.8f) : (wide ? 3.8f : 2.2f), own_wave = 4.f;
+    static constexpr float own_traffic = TK * D * 4 / 5.5e6f;
+};
+
 // How the work is cut: the same on every wave.  rows0: own rows of sequence `lane`.
 // No piece leaves its segment: the start and the end of a segment cost a workgroup several tiles' time.  Every lane prices one way to
 // deal the workgroups -- `splits` pieces of each segment, or with more segments than workgroups a share of the workgroups for
-// whole or halved segments -- and the cheapest is taken.  Prices in us, of a tile step that is not held up by the others' traffic
-// (STEP: measured; OWN_STEP likewise, of a wave); where traffic is the limit the shares hardly matter.
-template <int RS, int RO>
+// whole or halved segments -- and the cheapest is taken.
+template <int D, int RS, int RO>
 __device__ __forceinline__ Plan make_plan(const BranchParams &p, int units, int wgs, int rows0, int lane)
 {
-    constexpr float STEP = RS == 256 ? 1.35f : RS == 128 ? 1.5f : RS == 64 ? 2.2f : 2.5f, SHARED_FIXED = 6.f, OWN_STEP = 2.5f;
+    using P = Prices<D, RS, RO>;
     auto up = [](float x, float y) { return __builtin_ceilf(x * __builtin_amdgcn_rcpf(y)); };   // (a price may be off by the quotient's last bit)
     Plan plan;
     int own = (rows0 + TK - 1) / TK;
@@ -770,16 +787,19 @@ __device__ __forceinline__ Plan make_plan(const BranchParams &p, int units, int 
         const int top = min(p.by_segs.divide(most), units);
         splits = min((lane + 1) * ((top + 63) / 64), top);
         w = segs * splits;
-        price = up((float)units, (float)splits) * STEP;
+        price = up((float)units, (float)splits) * P::step + P::task;
     } else if (segs > 0) {
         w = max(most * (lane + 1) / 64, 1);
-        const float whole = up((float)segs, (float)w) * ((float)units * STEP + SHARED_FIXED);
-        const float half = up(2.f * (float)segs, (float)w) * ((float)((units + 1) / 2) * STEP + SHARED_FIXED);
+        const float whole = up((float)segs, (float)w) * ((float)units * P::step + P::task);
+        const float half = up(2.f * (float)segs, (float)w) * ((float)((units + 1) / 2) * P::step + P::task);
         splits = units > 1 && half < whole ? 2 : 1;
         price = fminf(whole, half);
     }
     const int others = (wgs - w) * NW;
-    if (plan.own_tiles > 0) price = fmaxf(price, up((float)plan.own_tiles, (float)others) * OWN_STEP);
+    if (plan.own_tiles > 0) {
+        const float own_price = fmaxf(up((float)plan.own_tiles, (float)others) * P::own_tile, (float)plan.own_tiles * P::own_traffic) + P::own_wave;
+        price = segs > 0 ? fmaxf(price, own_price) : own_price;
+    }
     const uint32_t cheap = ~__float_as_uint(price);   // (prices are not negative: the cheapest has the largest complement)
     uint32_t best = cheap;
     best = max(best, dpp_fetch<0x111, 0xF>(best));
@@ -809,7 +829,7 @@ __global__ __launch_bounds__(64 * NW) void branch_main_kernel(BranchParams p)
     constexpr int KW = RS > 32 ? NW / (RS / 32) : NW;   // tiles that a workgroup of the shared part works on at a time
     const int units = ((p.prefix_len + TK - 1) / TK + KW - 1) / KW;
     const int rows0 = lane < p.n_seqs ? own_rows(p, len0, asked0) : 0;
-    const Plan plan = make_plan<RS, RO>(p, units, wgs, rows0, lane);
+    const Plan plan = make_plan<D, RS, RO>(p, units, wgs, rows0, lane);
     if (blockIdx.x == 0 && wave == 0) {   // ... for the join
         if (lane == 0) {
             p.plan[0] = plan.splits;
