@@ -299,10 +299,12 @@ def _pack_form(hq, hkv, d, cos, sin, q_weight, k_weight, eps, device):
     elif q_weight is not k_weight:
         raise ValueError("q_weight and k_weight are given together or not at all")
     if cos is not None and sin is not None:
-        if cos.dim() != 2:
-            raise ValueError(f"cos must be a float32 table [positions][{d // 2}], got {tuple(cos.shape)}")
-        rows = cos.shape[0]
-        c, s = _dense("cos", cos, (rows, d // 2), torch.float32, device), _dense("sin", sin, (rows, d // 2), torch.float32, device)
+        shape = cos.shape
+        if not (len(shape) == 2 and shape[1] == d // 2 and sin.shape == shape and cos.dtype is sin.dtype is torch.float32
+                and cos.is_contiguous() and sin.is_contiguous() and cos.device == sin.device == device):
+            rows = shape[0] if len(shape) == 2 else 0
+            _dense("cos", cos, (rows, d // 2), torch.float32, device), _dense("sin", sin, (rows, d // 2), torch.float32, device)
+        rows, c, s = shape[0], cos.data_ptr(), sin.data_ptr()
     elif cos is not sin:
         raise ValueError("cos and sin are given together or not at all")
     return _ROW_FORM.pack(qw, kw, qs, ks, eps, c, s, rows)
@@ -347,9 +349,9 @@ def norm_rope(q, k, cos=None, sin=None, pos0: int = 0, positions=None, q_weight=
         _dense("k_out", k_out, (b, hkv, T, d), bf16, device)
     _need_gpu(device)
     if q_out is None:
-        q_out = torch.empty((b, hq, T, d), dtype=bf16, device=device)
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if k_out is None:
-        k_out = torch.empty((b, hkv, T, d), dtype=bf16, device=device)
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
     _enqueue(device, stream, load_library().keydiff_norm_rope, rq, rk, b, hq, hkv, d, T, int(pos0), at, form, q_out.data_ptr(),
              k_out.data_ptr())
     return q_out, k_out
@@ -397,7 +399,7 @@ def branch_append(q, k_new, v_new, k_pages, v_pages, table, lens, n_new=None, po
     form = _pack_form(hq, hkv, d, cos, sin, q_weight, k_weight, norm_eps, device)
     _need_gpu(device)
     if q is not None and q_out is None:
-        q_out = torch.empty((n, hq, Bt, d), dtype=bf16, device=device)
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         out = q_out.data_ptr()
     _enqueue(device, stream, load_library().keydiff_branch_append, b, rq, rk, rv, Bt, first, form, out)
     return q_out
@@ -465,7 +467,7 @@ def branch_attention(q, k_pages, v_pages, table, lens, prefix=None, n_new=None, 
     elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need or workspace.device != device:
         raise ValueError(f"workspace must be a contiguous uint8 tensor of at least {need} elements on {device}")
     if out is None:
-        out = torch.empty((n, hq, Bt, d), dtype=bf16, device=device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
         to = out.data_ptr()
     if cache is not None:
         _enqueue(device, stream, cache._L.keydiff_cache_branch_attention, cache._h, b, rq, Bt, to, workspace.data_ptr(), workspace.numel())
