@@ -8,7 +8,7 @@ Tolerances, from the arithmetic (u = 2^-24, the half step of float; 2^-8 the hal
                      two to spare, then one rounding to bf16
   attention          logits: 128 products summed in float, at most 128 u = 2^-17 of sum |q_i k_i| scale = A, and one rounding of the
                      scaled logit: a relative error of the weight of 2 * 2^-17 A; the exponential 2^-22, the weight as two
-                     bf16 numbers 2^-17, sums of n weights and values in float tile by tile (n / 32 + 60) u: e in all, on the
+                     bf16 numbers 2^-16, sums of n weights and values in float tile by tile (n / 32 + 60) u: e in all, on the
                      weights of numerator and denominator: |error| <= e (sum p |v| + |o|) + 2^-8 |o|
 """
 import math
@@ -278,7 +278,7 @@ def attention_reference(q, prefix, rows, own, j_of, scale):
         p = torch.softmax(a, -1)
         o = torch.bmm(p, v)
         A = torch.bmm(x.abs(), k.abs().transpose(1, 2).contiguous()).amax(-1, keepdim=True) * scale
-        e = 2.0 ** -16 * A + 2.0 ** -22 + 2.0 ** -17 + (k.shape[1] / 32 + 60) * 2.0 ** -24
+        e = 2.0 ** -16 * A + 2.0 ** -22 + 2.0 ** -16 + (k.shape[1] / 32 + 60) * 2.0 ** -24
         out[:, j] = o.view(hq, d)
         bound[:, j] = ((torch.bmm(p, v.abs()) + o.abs()) * e + U8 * o.abs()).view(hq, d)
     return out, bound
@@ -375,6 +375,31 @@ def test_branch_attention_dominant_keys_at_the_ends_of_pieces():
         own = k[:, N:].double(), v[:, N:].double()
         want, bound = attention_reference(q[0], (k.double(), v.double()), N, own, lambda j: L + 1, d ** -0.5)
         close(out[0], want, bound, f"key {at}")
+
+
+@pytest.mark.parametrize("fan", [3, 16, 40, 64])
+@pytest.mark.parametrize("power", [-90, 90])
+def test_branch_attention_values_of_extreme_size(fan, power):
+    # heads whose values differ by 2^30 from one another, all far from one
+    hq, hkv, d, N = 8, 2, 128, 700
+    g = gen(300 + fan + power)
+    lens = [(7 * i) % 60 for i in range(fan)]
+    k_pages, v_pages, table = paged(lens, 1, 16, hkv, d, g)
+    size = 2.0 ** (power + torch.randint(-15, 16, (hkv, 1, 1), **g).float())
+
+    def values(n):
+        return (torch.randn((hkv, n, d), **g) * size).bfloat16()
+
+    for s, L in enumerate(lens):
+        put_rows(k_pages, table, s, torch.randn((hkv, L + 1, d), **g).bfloat16())
+        put_rows(v_pages, table, s, values(L + 1))
+    kp, vp = torch.randn((1, hkv, N, d), **g).bfloat16(), values(N)[None]
+    q = torch.randn((fan, hq, 1, d), **g).bfloat16()
+    out = kd.branch_attention(q, k_pages, v_pages, table, ints(lens), prefix=(kp, vp.contiguous(), N))
+    for s, L in enumerate(lens):
+        own = rows_of(k_pages, table, s, L + 1), rows_of(v_pages, table, s, L + 1)
+        want, bound = attention_reference(q[s], (kp[0].double(), vp[0].double()), N, own, lambda j: L + 1, d ** -0.5)
+        close(out[s], want, bound, f"sequence {s}")
 
 
 def test_branch_attention_absent_pages():
