@@ -302,14 +302,18 @@ KEYDIFF_API int keydiff_branch_append(const keydiff_branches_t *b, const keydiff
  *   workspace           device, 256-byte aligned, of at least keydiff_branch_workspace_bytes; carries nothing between calls.
  *                       Calls that may overlap need workspaces of their own
  * The prompt's rows are read once for all sequences that share them.  Sums and softmax statistics are kept in float.
- * Inputs must be finite (those of rows that a query sees, and those of rows seen by another token of the same step).   */
+ * Meant for few tokens a sequence: a sequence's own rows are read once for every 32 of its query rows per KV head.
+ * Inputs must be finite (those of rows that a query sees, and those of rows seen by another token of the same step), values up to
+ * 2^100 in magnitude.  KEYDIFF_ESHAPE if the prompt has more than 2^23 rows, or if the tiles of 32 keys and 16 query rows that the
+ * prompts and the tables could hold do not fit in int32.                                                              */
 KEYDIFF_API int keydiff_branch_workspace_bytes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, size_t *bytes);
 KEYDIFF_API int keydiff_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt,
                              const void *k_prefix, const void *v_prefix, int32_t n_prefixes, int32_t prefix_len,
                              int64_t prefix_cap, float softmax_scale, void *out, void *workspace, size_t workspace_bytes,
                              void *stream);
 /* ... with the rows and the softmax scale of a KeyDiff cache: prompt i is sequence i of the cache's batch, and the rows are those it
- * holds when the call is made (a pending eviction is enqueued first).  The cache is not changed.                         */
+ * holds when the call is made (a pending eviction is enqueued first).  The cache is not changed.  (Profiling does not record these
+ * kernels.)                                                                                                              */
 KEYDIFF_API int keydiff_cache_branch_attention(keydiff_cache_t *prompt, const keydiff_branches_t *b, const keydiff_rows_t *q,
                                    int32_t Bt, void *out, void *workspace, size_t workspace_bytes, void *stream);
 

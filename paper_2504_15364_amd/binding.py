@@ -324,6 +324,21 @@ def _enqueue(device, stream, call, *args):
         _check(rc)
 
 
+def _on_stream(stream, device):
+    """Tensors allocated in this context belong to `stream` (an object of torch's or a handle): torch hands their memory out again in
+    the order of the work on it."""
+    import torch
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device))
+
+
+def _empty_like(t, stream):
+    import torch
+    if stream is None:
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    with _on_stream(stream, t.device):
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _need_gpu(device):
     if device.type != "cuda":
         raise ValueError(f"the tensors must live on a GPU, got {device}")
@@ -349,9 +364,9 @@ def norm_rope(q, k, cos=None, sin=None, pos0: int = 0, positions=None, q_weight=
         _dense("k_out", k_out, (b, hkv, T, d), bf16, device)
     _need_gpu(device)
     if q_out is None:
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        q_out = _empty_like(q, stream)
     if k_out is None:
-        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+        k_out = _empty_like(k, stream)
     _enqueue(device, stream, load_library().keydiff_norm_rope, rq, rk, b, hq, hkv, d, T, int(pos0), at, form, q_out.data_ptr(),
              k_out.data_ptr())
     return q_out, k_out
@@ -399,7 +414,7 @@ def branch_append(q, k_new, v_new, k_pages, v_pages, table, lens, n_new=None, po
     form = _pack_form(hq, hkv, d, cos, sin, q_weight, k_weight, norm_eps, device)
     _need_gpu(device)
     if q is not None and q_out is None:
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        q_out = _empty_like(q, stream)
         out = q_out.data_ptr()
     _enqueue(device, stream, load_library().keydiff_branch_append, b, rq, rk, rv, Bt, first, form, out)
     return q_out
@@ -461,13 +476,15 @@ def branch_attention(q, k_pages, v_pages, table, lens, prefix=None, n_new=None, 
     _need_gpu(device)
     need = _branch_workspace_bytes(n, hq, hkv, d, Bt, prompts, device.index)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        if stream is not None:   # torch must not hand the memory out again before the work on that stream is done
-            workspace.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device))
+        if stream is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        else:
+            with _on_stream(stream, device):
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
     elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need or workspace.device != device:
         raise ValueError(f"workspace must be a contiguous uint8 tensor of at least {need} elements on {device}")
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = _empty_like(q, stream)
         to = out.data_ptr()
     if cache is not None:
         _enqueue(device, stream, cache._L.keydiff_cache_branch_attention, cache._h, b, rq, Bt, to, workspace.data_ptr(), workspace.numel())

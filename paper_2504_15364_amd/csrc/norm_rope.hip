@@ -98,8 +98,7 @@ __device__ __forceinline__ void load_angles(const RowForm &f, int64_t position, 
 
 // The token and the heads of a group of D / 16 lanes: token blockIdx.x * tg + (group % tg), heads first, first + step, ... of `chunk` rounds
 struct Place {
-    int unit, first, step;
-    int64_t token;
+    int unit, first, step, token;
 };
 template <int D>
 __device__ __forceinline__ Place place_of(int tg_shift, int chunk)
@@ -110,7 +109,7 @@ __device__ __forceinline__ Place place_of(int tg_shift, int chunk)
     at.unit = (int)threadIdx.x % UPH;
     at.step = GROUPS >> tg_shift;
     at.first = (int)blockIdx.y * chunk * at.step + (group >> tg_shift);
-    at.token = (int64_t)blockIdx.x * tg + (group & (tg - 1));
+    at.token = (int)blockIdx.x * tg + (group & (tg - 1));
     return at;
 }
 
@@ -121,8 +120,8 @@ template <int D, bool APPEND>
 __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeParams p, int tg_shift, int chunk)
 {
     const Place at = place_of<D>(tg_shift, chunk);
-    if (at.token >= (int64_t)p.n_seqs * p.Bt) return;
-    const int seq = (int)(at.token / p.Bt), j = (int)(at.token % p.Bt);
+    if (at.token >= p.n_seqs * p.Bt) return;
+    const int seq = at.token / p.Bt, j = at.token % p.Bt;
     int64_t position;
     size_t page_at = 0;   // APPEND: element offset of head 0's row in the pools
     if constexpr (APPEND) {
@@ -174,8 +173,8 @@ __global__ __launch_bounds__(256) void norm_rope_layers_kernel(NormRopeLayers p,
 {
     const NormRopeLayer &l = p.layer[blockIdx.z];
     const Place at = place_of<D>(tg_shift, chunk);
-    if (at.token >= (int64_t)p.batch * p.Bt) return;
-    const int seq = (int)(at.token / p.Bt), j = (int)(at.token % p.Bt);
+    if (at.token >= p.batch * p.Bt) return;
+    const int seq = at.token / p.Bt, j = at.token % p.Bt;
     const bool rotate = l.form.cos_t != nullptr;
     f32x4 c[2], s[2];
 #pragma unroll

@@ -303,6 +303,11 @@ CASES = [
     (8, 2, 64, 1, 125, 777, 8, 1, [i % 50 - 1 for i in range(125)], None),
     (8, 2, 64, 1, 16, 3000, 8, 1, [1] * 16, None),
     (16, 4, 128, 1, 30, 2049, 8, 1, [1] * 30, None),
+    # more segments of shared rows than workgroups: whole ones in turn, or halves
+    (16, 8, 64, 40, 1, 700, 16, 1, [i % 33 for i in range(40)], None),
+    (20, 10, 64, 30, 20, 150, 16, 1, [i % 5 - 1 for i in range(600)], None),
+    (8, 8, 128, 65, 1, 2500, 8, 1, [0] * 65, None),
+    (16, 2, 128, 1, 40, 500, 16, 9, [i % 21 for i in range(40)], [i % 10 for i in range(40)]),   # 72 rows a sequence, 2880 of a prompt
 ]
 
 
@@ -529,7 +534,8 @@ def test_branch_attention_over_an_empty_cache_and_a_cache_of_other_heads():
     cache.close()
 
 
-def test_captured_steps_follow_the_lengths_they_find():
+@pytest.mark.parametrize("given", [True, False])
+def test_captured_steps_follow_the_lengths_they_find(given):
     # append and attention captured once, replayed with lengths, tables and inputs that change, against eager calls
     hq, hkv, d, N, page, n, steps = 8, 2, 128, 200, 16, 5, 6
     g = gen(82)
@@ -559,7 +565,7 @@ def test_captured_steps_follow_the_lengths_they_find():
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.stream(side):
         with torch.cuda.graph(graph, stream=side):
-            step(k_pages, v_pages, q_out, out, work)
+            step(k_pages, v_pages, q_out, out, work if given else None)   # (None: from the graph's own pool)
     torch.cuda.current_stream().wait_stream(side)
     for i in range(steps):
         x.copy_(torch.randn(x.shape, **g).bfloat16())
@@ -597,3 +603,11 @@ def test_calls_on_two_streams_with_workspaces_of_their_own():
             assert torch.equal(o, w)
             o.zero_()
         torch.cuda.synchronize()
+    # outputs allocated by the calls belong to their stream as well
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [kd.branch_attention(q, k_pages, v_pages, table, L, prefix=(kp, vp, N), stream=s) for q, s in zip(qs, streams)]
+    a = kd.norm_rope(qs[0], qs[0][:, :hkv], *tables(50, d), pos0=3, stream=streams[1].cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(got, want))
+    assert all(torch.equal(x, y) for x, y in zip(a, kd.norm_rope(qs[0], qs[0][:, :hkv], *tables(50, d), pos0=3)))
