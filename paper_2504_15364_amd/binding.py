@@ -1,4 +1,4 @@
-"""ctypes binding of include/keydiff.h -- argument marshalling only.
+"""Binding of include/keydiff.h -- argument marshalling only (ctypes; the calls of a generation step through csrc/calls.cpp).
 
 Every step of the path runs in the library's HIP kernels.  PyTorch appears only
 as the owner of device memory and streams.
@@ -6,9 +6,7 @@ as the owner of device memory and streams.
 from __future__ import annotations
 
 import ctypes as C
-import functools
 import os
-import struct
 from dataclasses import dataclass
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -225,8 +223,8 @@ def prefill_block_layers(caches, q, k_new, v_new, pos0: int, out=None, stream=No
         if not len(q_weights) == len(k_weights) == n:
             raise ValueError(f"norm needs one weight tensor per layer, got {len(q_weights)} and {len(k_weights)} for {n} layers")
         cos, sin = rope if rope is not None else (None, None)
-        forms = b"".join(_pack_form(c.cfg.n_q_heads, c.cfg.n_kv_heads, c.cfg.head_dim, cos, sin, wq, wk, eps, c.device)
-                         for c, wq, wk in zip(caches, q_weights, k_weights))
+        forms = b"".join(_native().row_form(c.cfg.n_q_heads, c.cfg.n_kv_heads, c.cfg.head_dim, cos, sin, wq, wk, eps, t)
+                         for c, wq, wk, t in zip(caches, q_weights, k_weights, q))
         _check(L.keydiff_prefill_block_layers_norm_rope(arr([c._h.value for c in caches]), n,
                                                         arr([t.data_ptr() for t in q]), arr([t.data_ptr() for t in k_new]),
                                                         arr([t.data_ptr() for t in v_new]), Bt, int(pos0), forms,
@@ -249,99 +247,42 @@ def prefill_block_layers(caches, q, k_new, v_new, pos0: int, out=None, stream=No
 
 
 # ------------------------------------------------------------------ norms and rotation alone; continuations of a prompt
-# The structures of these calls are packed into bytes: a tenth of the time that filling a ctypes structure takes (of 14 us a call on
-# the host, where the kernels of a generation step take 3 to 5).
-_ROWS = struct.Struct("Pqqq")               # keydiff_rows_t
-_ROW_FORM = struct.Struct("PPqqfPPq")       # keydiff_row_form_t
-_BRANCHES = struct.Struct("PPPPP7i4x")      # keydiff_branches_t
-assert (_ROWS.size, _ROW_FORM.size, _BRANCHES.size) == (C.sizeof(_Rows), C.sizeof(_RowForm), C.sizeof(_Branches))
+_calls = None
 
 
-def _pack_rows(name, t, n, heads, tokens, d, bf16, device):
-    """keydiff_rows_t of a tensor of rows [sequences][heads][tokens][head_dim]: bf16, the innermost dimension contiguous, other strides
-    free (views into a fused projection's output are fine)."""
-    s = t.stride()
-    if t.dtype is not bf16 or t.shape != (n, heads, tokens, d) or s[3] != 1:
-        raise ValueError(f"{name} must be a bf16 tensor of shape {(n, heads, tokens, d)} with a contiguous last dimension, "
-                         f"got {tuple(t.shape)} {t.dtype}, strides {s}")
-    if t.device != device:
-        raise ValueError(f"the tensors must live on one device, got {device} and {t.device} for {name}")
-    return _ROWS.pack(t.data_ptr(), s[0] if n > 1 else 0, s[1] if heads > 1 else 0, s[2] if tokens > 1 else 0)
+def _native():
+    """The compiled side of these calls (csrc/calls.cpp: checks, allocation and the call of the C ABI)."""
+    global _calls
+    if _calls is None:
+        import importlib
+
+        from torch import _C
+        L = load_library()
+        try:
+            m = importlib.import_module("._calls", __package__)
+        except ImportError as e:
+            raise ImportError(f"{e}: build it first (python -m paper_2504_15364_amd.build)") from e
+        address = lambda f: C.cast(f, C.c_void_p).value  # noqa: E731
+        m.bind(*(address(f) for f in (L.keydiff_norm_rope, L.keydiff_branch_append, L.keydiff_branch_workspace_bytes,
+                                      L.keydiff_branch_attention, L.keydiff_cache_branch_attention)),
+               _C._cuda_getCurrentRawStream)
+        _calls = m
+    return _calls
 
 
-def _dense(name, t, shape, dtype, device):
-    """The address of a contiguous tensor of this shape and type."""
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {tuple(t.shape)} {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"the tensors must live on one device, got {device} and {t.device} for {name}")
-    return t.data_ptr()
-
-
-def _weight(name, w, heads, d, bf16, device):
-    """The address and the stride from head to head of norm weights [d] or [heads][d]."""
-    shape, strides = w.shape, w.stride()
-    one = len(shape) == 1
-    if w.dtype is not bf16 or (shape != (d,) if one else shape != (heads, d)) or strides[-1] != 1:
-        raise ValueError(f"{name} must be a bf16 tensor of shape ({d},) or ({heads}, {d}), got {tuple(shape)} {w.dtype}")
-    if w.device != device:
-        raise ValueError(f"{name} must live on {device}, got {w.device}")
-    return w.data_ptr(), 0 if one or heads == 1 else strides[0]
-
-
-def _pack_form(hq, hkv, d, cos, sin, q_weight, k_weight, eps, device):
-    """keydiff_row_form_t of norm weights ([d] or [heads][d] bf16, or None) and rotary tables (float32 [positions][d / 2], or None)."""
-    import torch
-    qw = kw = qs = ks = c = s = rows = 0
-    if q_weight is not None and k_weight is not None:
-        qw, qs = _weight("q_weight", q_weight, hq, d, torch.bfloat16, device)
-        kw, ks = _weight("k_weight", k_weight, hkv, d, torch.bfloat16, device)
-    elif q_weight is not k_weight:
-        raise ValueError("q_weight and k_weight are given together or not at all")
-    if cos is not None and sin is not None:
-        shape = cos.shape
-        if not (len(shape) == 2 and shape[1] == d // 2 and sin.shape == shape and cos.dtype is sin.dtype is torch.float32
-                and cos.is_contiguous() and sin.is_contiguous() and cos.device == sin.device == device):
-            rows = shape[0] if len(shape) == 2 else 0
-            _dense("cos", cos, (rows, d // 2), torch.float32, device), _dense("sin", sin, (rows, d // 2), torch.float32, device)
-        rows, c, s = shape[0], cos.data_ptr(), sin.data_ptr()
-    elif cos is not sin:
-        raise ValueError("cos and sin are given together or not at all")
-    return _ROW_FORM.pack(qw, kw, qs, ks, eps, c, s, rows)
-
-
-def _enqueue(device, stream, call, *args):
-    """The call on `stream` (None: torch's current one) of the tensors' device, whichever device is current."""
-    from torch import _C
-    current, raw = getattr(_C, "_cuda_getDevice", None), getattr(_C, "_cuda_getCurrentRawStream", None)   # (see _stream_ptr)
-    if current is not None and raw is not None and current() == device.index:
-        rc = call(*args, raw(device.index) if stream is None else getattr(stream, "cuda_stream", stream))
+def _call(name, device, stream, *args):
+    """The compiled function on `stream`, an object of torch's or a handle (None: torch's current stream of the tensors' device).
+    Tensors that it allocates belong to that stream."""
+    f = getattr(_calls or _native(), name)
+    if stream is None:
+        r = f(*args)
     else:
         import torch
-        with torch.cuda.device(device):
-            rc = call(*args, _stream_ptr(stream))
-    if rc != OK:
-        _check(rc)
-
-
-def _on_stream(stream, device):
-    """Tensors allocated in this context belong to `stream` (an object of torch's or a handle): torch hands their memory out again in
-    the order of the work on it."""
-    import torch
-    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device))
-
-
-def _empty_like(t, stream):
-    import torch
-    if stream is None:
-        return torch.empty_like(t, memory_format=torch.contiguous_format)
-    with _on_stream(stream, t.device):
-        return torch.empty_like(t, memory_format=torch.contiguous_format)
-
-
-def _need_gpu(device):
-    if device.type != "cuda":
-        raise ValueError(f"the tensors must live on a GPU, got {device}")
+        with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device)):
+            r = f(*args)
+    if type(r) is int:
+        _check(r)
+    return r
 
 
 def norm_rope(q, k, cos=None, sin=None, pos0: int = 0, positions=None, q_weight=None, k_weight=None, norm_eps: float = 1e-6,
@@ -350,40 +291,7 @@ def norm_rope(q, k, cos=None, sin=None, pos0: int = 0, positions=None, q_weight=
     position embedding (float32 tables [positions][d / 2]; None: no rotation) in one pass.
     q [batch][Hq][T][d], k [batch][Hkv][T][d] bf16, any strides with a contiguous last dimension; token j is at position pos0 + j or
     at positions[b][j] (int32 [batch][T]; a token outside the tables is left out).  Returns contiguous (q_out, k_out)."""
-    import torch
-    if q.dim() != 4 or k.dim() != 4:
-        raise ValueError(f"q and k are [batch][heads][tokens][head_dim], got {tuple(q.shape)} and {tuple(k.shape)}")
-    b, hq, T, d = q.shape
-    hkv, device, bf16 = k.shape[1], q.device, torch.bfloat16
-    rq, rk = _pack_rows("q", q, b, hq, T, d, bf16, device), _pack_rows("k", k, b, hkv, T, d, bf16, device)
-    at = _dense("positions", positions, (b, T), torch.int32, device) if positions is not None else None
-    form = _pack_form(hq, hkv, d, cos, sin, q_weight, k_weight, norm_eps, device)
-    if q_out is not None:
-        _dense("q_out", q_out, (b, hq, T, d), bf16, device)
-    if k_out is not None:
-        _dense("k_out", k_out, (b, hkv, T, d), bf16, device)
-    _need_gpu(device)
-    if q_out is None:
-        q_out = _empty_like(q, stream)
-    if k_out is None:
-        k_out = _empty_like(k, stream)
-    _enqueue(device, stream, load_library().keydiff_norm_rope, rq, rk, b, hq, hkv, d, T, int(pos0), at, form, q_out.data_ptr(),
-             k_out.data_ptr())
-    return q_out, k_out
-
-
-def _pack_branches(n, hq, hkv, d, k_pages, v_pages, table, lens, n_new, bf16, i32, device):
-    """keydiff_branches_t: pools [pages][hkv][page_rows][d] bf16, table [n_seqs][width], lens and n_new [n_seqs] int32."""
-    shape = k_pages.shape
-    if len(shape) != 4 or shape[1] != hkv or shape[3] != d:
-        raise ValueError(f"k_pages must be [pages][{hkv}][page_rows][{d}], got {tuple(shape)}")
-    if table.dim() != 2:
-        raise ValueError(f"table must be [{n}][width], got {tuple(table.shape)}")
-    width = table.shape[1]
-    return _BRANCHES.pack(_dense("k_pages", k_pages, shape, bf16, device), _dense("v_pages", v_pages, shape, bf16, device),
-                          _dense("table", table, (n, width), i32, device), _dense("lens", lens, (n,), i32, device),
-                          _dense("n_new", n_new, (n,), i32, device) if n_new is not None else 0,
-                          n, hq, hkv, d, shape[2], shape[0], width)
+    return _call("norm_rope", q.device, stream, q, k, cos, sin, pos0, positions, q_weight, k_weight, norm_eps, q_out, k_out)
 
 
 def branch_append(q, k_new, v_new, k_pages, v_pages, table, lens, n_new=None, pos0=None, cos=None, sin=None, q_weight=None,
@@ -395,42 +303,16 @@ def branch_append(q, k_new, v_new, k_pages, v_pages, table, lens, n_new=None, po
     [pages][Hkv][page_rows][d]; table int32 [n_seqs][width]; n_new int32 [n_seqs] (None: all Bt).  Returns the contiguous queries
     for branch_attention; tokens that are left out (behind a sequence's n_new, lens < 0) keep their rows of q_out, which
     hold anything if it is None."""
-    import torch
-    if k_new.dim() != 4 or (q is not None and q.dim() != 4):
-        raise ValueError("q, k_new and v_new are [sequences][heads][tokens][head_dim]")
-    n, hkv, Bt, d = k_new.shape
-    hq = q.shape[1] if q is not None else hkv
-    device, bf16, i32 = k_new.device, torch.bfloat16, torch.int32
-    rk, rv = _pack_rows("k_new", k_new, n, hkv, Bt, d, bf16, device), _pack_rows("v_new", v_new, n, hkv, Bt, d, bf16, device)
-    b = _pack_branches(n, hq, hkv, d, k_pages, v_pages, table, lens, n_new, bf16, i32, device)
-    rq = out = None
-    if q is not None:
-        rq = _pack_rows("q", q, n, hq, Bt, d, bf16, device)
-    elif q_out is not None:
-        raise ValueError("q_out without q")
-    if q_out is not None:
-        out = _dense("q_out", q_out, (n, hq, Bt, d), bf16, device)
-    first = _dense("pos0", pos0, (n,), i32, device) if pos0 is not None else None
-    form = _pack_form(hq, hkv, d, cos, sin, q_weight, k_weight, norm_eps, device)
-    _need_gpu(device)
-    if q is not None and q_out is None:
-        q_out = _empty_like(q, stream)
-        out = q_out.data_ptr()
-    _enqueue(device, stream, load_library().keydiff_branch_append, b, rq, rk, rv, Bt, first, form, out)
-    return q_out
-
-
-@functools.lru_cache(maxsize=256)
-def _branch_workspace_bytes(n_seqs, hq, hkv, d, Bt, n_prefixes, device_index):
-    b = _Branches(n_seqs=n_seqs, n_q_heads=hq, n_kv_heads=hkv, head_dim=d)
-    size = C.c_size_t()
-    _check(load_library().keydiff_branch_workspace_bytes(C.byref(b), Bt, n_prefixes, C.byref(size)))
-    return size.value
+    return _call("branch_append", k_new.device, stream, q, k_new, v_new, k_pages, v_pages, table, lens, n_new, pos0, cos, sin, q_weight,
+                 k_weight, norm_eps, q_out)
 
 
 def branch_workspace_bytes(n_seqs, n_q_heads, n_kv_heads, head_dim, Bt=1, n_prefixes=0):
     """Bytes of the workspace that branch_attention needs for calls of these sizes on the current device."""
-    return _branch_workspace_bytes(n_seqs, n_q_heads, n_kv_heads, head_dim, Bt, n_prefixes, None)
+    b = _Branches(n_seqs=n_seqs, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim)
+    size = C.c_size_t()
+    _check(load_library().keydiff_branch_workspace_bytes(C.byref(b), Bt, n_prefixes, C.byref(size)))
+    return size.value
 
 
 def branch_attention(q, k_pages, v_pages, table, lens, prefix=None, n_new=None, softmax_scale: float = 0.0, out=None, workspace=None,
@@ -444,54 +326,15 @@ def branch_attention(q, k_pages, v_pages, table, lens, prefix=None, n_new=None, 
     workspace: a uint8 tensor of at least branch_workspace_bytes that no other call in flight uses (None: allocated for the call).
     Returns out [n_seqs][Hq][Bt][d]; rows behind a sequence's n_new, and those of a sequence with lens < 0, are left as they were
     (they hold anything where out is None)."""
-    import torch
-    if q.dim() != 4 or k_pages.dim() != 4:
-        raise ValueError("q is [sequences][heads][tokens][head_dim] and pools are [pages][heads][page_rows][head_dim]")
-    n, hq, Bt, d = q.shape
-    hkv = k_pages.shape[1]
-    device, bf16 = q.device, torch.bfloat16
-    rq = _pack_rows("q", q, n, hq, Bt, d, bf16, device)
-    b = _pack_branches(n, hq, hkv, d, k_pages, v_pages, table, lens, n_new, bf16, torch.int32, device)
-    to = _dense("out", out, (n, hq, Bt, d), bf16, device) if out is not None else None
-    cache = kp = vp = None
-    prompts = rows = cap = 0
-    if prefix is None:
-        pass
-    elif isinstance(prefix, KeyDiffCache):
-        cache = prefix
-        prompts = cache.cfg.batch
-        if softmax_scale > 0:
-            raise ValueError("softmax_scale is the cache's")
-        if cache.device != device:
-            raise ValueError(f"the cache lives on {cache.device}, the queries on {device}")
-    else:
-        kp, vp, rows = prefix
-        if kp.dim() != 4:
-            raise ValueError(f"prefix keys are [prompts][{hkv}][rows][{d}], got {tuple(kp.shape)}")
-        prompts, cap = kp.shape[0], kp.shape[2]
-        if not 0 <= rows <= cap:
-            raise ValueError(f"the prefix has {cap} rows a head, {rows} are to be read")
-        kp = _dense("prefix keys", kp, (prompts, hkv, cap, d), bf16, device)
-        vp = _dense("prefix values", vp, (prompts, hkv, cap, d), bf16, device)
-    _need_gpu(device)
-    need = _branch_workspace_bytes(n, hq, hkv, d, Bt, prompts, device.index)
-    if workspace is None:
-        if stream is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        else:
-            with _on_stream(stream, device):
-                workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.numel() < need or workspace.device != device:
-        raise ValueError(f"workspace must be a contiguous uint8 tensor of at least {need} elements on {device}")
-    if out is None:
-        out = _empty_like(q, stream)
-        to = out.data_ptr()
-    if cache is not None:
-        _enqueue(device, stream, cache._L.keydiff_cache_branch_attention, cache._h, b, rq, Bt, to, workspace.data_ptr(), workspace.numel())
-    else:
-        _enqueue(device, stream, load_library().keydiff_branch_attention, b, rq, Bt, kp, vp, prompts, int(rows), cap, softmax_scale, to,
-                 workspace.data_ptr(), workspace.numel())
-    return out
+    handle = batch = keys = values = rows = None
+    if isinstance(prefix, KeyDiffCache):
+        handle, batch = prefix._h.value or 0, prefix.cfg.batch
+        if prefix.device != q.device:
+            raise ValueError(f"the cache lives on {prefix.device}, the queries on {q.device}")
+    elif prefix is not None:
+        keys, values, rows = prefix
+    return _call("branch_attention", q.device, stream, q, k_pages, v_pages, table, lens, n_new, handle, batch, keys, values, rows,
+                 softmax_scale, out, workspace)
 
 
 class KeyDiffCache:
@@ -570,7 +413,7 @@ class KeyDiffCache:
         norm; tables None: no rotation."""
         Bt, out = self._block_args(q, k_new, v_new, out, scores_out)
         cfg = self.cfg
-        form = _pack_form(cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, cos, sin, q_weight, k_weight, norm_eps, self.device)
+        form = _native().row_form(cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, cos, sin, q_weight, k_weight, norm_eps, q)
         _check(self._L.keydiff_prefill_block_norm_rope(self._h, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), Bt,
                                                        int(pos0), form, out.data_ptr(),
                                                        scores_out.data_ptr() if scores_out is not None else None,

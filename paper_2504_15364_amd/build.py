@@ -8,6 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkeydiff.so")
+CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ["attention.hip", "few.hip", "evict.hip", "norm_rope.hip", "branch.hip", "keydiff_abi.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
@@ -32,6 +33,20 @@ def scratch_users(remarks):
             if n:
                 found.append((name, n))
     return found
+
+
+def build_calls() -> str:
+    """The Python side of the calls beside the block step (_calls.so): a host compiler and torch's headers, no GPU code."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    lib_dir = cpp_extension.library_paths()[0]
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           os.path.join(CSRC, "calls.cpp"), "-o", CALLS, *[f"-isystem{p}" for p in cpp_extension.include_paths()],
+           f"-I{sysconfig.get_paths()['include']}", f"-L{lib_dir}", "-ltorch_python", "-ltorch_cpu", "-lc10", f"-Wl,-rpath,{lib_dir}"]
+    subprocess.run(cmd, check=True)
+    return CALLS
 
 
 def build(verbose: bool = False, timeline: bool = False) -> str:
@@ -69,6 +84,8 @@ def build(verbose: bool = False, timeline: bool = False) -> str:
     lib = TIMELINE_LIB if timeline else LIB
     link = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", lib, *objs]
     subprocess.run(link, check=True)
+    if not timeline:
+        build_calls()
     return lib
 
 

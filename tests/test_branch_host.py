@@ -1,5 +1,6 @@
 """norm_rope, branch_append and branch_attention: what they refuse, found before anything is enqueued (no GPU needed)."""
 import ctypes as C
+import sys
 
 import pytest
 
@@ -190,3 +191,25 @@ def test_wrapper_refuses_tensors_that_do_not_fit():
         kd.branch_attention(q, pages, pages, table, lens, prefix=(z(1, 2, 30, 64), z(1, 2, 30, 64), 31))
     with pytest.raises(ValueError, match="out"):
         kd.branch_attention(q, pages, pages, table, lens, out=q[:1])
+
+
+def test_wrapper_refuses_what_is_no_tensor_and_leaks_no_reference():
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt)  # noqa: E731
+    q, pages, table, lens = z(2, 8, 3, 64), z(5, 2, 16, 64), z(2, 4, dt=torch.int32), z(2, dt=torch.int32)
+    before = [sys.getrefcount(t) for t in (q, pages, table, lens)]
+    for _ in range(3):
+        with pytest.raises(ValueError, match="k must be a tensor"):
+            kd.norm_rope(q, [1, 2])
+        with pytest.raises(TypeError):
+            kd.norm_rope(q, q[:, :2], q_weight=z(64), k_weight=z(64), norm_eps="small")
+        with pytest.raises(TypeError):
+            kd.norm_rope(q, q[:, :2], q_weight=z(64), k_weight=z(64), pos0=0.5)
+        with pytest.raises(ValueError, match="four dimensions"):
+            kd.branch_attention(q[0], pages, pages, table, lens)
+        with pytest.raises(ValueError, match="prefix values must be a tensor"):
+            kd.branch_attention(q, pages, pages, table, lens, prefix=(z(1, 2, 30, 64), None, 30))
+        with pytest.raises(ValueError):
+            kd.branch_attention(q, pages, pages, table, lens, prefix=(z(1, 2, 30, 64), z(1, 2, 30, 64)))
+        with pytest.raises(ValueError, match="GPU"):
+            kd.branch_attention(q, pages, pages, table, lens, out=q.clone())
+    assert [sys.getrefcount(t) for t in (q, pages, table, lens)] == before

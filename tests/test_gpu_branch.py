@@ -611,3 +611,31 @@ def test_calls_on_two_streams_with_workspaces_of_their_own():
     torch.cuda.synchronize()
     assert all(torch.equal(o, w) for o, w in zip(got, want))
     assert all(torch.equal(x, y) for x, y in zip(a, kd.norm_rope(qs[0], qs[0][:, :hkv], *tables(50, d), pos0=3)))
+
+
+def test_calls_return_what_is_given_and_hold_no_memory():
+    g = gen(31)
+    q, kv = torch.randn(3, 8, 1, 64, **g).bfloat16(), torch.randn(2, 3, 2, 1, 64, **g).bfloat16()
+    w = torch.ones(64, device="cuda", dtype=torch.bfloat16)
+    pools = torch.zeros(2, 4, 2, 16, 64, device="cuda", dtype=torch.bfloat16)
+    table, lens = torch.arange(3, device="cuda", dtype=torch.int32)[:, None].contiguous(), ints([0, 3, 15])
+    outs = [torch.empty_like(q), torch.empty_like(kv[0])]
+    work = torch.empty(kd.branch_workspace_bytes(3, 8, 2, 64, 1, 0), device="cuda", dtype=torch.uint8)
+    a, b = kd.norm_rope(q, kv[0], q_weight=w, k_weight=w, q_out=outs[0], k_out=outs[1])
+    assert a is outs[0] and b is outs[1]
+    assert kd.branch_append(q, kv[0], kv[1], *pools, table, lens, q_weight=w, k_weight=w, q_out=outs[0]) is outs[0]
+    assert kd.branch_append(None, kv[0], kv[1], *pools, table, lens) is None
+    assert kd.branch_attention(q, *pools, table, lens, out=outs[0], workspace=work) is outs[0]
+    torch.cuda.synchronize()
+    held = torch.cuda.memory_allocated()
+    for _ in range(20):
+        x, _ = kd.norm_rope(q, kv[0], q_weight=w, k_weight=w)
+        x = kd.branch_append(x, kv[0], kv[1], *pools, table, lens)
+        x = kd.branch_attention(x, *pools, table, lens)
+        with pytest.raises(kd.KeyDiffError):
+            kd.branch_append(x, kv[0], kv[1], pools[0], pools[0], table, lens)   # the pools overlap
+        with pytest.raises(ValueError, match="workspace"):
+            kd.branch_attention(x, *pools, table, lens, workspace=work[:8])
+    del x, _
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() == held
