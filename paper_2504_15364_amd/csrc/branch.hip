@@ -20,6 +20,8 @@
 // Measured (8192 shared rows, 8 KV heads of 128, both launches, back to back): one sequence 14.8 us (35 MB), 16 with up to 777 own rows 21.7
 // (60 MB), 64 with up to 4096 own rows 114 (571 MB: 5.0 TB/s; its first launch alone 5.5), 256 of three query heads to a KV head with up to 33 own
 // rows 61 (26 GFLOP).
+#include <algorithm>
+
 #include "kd_branch.h"
 #include "kd_device.h"
 #include "kd_select.h"
@@ -760,14 +762,17 @@ constexpr int lds_bytes()
 
 // Prices in us, measured by stamps of the clock inside the kernel where neither part waits for the other's traffic: a step of the shared part
 // (every group of waves a tile) and what a task takes besides; a tile of a wave of the own part and what a wave takes besides; and what a
-// tile of own rows takes at the rate that memory gives all workgroups together, which no share of them changes.
+// tile of own rows takes at the rate that memory gives all workgroups together, which no share of them changes.  own_end: what the end of a
+// segment adds to its tile (without it the own rows of 192 sequences that had just begun got half the workgroups they needed: 87 us, now 63).
+// partial: a row of a partial of the shared part written, and read again by the join (the slope of the time of calls over the bytes of their
+// partials, at blocks of 64, 128 and 256 rows).
 template <int D, int RS, int RO>
 struct Prices {
     static constexpr bool wide = D == 128;
     static constexpr float step = RS == 256 ? (wide ? 1.3f : 1.0f) : RS == 128 ? (wide ? 1.45f : 1.1f) : RS == 64 ? (wide ? 2.35f : 1.1f) : (wide ? 2.5f : 1.5f);
     static constexpr float task = RS == 256 ? (wide ? 9.f : 7.f) : RS == 128 ? (wide ? 9.5f : 6.5f) : RS == 64 ? (wide ? 8.8f : 5.5f) : (wide ? 4.5f : 4.f);
-    static constexpr float own_tile = RO == 16 ? (wide ? 2.7f : 1.8f) : (wide ? 3.8f : 2.2f), own_wave = 4.f;
-    static constexpr float own_traffic = TK * D * 4 / 5.5e6f;
+    static constexpr float own_tile = RO == 16 ? (wide ? 2.7f : 1.8f) : (wide ? 3.8f : 2.2f), own_end = 0.7f, own_wave = 4.f;
+    static constexpr float own_traffic = TK * D * 4 / 5.5e6f, partial = D * 4 / 2e6f;
 };
 
 // How the work is cut: the same on every wave.  rows0: own rows of sequence `lane`.
@@ -781,8 +786,15 @@ __device__ __forceinline__ Plan make_plan(const BranchParams &p, int units, int 
     auto up = [](float x, float y) { return __builtin_ceilf(x * __builtin_amdgcn_rcpf(y)); };   // (a price may be off by the quotient's last bit)
     Plan plan;
     int own = (rows0 + TK - 1) / TK;
-    for (int base = 64; base < p.n_seqs; base += 64) own += base + lane < p.n_seqs ? (own_rows(p, base + lane) + TK - 1) / TK : 0;
-    plan.own_tiles = __builtin_amdgcn_readlane((int)wave_inclusive_scan((uint32_t)own), 63) * p.hkv * ((p.G * p.Bt + RO - 1) / RO);
+    int used = __popcll(__builtin_amdgcn_ballot_w64(own > 0));   // sequences with own rows
+    for (int base = 64; base < p.n_seqs; base += 64) {
+        const int more = base + lane < p.n_seqs ? (own_rows(p, base + lane) + TK - 1) / TK : 0;
+        own += more;
+        used += __popcll(__builtin_amdgcn_ballot_w64(more > 0));
+    }
+    const int per_seq = p.hkv * ((p.G * p.Bt + RO - 1) / RO);
+    plan.own_tiles = __builtin_amdgcn_readlane((int)wave_inclusive_scan((uint32_t)own), 63) * per_seq;
+    const float own_work = (float)plan.own_tiles * P::own_tile + (float)(used * per_seq) * P::own_end;
     const int segs = p.shared_segs, most = plan.own_tiles > 0 ? wgs - 1 : wgs;
     int w = 0, splits = 1;
     float price = INFINITY;
@@ -800,7 +812,7 @@ __device__ __forceinline__ Plan make_plan(const BranchParams &p, int units, int 
     }
     const int others = (wgs - w) * NW;
     if (plan.own_tiles > 0) {
-        const float own_price = fmaxf(up((float)plan.own_tiles, (float)others) * P::own_tile, (float)plan.own_tiles * P::own_traffic) + P::own_wave;
+        const float own_price = fmaxf(up(own_work, (float)others), (float)plan.own_tiles * P::own_traffic) + P::own_wave;
         price = segs > 0 ? fmaxf(price, own_price) : own_price;
     }
     const uint32_t cheap = ~__float_as_uint(price);   // (prices are not negative: the cheapest has the largest complement)
@@ -948,15 +960,37 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
     *reinterpret_cast<bf16x4 *>(p.out + (((size_t)s * p.hkv + h) * Mt + m) * D + d0) = o;
 }
 
-// Query rows of a block: of the own part 16, or 32 where a sequence has more; of the shared part 16, or two, four or eight waves of 32
-// rows.  Above four waves' rows, blocks of four or of eight waves, whichever leaves fewer waves without rows.
+// Query rows of a block of the own part: 16, or 32 where a sequence has more
 int own_block(int64_t rows) { return rows > 16 ? 32 : 16; }
-int shared_block(int64_t rows)
+
+// What the shared part takes with blocks of RS rows, as make_plan prices it, a sixteenth of the workgroups left to the own part, and its partials
+template <int D, int RS>
+float shared_price(int64_t rows, int heads, int prefix_len, int cus)
+{
+    using P = Prices<D, RS, 16>;
+    auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+    const int64_t segs = heads * up(rows, RS), units = up(up(prefix_len, TK), NW / (RS / 32)), wgs = std::max(cus - cus / 16, 1);
+    if (segs <= wgs) {
+        const int64_t splits = std::min(wgs / segs, units);
+        return (float)up(units, splits) * P::step + P::task + (float)(splits * heads * rows) * P::partial;
+    }
+    return (float)up(segs, wgs) * ((float)units * P::step + P::task) + (float)(heads * rows) * P::partial;
+}
+// Query rows of a block of the shared part: 16 where that is all, or two, four or eight waves of 32 rows; of those that rows half fill at
+// least, the cheapest.  Small blocks have fewer pieces of each segment, and so fewer partials, large ones read a tile from LDS for more
+// rows.  Measured with blocks of 64, 128 and 256 (D 128, 8 KV heads): 256 rows over 1024 shared ones 19.2, 21.7 and 23.1 us, over 8192 31.1,
+// 29.1 and 33.7; 1024 rows over 8192 110, 71 and 66.  Over 210 sizes the price's choice is 0.9 % off the best on average; that by
+// rows alone was 8.7 % off.
+int shared_block(int64_t rows, int heads, int prefix_len, int D, int cus)
 {
     if (rows <= 16) return 16;
     if (rows <= 64) return 64;
-    if (rows <= 128) return 128;
-    return (rows + 255) / 256 * 2 <= (rows + 127) / 128 ? 256 : 128;
+    const bool wide = D == 128;
+    const float by64 = wide ? shared_price<128, 64>(rows, heads, prefix_len, cus) : shared_price<64, 64>(rows, heads, prefix_len, cus);
+    const float by128 = wide ? shared_price<128, 128>(rows, heads, prefix_len, cus) : shared_price<64, 128>(rows, heads, prefix_len, cus);
+    if (rows <= 128) return by64 <= by128 ? 64 : 128;
+    const float by256 = wide ? shared_price<128, 256>(rows, heads, prefix_len, cus) : shared_price<64, 256>(rows, heads, prefix_len, cus);
+    return by64 <= std::min(by128, by256) ? 64 : by128 <= by256 ? 128 : 256;
 }
 
 }  // namespace
@@ -964,8 +998,11 @@ int shared_block(int64_t rows)
 size_t branch_workspace(int n_seqs, int n_prefixes, int hkv, int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_plan)
 {
     const int64_t Mt = (int64_t)G * Bt, fan = n_prefixes > 0 ? n_seqs / n_prefixes : 0;
-    const size_t RS = shared_block(fan * Mt), RO = own_block(Mt);
-    const size_t shared = shared_slots(n_prefixes, (int)fan, hkv, (int)Mt, (int)RS, cus) * RS;
+    const size_t RO = own_block(Mt);
+    size_t shared = 0;   // (the length of the prompts' rows is not known here: the most that any block takes)
+    for (const int RS : {16, 64, 128, 256})
+        if (RS == 16 ? fan * Mt <= 16 : RS == 64 || fan * Mt > RS / 2)
+            shared = std::max(shared, shared_slots(n_prefixes, (int)fan, hkv, (int)Mt, RS, cus) * RS);
     const size_t own = ((size_t)n_seqs * hkv * ((Mt + RO - 1) / RO) + (size_t)cus * NW) * RO;
     size_t off = (shared + own) * D * 4;
     off = (off + 255) & ~(size_t)255;
@@ -1009,7 +1046,7 @@ hipError_t launch(const BranchParams &p, int RS, hipStream_t s)
 hipError_t launch_branch_attention(BranchParams p, hipStream_t s)
 {
     const int64_t Mt = (int64_t)p.G * p.Bt;
-    const int RS = shared_block(p.fan * Mt), RO = own_block(Mt);
+    const int RS = shared_block(p.fan * Mt, p.n_prefixes * p.hkv, std::max(p.prefix_len, 1), p.D, p.cus), RO = own_block(Mt);
     p.shared_segs = p.prefix_len > 0 ? (int32_t)(p.n_prefixes * p.hkv * ((p.fan * Mt + RS - 1) / RS)) : 0;
     p.by_segs.set(p.shared_segs > 0 ? p.shared_segs : 1);
     p.by_heads.set(p.n_prefixes > 0 ? p.n_prefixes * p.hkv : 1);

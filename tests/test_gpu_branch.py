@@ -11,6 +11,7 @@ Tolerances, from the arithmetic (u = 2^-24, the half step of float; 2^-8 the hal
                      bf16 numbers 2^-16, sums of n weights and values in float tile by tile (n / 32 + 60) u: e in all, on the
                      weights of numerator and denominator: |error| <= e (sum p |v| + |o|) + 2^-8 |o|
 """
+import gc
 import math
 
 import pytest
@@ -626,7 +627,7 @@ def test_calls_return_what_is_given_and_hold_no_memory():
     assert kd.branch_append(q, kv[0], kv[1], *pools, table, lens, q_weight=w, k_weight=w, q_out=outs[0]) is outs[0]
     assert kd.branch_append(None, kv[0], kv[1], *pools, table, lens) is None
     assert kd.branch_attention(q, *pools, table, lens, out=outs[0], workspace=work) is outs[0]
-    torch.cuda.synchronize()
+    gc.collect()   # (what tests before this one left in cycles)
     held = torch.cuda.memory_allocated()
     for _ in range(20):
         x, _ = kd.norm_rope(q, kv[0], q_weight=w, k_weight=w)
@@ -637,5 +638,5 @@ def test_calls_return_what_is_given_and_hold_no_memory():
         with pytest.raises(ValueError, match="workspace"):
             kd.branch_attention(x, *pools, table, lens, workspace=work[:8])
     del x, _
-    torch.cuda.synchronize()
+    gc.collect()
     assert torch.cuda.memory_allocated() == held
