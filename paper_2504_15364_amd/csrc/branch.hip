@@ -17,6 +17,7 @@
 //                contiguous piece and stores a partial where the piece leaves a segment: no wave waits for another one, and
 //                ragged lengths cost nothing, because the list is cut by tiles and not by sequences
 // All of this follows from the lengths on the device: the launch itself does not depend on them and may be replayed from a graph.
+// Where the prompts' rows and those that the tables can name are few, one launch does it, a workgroup a segment (one_launch).
 // Measured (8192 shared rows, 8 KV heads of 128, both launches, back to back): one sequence 14.8 us (35 MB), 16 with up to 777 own rows 21.7
 // (60 MB), 64 with up to 4096 own rows 114 (571 MB: 5.0 TB/s; its first launch alone 5.5), 256 of three query heads to a KV head with up to 33 own
 // rows 61 (26 GFLOP).
@@ -253,6 +254,33 @@ __device__ __forceinline__ Segment segment_of(const BranchParams &p, int task)
 template <int D>
 constexpr int OUT_PITCH = D + 4;
 
+// The eight waves' results of 16 rows, in LDS, become one: store(row, column, four columns of its output, reference maximum, weight sum)
+template <int D, class Store>
+__device__ __forceinline__ void join_waves(const float *outs, const float2 (&ml_s)[NW][16], int rows, int tid, Store store)
+{
+    for (int it = tid; it < rows * (D / 4); it += 64 * NW) {
+        const int m = it / (D / 4), d0 = it % (D / 4) * 4;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) mx = fmaxf(mx, ml_s[w][m].x);
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        float L = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float2 ml = ml_s[w][m];
+            const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - mx);
+            const f32x4 o = *reinterpret_cast<const f32x4 *>(outs + ((size_t)w * 16 + m) * OUT_PITCH<D> + d0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] += f * o[i];
+            L += f * ml.y;
+        }
+        const float inv = L > 0.f ? 1.f / L : 0.f;   // (no key seen: zero)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] *= inv;
+        store(m, d0, acc, mx, L);
+    }
+}
+
 // The shared part with at most 16 query rows: one workgroup, its piece of the list, every wave tiles of its own
 template <int D, int CB>
 __device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned char *smem)
@@ -324,28 +352,10 @@ __device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned cha
             if (g == 0) ml_s[wave][c16] = make_float2(st.m[cb], l);
             __syncthreads();
             const int rows = min(16, M - mb * R - 16 * cb);
-            for (int it = tid; it < rows * (D / 4); it += 64 * NW) {
-                const int m = it / (D / 4), d0 = it % (D / 4) * 4;
-                float mx = -INFINITY;
-#pragma unroll
-                for (int w = 0; w < NW; ++w) mx = fmaxf(mx, ml_s[w][m].x);
-                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-                float L = 0.f;
-#pragma unroll
-                for (int w = 0; w < NW; ++w) {
-                    const float2 ml = ml_s[w][m];
-                    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - mx);
-                    const f32x4 o = *reinterpret_cast<const f32x4 *>(outs + ((size_t)w * 16 + m) * OUT_PITCH<D> + d0);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[i] += f * o[i];
-                    L += f * ml.y;
-                }
-                const float inv = L > 0.f ? 1.f / L : 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i] *= inv;
+            join_waves<D>(outs, ml_s, rows, tid, [&](int m, int d0, f32x4 acc, float mx, float L) {
                 *reinterpret_cast<f32x4 *>(p.part_o + (slot * R + 16 * cb + m) * D + d0) = acc;
                 if (d0 == 0) p.part_ml[slot * R + 16 * cb + m] = make_float2(mx, L);
-            }
+            });
         }
         __syncthreads();   // the outputs are read before the next segment's V tiles overwrite them
     }
@@ -960,6 +970,124 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
     *reinterpret_cast<bf16x4 *>(p.out + (((size_t)s * p.hkv + h) * Mt + m) * D + d0) = o;
 }
 
+// Few rows: one launch, a workgroup for every (sequence, head, block of rows), whose waves take tiles of the prompt's and of the own rows in
+// turn and join their results in LDS; no partials, no plan and no second launch.
+template <int D, int RO>
+__global__ __launch_bounds__(64 * NW) void branch_short_kernel(BranchParams p)
+{
+    constexpr int CB = RO / 16, NC = D / 32, NDB = D / 16, UPR = D / 8, ROWB = D * 2, RPL = 64 / UPR, NV = TK / RPL;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[lds_bytes<D, 16>()];
+    __shared__ float2 ml_s[NW][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c16 = lane & 15, g = lane >> 4;
+    const int Mt = p.G * p.Bt, blocks = (Mt + RO - 1) / RO;
+    const int sh = p.by_own_blocks.divide(blockIdx.x), m0 = ((int)blockIdx.x - sh * blocks) * RO, s = p.by_hkv.divide(sh), h = sh - s * p.hkv;
+    const int asked = asked_of(p, s), held = p.pages.lens[s];
+    const int np = (p.prefix_len + TK - 1) / TK, shift = p.pages.page_shift;
+    const size_t ch = (size_t)p.by_fan.divide(s) * p.hkv + h;
+    const char *kh = reinterpret_cast<const char *>(p.k_prefix + ch * p.prefix_cap * D), *vh = reinterpret_cast<const char *>(p.v_prefix + ch * p.prefix_cap * D);
+    const int32_t *table = p.pages.table + (size_t)s * p.pages.width;
+    unsigned char *vt = smem + (size_t)wave * TK * ROWB;
+    State<D, CB> st;
+    st.reset();
+    u32x4 kr[2][NC], vr[NV];
+    uint32_t absent = 0;   // bit i: rows 8 i .. of the tile in registers lie on a page that does not exist
+    auto load_shared = [&](int t) {   // (rows past the last repeat it: their weights are masked to zero)
+#pragma unroll
+        for (int kg = 0; kg < 2; ++kg) {
+            const uint32_t off = (uint32_t)min(t * TK + 16 * kg + c16, p.prefix_len - 1) * ROWB + 16 * g;
+#pragma unroll
+            for (int cc = 0; cc < NC; ++cc) kr[kg][cc] = *reinterpret_cast<const u32x4 *>(kh + off + cc * 64);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            vr[i] = *reinterpret_cast<const u32x4 *>(vh + (uint32_t)min(t * TK + i * RPL + lane / UPR, p.prefix_len - 1) * ROWB + lane % UPR * 16);
+        absent = 0;
+    };
+    const int n = own_rows(p, held, asked), len = min(held, n), total = np + (n + TK - 1) / TK;
+    auto load_own = [&](int t) {
+        const uint16_t *kg8[4], *vg8[4];   // first row of each group of eight, which lies on one page
+        absent = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = min(t * TK + 8 * i, (n - 1) & ~7);
+            int page = table[row >> shift];
+            if ((uint32_t)page >= (uint32_t)p.pages.n_pages) {
+                absent |= 1u << i;
+                page = 0;
+            }
+            const size_t off = ((((size_t)page * p.hkv + h) << shift) + (size_t)(row & ((1 << shift) - 1))) * D;
+            kg8[i] = p.pages.k + off;
+            vg8[i] = p.pages.v + off;
+        }
+#pragma unroll
+        for (int kg = 0; kg < 2; ++kg) {
+            const uint16_t *kb = (c16 < 8 ? kg8[2 * kg] : kg8[2 * kg + 1]) + (min(t * TK + 16 * kg + c16, n - 1) & 7) * D + 8 * g;
+#pragma unroll
+            for (int cc = 0; cc < NC; ++cc) kr[kg][cc] = *reinterpret_cast<const u32x4 *>(kb + cc * 32);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            vr[i] = *reinterpret_cast<const u32x4 *>(vg8[i * RPL / 8] + (min(t * TK + i * RPL + lane / UPR, n - 1) & 7) * D + lane % UPR * 8);
+            if (absent >> (i * RPL / 8) & 1) vr[i] = u32x4{0u, 0u, 0u, 0u};   // (what is there may be anything)
+        }
+    };
+    auto load = [&](int t) {
+        if (t < np) load_shared(t);
+        else if (t < total) load_own(t - np);
+    };
+    load(wave);
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        const uint16_t *qr = query_row(p, s, h, min(m0 + 16 * cb + c16, Mt - 1)) + 8 * g;
+#pragma unroll
+        for (int cc = 0; cc < NC; ++cc) st.q[cb][cc] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qr + cc * 32));
+    }
+    const int fresh = new_of(p, held, asked);
+    if (fresh == 0) return;   // uniform: its rows are left as they were
+    for (int t = wave; t < total; t += NW) {
+        const uint32_t hidden = absent;
+        store_v<D>(vt, vr, lane);
+        tile_step<D, CB>(
+            st, vt, p.scale_log2e, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); }, [&]() { load(t + NW); },
+            [&](f32x4 (&sc)[CB][2]) {
+                if (t < np) {   // uniform
+                    if ((t + 1) * TK > p.prefix_len) hide_from<CB>(sc, p.prefix_len - t * TK, g);
+                } else if ((t - np + 1) * TK > len || hidden) {
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb) {
+                        const int m = min(m0 + 16 * cb + c16, Mt - 1), lim = min(len + m - p.by_Bt.divide(m) * p.Bt + 1, n) - (t - np) * TK - 4 * g;
+#pragma unroll
+                        for (int kg = 0; kg < 2; ++kg) {
+                            const bool gone = hidden >> (2 * kg + (g >> 1)) & 1;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) sc[cb][kg][i] = 16 * kg + i < lim && !gone ? sc[cb][kg][i] : -INFINITY;
+                        }
+                    }
+                }
+            });
+    }
+    float *outs = reinterpret_cast<float *>(smem);
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        const float l = sum_over_rows(st.l[cb]);
+        __syncthreads();   // nobody reads V tiles, or the block of rows before, any more
+        float *ow = outs + (size_t)wave * 16 * OUT_PITCH<D>;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(ow + c16 * OUT_PITCH<D> + 16 * db + 4 * g) = st.o[cb][db];
+        if (g == 0) ml_s[wave][c16] = make_float2(st.m[cb], l);
+        __syncthreads();
+        join_waves<D>(outs, ml_s, min(16, Mt - m0 - 16 * cb), tid, [&](int row, int d0, f32x4 acc, float, float) {
+            const int m = m0 + 16 * cb + row;
+            if (m - p.by_Bt.divide(m) * p.Bt >= fresh) return;
+            bf16x4 o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = (__bf16)acc[i];
+            *reinterpret_cast<bf16x4 *>(p.out + ((size_t)sh * Mt + m) * D + d0) = o;
+        });
+    }
+}
+
 // Query rows of a block of the own part: 16, or 32 where a sequence has more
 int own_block(int64_t rows) { return rows > 16 ? 32 : 16; }
 
@@ -969,28 +1097,51 @@ float shared_price(int64_t rows, int heads, int prefix_len, int cus)
 {
     using P = Prices<D, RS, 16>;
     auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
-    const int64_t segs = heads * up(rows, RS), units = up(up(prefix_len, TK), NW / (RS / 32)), wgs = std::max(cus - cus / 16, 1);
+    constexpr int KW = RS == 16 ? NW : NW / (RS / 32);
+    const int64_t segs = heads * up(rows, RS), units = up(up(prefix_len, TK), KW), wgs = std::max(cus - cus / 16, 1);
     if (segs <= wgs) {
         const int64_t splits = std::min(wgs / segs, units);
         return (float)up(units, splits) * P::step + P::task + (float)(splits * heads * rows) * P::partial;
     }
     return (float)up(segs, wgs) * ((float)units * P::step + P::task) + (float)(heads * rows) * P::partial;
 }
-// Query rows of a block of the shared part: 16 where that is all, or two, four or eight waves of 32 rows; of those that rows half fill at
-// least, the cheapest.  Small blocks have fewer pieces of each segment, and so fewer partials, large ones read a tile from LDS for more
-// rows.  Measured with blocks of 64, 128 and 256 (D 128, 8 KV heads): 256 rows over 1024 shared ones 19.2, 21.7 and 23.1 us, over 8192 31.1,
-// 29.1 and 33.7; 1024 rows over 8192 110, 71 and 66.  Over 210 sizes the price's choice is 0.9 % off the best on average; that by
-// rows alone was 8.7 % off.
-int shared_block(int64_t rows, int heads, int prefix_len, int D, int cus)
+
+// Query rows of a block of the shared part, and what it takes (rows, prefix_len >= 1): 16 where that is all, or two, four or eight waves of
+// 32 rows; of those that rows half fill at least, the cheapest.  Small blocks have fewer pieces of each segment, and so fewer partials, large
+// ones read a tile from LDS for more rows.  Measured with blocks of 64, 128 and 256 (D 128, 8 KV heads): 256 rows over 1024 shared ones 19.2,
+// 21.7 and 23.1 us, over 8192 31.1, 29.1 and 33.7; 1024 rows over 8192 110, 71 and 66.  Over 210 sizes the price's choice is 0.9 % off
+// the best on average; that by rows alone was 8.7 % off.
+struct SharedBlock {
+    int rows;
+    float price;
+};
+template <int D>
+SharedBlock shared_block(int64_t rows, int heads, int prefix_len, int cus)
 {
-    if (rows <= 16) return 16;
-    if (rows <= 64) return 64;
-    const bool wide = D == 128;
-    const float by64 = wide ? shared_price<128, 64>(rows, heads, prefix_len, cus) : shared_price<64, 64>(rows, heads, prefix_len, cus);
-    const float by128 = wide ? shared_price<128, 128>(rows, heads, prefix_len, cus) : shared_price<64, 128>(rows, heads, prefix_len, cus);
-    if (rows <= 128) return by64 <= by128 ? 64 : 128;
-    const float by256 = wide ? shared_price<128, 256>(rows, heads, prefix_len, cus) : shared_price<64, 256>(rows, heads, prefix_len, cus);
-    return by64 <= std::min(by128, by256) ? 64 : by128 <= by256 ? 128 : 256;
+    if (rows <= 16) return {16, shared_price<D, 16>(rows, heads, prefix_len, cus)};
+    SharedBlock best{64, shared_price<D, 64>(rows, heads, prefix_len, cus)};
+    auto consider = [&](SharedBlock other) { best = other.price < best.price ? other : best; };
+    if (rows > 64) consider({128, shared_price<D, 128>(rows, heads, prefix_len, cus)});
+    if (rows > 128) consider({256, shared_price<D, 256>(rows, heads, prefix_len, cus)});
+    return best;
+}
+
+// Whether one launch with a workgroup a segment (branch_short_kernel) takes the call: its time, with as many own rows as the tables can name
+// (the lengths themselves are on the device), against the two launches' with the prompts' part alone, whose pieces are dealt to all workgroups.
+// Lines through the times of 345 sizes, of which the choice is 0.8 % off the better on average (two launches always: 36 %).  Measured, one
+// launch against two (D 128, 8 KV heads of 4 query heads): one sequence, 40 shared and 10 own rows 4.5 us against 9.1, 200 and 100 6.8
+// and 9.8, 1000 and 300 15.6 and 10.4; 32 sequences, 200 and 100 7.2 and 14.8, 1000 and 100 13.7 and 16.7, 2000 and 100 22.5 and 18.6;
+// 128 sequences, 40 and 10 13.9 and 17.5, 500 and 10 30.9 and 20.5.
+template <int D, int RO>
+bool one_launch(const BranchParams &p, float shared)
+{
+    constexpr bool wide = D == 128;
+    constexpr float start = RO == 16 ? (wide ? 2.f : 1.3f) : (wide ? 4.4f : 3.2f), tile = RO == 16 ? (wide ? 2.2f : 1.15f) : (wide ? 2.4f : 1.13f);
+    const int64_t segs = (int64_t)p.n_seqs * p.hkv * ((p.G * p.Bt + RO - 1) / RO);
+    const int64_t own = ((int64_t)p.pages.width << p.pages.page_shift) / TK + 1, tiles = (p.prefix_len + TK - 1) / TK + own;
+    const float one = 1.7f + std::max((float)segs / (float)p.cus, 1.f) * (start + tile / NW * (float)tiles);
+    using P = Prices<D, 16, RO>;
+    return one <= 2.f + (p.shared_segs > 0 ? shared : P::own_wave + P::own_tile);
 }
 
 }  // namespace
@@ -1016,7 +1167,7 @@ size_t branch_workspace(int n_seqs, int n_prefixes, int hkv, int G, int Bt, int 
 namespace {
 
 template <int D, int RS, int RO>
-hipError_t launch(const BranchParams &p, hipStream_t s)
+hipError_t launch_both(const BranchParams &p, hipStream_t s)
 {
     const int64_t rows = (int64_t)p.n_seqs * p.hkv * p.G * p.Bt;
     const int units = 256 / (D / 4);
@@ -1031,32 +1182,38 @@ hipError_t launch(const BranchParams &p, hipStream_t s)
 }
 
 template <int D, int RO>
-hipError_t launch(const BranchParams &p, int RS, hipStream_t s)
+hipError_t launch(BranchParams p, hipStream_t s)
 {
-    switch (RS) {
-    case 16: return launch<D, 16, RO>(p, s);
-    case 64: return launch<D, 64, RO>(p, s);
-    case 128: return launch<D, 128, RO>(p, s);
-    default: return launch<D, 256, RO>(p, s);
+    const int64_t rows = (int64_t)p.fan * p.G * p.Bt;
+    const int blocks = (p.G * p.Bt + RO - 1) / RO, heads = p.n_prefixes * p.hkv;
+    const SharedBlock block = shared_block<D>(std::max<int64_t>(rows, 1), std::max(heads, 1), std::max(p.prefix_len, 1), p.cus);
+    p.shared_segs = p.prefix_len > 0 ? (int32_t)(heads * ((rows + block.rows - 1) / block.rows)) : 0;
+    p.by_segs.set(std::max(p.shared_segs, 1));
+    p.by_heads.set(std::max(heads, 1));
+    p.by_hkv.set(p.hkv);
+    p.by_Mt.set((uint32_t)(p.G * p.Bt));
+    p.by_Bt.set(p.Bt);
+    p.by_fan.set(std::max(p.fan, 1));
+    p.by_own_blocks.set((uint32_t)blocks);
+    if (one_launch<D, RO>(p, block.price)) {
+        hipLaunchKernelGGL((branch_short_kernel<D, RO>), dim3((unsigned)(p.n_seqs * p.hkv * blocks)), dim3(64 * NW), 0, s, p);
+        return hipGetLastError();
+    }
+    switch (block.rows) {
+    case 16: return launch_both<D, 16, RO>(p, s);
+    case 64: return launch_both<D, 64, RO>(p, s);
+    case 128: return launch_both<D, 128, RO>(p, s);
+    default: return launch_both<D, 256, RO>(p, s);
     }
 }
 
 }  // namespace
 
-hipError_t launch_branch_attention(BranchParams p, hipStream_t s)
+hipError_t launch_branch_attention(const BranchParams &p, hipStream_t s)
 {
-    const int64_t Mt = (int64_t)p.G * p.Bt;
-    const int RS = shared_block(p.fan * Mt, p.n_prefixes * p.hkv, std::max(p.prefix_len, 1), p.D, p.cus), RO = own_block(Mt);
-    p.shared_segs = p.prefix_len > 0 ? (int32_t)(p.n_prefixes * p.hkv * ((p.fan * Mt + RS - 1) / RS)) : 0;
-    p.by_segs.set(p.shared_segs > 0 ? p.shared_segs : 1);
-    p.by_heads.set(p.n_prefixes > 0 ? p.n_prefixes * p.hkv : 1);
-    p.by_hkv.set(p.hkv);
-    p.by_Mt.set((uint32_t)Mt);
-    p.by_Bt.set(p.Bt);
-    p.by_fan.set(p.fan > 0 ? p.fan : 1);
-    p.by_own_blocks.set((uint32_t)((Mt + RO - 1) / RO));
-    if (p.D == 128) return RO == 16 ? launch<128, 16>(p, RS, s) : launch<128, 32>(p, RS, s);
-    if (p.D == 64) return RO == 16 ? launch<64, 16>(p, RS, s) : launch<64, 32>(p, RS, s);
+    const bool few = own_block((int64_t)p.G * p.Bt) == 16;
+    if (p.D == 128) return few ? launch<128, 16>(p, s) : launch<128, 32>(p, s);
+    if (p.D == 64) return few ? launch<64, 16>(p, s) : launch<64, 32>(p, s);
     return hipErrorInvalidValue;
 }
 

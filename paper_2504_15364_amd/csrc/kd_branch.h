@@ -90,6 +90,6 @@ struct BranchParams {
 };
 constexpr int BRANCH_PLAN_WORDS = 8;
 size_t branch_workspace(int n_seqs, int n_prefixes, int hkv, int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_plan);
-hipError_t launch_branch_attention(BranchParams p, hipStream_t s);   // (segments and divisors are filled in here)
+hipError_t launch_branch_attention(const BranchParams &p, hipStream_t s);   // (it fills in segments and divisors)
 
 }  // namespace kd

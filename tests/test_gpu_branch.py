@@ -173,10 +173,17 @@ def test_block_step_with_norm_alone_and_its_refusals():
 
 
 # ------------------------------------------------------------------------------------------------ continuations
-def paged(lens, extra, page, hkv, d, g, spare=4, pages=None):
+@pytest.fixture(params=[0, 1 << 16], ids=["narrow", "wide"])
+def wide(request):
+    """Rows that tables could name beyond those that lengths ask for.  A call whose tables name few rows of few sequences is one launch;
+    one whose tables could name this many is two."""
+    return request.param
+
+
+def paged(lens, extra, page, hkv, d, g, spare=4, wide=0):
     """Pools whose every row is NaN, a table of shuffled pages for lens[i] + extra rows each."""
     need = [max(0, -(-(max(n, 0) + extra) // page)) for n in lens]
-    width, total = max(max(need), 1), sum(need) + spare
+    width, total = max(max(need), 1) + wide // page, sum(need) + spare
     pool = torch.full((total, hkv, page, d), float("nan"), dtype=torch.bfloat16, device="cuda")
     order = torch.randperm(total, generator=g["generator"], device="cuda").cpu()
     table, at = torch.full((len(lens), width), -1, dtype=torch.int32), 0
@@ -314,11 +321,11 @@ CASES = [
 
 @pytest.mark.parametrize("case", CASES, ids=[str(i) for i in range(len(CASES))])
 @pytest.mark.parametrize("values", ["plain", "peaked"])
-def test_branch_attention(case, values):
+def test_branch_attention(case, values, wide):
     hq, hkv, d, prompts, fan, N, page, Bt, lens, n_new = case
     n = max(prompts, 1) * fan
     g = gen(1000 + hq * N + page)
-    k_pages, v_pages, table = paged(lens, Bt, page, hkv, d, g)
+    k_pages, v_pages, table = paged(lens, Bt, page, hkv, d, g, wide=wide)
     size = 1.0 if values == "plain" else 6.0                    # peaked: logits up to hundreds, one key takes nearly all
     for s, L in enumerate(lens):
         if L >= 0:   # rows behind the new ones stay NaN
@@ -366,12 +373,12 @@ def test_branch_attention_long_prompts_and_long_own_rows():
         close(out[s], want, bound, f"sequence {s}")
 
 
-def test_branch_attention_dominant_keys_at_the_ends_of_pieces():
+def test_branch_attention_dominant_keys_at_the_ends_of_pieces(wide):
     # one key of a row holds nearly all the weight, wherever it lies; all other keys far below
     hq, hkv, d, N, L = 4, 1, 64, 300, 90
     g = gen(78)
     for at in (0, 31, 32, 255, 256, 299, 300, 331, 390):
-        k_pages, v_pages, table = paged([L], 1, 16, hkv, d, g)
+        k_pages, v_pages, table = paged([L], 1, 16, hkv, d, g, wide=wide)
         k, v = torch.randn((hkv, N + L + 1, d), **g).bfloat16(), torch.randn((hkv, N + L + 1, d), **g).bfloat16()
         q = torch.randn((1, hq, 1, d), **g).bfloat16()
         k[0, at] = (60.0 * q[0, 1, 0].float() / q[0, 1, 0].float().norm()).bfloat16()
@@ -385,12 +392,12 @@ def test_branch_attention_dominant_keys_at_the_ends_of_pieces():
 
 @pytest.mark.parametrize("fan", [3, 16, 40, 64])
 @pytest.mark.parametrize("power", [-90, 90])
-def test_branch_attention_values_of_extreme_size(fan, power):
+def test_branch_attention_values_of_extreme_size(fan, power, wide):
     # heads whose values differ by 2^30 from one another, all far from one
     hq, hkv, d, N = 8, 2, 128, 700
     g = gen(300 + fan + power)
     lens = [(7 * i) % 60 for i in range(fan)]
-    k_pages, v_pages, table = paged(lens, 1, 16, hkv, d, g)
+    k_pages, v_pages, table = paged(lens, 1, 16, hkv, d, g, wide=wide)
     size = 2.0 ** (power + torch.randint(-15, 16, (hkv, 1, 1), **g).float())
 
     def values(n):
@@ -408,11 +415,11 @@ def test_branch_attention_values_of_extreme_size(fan, power):
         close(out[s], want, bound, f"sequence {s}")
 
 
-def test_branch_attention_absent_pages():
+def test_branch_attention_absent_pages(wide):
     # a page outside the pool: its keys are absent; a query without any key gets zeros
     hq, hkv, d, page = 8, 2, 128, 8
     g = gen(79)
-    k_pages, v_pages, table = paged([60, 5, 70], 2, page, hkv, d, g)
+    k_pages, v_pages, table = paged([60, 5, 70], 2, page, hkv, d, g, wide=wide)
     for s, L in enumerate((60, 5, 70)):
         put_rows(k_pages, table, s, torch.randn((hkv, L + 2, d), **g).bfloat16())
         put_rows(v_pages, table, s, torch.randn((hkv, L + 2, d), **g).bfloat16())
@@ -430,8 +437,7 @@ def test_branch_attention_absent_pages():
     none = (own[0][:, :0], own[1][:, :0])
     want, bound = attention_reference(q[0], none, 0, own, lambda j: len(seen) - 1 + j, d ** -0.5)
     close(out[0], want, bound)
-    rows = table.shape[1] * page
-    assert rows == 72
+    rows = 72   # (a wide table's other columns name no pages)
     own = rows_of(k_pages, table_ok, 2, rows)[:, page:], rows_of(v_pages, table_ok, 2, rows)[:, page:]
     want, bound = attention_reference(q[2], none, 0, own, lambda j: rows - page, d ** -0.5)
     close(out[2], want, bound)
@@ -459,7 +465,7 @@ def test_branch_attention_shared_own_pages_and_pools_past_32_bits():
         close(out[s], want, bound, f"sequence {s}")
 
 
-def continue_prompt(layout, steps=5, fan=3, prompts=2, layers=2, page=8):
+def continue_prompt(layout, wide, steps=5, fan=3, prompts=2, layers=2, page=8):
     """A run as a program makes it: prompts through blocks that norm and rotate, then `fan` continuations of each, token by token;
     yields (out, reference, bound) of every layer and step."""
     hq, hkv, d, N, B, T = 8, 2, 64, 64, 32, 110
@@ -475,7 +481,7 @@ def continue_prompt(layout, steps=5, fan=3, prompts=2, layers=2, page=8):
         for l, c in enumerate(caches):   # layer by layer, evictions pending from layer to layer
             q, k = kd.norm_rope(x[l][0], x[l][1], cos, sin, pos0=t, q_weight=wq[l], k_weight=wk[l])
             c.prefill_block_deferred(q, k, x[l][2], t, carry=caches[l - 1])
-    pools = [paged([0] * n, steps + 2, page, hkv, d, g) for _ in range(layers)]
+    pools = [paged([0] * n, steps + 2, page, hkv, d, g, wide=wide) for _ in range(layers)]
     table, lens, pos0 = pools[0][2], torch.zeros(n, dtype=torch.int32, device="cuda"), ints([T] * n)
     for k, v, _ in pools:
         assert k.shape == pools[0][0].shape
@@ -494,9 +500,9 @@ def continue_prompt(layout, steps=5, fan=3, prompts=2, layers=2, page=8):
 
 
 @pytest.mark.parametrize("layout", [kd.LAYOUT_FILL, kd.LAYOUT_ORDERED])
-def test_continuations_of_prompts_held_by_keydiff_caches(layout):
+def test_continuations_of_prompts_held_by_keydiff_caches(layout, wide):
     seen = 0
-    for step, l, q, out, cache, k_pages, v_pages, table, x, wq, cos, sin, T in continue_prompt(layout):
+    for step, l, q, out, cache, k_pages, v_pages, table, x, wq, cos, sin, T in continue_prompt(layout, wide):
         n, hq = q.shape[:2]
         assert cache.len == cache.cfg.budget_N
         want, bound = formed(x[:, :hq], wq, cos, sin, torch.full((n, 1), T + step, device="cuda"), 1e-6)
@@ -510,11 +516,11 @@ def test_continuations_of_prompts_held_by_keydiff_caches(layout):
     assert seen == 10
 
 
-def test_branch_attention_over_an_empty_cache_and_a_cache_of_other_heads():
+def test_branch_attention_over_an_empty_cache_and_a_cache_of_other_heads(wide):
     hq, hkv, d = 4, 2, 64
     g = gen(81)
     cache = kd.KeyDiffCache(kd.KeyDiffConfig(1, hq, hkv, d, 64, 16, softmax_scale=0.5))
-    k_pages, v_pages, table = paged([10, 0], 1, 8, hkv, d, g)
+    k_pages, v_pages, table = paged([10, 0], 1, 8, hkv, d, g, wide=wide)
     for s, L in enumerate((10, 0)):
         put_rows(k_pages, table, s, torch.randn((hkv, L + 1, d), **g).bfloat16())
         put_rows(v_pages, table, s, torch.randn((hkv, L + 1, d), **g).bfloat16())
@@ -536,11 +542,11 @@ def test_branch_attention_over_an_empty_cache_and_a_cache_of_other_heads():
 
 
 @pytest.mark.parametrize("given", [True, False])
-def test_captured_steps_follow_the_lengths_they_find(given):
+def test_captured_steps_follow_the_lengths_they_find(given, wide):
     # append and attention captured once, replayed with lengths, tables and inputs that change, against eager calls
     hq, hkv, d, N, page, n, steps = 8, 2, 128, 200, 16, 5, 6
     g = gen(82)
-    k_pages, v_pages, table = paged([90] * n, steps + 1, page, hkv, d, g)
+    k_pages, v_pages, table = paged([90] * n, steps + 1, page, hkv, d, g, wide=wide)
     first = [0, 3, 40, -1, 90]
     for s, L in enumerate(first):
         if L > 0:
