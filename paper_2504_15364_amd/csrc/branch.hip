@@ -780,6 +780,8 @@ template <int D, int RS, int RO>
 struct Prices {
     static constexpr bool wide = D == 128;
     static constexpr float step = RS == 256 ? (wide ? 1.3f : 1.0f) : RS == 128 ? (wide ? 1.45f : 1.1f) : RS == 64 ? (wide ? 2.35f : 1.1f) : (wide ? 2.5f : 1.5f);
+    // (blocks of 16 rows read every tile for themselves)
+    static __host__ __device__ float step_of(int blocks) { return RS == 16 ? step * (0.85f + 0.15f * (float)blocks) : step; }
     static constexpr float task = RS == 256 ? (wide ? 9.f : 7.f) : RS == 128 ? (wide ? 9.5f : 6.5f) : RS == 64 ? (wide ? 8.8f : 5.5f) : (wide ? 4.5f : 4.f);
     static constexpr float own_tile = RO == 16 ? (wide ? 2.7f : 1.8f) : (wide ? 3.8f : 2.2f), own_end = 0.7f, own_wave = 4.f;
     static constexpr float own_traffic = TK * D * 4 / 5.5e6f, partial = D * 4 / 2e6f;
@@ -806,17 +808,18 @@ __device__ __forceinline__ Plan make_plan(const BranchParams &p, int units, int 
     plan.own_tiles = __builtin_amdgcn_readlane((int)wave_inclusive_scan((uint32_t)own), 63) * per_seq;
     const float own_work = (float)plan.own_tiles * P::own_tile + (float)(used * per_seq) * P::own_end;
     const int segs = p.shared_segs, most = plan.own_tiles > 0 ? wgs - 1 : wgs;
+    const float step = P::step_of((p.fan * p.G * p.Bt + RS - 1) / RS);
     int w = 0, splits = 1;
     float price = INFINITY;
     if (segs > 0 && segs <= most) {
         const int top = min(p.by_segs.divide(most), units);
         splits = min((lane + 1) * ((top + 63) / 64), top);
         w = segs * splits;
-        price = up((float)units, (float)splits) * P::step + P::task;
+        price = up((float)units, (float)splits) * step + P::task;
     } else if (segs > 0) {
         w = max(most * (lane + 1) / 64, 1);
-        const float whole = up((float)segs, (float)w) * ((float)units * P::step + P::task);
-        const float half = up(2.f * (float)segs, (float)w) * ((float)((units + 1) / 2) * P::step + P::task);
+        const float whole = up((float)segs, (float)w) * ((float)units * step + P::task);
+        const float half = up(2.f * (float)segs, (float)w) * ((float)((units + 1) / 2) * step + P::task);
         splits = units > 1 && half < whole ? 2 : 1;
         price = fminf(whole, half);
     }
@@ -1098,18 +1101,20 @@ float shared_price(int64_t rows, int heads, int prefix_len, int cus)
     using P = Prices<D, RS, 16>;
     auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
     constexpr int KW = RS == 16 ? NW : NW / (RS / 32);
+    const float step = P::step_of((int)up(rows, RS));
     const int64_t segs = heads * up(rows, RS), units = up(up(prefix_len, TK), KW), wgs = std::max(cus - cus / 16, 1);
     if (segs <= wgs) {
         const int64_t splits = std::min(wgs / segs, units);
-        return (float)up(units, splits) * P::step + P::task + (float)(splits * heads * rows) * P::partial;
+        return (float)up(units, splits) * step + P::task + (float)(splits * heads * rows) * P::partial;
     }
-    return (float)up(segs, wgs) * ((float)units * P::step + P::task) + (float)(heads * rows) * P::partial;
+    return (float)up(segs, wgs) * ((float)units * step + P::task) + (float)(heads * rows) * P::partial;
 }
 
-// Query rows of a block of the shared part, and what it takes (rows, prefix_len >= 1): 16 where that is all, or two, four or eight waves of
-// 32 rows; of those that rows half fill at least, the cheapest.  Small blocks have fewer pieces of each segment, and so fewer partials, large
-// ones read a tile from LDS for more rows.  Measured with blocks of 64, 128 and 256 (D 128, 8 KV heads): 256 rows over 1024 shared ones 19.2,
-// 21.7 and 23.1 us, over 8192 31.1, 29.1 and 33.7; 1024 rows over 8192 110, 71 and 66.  Over 210 sizes the price's choice is 0.9 % off
+// Query rows of a block of the shared part, and what it takes (rows, prefix_len >= 1): 16, whose waves work each for itself, or two, four or
+// eight waves of 32 rows, which share tiles; of those that rows half fill at least (and of 16 up to four blocks), the cheapest.  Small blocks
+// have fewer pieces of each segment, and so fewer partials, large ones read a tile for more rows.  Measured with blocks of 64, 128 and 256
+// (D 128, 8 KV heads): 256 rows over 1024 shared ones 19.2, 21.7 and 23.1 us, over 8192 31.1, 29.1 and 33.7; 1024 rows over 8192 110, 71 and
+// 66; with 16 and 64: 48 rows over 2000 12.2 and 14.7, over 12288 21.6 and 20.1.  Over 210 sizes the choice of 64, 128 or 256 is 0.9 % off
 // the best on average; that by rows alone was 8.7 % off.
 struct SharedBlock {
     int rows;
@@ -1118,9 +1123,9 @@ struct SharedBlock {
 template <int D>
 SharedBlock shared_block(int64_t rows, int heads, int prefix_len, int cus)
 {
-    if (rows <= 16) return {16, shared_price<D, 16>(rows, heads, prefix_len, cus)};
-    SharedBlock best{64, shared_price<D, 64>(rows, heads, prefix_len, cus)};
+    SharedBlock best{16, rows <= 64 ? shared_price<D, 16>(rows, heads, prefix_len, cus) : INFINITY};
     auto consider = [&](SharedBlock other) { best = other.price < best.price ? other : best; };
+    if (rows > 16) consider({64, shared_price<D, 64>(rows, heads, prefix_len, cus)});
     if (rows > 64) consider({128, shared_price<D, 128>(rows, heads, prefix_len, cus)});
     if (rows > 128) consider({256, shared_price<D, 256>(rows, heads, prefix_len, cus)});
     return best;
@@ -1128,12 +1133,12 @@ SharedBlock shared_block(int64_t rows, int heads, int prefix_len, int cus)
 
 // Whether one launch with a workgroup a segment (branch_short_kernel) takes the call: its time, with as many own rows as the tables can name
 // (the lengths themselves are on the device), against the two launches' with the prompts' part alone, whose pieces are dealt to all workgroups.
-// Lines through the times of 345 sizes, of which the choice is 0.8 % off the better on average (two launches always: 36 %).  Measured, one
+// Lines through the times of 345 sizes, of which the choice is as fast as the better on average (two launches always: 36 % slower).  Measured, one
 // launch against two (D 128, 8 KV heads of 4 query heads): one sequence, 40 shared and 10 own rows 4.5 us against 9.1, 200 and 100 6.8
 // and 9.8, 1000 and 300 15.6 and 10.4; 32 sequences, 200 and 100 7.2 and 14.8, 1000 and 100 13.7 and 16.7, 2000 and 100 22.5 and 18.6;
 // 128 sequences, 40 and 10 13.9 and 17.5, 500 and 10 30.9 and 20.5.
 template <int D, int RO>
-bool one_launch(const BranchParams &p, float shared)
+bool one_launch(const BranchParams &p, const SharedBlock &block)
 {
     constexpr bool wide = D == 128;
     constexpr float start = RO == 16 ? (wide ? 2.f : 1.3f) : (wide ? 4.4f : 3.2f), tile = RO == 16 ? (wide ? 2.2f : 1.15f) : (wide ? 2.4f : 1.13f);
@@ -1141,7 +1146,8 @@ bool one_launch(const BranchParams &p, float shared)
     const int64_t own = ((int64_t)p.pages.width << p.pages.page_shift) / TK + 1, tiles = (p.prefix_len + TK - 1) / TK + own;
     const float one = 1.7f + std::max((float)segs / (float)p.cus, 1.f) * (start + tile / NW * (float)tiles);
     using P = Prices<D, 16, RO>;
-    return one <= 2.f + (p.shared_segs > 0 ? shared : P::own_wave + P::own_tile);
+    const float both = p.shared_segs > 0 ? block.price + (block.rows == 16 ? 3.5f : 2.f) : P::own_wave + P::own_tile + 2.f;   // start and join
+    return one <= both;
 }
 
 }  // namespace
@@ -1152,7 +1158,7 @@ size_t branch_workspace(int n_seqs, int n_prefixes, int hkv, int G, int Bt, int 
     const size_t RO = own_block(Mt);
     size_t shared = 0;   // (the length of the prompts' rows is not known here: the most that any block takes)
     for (const int RS : {16, 64, 128, 256})
-        if (RS == 16 ? fan * Mt <= 16 : RS == 64 || fan * Mt > RS / 2)
+        if (RS == 16 ? fan * Mt <= 64 : fan * Mt > (RS == 64 ? 16 : RS / 2))
             shared = std::max(shared, shared_slots(n_prefixes, (int)fan, hkv, (int)Mt, RS, cus) * RS);
     const size_t own = ((size_t)n_seqs * hkv * ((Mt + RO - 1) / RO) + (size_t)cus * NW) * RO;
     size_t off = (shared + own) * D * 4;
@@ -1195,7 +1201,7 @@ hipError_t launch(BranchParams p, hipStream_t s)
     p.by_Bt.set(p.Bt);
     p.by_fan.set(std::max(p.fan, 1));
     p.by_own_blocks.set((uint32_t)blocks);
-    if (one_launch<D, RO>(p, block.price)) {
+    if (one_launch<D, RO>(p, block)) {
         hipLaunchKernelGGL((branch_short_kernel<D, RO>), dim3((unsigned)(p.n_seqs * p.hkv * blocks)), dim3(64 * NW), 0, s, p);
         return hipGetLastError();
     }
