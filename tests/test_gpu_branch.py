@@ -316,6 +316,11 @@ CASES = [
     (20, 10, 64, 30, 20, 150, 16, 1, [i % 5 - 1 for i in range(600)], None),
     (8, 8, 128, 65, 1, 2500, 8, 1, [0] * 65, None),
     (16, 2, 128, 1, 40, 500, 16, 9, [i % 21 for i in range(40)], [i % 10 for i in range(40)]),   # 72 rows a sequence, 2880 of a prompt
+    # blocks of 128 and 256 shared rows, filled in part
+    (64, 16, 128, 4, 31, 1021, 16, 1, [i % 35 for i in range(124)], None),
+    (80, 20, 64, 10, 30, 1021, 16, 1, [i % 35 for i in range(300)], None),
+    (64, 16, 128, 4, 120, 515, 16, 1, [i % 9 - 1 for i in range(480)], None),
+    (64, 16, 64, 4, 120, 515, 16, 1, [i % 9 - 1 for i in range(480)], None),
 ]
 
 
