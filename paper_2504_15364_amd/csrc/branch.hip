@@ -1147,7 +1147,7 @@ bool one_launch(const BranchParams &p, const SharedBlock &block)
     const float one = 1.7f + std::max((float)segs / (float)p.cus, 1.f) * (start + tile / NW * (float)tiles);
     using P = Prices<D, 16, RO>;
     const float both = p.shared_segs > 0 ? block.price + (block.rows == 16 ? 3.5f : 2.f) : P::own_wave + P::own_tile + 2.f;   // start and join
-    return one <= both;
+    return one <= both && segs < (1 << 22);   // (a launch counts its threads in 32 bits)
 }
 
 }  // namespace

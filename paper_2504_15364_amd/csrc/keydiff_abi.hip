@@ -1231,6 +1231,7 @@ int check_heads(int32_t n_seqs, int32_t hq, int32_t hkv, int32_t head_dim, int32
     if (head_dim != 64 && head_dim != 128) return fail(KEYDIFF_ESHAPE, "head_dim must be 64 or 128");
     if (hq > kMaxHeads) return fail(KEYDIFF_ESHAPE, "n_q_heads must not exceed %d", kMaxHeads);
     if ((int64_t)n_seqs * Bt * hq > 0x7fffffff) return fail(KEYDIFF_ESHAPE, "sequences * Bt * n_q_heads must fit in int32");
+    if ((int64_t)n_seqs * Bt > (1 << 27)) return fail(KEYDIFF_ESHAPE, "sequences * Bt must not exceed 2^27");   // (a launch counts threads in 32 bits)
     return KEYDIFF_OK;
 }
 
@@ -1326,6 +1327,7 @@ int branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32
 int check_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *out, const void *workspace)
 {
     if (int rc = check_branches(b, Bt)) return rc;
+    if ((int64_t)b->n_seqs * Bt * b->n_q_heads > (1 << 26)) return fail(KEYDIFF_ESHAPE, "sequences * Bt * n_q_heads must not exceed 2^26");
     if (int rc = check_rows(q, "q")) return rc;
     if (!out || !workspace) return fail(KEYDIFF_EINVAL, "null pointer");
     if (misaligned(out)) return fail(KEYDIFF_EINVAL, "out must be 16-byte aligned");

@@ -42,6 +42,7 @@ def norm_rope(q=rows(), k=rows(), batch=1, hq=8, hkv=2, d=128, Bt=4, pos0=0, pos
     (dict(Bt=0), kd.ESHAPE),
     (dict(batch=0), kd.ESHAPE),
     (dict(hq=8192, hkv=1), kd.ESHAPE),
+    (dict(hq=1, hkv=1, Bt=1 << 27, batch=2), kd.ESHAPE),
     (dict(q_out=None), kd.EINVAL),
     (dict(k_out=(1 << 33) + 8), kd.EINVAL),
     (dict(q_out=P), kd.EINVAL),                             # in place
@@ -121,6 +122,7 @@ def attention(b=None, q=rows(), Bt=1, kp=P, vp=P, prompts=2, rows_=100, cap=100,
     (dict(cap=99), kd.ESHAPE),
     (dict(kp=None), kd.EINVAL),
     (dict(vp=P + 8), kd.EINVAL),
+    (dict(b=branches(n_seqs=1 << 24, table_width=1), prompts=0), kd.ESHAPE),                                    # 2^27 query rows
     (dict(b=branches(n_seqs=1 << 20, n_q_heads=8, n_kv_heads=8, table_width=1 << 20), prompts=0), kd.ESHAPE),   # tiles do not fit int32
 ])
 def test_branch_attention_refuses(kw, code):

@@ -623,6 +623,8 @@ def test_calls_on_two_streams_with_workspaces_of_their_own():
     torch.cuda.synchronize()
     assert all(torch.equal(o, w) for o, w in zip(got, want))
     assert all(torch.equal(x, y) for x, y in zip(a, kd.norm_rope(qs[0], qs[0][:, :hkv], *tables(50, d), pos0=3)))
+    b = kd.norm_rope(qs[0], qs[0][:, :hkv], *tables(50, d), pos0=3, stream=0)   # the default stream's handle
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
 
 
 def test_calls_return_what_is_given_and_hold_no_memory():
