@@ -18,9 +18,9 @@
 //                ragged lengths cost nothing, because the list is cut by tiles and not by sequences
 // All of this follows from the lengths on the device: the launch itself does not depend on them and may be replayed from a graph.
 // Where the prompts' rows and those that the tables can name are few, one launch does it, a workgroup a segment (one_launch).
-// Measured (8192 shared rows, 8 KV heads of 128, both launches, back to back): one sequence 14.8 us (35 MB), 16 with up to 777 own rows 21.7
-// (60 MB), 64 with up to 4096 own rows 114 (571 MB: 5.0 TB/s; its first launch alone 5.5), 256 of three query heads to a KV head with up to 33 own
-// rows 61 (26 GFLOP).
+// Measured (8192 shared rows, 8 KV heads of 128, both launches, back to back): one sequence 14.4 us (35 MB), 16 with up to 777 own rows 21.0
+// (60 MB), 64 with up to 4096 own rows 112 (571 MB: 5.1 TB/s; its first launch alone 5.4), 256 of three query heads to a KV head with up to 33 own
+// rows 57 (26 GFLOP).
 #include <algorithm>
 
 #include "kd_branch.h"
@@ -281,7 +281,7 @@ __device__ __forceinline__ void join_waves(const float *outs, const float2 (&ml_
     }
 }
 
-// The shared part with at most 16 query rows: one workgroup, its piece of the list, every wave tiles of its own
+// The shared part in blocks of 16 query rows: a workgroup its piece of a segment, every wave tiles of its own
 template <int D, int CB>
 __device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned char *smem)
 {
