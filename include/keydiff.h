@@ -312,7 +312,8 @@ KEYDIFF_API int keydiff_branch_attention(const keydiff_branches_t *b, const keyd
                              int64_t prefix_cap, float softmax_scale, void *out, void *workspace, size_t workspace_bytes,
                              void *stream);
 /* ... with the rows and the softmax scale of a KeyDiff cache: prompt i is sequence i of the cache's batch, and the rows are those it
- * holds when the call is made (a pending eviction is enqueued first).  The cache is not changed.  (Profiling does not record these
+ * holds when the call is made (a pending eviction is enqueued first; ESTATE if the stream is being captured and there is one, because
+ * every replay would repeat it).  The cache is not changed.  (Profiling does not record these
  * kernels.)                                                                                                              */
 KEYDIFF_API int keydiff_cache_branch_attention(keydiff_cache_t *prompt, const keydiff_branches_t *b, const keydiff_rows_t *q,
                                    int32_t Bt, void *out, void *workspace, size_t workspace_bytes, void *stream);

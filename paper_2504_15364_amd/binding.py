@@ -322,13 +322,14 @@ def branch_attention(q, k_pages, v_pages, table, lens, prefix=None, n_new=None, 
     q [n_seqs][Hq][Bt][d] bf16 (any strides with a contiguous last dimension).
     prefix: the prompts' rows, shared by the sequences that continue them: a KeyDiffCache whose batch holds the prompts, or
     (k, v, rows) with k, v bf16 [prompts][Hkv][at least rows][d]; sequence s continues prompt s / (n_seqs / prompts).  None: own rows
-    alone.  softmax_scale <= 0: 1/sqrt(d), or the cache's.
+    alone.  (A cache with a pending eviction is finished first; ahead of a captured call, finish() it: a replay would repeat that.)
+    softmax_scale <= 0: 1/sqrt(d), or the cache's.
     workspace: a uint8 tensor of at least branch_workspace_bytes that no other call in flight uses (None: allocated for the call).
     Returns out [n_seqs][Hq][Bt][d]; rows behind a sequence's n_new, and those of a sequence with lens < 0, are left as they were
     (they hold anything where out is None)."""
     handle = batch = keys = values = rows = None
     if isinstance(prefix, KeyDiffCache):
-        handle, batch = prefix._h.value or 0, prefix.cfg.batch
+        handle, batch = prefix._h.value if prefix._h else 0, prefix.cfg.batch
         if prefix.device != q.device:
             raise ValueError(f"the cache lives on {prefix.device}, the queries on {q.device}")
     elif prefix is not None:

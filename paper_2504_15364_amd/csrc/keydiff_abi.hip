@@ -1463,6 +1463,9 @@ int keydiff_cache_branch_attention(keydiff_cache_t *c, const keydiff_branches_t 
                                              std::max(compute_units(), 2), &off_ml, &off_plan);
     if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
     hipStream_t s = static_cast<hipStream_t>(stream);
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if ((c->pending || c->shift_pending) && hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone)
+        return fail(KEYDIFF_ESTATE, "the cache has a pending eviction, which every replay would repeat: keydiff_finish it ahead of the capture");
     if (int rc = finish_pending(c, s)) return rc;
     return branch_attention(b, q, Bt, c->k, c->v, c->cfg.batch, c->len, c->L.cap, c->scale_log2e, out, workspace, workspace_bytes, s);
 }

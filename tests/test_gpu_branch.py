@@ -544,6 +544,9 @@ def test_branch_attention_over_an_empty_cache_and_a_cache_of_other_heads(wide):
     with pytest.raises(ValueError, match="workspace"):
         kd.branch_attention(q, k_pages, v_pages, table, ints([10, 0]), workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
     cache.close()
+    with pytest.raises(kd.KeyDiffError) as e:
+        kd.branch_attention(q, k_pages, v_pages, table, ints([10, 0]), prefix=cache)
+    assert e.value.code == -1
 
 
 @pytest.mark.parametrize("given", [True, False])
@@ -590,6 +593,46 @@ def test_captured_steps_follow_the_lengths_they_find(given, wide):
             lens[3], lens[4] = 0, -1     # a slot is given to another sequence, one is freed
         table.copy_(table)
     assert bool(torch.isfinite(out.float()).all())
+
+
+@pytest.mark.parametrize("layout", [kd.LAYOUT_FILL, kd.LAYOUT_ORDERED])
+def test_a_captured_call_takes_no_pending_eviction_along(layout):
+    hq, hkv, d, N, B = 8, 2, 64, 64, 32
+    g = gen(84)
+    cache = kd.KeyDiffCache(kd.KeyDiffConfig(1, hq, hkv, d, N, B, layout=layout))
+    for t in range(0, 4 * B, B):
+        cache.prefill_block_deferred(*(torch.randn((1, h, B, d), **g).bfloat16() for h in (hq, hkv, hkv)), t)
+    k_pages, v_pages, table = paged([5, 0, 9], 1, 8, hkv, d, g)
+    for s, L in enumerate((5, 0, 9)):
+        put_rows(k_pages, table, s, torch.randn((hkv, L + 1, d), **g).bfloat16())
+        put_rows(v_pages, table, s, torch.randn((hkv, L + 1, d), **g).bfloat16())
+    q, lens = torch.randn((3, hq, 1, d), **g).bfloat16(), ints([5, 0, 9])
+    out = torch.zeros_like(q)
+    work = torch.empty(kd.branch_workspace_bytes(3, hq, hkv, d, 1, 1), dtype=torch.uint8, device="cuda")
+
+    def capture():
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        error = None
+        with torch.cuda.graph(graph):
+            out.mul_(0)
+            try:
+                kd.branch_attention(q, k_pages, v_pages, table, lens, prefix=cache, out=out, workspace=work)
+            except kd.KeyDiffError as e:
+                error = e
+        return graph, error
+
+    assert capture()[1].code == -3          # (the step of the last block has left its eviction pending)
+    cache.finish()
+    graph, error = capture()
+    assert error is None
+    want = kd.branch_attention(q, k_pages, v_pages, table, lens, prefix=cache)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert cache.status() == 0 and cache.len == N
+    cache.close()
 
 
 def test_calls_on_two_streams_with_workspaces_of_their_own():
