@@ -1,0 +1,62 @@
+"""branch_append and branch_attention at the ends of what their documentation allows, against plain forms in 64 bits.  Tolerances: those of
+test_gpu_branch.py, whose derivation does not depend on the sizes below."""
+import pytest
+
+import paper_2504_15364_amd as kd
+from test_gpu_branch import attention_reference, close, gen, ints, paged, put_rows, rows_of, wide  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+# ------------------------------------------------------------------------------------------------ the largest values
+def rising(hkv, n, d, g):
+    """n keys and values: the logits of the first two fifths are 0, the others' 15.9 (log2 units, with SCALE and queries (1, 0, ..)), a weight
+    just below 2^16 of the first ones'.  Values of one sign, up to 2^100."""
+    k = torch.zeros((hkv, n, d), dtype=torch.bfloat16, device="cuda")
+    k[:, 2 * n // 5:, 0] = 1
+    v = ((0.5 + 0.5 * torch.rand((hkv, n, d), **g)) * 2.0 ** 100).bfloat16().clamp_(max=2.0 ** 100)
+    return k, v
+
+
+SCALE = 15.9 / 1.4426950408889634
+
+
+@pytest.mark.parametrize("prompts,fan,hq,hkv,d", [(1, 1, 32, 8, 128), (1, 16, 16, 8, 128), (1, 64, 16, 8, 64), (1, 100, 24, 8, 128), (40, 1, 8, 8, 64)])
+def test_values_of_the_largest_size_over_long_prompts(prompts, fan, hq, hkv, d, wide):  # noqa: F811
+    # one sign, so that sums grow with the rows: 8192 rows of weight 2^15.9 and value 2^100 would pass float's range.  (Where a prompt is cut
+    # into pieces, each takes every so manieth tile: all of them meet the small logits first.)
+    N, n = 32768, prompts * fan
+    g = gen(7000 + n)
+    k_pages, v_pages, table = paged([3] * n, 1, 16, hkv, d, g, wide=wide)
+    own = torch.zeros((hkv, 4, d), dtype=torch.bfloat16, device="cuda"), rising(hkv, 4, d, g)[1]
+    for s in range(n):
+        put_rows(k_pages, table, s, own[0])
+        put_rows(v_pages, table, s, own[1])
+    prefix = [rising(hkv, N, d, g) for _ in range(prompts)]
+    kp, vp = (torch.stack([x[i] for x in prefix]) for i in range(2))
+    q = torch.zeros((n, hq, 1, d), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1
+    out = kd.branch_attention(q, k_pages, v_pages, table, ints([3] * n), prefix=(kp, vp, N), softmax_scale=SCALE)
+    for c in range(prompts):   # (the sequences of a prompt are alike)
+        want, bound = attention_reference(q[c * fan], (kp[c].double(), vp[c].double()), N, (own[0].double(), own[1].double()), lambda j: 4, SCALE)
+        for s in range(c * fan, (c + 1) * fan):
+            close(out[s], want, bound, f"sequence {s}")
+
+
+@pytest.mark.parametrize("n", [1, 600])
+def test_values_of_the_largest_size_in_long_own_rows(n):
+    # (600 sequences that read the same pages: a wave then sums thousands of rows by itself)
+    hq, hkv, d, L = 8, 2, 64, 16383
+    g = gen(7100 + n)
+    k_pages, v_pages, table = paged([L], 1, 64, hkv, d, g)
+    k, v = rising(hkv, L + 1, d, g)
+    put_rows(k_pages, table, 0, k)
+    put_rows(v_pages, table, 0, v)
+    q = torch.zeros((n, hq, 1, d), dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1
+    out = kd.branch_attention(q, k_pages, v_pages, table.expand(n, -1).contiguous(), ints([L] * n), softmax_scale=SCALE)
+    none = k[:, :0].double()
+    want, bound = attention_reference(q[0], (none, none), 0, (k.double(), v.double()), lambda j: L + 1, SCALE)
+    for s in range(n):
+        close(out[s], want, bound, f"sequence {s}")
