@@ -936,14 +936,14 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
         float top = mx;
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) top = fmaxf(top, ml[k].x);
-        if (top == -INFINITY) continue;
-        const float old = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - top);
+        // (a piece without a key has reference -inf and sum 0; one whose logits are NaN reference -inf and sum NaN, which must not be lost)
+        const float ref = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(mx - ref);
         L *= old;
         acc *= old;
         mx = top;
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
-            const float f = ml[k].x == -INFINITY ? 0.f : ml[k].y * __builtin_amdgcn_exp2f(ml[k].x - mx);
+            const float f = ml[k].y * __builtin_amdgcn_exp2f(ml[k].x - ref);
             acc += f * o[k];
             L += f;
         }
@@ -955,11 +955,12 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
         if (group != 0) return;
         float top = -INFINITY;
         for (int k = 0; k < groups; ++k) top = fmaxf(top, ml_s[unit + k].x);
+        const float ref = top == -INFINITY ? 0.f : top;
         acc = f32x4{0.f, 0.f, 0.f, 0.f};
         L = 0.f;
         for (int k = 0; k < groups; ++k) {
             const float2 ml = ml_s[unit + k];
-            const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+            const float f = __builtin_amdgcn_exp2f(ml.x - ref);
             acc += f * acc_s[threadIdx.x + k * TPR];
             L += f * ml.y;
         }

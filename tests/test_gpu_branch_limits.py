@@ -60,3 +60,27 @@ def test_values_of_the_largest_size_in_long_own_rows(n):
     want, bound = attention_reference(q[0], (none, none), 0, (k.double(), v.double()), lambda j: L + 1, SCALE)
     for s in range(n):
         close(out[s], want, bound, f"sequence {s}")
+
+
+# ------------------------------------------------------------------------------------------------ a layer above that is broken
+@pytest.mark.parametrize("fan,N", [(3, 100), (1, 9000), (64, 3000), (300, 700)])
+def test_queries_that_are_nan_give_nan(fan, N, wide):  # noqa: F811
+    # whatever the launches (zeros would hide it), and the other sequences' outputs stay what they are
+    hq, hkv, d = 8, 2, 64
+    g = gen(7200 + fan)
+    lens = [(5 * i) % 40 for i in range(fan)]
+    k_pages, v_pages, table = paged(lens, 1, 16, hkv, d, g, wide=wide)
+    for s, L in enumerate(lens):
+        put_rows(k_pages, table, s, torch.randn((hkv, L + 1, d), **g).bfloat16())
+        put_rows(v_pages, table, s, torch.randn((hkv, L + 1, d), **g).bfloat16())
+    prefix = torch.randn((1, hkv, N, d), **g).bfloat16(), torch.randn((1, hkv, N, d), **g).bfloat16(), N
+    q = torch.randn((fan, hq, 1, d), **g).bfloat16()
+    want = kd.branch_attention(q, k_pages, v_pages, table, ints(lens), prefix=prefix)
+    for bad in {0, fan // 2, fan - 1}:
+        broken = q.clone()
+        broken[bad, 2] = float("nan")                        # one head
+        broken[bad, 5, 0, 7] = float("nan")                  # one value of another: every logit is NaN all the same
+        out = kd.branch_attention(broken, k_pages, v_pages, table, ints(lens), prefix=prefix)
+        assert bool(out[bad, [2, 5]].isnan().all())
+        out[bad, [2, 5]] = want[bad, [2, 5]]
+        assert torch.equal(out, want)
