@@ -304,8 +304,8 @@ KEYDIFF_API int keydiff_branch_append(const keydiff_branches_t *b, const keydiff
  * The prompt's rows come from memory once for all sequences that share them.  Sums and softmax statistics are kept in float.
  * Meant for few tokens a sequence: a sequence's own rows are read once for every 32 of its query rows per KV head.
  * Inputs must be finite (those of rows that a query sees, and those of rows seen by another token of the same step), and so must the
- * products of queries and keys be; values up to 2^100 in magnitude (2^96 where prefix_len + table_width * page_rows
- * exceeds 2^27).  KEYDIFF_ESHAPE if the prompt has more than 2^23 rows, if there are more than 2^26 query rows, or if
+ * products of queries and keys be; values up to 2^100 in magnitude (2^92 where table_width * page_rows exceeds
+ * 2^23).  KEYDIFF_ESHAPE if the prompt has more than 2^23 rows, if there are more than 2^26 query rows, or if
  * the tiles of 32 keys and 16 query rows that the prompts and the tables could hold do not fit in int32.               */
 KEYDIFF_API int keydiff_branch_workspace_bytes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, size_t *bytes);
 KEYDIFF_API int keydiff_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt,

@@ -40,6 +40,10 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int NW = 8;                 // waves of a workgroup
 constexpr int TK = 32;                // keys of a tile
+// The reference of a row's weights is put 2^LIFT above the largest logit seen and moves when one exceeds it by 2^SLACK: moving it costs a pass
+// over the outputs, and with 2^16 between the two it hardly ever does.  A weight is 2^SLACK at most, so sums over the 2^24 rows that
+// a prompt and a table of 2^23 each can hold stay below 2^127 with values of 2^100.
+constexpr float LIFT = 13.f, SLACK = 3.f;
 
 // max and sum over the four 16-lane rows of a wave, position by position (every lane gets it)
 __device__ __forceinline__ float max_over_rows(float x)
@@ -79,7 +83,7 @@ struct Plan {
 template <int D, int CB>
 struct State {
     f32x4 o[CB][D / 16];   // element i of block db: column 16 db + 4 g + i of the output
-    float l[CB], m[CB];    // weight sum of the lane's own keys; reference maximum (log2 units), the same in the four lanes of a row
+    float l[CB], m[CB];    // weight sum of the lane's own keys; reference (log2 units), the same in the four lanes of a row
     bf16x8 q[CB][D / 32];
 
     __device__ __forceinline__ void reset()
@@ -128,17 +132,17 @@ __device__ __forceinline__ void tile_logits(const State<D, CB> &st, f32x4 (&s)[C
 
 __device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // (fmaxf would quiet both first)
 
-// Weights 2^(s - m) of one block of rows.  The reference maximum m may lag by p.slack: moving it costs a pass over the outputs.  They go into the second product as two bf16 numbers, the upper half of the float and the
+// Weights 2^(s - m) of one block of rows.  They go into the second product as two bf16 numbers, the upper half of the float and the
 // rest (16 bits in all): rounded to one, their error alone would be as large as the output's own rounding.
 template <int D, int CB>
-__device__ __forceinline__ void tile_weights(State<D, CB> &st, const f32x4 (&s)[2], int cb, const BranchParams &p, bf16x8 &ph, bf16x8 &pl)
+__device__ __forceinline__ void tile_weights(State<D, CB> &st, const f32x4 (&s)[2], int cb, float scale_log2e, bf16x8 &ph, bf16x8 &pl)
 {
     const float top = max2(max2(max2(s[0][0], s[0][1]), max2(s[0][2], s[0][3])), max2(max2(s[1][0], s[1][1]), max2(s[1][2], s[1][3])));
-    if (__builtin_amdgcn_ballot_w64(top * p.scale_log2e > st.m[cb] + p.slack) != 0) {   // rare: the reference moves
-        const float mx = max_over_rows(top) * p.scale_log2e;
-        const bool need = mx > st.m[cb] + p.slack;
-        const float alpha = need ? __builtin_amdgcn_exp2f(st.m[cb] - mx) : 1.f;
-        st.m[cb] = need ? mx : st.m[cb];
+    if (__builtin_amdgcn_ballot_w64(top * scale_log2e > st.m[cb] + SLACK) != 0) {   // rare: the reference moves
+        const float mx = max_over_rows(top) * scale_log2e;
+        const bool need = mx > st.m[cb] + SLACK;
+        const float alpha = need ? __builtin_amdgcn_exp2f(st.m[cb] - (mx + LIFT)) : 1.f;
+        st.m[cb] = need ? mx + LIFT : st.m[cb];
         st.l[cb] *= alpha;
 #pragma unroll
         for (int db = 0; db < D / 16; ++db)
@@ -150,7 +154,7 @@ __device__ __forceinline__ void tile_weights(State<D, CB> &st, const f32x4 (&s)[
     u32x4 hi;
     float l[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(__builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], p.scale_log2e, nm)));
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(__builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], scale_log2e, nm)));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         l[i] = __uint_as_float(w[2 * i]) + __uint_as_float(w[2 * i + 1]);
@@ -185,7 +189,7 @@ __device__ __forceinline__ void tile_outputs(State<D, CB> &st, int db, bf16x8 va
 
 // The three in turn; `between` runs once the keys have been used, `mask(s)` sets logits that are not seen to -inf.
 template <int D, int CB, class Key, class Between, class Mask>
-__device__ __forceinline__ void tile_step(State<D, CB> &st, const unsigned char *vt, const BranchParams &p, int lane, Key key, Between between, Mask mask)
+__device__ __forceinline__ void tile_step(State<D, CB> &st, const unsigned char *vt, float scale_log2e, int lane, Key key, Between between, Mask mask)
 {
     f32x4 s[CB][2];
     tile_logits<D, CB>(st, s, key);
@@ -193,7 +197,7 @@ __device__ __forceinline__ void tile_step(State<D, CB> &st, const unsigned char 
     mask(s);
     bf16x8 ph[CB], pl[CB];
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) tile_weights<D, CB>(st, s[cb], cb, p, ph[cb], pl[cb]);
+    for (int cb = 0; cb < CB; ++cb) tile_weights<D, CB>(st, s[cb], cb, scale_log2e, ph[cb], pl[cb]);
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) tile_outputs<D, CB>(st, db, value_operand<D>(vt, lane, db), ph, pl);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -328,7 +332,7 @@ __device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned cha
         for (; t < nt; t += stride) {
             store_v<D>(vt, vr, lane);
             tile_step<D, CB>(
-                st, vt, p, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); },
+                st, vt, p.scale_log2e, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); },
                 [&]() {
                     if (t + stride < nt) {
                         load_k(t + stride);
@@ -444,7 +448,7 @@ __device__ void shared_many(const BranchParams &p, const Plan &plan, unsigned ch
                 if (!active || t >= nt) continue;   // uniform in the wave
                 const unsigned char *kt = lds_of(it);
                 tile_step<D, CB>(
-                    st, kt + TILEB, p, lane, [&](int kg, int cc) { return key_operand(kt, kg, cc); }, [&]() {},
+                    st, kt + TILEB, p.scale_log2e, lane, [&](int kg, int cc) { return key_operand(kt, kg, cc); }, [&]() {},
                     [&](f32x4 (&s)[CB][2]) {
                         if ((t + 1) * TK > p.prefix_len) hide_from<CB>(s, p.prefix_len - t * TK, g);   // uniform
                     });
@@ -507,7 +511,7 @@ __device__ void shared_many(const BranchParams &p, const Plan &plan, unsigned ch
                     const int t = tile_of(it);
                     if ((t + 1) * TK > p.prefix_len) hide_from<CB>(s, p.prefix_len - t * TK, g);   // uniform; a tile behind the last: all of it
 #pragma unroll
-                    for (int cb = 0; cb < CB; ++cb) tile_weights<D, CB>(st, s[cb], cb, p, ph[cb], pl[cb]);
+                    for (int cb = 0; cb < CB; ++cb) tile_weights<D, CB>(st, s[cb], cb, p.scale_log2e, ph[cb], pl[cb]);
                 }
             };
 #pragma unroll
@@ -702,7 +706,7 @@ __device__ void own_part(const BranchParams &p, const Plan &plan, int own_wave, 
         }
         store_v<D>(vt, vr, lane);
         tile_step<D, CB>(
-            st, vt, p, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); },
+            st, vt, p.scale_log2e, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); },
             [&]() {
                 if (at + 1 < end) {
                     load(nxt);
@@ -1052,7 +1056,7 @@ __global__ __launch_bounds__(64 * NW) void branch_short_kernel(BranchParams p)
         const uint32_t hidden = absent;
         store_v<D>(vt, vr, lane);
         tile_step<D, CB>(
-            st, vt, p, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); }, [&]() { load(t + NW); },
+            st, vt, p.scale_log2e, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); }, [&]() { load(t + NW); },
             [&](f32x4 (&sc)[CB][2]) {
                 if (t < np) {   // uniform
                     if ((t + 1) * TK > p.prefix_len) hide_from<CB>(sc, p.prefix_len - t * TK, g);

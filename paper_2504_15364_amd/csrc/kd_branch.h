@@ -85,7 +85,6 @@ struct BranchParams {
     int64_t prefix_cap;
     int32_t cus;
     float scale_log2e;
-    float slack;                          // by how much the reference maximum may lag (log2 units)
     int32_t shared_segs;                  // (prompt, head, block of rows) segments of the shared part; 0: there is none
     Divisor by_segs, by_heads, by_hkv, by_Mt, by_Bt, by_fan, by_own_blocks;   // heads: n_prefixes hkv; Mt: G Bt
 };

@@ -1313,10 +1313,6 @@ int branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32
     p.prefix_cap = prefix_cap;
     p.cus = std::max(compute_units(), 2);
     p.scale_log2e = scale_log2e;
-    // A weight is 2^slack at most: sums over as many rows as a query can see, ahead of their quotient, stay below 2^127.9 with values of
-    // 2^100.  (16, at which the reference hardly ever moves, up to 3800 rows.)
-    const double seen = (double)p.prefix_len + (double)b->table_width * b->page_rows;
-    p.slack = (float)std::min(std::max(27.9 - std::log2(seen), 0.0), 16.0);
     size_t off_ml = 0, off_plan = 0;
     const size_t need = kd::branch_workspace(p.n_seqs, n_prefixes, p.hkv, p.G, Bt, p.D, p.cus, &off_ml, &off_plan);
     if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
