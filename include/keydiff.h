@@ -301,6 +301,7 @@ KEYDIFF_API int keydiff_branch_append(const keydiff_branches_t *b, const keydiff
  *   out                 [n_seqs][n_q_heads][Bt][head_dim]; a query that sees no key (every page absent) gets zeros
  *   workspace           device, 256-byte aligned, of at least keydiff_branch_workspace_bytes; carries nothing between calls.
  *                       Calls that may overlap need workspaces of their own
+ * out and the workspace must not overlap anything that the call reads or one another, but out may be q itself where q is contiguous.
  * The prompt's rows come from memory once for all sequences that share them.  Sums and softmax statistics are kept in float.
  * Meant for few tokens a sequence: a sequence's own rows are read once for every 32 of its query rows per KV head.
  * Inputs must be finite (those of rows that a query sees, and those of rows seen by another token of the same step), and so must the

@@ -325,6 +325,7 @@ def branch_attention(q, k_pages, v_pages, table, lens, prefix=None, n_new=None, 
     alone.  (A cache with a pending eviction is finished first; ahead of a captured call, finish() it: a replay would repeat that.)
     softmax_scale <= 0: 1/sqrt(d), or the cache's.
     workspace: a uint8 tensor of at least branch_workspace_bytes that no other call in flight uses (None: allocated for the call).
+    out may be q itself where q is contiguous, and must else overlap nothing that the call reads.
     Returns out [n_seqs][Hq][Bt][d]; rows behind a sequence's n_new, and those of a sequence with lens < 0, are left as they were
     (they hold anything where out is None)."""
     handle = batch = keys = values = rows = None

@@ -1292,9 +1292,36 @@ int check_prefixes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, 
     return KEYDIFF_OK;
 }
 
+// The workspace is large enough, and what the call writes, `out` and the workspace, is nothing that it reads, but for `out` in the place of
+// the queries: a row is stored by the workgroup that has read it, or behind the launch that has.
+int check_buffers(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix,
+                  int32_t n_prefixes, int64_t prefix_cap, const void *out, const void *workspace, size_t workspace_bytes)
+{
+    const int32_t hq = b->n_q_heads, D = b->head_dim;
+    size_t off_ml = 0, off_plan = 0;
+    const size_t need = kd::branch_workspace(b->n_seqs, n_prefixes, b->n_kv_heads, hq / b->n_kv_heads, Bt, D, std::max(compute_units(), 2), &off_ml, &off_plan);
+    if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
+    const size_t rows = (size_t)b->n_seqs * hq * Bt * D * 2, pool = (size_t)b->n_pages * b->n_kv_heads * b->page_rows * D * 2;
+    const size_t prefix = k_prefix ? (size_t)n_prefixes * b->n_kv_heads * prefix_cap * D * 2 : 0;
+    const struct {
+        const void *at;
+        size_t bytes;
+    } read[] = {{b->k_pages, pool}, {b->v_pages, pool}, {k_prefix, prefix}, {v_prefix, prefix}, {b->lens, (size_t)b->n_seqs * 4},
+                {b->table, (size_t)b->n_seqs * b->table_width * 4}, {b->n_new, b->n_new ? (size_t)b->n_seqs * 4 : 0}};
+    for (const auto &r : read)
+        if (r.bytes && (overlap(out, rows, r.at, r.bytes) || overlap(workspace, need, r.at, r.bytes)))
+            return fail(KEYDIFF_EINVAL, "out and the workspace must not overlap the pages, the prefix, the table or the lengths");
+    const size_t q_bytes = 2 * span(*q, b->n_seqs, hq, Bt, D);
+    if (overlap(workspace, need, out, rows) || overlap(workspace, need, q->data, q_bytes))
+        return fail(KEYDIFF_EINVAL, "the workspace must not overlap q or out");
+    const bool in_place = out == q->data && (Bt == 1 || q->token_stride == D) && (hq == 1 || q->head_stride == (int64_t)Bt * D) &&
+                          (b->n_seqs == 1 || q->seq_stride == (int64_t)hq * Bt * D);
+    if (!in_place && overlap(out, rows, q->data, q_bytes)) return fail(KEYDIFF_EINVAL, "out must not overlap q, unless it is q, contiguous");
+    return KEYDIFF_OK;
+}
+
 int branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix,
-                     int32_t n_prefixes, int32_t prefix_len, int64_t prefix_cap, float scale_log2e, void *out, void *workspace,
-                     size_t workspace_bytes, hipStream_t s)
+                     int32_t n_prefixes, int32_t prefix_len, int64_t prefix_cap, float scale_log2e, void *out, void *workspace, hipStream_t s)
 {
     kd::BranchParams p{};
     p.q = rows_of(*q);
@@ -1314,8 +1341,7 @@ int branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32
     p.cus = std::max(compute_units(), 2);
     p.scale_log2e = scale_log2e;
     size_t off_ml = 0, off_plan = 0;
-    const size_t need = kd::branch_workspace(p.n_seqs, n_prefixes, p.hkv, p.G, Bt, p.D, p.cus, &off_ml, &off_plan);
-    if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
+    kd::branch_workspace(p.n_seqs, n_prefixes, p.hkv, p.G, Bt, p.D, p.cus, &off_ml, &off_plan);
     unsigned char *w = static_cast<unsigned char *>(workspace);
     p.part_o = reinterpret_cast<float *>(w);
     p.part_ml = reinterpret_cast<float2 *>(w + off_ml);
@@ -1442,9 +1468,11 @@ int keydiff_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *
         if (misaligned(k_prefix) || misaligned(v_prefix)) return fail(KEYDIFF_EINVAL, "tensors must be 16-byte aligned");
         if (prefix_cap < prefix_len) return fail(KEYDIFF_ESHAPE, "prefix_cap must be at least prefix_len");
     }
+    const bool shared = n_prefixes > 0 && prefix_len > 0;
+    if (int rc = check_buffers(b, q, Bt, shared ? k_prefix : nullptr, v_prefix, n_prefixes, prefix_cap, out, workspace, workspace_bytes)) return rc;
     const double scale = softmax_scale > 0.f ? (double)softmax_scale : 1.0 / std::sqrt((double)b->head_dim);
     return branch_attention(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, (float)(scale * 1.4426950408889634), out,
-                            workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+                            workspace, static_cast<hipStream_t>(stream));
 }
 
 int keydiff_cache_branch_attention(keydiff_cache_t *c, const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, void *out,
@@ -1458,16 +1486,13 @@ int keydiff_cache_branch_attention(keydiff_cache_t *c, const keydiff_branches_t 
     // (a pending eviction leaves the budget's rows)
     const int32_t rows = c->len;
     if (int rc = check_prefixes(b, Bt, c->cfg.batch, rows)) return rc;
-    size_t off_ml = 0, off_plan = 0;
-    const size_t need = kd::branch_workspace(b->n_seqs, c->cfg.batch, b->n_kv_heads, b->n_q_heads / b->n_kv_heads, Bt, b->head_dim,
-                                             std::max(compute_units(), 2), &off_ml, &off_plan);
-    if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
+    if (int rc = check_buffers(b, q, Bt, c->k, c->v, c->cfg.batch, c->L.cap, out, workspace, workspace_bytes)) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     if ((c->pending || c->shift_pending) && hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone)
         return fail(KEYDIFF_ESTATE, "the cache has a pending eviction, which every replay would repeat: keydiff_finish it ahead of the capture");
     if (int rc = finish_pending(c, s)) return rc;
-    return branch_attention(b, q, Bt, c->k, c->v, c->cfg.batch, c->len, c->L.cap, c->scale_log2e, out, workspace, workspace_bytes, s);
+    return branch_attention(b, q, Bt, c->k, c->v, c->cfg.batch, c->len, c->L.cap, c->scale_log2e, out, workspace, s);
 }
 
 int keydiff_finish(keydiff_cache_t *c, void *stream)

@@ -1,0 +1,43 @@
+"""Calls of norm_rope, branch_append and branch_attention that are refused although every argument is well formed by itself (no GPU needed:
+they are refused before anything is enqueued)."""
+import ctypes as C
+
+import pytest
+
+from paper_2504_15364_amd import binding as kd
+
+G = 1 << 30   # pointers below stand for device memory, far apart unless a case moves one
+
+
+def rows(data, seq, head, token):
+    return kd._Rows(data, seq, head, token)
+
+
+def attention(n=4, hq=8, hkv=2, d=128, Bt=2, page_rows=16, pages=10, width=4, q=None, out=8 * G, ws=12 * G, cap=100, n_new=None,
+              kp=5 * G, vp=6 * G, prompts=2, prefix_len=100, **at):
+    at = dict(dict(k_pages=1 * G, v_pages=2 * G, table=3 * G, lens=4 * G), **at)
+    b = kd._Branches(n_new=n_new, n_seqs=n, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_rows=page_rows, n_pages=pages, table_width=width, **at)
+    q = rows(7 * G, hq * Bt * d, Bt * d, d) if q is None else q
+    need = kd.branch_workspace_bytes(n, hq, hkv, d, Bt, prompts)
+    return kd.load_library().keydiff_branch_attention(C.byref(b), C.byref(q), Bt, kp, vp, prompts, prefix_len, cap, 0.0, out, ws, need, None)
+
+
+ROWS = 4 * 8 * 2 * 128 * 2             # bytes of q and out above
+POOL = 10 * 2 * 16 * 128 * 2
+PREFIX = 2 * 2 * 100 * 128 * 2
+
+
+@pytest.mark.parametrize("kw", [
+    dict(out=7 * G + 16), dict(out=7 * G - ROWS + 16),                               # out over q, shifted
+    dict(out=7 * G, q=rows(7 * G, 8 * 2 * 128, 128, 8 * 128)),                       # ... in its place, but q is laid out token by token
+    dict(out=7 * G, q=rows(7 * G, 2 * 8 * 2 * 128, 2 * 128, 128)),                   # ... but q has gaps between sequences
+    dict(out=7 * G + 8 * 2 * 128 * 2, q=rows(7 * G, 16 * 2 * 128, 2 * 128, 128)),    # ... in such a gap: within q's extent all the same
+    dict(out=1 * G + POOL - 16), dict(out=2 * G), dict(out=5 * G + PREFIX - 16), dict(out=6 * G - 16), dict(out=3 * G), dict(out=4 * G),
+    dict(out=9 * G, n_new=9 * G),
+    dict(ws=7 * G), dict(ws=8 * G), dict(ws=1 * G), dict(ws=2 * G), dict(ws=5 * G), dict(ws=6 * G), dict(ws=3 * G), dict(ws=4 * G),
+    dict(ws=8 * G + ROWS - 256), dict(ws=9 * G, n_new=9 * G),
+])
+def test_branch_attention_refuses_outputs_over_what_it_reads(kw):
+    assert attention(**kw) == kd.EINVAL
+    assert b"overlap" in kd.load_library().keydiff_last_error()
+

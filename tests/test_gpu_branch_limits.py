@@ -84,3 +84,24 @@ def test_queries_that_are_nan_give_nan(fan, N, wide):  # noqa: F811
         assert bool(out[bad, [2, 5]].isnan().all())
         out[bad, [2, 5]] = want[bad, [2, 5]]
         assert torch.equal(out, want)
+
+
+# ------------------------------------------------------------------------------------------------ where outputs may lie
+@pytest.mark.parametrize("fan,N,Bt", [(3, 100, 1), (5, 60, 9), (40, 3000, 2), (1, 9000, 1)])
+def test_outputs_in_the_place_of_the_queries_and_next_to_what_is_read(fan, N, Bt, wide):  # noqa: F811
+    hq, hkv, d = 12, 2, 64
+    g = gen(7300 + fan)
+    lens = [(5 * i) % 40 for i in range(fan)]
+    k_pages, v_pages, table = paged(lens, Bt, 16, hkv, d, g, wide=wide)
+    for s, L in enumerate(lens):
+        put_rows(k_pages, table, s, torch.randn((hkv, L + Bt, d), **g).bfloat16())
+        put_rows(v_pages, table, s, torch.randn((hkv, L + Bt, d), **g).bfloat16())
+    prefix = torch.randn((1, hkv, N, d), **g).bfloat16(), torch.randn((1, hkv, N, d), **g).bfloat16(), N
+    both = torch.randn((3, fan, hq, Bt, d), **g).bfloat16()   # the queries, between two places for outputs
+    q = both[1].clone()
+    want = kd.branch_attention(q, k_pages, v_pages, table, ints(lens), prefix=prefix)
+    for to in (0, 2, 1):
+        out = kd.branch_attention(both[1], k_pages, v_pages, table, ints(lens), prefix=prefix, out=both[to])
+        assert out.data_ptr() == both[to].data_ptr() and torch.equal(out, want)
+    with pytest.raises(kd.KeyDiffError, match="overlap"):
+        kd.branch_attention(both[0], k_pages, v_pages, table, ints(lens), prefix=prefix, out=both.view(-1)[d:d + q.numel()].view(q.shape))
