@@ -60,6 +60,9 @@ __device__ __forceinline__ float sum_over_rows(float x)
     const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+// What a piece of a row leaves for the join: its reference and weight sum.  A reference of -inf stands for a piece without a key, which the join
+// skips; one whose logits are all NaN has none either, and its NaN must not be lost.
+__device__ __forceinline__ float2 piece_ml(float m, float L) { return make_float2(L == L ? m : 0.f, L); }
 // New tokens of a sequence that holds `len` rows, and rows that are keys of theirs (its own and the new ones); 0 where it has nothing to do
 __device__ __forceinline__ int new_of(const BranchParams &p, int len, int asked) { return len < 0 ? 0 : max(0, min(asked, p.Bt)); }
 __device__ __forceinline__ int own_rows(const BranchParams &p, int len, int asked)
@@ -357,7 +360,7 @@ __device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned cha
             const int rows = min(16, M - mb * R - 16 * cb);
             join_waves<D>(outs, ml_s, rows, tid, [&](int m, int d0, f32x4 acc, float mx, float L) {
                 *reinterpret_cast<f32x4 *>(p.part_o + (slot * R + 16 * cb + m) * D + d0) = acc;
-                if (d0 == 0) p.part_ml[slot * R + 16 * cb + m] = make_float2(mx, L);
+                if (d0 == 0) p.part_ml[slot * R + 16 * cb + m] = piece_ml(mx, L);
             });
         }
         __syncthreads();   // the outputs are read before the next segment's V tiles overwrite them
@@ -544,7 +547,7 @@ __device__ void shared_many(const BranchParams &p, const Plan &plan, unsigned ch
                     const size_t r = slot * R + 32 * rw + 16 * cb + c16;
 #pragma unroll
                     for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(p.part_o + r * D + 16 * db + 4 * g) = st.o[cb][db] * inv;
-                    if (g == 0) p.part_ml[r] = make_float2(st.m[cb], L);
+                    if (g == 0) p.part_ml[r] = piece_ml(st.m[cb], L);
                 }
             }
             __syncthreads();   // every wave's copies have landed and its reads are done: the ring is free
@@ -577,7 +580,7 @@ __device__ void shared_many(const BranchParams &p, const Plan &plan, unsigned ch
                     }
                     const size_t r = slot * R + 32 * w0 + 16 * cb + m;
                     *reinterpret_cast<f32x4 *>(p.part_o + r * D + d0) = acc * (L > 0.f ? 1.f / L : 0.f);
-                    if (d0 == 0) p.part_ml[r] = make_float2(mx, L);
+                    if (d0 == 0) p.part_ml[r] = piece_ml(mx, L);
                 }
             }
             __syncthreads();   // the outputs are read before the next segment's tiles overwrite them
@@ -743,7 +746,7 @@ __device__ void own_part(const BranchParams &p, const Plan &plan, int own_wave, 
                     float *ow = part_o + (slot * R + 16 * cb + c16) * D;
 #pragma unroll
                     for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(ow + 16 * db + 4 * g) = st.o[cb][db] * inv;
-                    if (g == 0) part_ml[slot * R + 16 * cb + c16] = make_float2(st.m[cb], L);
+                    if (g == 0) part_ml[slot * R + 16 * cb + c16] = piece_ml(st.m[cb], L);
                 }
             }
             st.reset();
@@ -940,14 +943,14 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
         float top = mx;
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) top = fmaxf(top, ml[k].x);
-        // (a piece without a key has reference -inf and sum 0; one whose logits are NaN reference -inf and sum NaN, which must not be lost)
-        const float ref = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(mx - ref);
+        if (top == -INFINITY) continue;
+        const float old = mx == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mx - top);
         L *= old;
         acc *= old;
         mx = top;
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
-            const float f = ml[k].y * __builtin_amdgcn_exp2f(ml[k].x - ref);
+            const float f = ml[k].x == -INFINITY ? 0.f : ml[k].y * __builtin_amdgcn_exp2f(ml[k].x - mx);
             acc += f * o[k];
             L += f;
         }
@@ -959,12 +962,11 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
         if (group != 0) return;
         float top = -INFINITY;
         for (int k = 0; k < groups; ++k) top = fmaxf(top, ml_s[unit + k].x);
-        const float ref = top == -INFINITY ? 0.f : top;
         acc = f32x4{0.f, 0.f, 0.f, 0.f};
         L = 0.f;
         for (int k = 0; k < groups; ++k) {
             const float2 ml = ml_s[unit + k];
-            const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+            const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
             acc += f * acc_s[threadIdx.x + k * TPR];
             L += f * ml.y;
         }
