@@ -409,6 +409,10 @@ int plan_with_shift(const keydiff_cache *c, kd::StepParams &p, const kd::StepPar
     return parts;
 }
 
+// Bt positions from pos0 on lie below `end`  (no sum of the two, which may not fit)
+bool below(int64_t pos0, int32_t Bt, int64_t end) { return Bt >= 0 && end >= Bt && pos0 <= end - Bt; }
+bool positions_fit(int64_t pos0, int32_t Bt) { return pos0 >= 0 && below(pos0, Bt, 0x7fffffff); }
+
 bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 
 bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
@@ -575,8 +579,8 @@ int check_rope(const Rope &r, int head_dim, int64_t pos0, int32_t Bt)
     }
     if (!r.cos_t || !r.sin_t) return fail(KEYDIFF_EINVAL, "null rotary table");
     if (misaligned(r.cos_t) || misaligned(r.sin_t)) return fail(KEYDIFF_EINVAL, "rotary tables must be 16-byte aligned");
-    if (pos0 + Bt > r.rows) return fail(KEYDIFF_ESHAPE, "the rotary tables hold %lld positions; the block ends at %lld",
-                                        (long long)r.rows, (long long)(pos0 + Bt));
+    if (!below(pos0, Bt, r.rows)) return fail(KEYDIFF_ESHAPE, "the rotary tables hold %lld positions; the block has %d from %lld on",
+                                              (long long)r.rows, Bt, (long long)pos0);
     return KEYDIFF_OK;
 }
 
@@ -610,7 +614,7 @@ int block_step(keydiff_cache *c, const void *q, const void *k_new, const void *v
     if (misaligned(q) || misaligned(k_new) || misaligned(v_new) || misaligned(out))
         return fail(KEYDIFF_EINVAL, "tensors must be 16-byte aligned");
     if (Bt < 1 || Bt > c->cfg.block_B) return fail(KEYDIFF_ESHAPE, "Bt must lie in [1, block_B], got %d", Bt);
-    if (pos0 < 0 || pos0 + Bt > 0x7fffffffLL) return fail(KEYDIFF_ESHAPE, "positions must fit in int32");
+    if (!positions_fit(pos0, Bt)) return fail(KEYDIFF_ESHAPE, "positions must fit in int32");
     if (carry == c) return fail(KEYDIFF_EINVAL, "a cache cannot carry its own eviction");
     if (rope)
         if (int rc = check_rope(*rope, c->cfg.head_dim, pos0, Bt)) return rc;
@@ -871,7 +875,7 @@ bool layers_alike(keydiff_cache *const *caches, int n_layers, const void *const 
 {
     const keydiff_cache *c0 = caches[0];
     const keydiff_config_t &cf = c0->cfg;
-    if (Bt < 1 || Bt > cf.block_B || pos0 < 0 || pos0 + Bt > 0x7fffffffLL) return false;
+    if (Bt < 1 || Bt > cf.block_B || !positions_fit(pos0, Bt)) return false;
     const bool windowed_eviction = cf.window_W > 0 && c0->len + Bt > cf.budget_N;
     struct Span {
         uintptr_t from, to;
@@ -1116,8 +1120,8 @@ static int block_layers(keydiff_cache_t *const *caches, int32_t n_layers, const 
     // rotation depends on and the layers are shaped alike; else each step rotates its own block, so that what
     // is enqueued before an error is found is the same as ever.
     bool rotated = (forms || (rope && rope->cos_t && rope->sin_t && !misaligned(rope->cos_t) && !misaligned(rope->sin_t) &&
-                              pos0 + Bt <= rope->rows)) &&
-                   n_layers > 1 && Bt >= 1 && pos0 >= 0 && pos0 + Bt <= 0x7fffffffLL;
+                              below(pos0, Bt, rope->rows))) &&
+                   n_layers > 1 && Bt >= 1 && positions_fit(pos0, Bt);
     for (int l = 0; l < n_layers && rotated; ++l) {
         const keydiff_config_t &cf = caches[l]->cfg, &c0 = caches[0]->cfg;
         rotated = cf.batch == c0.batch && cf.n_q_heads == c0.n_q_heads && cf.n_kv_heads == c0.n_kv_heads &&
@@ -1373,10 +1377,10 @@ int keydiff_norm_rope(const keydiff_rows_t *q, const keydiff_rows_t *k, int32_t 
     if (!q_out || !k_out) return fail(KEYDIFF_EINVAL, "null pointer");
     if (misaligned(q_out) || misaligned(k_out)) return fail(KEYDIFF_EINVAL, "tensors must be 16-byte aligned");
     if (int rc = check_form(form, head_dim, true)) return rc;
-    if (pos0 < 0 || pos0 + Bt > 0x7fffffffLL) return fail(KEYDIFF_ESHAPE, "positions must fit in int32");
-    if (form->cos_table && !positions && pos0 + Bt > form->table_rows)
-        return fail(KEYDIFF_ESHAPE, "the rotary tables hold %lld positions; the block ends at %lld", (long long)form->table_rows,
-                    (long long)(pos0 + Bt));
+    if (!positions_fit(pos0, Bt)) return fail(KEYDIFF_ESHAPE, "positions must fit in int32");
+    if (form->cos_table && !positions && !below(pos0, Bt, form->table_rows))
+        return fail(KEYDIFF_ESHAPE, "the rotary tables hold %lld positions; the block has %d from %lld on", (long long)form->table_rows, Bt,
+                    (long long)pos0);
     const size_t q_in = 2 * span(*q, batch, n_q_heads, Bt, head_dim), k_in = 2 * span(*k, batch, n_kv_heads, Bt, head_dim);
     const size_t token = (size_t)batch * Bt * head_dim * 2, q_bytes = token * n_q_heads, k_bytes = token * n_kv_heads;
     if (overlap(q_out, q_bytes, q->data, q_in) || overlap(q_out, q_bytes, k->data, k_in) || overlap(k_out, k_bytes, q->data, q_in) ||

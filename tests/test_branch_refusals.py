@@ -41,3 +41,13 @@ def test_branch_attention_refuses_outputs_over_what_it_reads(kw):
     assert attention(**kw) == kd.EINVAL
     assert b"overlap" in kd.load_library().keydiff_last_error()
 
+
+@pytest.mark.parametrize("pos0", [2 ** 63 - 1, 2 ** 63 - 4, 2 ** 31 - 4, 97])
+def test_norm_rope_refuses_positions_whose_sum_with_the_tokens_does_not_fit(pos0):
+    q, k = rows(1 * G, 0, 128, 128), rows(2 * G, 0, 128, 128)
+    for tables in (3 * G, None):
+        form = kd._RowForm(q_weight=5 * G, k_weight=5 * G, norm_eps=1e-6, cos_table=tables, sin_table=tables, table_rows=100)
+        if tables is None and pos0 == 97:
+            continue   # (without tables any position will do)
+        rc = kd.load_library().keydiff_norm_rope(C.byref(q), C.byref(k), 1, 1, 1, 128, 4, pos0, None, C.byref(form), 6 * G, 7 * G, None)
+        assert rc == kd.ESHAPE and b"position" in kd.load_library().keydiff_last_error()

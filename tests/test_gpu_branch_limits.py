@@ -105,3 +105,27 @@ def test_outputs_in_the_place_of_the_queries_and_next_to_what_is_read(fan, N, Bt
         assert out.data_ptr() == both[to].data_ptr() and torch.equal(out, want)
     with pytest.raises(kd.KeyDiffError, match="overlap"):
         kd.branch_attention(both[0], k_pages, v_pages, table, ints(lens), prefix=prefix, out=both.view(-1)[d:d + q.numel()].view(q.shape))
+
+
+# ------------------------------------------------------------------------------------------------ positions at the end of 64 bits
+def test_blocks_whose_positions_do_not_fit_are_refused():
+    hq, hkv, d, B = 4, 2, 64, 16
+    g = gen(7400)
+    caches = [kd.KeyDiffCache(kd.KeyDiffConfig(1, hq, hkv, d, 32, B)) for _ in range(2)]
+    q, k, v = (torch.randn((1, h, B, d), **g).bfloat16() for h in (hq, hkv, hkv))
+    table, w = torch.ones((100, d // 2), device="cuda"), torch.ones((d,), dtype=torch.bfloat16, device="cuda")
+    for pos0 in (2 ** 63 - 1, 2 ** 63 - B, 2 ** 31 - B, -1, 85):
+        calls = [lambda: caches[0].prefill_block_rope(q, k, v, pos0, table, table),
+                 lambda: caches[0].prefill_block_norm_rope(q, k, v, pos0, table, table, w, w),
+                 lambda: kd.prefill_block_layers(caches, [q, q], [k, k], [v, v], pos0, rope=(table, table)),
+                 lambda: kd.prefill_block_layers(caches, [q, q], [k, k], [v, v], pos0, rope=(table, table), norm=([w, w], [w, w], 1e-6))]
+        if pos0 != 85:   # (85: the block ends behind the tables)
+            calls += [lambda: caches[0].prefill_block(q, k, v, pos0), lambda: kd.prefill_block_layers(caches, [q, q], [k, k], [v, v], pos0),
+                      lambda: caches[0].prefill_block_norm_rope(q, k, v, pos0, None, None, w, w)]
+        for call in calls:
+            with pytest.raises(kd.KeyDiffError) as e:
+                call()
+            assert e.value.code == -2
+    for c in caches:
+        assert c.len == 0 and c.status() == 0
+        c.close()
