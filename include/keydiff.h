@@ -297,7 +297,7 @@ KEYDIFF_API int keydiff_branch_append(const keydiff_branches_t *b, const keydiff
  * s / (n_seqs / n_prefixes) and the sequence's own rows 0 .. lens[s] + j.
  *   k_prefix, v_prefix  device, bf16 [n_prefixes][n_kv_heads][prefix_cap][head_dim]; null with n_prefixes 0: own rows alone
  *   n_prefixes          must divide n_seqs; sequences of one prompt follow one another
- *   softmax_scale       <= 0 selects 1/sqrt(head_dim)
+ *   softmax_scale       <= 0 selects 1/sqrt(head_dim); EINVAL if it is not finite
  *   out                 [n_seqs][n_q_heads][Bt][head_dim]; a query that sees no key (every page absent) gets zeros
  *   workspace           device, 256-byte aligned, of at least keydiff_branch_workspace_bytes; carries nothing between calls.
  *                       Calls that may overlap need workspaces of their own

@@ -277,7 +277,7 @@ PyObject *branch_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     }
     const double scale = PyFloat_AsDouble(a[11]);
     if (PyErr_Occurred()) throw python_error();
-    if (cached && scale > 0) throw Refused("softmax_scale is the cache's");
+    if (cached && !(scale <= 0)) throw Refused("softmax_scale is the cache's");
     on.on_gpu();
     const c10::DeviceGuard guard(on.device);
     size_t need = 0;

@@ -14,12 +14,12 @@ def rows(data, seq, head, token):
 
 
 def attention(n=4, hq=8, hkv=2, d=128, Bt=2, page_rows=16, pages=10, width=4, q=None, out=8 * G, ws=12 * G, cap=100, n_new=None,
-              kp=5 * G, vp=6 * G, prompts=2, prefix_len=100, **at):
+              kp=5 * G, vp=6 * G, prompts=2, prefix_len=100, scale=0.0, **at):
     at = dict(dict(k_pages=1 * G, v_pages=2 * G, table=3 * G, lens=4 * G), **at)
     b = kd._Branches(n_new=n_new, n_seqs=n, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_rows=page_rows, n_pages=pages, table_width=width, **at)
     q = rows(7 * G, hq * Bt * d, Bt * d, d) if q is None else q
     need = kd.branch_workspace_bytes(n, hq, hkv, d, Bt, prompts)
-    return kd.load_library().keydiff_branch_attention(C.byref(b), C.byref(q), Bt, kp, vp, prompts, prefix_len, cap, 0.0, out, ws, need, None)
+    return kd.load_library().keydiff_branch_attention(C.byref(b), C.byref(q), Bt, kp, vp, prompts, prefix_len, cap, scale, out, ws, need, None)
 
 
 ROWS = 4 * 8 * 2 * 128 * 2             # bytes of q and out above
@@ -51,3 +51,9 @@ def test_norm_rope_refuses_positions_whose_sum_with_the_tokens_does_not_fit(pos0
             continue   # (without tables any position will do)
         rc = kd.load_library().keydiff_norm_rope(C.byref(q), C.byref(k), 1, 1, 1, 128, 4, pos0, None, C.byref(form), 6 * G, 7 * G, None)
         assert rc == kd.ESHAPE and b"position" in kd.load_library().keydiff_last_error()
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), 1e39])   # (1e39: infinite as a float)
+def test_branch_attention_refuses_a_scale_that_is_no_number(scale):
+    assert attention(scale=C.c_float(scale)) == kd.EINVAL
+    assert b"softmax_scale" in kd.load_library().keydiff_last_error()
