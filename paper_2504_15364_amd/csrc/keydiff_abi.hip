@@ -1355,10 +1355,16 @@ int branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32
     return KEYDIFF_OK;
 }
 
+int check_query_rows(const keydiff_branches_t *b, int32_t Bt)
+{
+    if ((int64_t)b->n_seqs * Bt * b->n_q_heads > (1 << 26)) return fail(KEYDIFF_ESHAPE, "sequences * Bt * n_q_heads must not exceed 2^26");
+    return KEYDIFF_OK;
+}
+
 int check_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *out, const void *workspace)
 {
     if (int rc = check_branches(b, Bt)) return rc;
-    if ((int64_t)b->n_seqs * Bt * b->n_q_heads > (1 << 26)) return fail(KEYDIFF_ESHAPE, "sequences * Bt * n_q_heads must not exceed 2^26");
+    if (int rc = check_query_rows(b, Bt)) return rc;
     if (int rc = check_rows(q, "q")) return rc;
     if (!out || !workspace) return fail(KEYDIFF_EINVAL, "null pointer");
     if (misaligned(out)) return fail(KEYDIFF_EINVAL, "out must be 16-byte aligned");
@@ -1454,6 +1460,7 @@ int keydiff_branch_workspace_bytes(const keydiff_branches_t *b, int32_t Bt, int3
 {
     if (!b || !bytes) return fail(KEYDIFF_EINVAL, "null pointer");
     if (int rc = check_heads(b->n_seqs, b->n_q_heads, b->n_kv_heads, b->head_dim, Bt)) return rc;
+    if (int rc = check_query_rows(b, Bt)) return rc;
     if (n_prefixes < 0 || (n_prefixes > 0 && b->n_seqs % n_prefixes))
         return fail(KEYDIFF_ESHAPE, "n_prefixes must divide the %d sequences, got %d", b->n_seqs, n_prefixes);
     size_t off_ml = 0, off_plan = 0;

@@ -57,3 +57,11 @@ def test_norm_rope_refuses_positions_whose_sum_with_the_tokens_does_not_fit(pos0
 def test_branch_attention_refuses_a_scale_that_is_no_number(scale):
     assert attention(scale=C.c_float(scale)) == kd.EINVAL
     assert b"softmax_scale" in kd.load_library().keydiff_last_error()
+
+
+def test_no_workspace_for_calls_that_are_refused():
+    # (2^27 query rows: the wrapper would allocate its gigabytes ahead of the refusal)
+    assert kd.branch_workspace_bytes(1 << 23, 8, 2, 128, 1, 0) > 0
+    with pytest.raises(kd.KeyDiffError) as e:
+        kd.branch_workspace_bytes(1 << 24, 8, 2, 128, 1, 0)
+    assert e.value.code == kd.ESHAPE
