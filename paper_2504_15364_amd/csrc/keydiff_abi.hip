@@ -7,7 +7,6 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
-#include <limits>
 #include <memory>
 #include <new>
 #include <vector>
@@ -1474,7 +1473,7 @@ int keydiff_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *
                              void *workspace, size_t workspace_bytes, void *stream)
 {
     if (int rc = check_branch_attention(b, q, Bt, out, workspace)) return rc;
-    if (!(softmax_scale <= std::numeric_limits<float>::max())) return fail(KEYDIFF_EINVAL, "softmax_scale must be finite");
+    if (!std::isfinite(softmax_scale)) return fail(KEYDIFF_EINVAL, "softmax_scale must be finite");
     if (int rc = check_prefixes(b, Bt, n_prefixes, prefix_len)) return rc;
     if (n_prefixes > 0 && prefix_len > 0) {
         if (!k_prefix || !v_prefix) return fail(KEYDIFF_EINVAL, "null pointer: prefix rows");

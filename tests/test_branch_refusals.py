@@ -53,7 +53,7 @@ def test_norm_rope_refuses_positions_whose_sum_with_the_tokens_does_not_fit(pos0
         assert rc == kd.ESHAPE and b"position" in kd.load_library().keydiff_last_error()
 
 
-@pytest.mark.parametrize("scale", [float("nan"), float("inf"), 1e39])   # (1e39: infinite as a float)
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), float("-inf"), 1e39])   # (1e39: infinite as a float)
 def test_branch_attention_refuses_a_scale_that_is_no_number(scale):
     assert attention(scale=C.c_float(scale)) == kd.EINVAL
     assert b"softmax_scale" in kd.load_library().keydiff_last_error()
