@@ -278,6 +278,8 @@ def _call(name, device, stream, *args):
         r = f(*args)
     else:
         import torch
+        if hasattr(stream, "cuda_stream") and stream.device != device:   # (the call would run on the current stream of the tensors' device)
+            raise ValueError(f"the stream belongs to {stream.device}, the tensors live on {device}")
         with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device)):
             r = f(*args)
     if type(r) is int:

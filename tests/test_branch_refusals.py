@@ -65,3 +65,17 @@ def test_no_workspace_for_calls_that_are_refused():
     with pytest.raises(kd.KeyDiffError) as e:
         kd.branch_workspace_bytes(1 << 24, 8, 2, 128, 1, 0)
     assert e.value.code == kd.ESHAPE
+
+
+def test_a_stream_of_another_device_is_refused():
+    torch = pytest.importorskip("torch")
+
+    class Elsewhere:
+        cuda_stream, device = 64, torch.device("cuda:1")
+
+    x = torch.zeros((1, 2, 1, 64), dtype=torch.bfloat16)
+    pages, table = torch.zeros((1, 2, 8, 64), dtype=torch.bfloat16), torch.zeros((1, 1), dtype=torch.int32)
+    for call in (lambda: kd.norm_rope(x, x, stream=Elsewhere()), lambda: kd.branch_append(x, x, x, pages, pages, table, table[0], stream=Elsewhere()),
+                 lambda: kd.branch_attention(x, pages, pages, table, table[0], stream=Elsewhere())):
+        with pytest.raises(ValueError, match="stream belongs to cuda:1"):
+            call()
