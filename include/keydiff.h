@@ -233,13 +233,20 @@ KEYDIFF_API int keydiff_prefill_block_layers_rope(keydiff_cache_t *const *caches
  *   q_weight, k_weight        device, bf16 [head_dim] for all heads (stride 0) or [heads][head_dim] with a stride in elements, a
  *                             multiple of 8; 16-byte aligned.  Both null: no norm
  *   cos_table, sin_table      as above.  Both null: no rotation (table_rows is not used then)
+ *   status                    device int32, nullable, not used by block steps: keydiff_norm_rope and keydiff_branch_append set bits of it, and
+ *                             clear none, where they leave a token out: KEYDIFF_LEFT_OUT_POSITION, its position lies outside the
+ *                             tables; KEYDIFF_LEFT_OUT_ROW, its row lies outside the table or on a page outside the pool.  (Tokens behind
+ *                             n_new and those of sequences not in use are not left out.)
  * A step needs one of the two at least.  `_layers`: `form` is an array, one entry per layer.                         */
+#define KEYDIFF_LEFT_OUT_POSITION 1
+#define KEYDIFF_LEFT_OUT_ROW 2
 typedef struct {
     const void *q_weight, *k_weight;
     int64_t q_weight_stride, k_weight_stride;
     float norm_eps;
     const float *cos_table, *sin_table;
     int64_t table_rows;
+    int32_t *status;
 } keydiff_row_form_t;
 KEYDIFF_API int keydiff_prefill_block_norm_rope(keydiff_cache_t *cache, const void *q, const void *k_new, const void *v_new,
                                int32_t Bt, int64_t pos0, const keydiff_row_form_t *form, void *out, float *scores_out,
@@ -288,7 +295,8 @@ typedef struct {
  * of its prompt).  `form` (nullable: rows are taken as they are) norms and rotates queries and keys on the way;
  * the queries are written to q_out [n_seqs][n_q_heads][Bt][head_dim] for keydiff_branch_attention (q and q_out null:
  * keys and values only).  lens is not changed: all layers of a step read the same lengths, and the caller advances them
- * behind the last one.  A token at a position outside the tables is left out.                                         */
+ * behind the last one.  A token at a position outside the tables is left out; keydiff_branch_attention, which knows no positions,
+ * counts its row as one of the sequence's all the same, whatever lies there: form->status tells.                       */
 KEYDIFF_API int keydiff_branch_append(const keydiff_branches_t *b, const keydiff_rows_t *q, const keydiff_rows_t *k,
                           const keydiff_rows_t *v, int32_t Bt, const int32_t *pos0, const keydiff_row_form_t *form,
                           void *q_out, void *stream);

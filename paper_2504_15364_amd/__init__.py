@@ -10,6 +10,8 @@ from .binding import (  # noqa: F401
     KERNEL_NAMES,
     LAYOUT_FILL,
     LAYOUT_ORDERED,
+    LEFT_OUT_POSITION,
+    LEFT_OUT_ROW,
     KeyDiffCache,
     KeyDiffConfig,
     KeyDiffError,

@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libkeydiff.so")
 OK, EINVAL, ESHAPE, ESTATE, EHIP = 0, -1, -2, -3, -4
 ANCHOR_MEAN_KEY, ANCHOR_MEAN_UNIT_KEY = 0, 1
 LAYOUT_ORDERED, LAYOUT_FILL = 0, 1
+LEFT_OUT_POSITION, LEFT_OUT_ROW = 1, 2   # bits that norm_rope and branch_append set in `status`
 KERNEL_NAMES = ("step_main", "step_score", "step_post", "compact_ordered", "aux", "event_pair", "select_alone")
 
 EXPORTS = (
@@ -44,7 +45,7 @@ class _Config(C.Structure):
 class _RowForm(C.Structure):
     _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("q_weight_stride", C.c_int64),
                 ("k_weight_stride", C.c_int64), ("norm_eps", C.c_float), ("cos_table", C.c_void_p),
-                ("sin_table", C.c_void_p), ("table_rows", C.c_int64)]
+                ("sin_table", C.c_void_p), ("table_rows", C.c_int64), ("status", C.c_void_p)]
 
 
 class _Rows(C.Structure):
@@ -288,25 +289,30 @@ def _call(name, device, stream, *args):
 
 
 def norm_rope(q, k, cos=None, sin=None, pos0: int = 0, positions=None, q_weight=None, k_weight=None, norm_eps: float = 1e-6,
-              q_out=None, k_out=None, stream=None):
+              q_out=None, k_out=None, stream=None, status=None):
     """Root mean square norms of the queries and keys of each head (bf16 weights [d] or [heads][d]; None: no norm) and the rotary
     position embedding (float32 tables [positions][d / 2]; None: no rotation) in one pass.
     q [batch][Hq][T][d], k [batch][Hkv][T][d] bf16, any strides with a contiguous last dimension; token j is at position pos0 + j or
-    at positions[b][j] (int32 [batch][T]; a token outside the tables is left out).  Returns contiguous (q_out, k_out)."""
-    return _call("norm_rope", q.device, stream, q, k, cos, sin, pos0, positions, q_weight, k_weight, norm_eps, q_out, k_out)
+    at positions[b][j] (int32 [batch][T]; a token outside the tables is left out, its rows of the outputs stay as they are).
+    status: an int32 tensor of one element; LEFT_OUT_POSITION is set in it, and nothing cleared, if a token was left out.
+    Returns contiguous (q_out, k_out)."""
+    return _call("norm_rope", q.device, stream, q, k, cos, sin, pos0, positions, q_weight, k_weight, norm_eps, q_out, k_out, status)
 
 
 def branch_append(q, k_new, v_new, k_pages, v_pages, table, lens, n_new=None, pos0=None, cos=None, sin=None, q_weight=None,
-                  k_weight=None, norm_eps: float = 1e-6, q_out=None, stream=None):
+                  k_weight=None, norm_eps: float = 1e-6, q_out=None, stream=None, status=None):
     """New tokens of sequences that continue prompts: norms and rotation of q and k_new as in norm_rope, keys and values into the
     sequences' pages behind the lens[s] rows they hold, at positions pos0[s] + lens[s] + j (pos0: int32 [n_seqs], the length of the
     sequence's prompt; None: zeros).  lens is not changed.
     q [n_seqs][Hq][Bt][d] (None: keys and values only), k_new, v_new [n_seqs][Hkv][Bt][d]; k_pages, v_pages
     [pages][Hkv][page_rows][d]; table int32 [n_seqs][width]; n_new int32 [n_seqs] (None: all Bt).  Returns the contiguous queries
-    for branch_attention; tokens that are left out (behind a sequence's n_new, lens < 0) keep their rows of q_out, which
-    hold anything if it is None."""
+    for branch_attention; tokens that are not taken (behind a sequence's n_new, lens < 0) keep their rows of q_out, which
+    hold anything if it is None.
+    A token is left out as well where its position lies outside the tables (branch_attention counts its row all the same), its row
+    outside the table or its page outside the pool.  status: an int32 tensor of one element, in which such tokens set
+    LEFT_OUT_POSITION or LEFT_OUT_ROW, and nothing is cleared."""
     return _call("branch_append", k_new.device, stream, q, k_new, v_new, k_pages, v_pages, table, lens, n_new, pos0, cos, sin, q_weight,
-                 k_weight, norm_eps, q_out)
+                 k_weight, norm_eps, q_out, status)
 
 
 def branch_workspace_bytes(n_seqs, n_q_heads, n_kv_heads, head_dim, Bt=1, n_prefixes=0):

@@ -182,11 +182,11 @@ PyObject *given_or(PyObject *o, at::Tensor &made)
     }                                                     \
     END_HANDLE_TH_ERRORS
 
-// q, k, cos, sin, pos0, positions, q_weight, k_weight, norm_eps, q_out, k_out
+// q, k, cos, sin, pos0, positions, q_weight, k_weight, norm_eps, q_out, k_out, status
 PyObject *norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     KD_TRY
-    arguments(n, 11);
+    arguments(n, 12);
     const at::Tensor &q = tensor_of(a[0], "q"), &k = tensor_of(a[1], "k");
     four("q", q);
     four("k", k);
@@ -194,7 +194,8 @@ PyObject *norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
     const Checked on{q.device()};
     const keydiff_rows_t rq = on.rows("q", q, b, hq, T, d), rk = on.rows("k", k, b, hkv, T, d);
     const int32_t *positions = static_cast<const int32_t *>(on.dense_or_null("positions", a[5], {b, T}, at::kInt));
-    const keydiff_row_form_t form = on.form(hq, hkv, d, a[2], a[3], a[6], a[7], a[8]);
+    keydiff_row_form_t form = on.form(hq, hkv, d, a[2], a[3], a[6], a[7], a[8]);
+    form.status = static_cast<int32_t *>(on.dense_or_null("status", a[11], {1}, at::kInt));
     void *q_out = on.dense_or_null("q_out", a[9], {b, hq, T, d}, at::kBFloat16), *k_out = on.dense_or_null("k_out", a[10], {b, hkv, T, d}, at::kBFloat16);
     const int64_t pos0 = whole(a[4]);
     on.on_gpu();
@@ -212,11 +213,11 @@ PyObject *norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n)
     KD_END
 }
 
-// q, k_new, v_new, k_pages, v_pages, table, lens, n_new, pos0, cos, sin, q_weight, k_weight, norm_eps, q_out
+// q, k_new, v_new, k_pages, v_pages, table, lens, n_new, pos0, cos, sin, q_weight, k_weight, norm_eps, q_out, status
 PyObject *branch_append(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
     KD_TRY
-    arguments(n_args, 15);
+    arguments(n_args, 16);
     const at::Tensor &k = tensor_of(a[1], "k_new"), &v = tensor_of(a[2], "v_new");
     four("k_new", k);
     const int64_t n = k.size(0), hkv = k.size(1), Bt = k.size(2), d = k.size(3);
@@ -236,7 +237,8 @@ PyObject *branch_append(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     }
     const keydiff_branches_t b = on.branches(n, hq, hkv, d, a[3], a[4], a[5], a[6], a[7]);
     const int32_t *pos0 = static_cast<const int32_t *>(on.dense_or_null("pos0", a[8], {n}, at::kInt));
-    const keydiff_row_form_t form = on.form(hq, hkv, d, a[9], a[10], a[11], a[12], a[13]);
+    keydiff_row_form_t form = on.form(hq, hkv, d, a[9], a[10], a[11], a[12], a[13]);
+    form.status = static_cast<int32_t *>(on.dense_or_null("status", a[15], {1}, at::kInt));
     on.on_gpu();
     const c10::DeviceGuard guard(on.device);
     at::Tensor q_new;

@@ -35,8 +35,10 @@ struct NormRopeParams {
     const int32_t *positions;    // norm_rope: nullable [n_seqs][Bt]; append: [n_seqs], the position of a sequence's first own row
     int64_t pos0;
     Pages pages;                 // append only
+    int32_t *status;             // nullable: bits of tokens that were left out
     int32_t n_seqs, hq, hkv, Bt, D;
 };
+constexpr int LEFT_OUT_POSITION = 1, LEFT_OUT_ROW = 2;
 hipError_t launch_norm_rope(const NormRopeParams &p, hipStream_t s);
 hipError_t launch_branch_append(const NormRopeParams &p, hipStream_t s);
 

@@ -538,6 +538,7 @@ int check_form(const keydiff_row_form_t *f, int head_dim, bool needed)
 {
     if (!f) return fail(KEYDIFF_EINVAL, "null pointer");
     const bool norm = f->q_weight || f->k_weight, rope = f->cos_table || f->sin_table;
+    if (reinterpret_cast<uintptr_t>(f->status) & 3) return fail(KEYDIFF_EINVAL, "status must be 4-byte aligned");
     if (needed && !norm && !rope) return fail(KEYDIFF_EINVAL, "neither norm weights nor rotary tables");
     if (norm) {
         if (!f->q_weight || !f->k_weight) return fail(KEYDIFF_EINVAL, "null norm weight");
@@ -1399,6 +1400,7 @@ int keydiff_norm_rope(const keydiff_rows_t *q, const keydiff_rows_t *k, int32_t 
     p.k_out = static_cast<uint16_t *>(k_out);
     p.form = row_form(form);
     p.positions = positions;
+    p.status = form->status;
     p.pos0 = pos0;
     p.n_seqs = batch;
     p.hq = n_q_heads;
@@ -1444,6 +1446,7 @@ int keydiff_branch_append(const keydiff_branches_t *b, const keydiff_rows_t *q, 
     p.v = rows_of(*v);
     p.q_out = static_cast<uint16_t *>(q_out);
     p.form = row_form(form);
+    p.status = form ? form->status : nullptr;
     p.positions = pos0;
     p.pages = pages_of(b);
     p.n_seqs = b->n_seqs;

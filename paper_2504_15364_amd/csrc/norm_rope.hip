@@ -115,13 +115,16 @@ __device__ __forceinline__ Place place_of(int tg_shift, int chunk)
 
 // APPEND: keys and values go to the rows behind those that the token's sequence holds, in its pages, queries to q_out.  A token that
 // has no place -- its sequence not in use, behind the sequence's new tokens, its position not in the tables, its row or page not in
-// the table or the pool -- is left out: nothing of it is written.
+// the table or the pool -- is left out: nothing of it is written, and of the last two the caller's status word tells.
 template <int D, bool APPEND>
 __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeParams p, int tg_shift, int chunk)
 {
     const Place at = place_of<D>(tg_shift, chunk);
     if (at.token >= p.n_seqs * p.Bt) return;
     const int seq = at.token / p.Bt, j = at.token % p.Bt;
+    auto left_out = [&](int bit) {   // (one lane a token)
+        if (p.status && at.unit == 0 && at.first == 0) atomicOr(p.status, bit);
+    };
     int64_t position;
     size_t page_at = 0;   // APPEND: element offset of head 0's row in the pools
     if constexpr (APPEND) {
@@ -129,9 +132,9 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeParams p, int tg
         if (len < 0 || (p.pages.n_new && j >= p.pages.n_new[seq])) return;
         const int64_t row = (int64_t)len + j;
         const int64_t at_page = row >> p.pages.page_shift;
-        if (at_page >= p.pages.width) return;
+        if (at_page >= p.pages.width) return left_out(LEFT_OUT_ROW);
         const int page = p.pages.table[(size_t)seq * p.pages.width + at_page];
-        if ((uint32_t)page >= (uint32_t)p.pages.n_pages) return;
+        if ((uint32_t)page >= (uint32_t)p.pages.n_pages) return left_out(LEFT_OUT_ROW);
         page_at = ((((size_t)page * p.hkv) << p.pages.page_shift) + (size_t)(row & ((1 << p.pages.page_shift) - 1))) * D;
         position = (p.positions ? (int64_t)p.positions[seq] : 0) + row;
     } else {
@@ -142,7 +145,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeParams p, int tg
 #pragma unroll
     for (int i = 0; i < 2; ++i) c[i] = s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (rotate) {
-        if (position < 0 || position >= p.form.table_rows) return;
+        if (position < 0 || position >= p.form.table_rows) return left_out(LEFT_OUT_POSITION);
         load_angles<D>(p.form, position, at.unit, c, s);
     }
     const int heads = p.hq + p.hkv + (APPEND ? p.hkv : 0);

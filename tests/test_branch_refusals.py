@@ -79,3 +79,18 @@ def test_a_stream_of_another_device_is_refused():
                  lambda: kd.branch_attention(x, pages, pages, table, table[0], stream=Elsewhere())):
         with pytest.raises(ValueError, match="stream belongs to cuda:1"):
             call()
+
+
+def test_status_words_that_do_not_fit_are_refused():
+    torch = pytest.importorskip("torch")
+    q, k = rows(1 * G, 0, 128, 128), rows(2 * G, 0, 128, 128)
+    form = kd._RowForm(q_weight=5 * G, k_weight=5 * G, norm_eps=1e-6, status=8 * G + 2)
+    assert kd.load_library().keydiff_norm_rope(C.byref(q), C.byref(k), 1, 1, 1, 128, 4, 0, None, C.byref(form), 6 * G, 7 * G, None) == kd.EINVAL
+    assert b"status" in kd.load_library().keydiff_last_error()
+    x = torch.zeros((1, 2, 1, 64), dtype=torch.bfloat16)
+    pages, table = torch.zeros((1, 2, 8, 64), dtype=torch.bfloat16), torch.zeros((1, 1), dtype=torch.int32)
+    for status in (torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.int64), torch.tensor(0, dtype=torch.int32), 3):
+        with pytest.raises(ValueError, match="status"):
+            kd.norm_rope(x, x, q_weight=x[0, 0, 0], k_weight=x[0, 0, 0], status=status)
+        with pytest.raises(ValueError, match="status"):
+            kd.branch_append(x, x, x, pages, pages, table, table[0], status=status)

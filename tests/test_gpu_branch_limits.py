@@ -129,3 +129,46 @@ def test_blocks_whose_positions_do_not_fit_are_refused():
     for c in caches:
         assert c.len == 0 and c.status() == 0
         c.close()
+
+
+# ------------------------------------------------------------------------------------------------ tokens that are left out
+@pytest.mark.parametrize("Bt", [1, 3, 70])
+def test_status_tells_of_tokens_that_were_left_out(Bt):
+    hq, hkv, d, page, n = 6, 2, 64, 16, 5
+    g = gen(7500 + Bt)
+    x = torch.randn((n, hq + 2 * hkv, Bt, d), **g).bfloat16()
+    q, k, v = x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:]
+    table = torch.ones((200, d // 2), device="cuda")
+    status = ints([0])
+
+    def positions(at):
+        status.zero_()
+        kd.norm_rope(q, k, table, table, positions=ints([[p + j for j in range(Bt)] for p in at]), status=status)
+        return status.item()
+
+    assert positions([0, 1, 2, 3, 200 - Bt]) == 0
+    assert positions([0, 1, 201 - Bt, 3, 4]) == kd.LEFT_OUT_POSITION
+    assert positions([-1, 1, 2, 3, 4]) == kd.LEFT_OUT_POSITION
+    kd.norm_rope(q, k, table, table, status=status)
+    assert status.item() == kd.LEFT_OUT_POSITION   # nothing is cleared
+
+    k_pages, v_pages, pages = paged([100] * n, Bt, page, hkv, d, g)
+    width = pages.shape[1]
+
+    def append(lens, pos0=None, n_new=None, pages=pages, rope=True):
+        status.zero_()
+        kd.branch_append(q, k, v, k_pages, v_pages, pages, ints(lens), n_new=n_new, pos0=pos0, cos=table if rope else None,
+                         sin=table if rope else None, status=status)
+        return status.item()
+
+    lens = [100, 0, 50, 7, 30]
+    assert append(lens) == 0 and append(lens, rope=False) == 0
+    assert append(lens, pos0=ints([0, 0, 0, 194 - Bt, 0])) == kd.LEFT_OUT_POSITION       # its last token at 200
+    assert append(lens, pos0=ints([0, 0, 0, 193 - Bt, 0])) == 0
+    assert append([100, 0, 50, -1, 30], pos0=ints([0, 0, 0, 10 ** 6, 0])) == 0                                # not in use
+    assert append(lens, pos0=ints([0, 0, 0, 10 ** 6, 0]), n_new=ints([Bt, Bt, Bt, 0, Bt])) == 0               # takes none
+    assert append([100, 0, width * page + 1 - Bt, 7, 30], rope=False) == kd.LEFT_OUT_ROW                       # behind the table's last row
+    gone = pages.clone()
+    gone[1, 0] = k_pages.shape[0]
+    assert append(lens, pages=gone, rope=False) == kd.LEFT_OUT_ROW
+    assert append(lens, pages=gone, pos0=ints([0, 0, 0, 10 ** 6, 0])) == kd.LEFT_OUT_ROW | kd.LEFT_OUT_POSITION
