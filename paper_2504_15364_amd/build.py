@@ -1,9 +1,12 @@
 """Build libkeydiff.so (gfx950 only) in-tree with hipcc."""
 from __future__ import annotations
 
+import importlib.util
 import os
+import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -35,10 +38,20 @@ def scratch_users(remarks):
     return found
 
 
+def calls_lack():
+    """What build_calls needs and does not find (None: nothing)."""
+    if importlib.util.find_spec("torch") is None:
+        return "torch is not installed"
+    if shutil.which("g++") is None:
+        return "there is no g++"
+    include = sysconfig.get_paths()["include"]
+    if not os.path.exists(os.path.join(include, "Python.h")):
+        return f"there is no Python.h in {include}"
+    return None
+
+
 def build_calls() -> str:
     """The Python side of the calls beside the block step (_calls.so): a host compiler and torch's headers, no GPU code."""
-    import sysconfig
-
     import torch
     from torch.utils import cpp_extension
     lib_dir = cpp_extension.library_paths()[0]
@@ -85,7 +98,13 @@ def build(verbose: bool = False, timeline: bool = False) -> str:
     link = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", lib, *objs]
     subprocess.run(link, check=True)
     if not timeline:
-        build_calls()
+        lack = calls_lack()
+        if lack is None:
+            build_calls()
+        else:   # the C ABI needs none of it; the Python calls say that they are not built
+            print(f"warning: {os.path.basename(CALLS)} is not built: {lack}", file=sys.stderr)
+            if os.path.exists(CALLS):
+                os.remove(CALLS)   # (of an earlier build)
     return lib
 
 
