@@ -801,7 +801,9 @@ template <int D, int RS, int RO>
 __device__ __forceinline__ Plan make_plan(const BranchParams &p, int units, int wgs, int rows0, int lane)
 {
     using P = Prices<D, RS, RO>;
-    auto up = [](float x, float y) { return __builtin_ceilf(x * __builtin_amdgcn_rcpf(y)); };   // (a price may be off by the quotient's last bit)
+    // (An exact quotient that the reciprocal makes a bit too large counts one too many, which the host's prices below do not.  With exact counts
+    // 59 sizes took 1.003 of the time on average, from 0.995 to 1.026: the choice hardly ever changes.)
+    auto up = [](float x, float y) { return __builtin_ceilf(x * __builtin_amdgcn_rcpf(y)); };
     Plan plan;
     int own = (rows0 + TK - 1) / TK;
     int used = __popcll(__builtin_amdgcn_ballot_w64(own > 0));   // sequences with own rows
