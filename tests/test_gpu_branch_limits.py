@@ -3,7 +3,7 @@ test_gpu_branch.py, whose derivation does not depend on the sizes below."""
 import pytest
 
 import paper_2504_15364_amd as kd
-from test_gpu_branch import attention_reference, close, gen, ints, paged, put_rows, rows_of, wide  # noqa: F401
+from test_gpu_branch import CASES, attention_reference, close, gen, ints, paged, put_rows, rows_of, tables, wide  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -172,3 +172,106 @@ def test_status_tells_of_tokens_that_were_left_out(Bt):
     gone[1, 0] = k_pages.shape[0]
     assert append(lens, pages=gone, rope=False) == kd.LEFT_OUT_ROW
     assert append(lens, pages=gone, pos0=ints([0, 0, 0, 10 ** 6, 0])) == kd.LEFT_OUT_ROW | kd.LEFT_OUT_POSITION
+
+
+# ------------------------------------------------------------------------------------------------ pieces of many tokens
+@pytest.mark.parametrize("hq,hkv,d,N,page,Bt,lens,n_new", [
+    (8, 2, 128, 500, 16, 130, [0, 5, 700], [130, 7, 129]),
+    (6, 2, 64, 0, 32, 300, [0, 31, 1000, 64], [300, 1, 33, 0]),
+    (7, 1, 128, 3000, 64, 41, [90, 0], None),
+])
+def test_pieces_of_many_tokens(hq, hkv, d, N, page, Bt, lens, n_new):
+    g = gen(7600 + Bt)
+    n = len(lens)
+    k_pages, v_pages, table = paged(lens, Bt, page, hkv, d, g)
+    x = torch.randn((n, Bt, hq + 2 * hkv, d), **g).bfloat16().transpose(1, 2)
+    for s, L in enumerate(lens):
+        if L:
+            put_rows(k_pages, table, s, torch.randn((hkv, L, d), **g).bfloat16())
+            put_rows(v_pages, table, s, torch.randn((hkv, L, d), **g).bfloat16())
+    taken = None if n_new is None else ints(n_new)
+    kd.branch_append(None, x[:, hq:hq + hkv], x[:, hq + hkv:], k_pages, v_pages, table, ints(lens), n_new=taken)
+    kp, vp = torch.randn((1, hkv, max(N, 1), d), **g).bfloat16(), torch.randn((1, hkv, max(N, 1), d), **g).bfloat16()
+    out = torch.full((n, hq, Bt, d), 9.0, dtype=torch.bfloat16, device="cuda")
+    kd.branch_attention(x[:, :hq], k_pages, v_pages, table, ints(lens), prefix=(kp, vp, N) if N else None, n_new=taken, out=out)
+    for s, L in enumerate(lens):
+        m = Bt if n_new is None else n_new[s]
+        assert bool((out[s, :, m:] == 9).all())
+        if m:
+            own = rows_of(k_pages, table, s, L + m), rows_of(v_pages, table, s, L + m)
+            want, bound = attention_reference(x[s, :hq, :m], (kp[0].double(), vp[0].double()), N, own, lambda j: L + j + 1, d ** -0.5)
+            close(out[s, :, :m], want, bound, f"sequence {s}")
+
+
+# ------------------------------------------------------------------------------------------------ workspaces and captured steps
+@pytest.mark.parametrize("case", CASES, ids=[str(i) for i in range(len(CASES))])
+def test_nothing_is_written_behind_the_workspace(case, wide):  # noqa: F811
+    hq, hkv, d, prompts, fan, N, page, Bt, lens, n_new = case
+    n = max(prompts, 1) * fan
+    g = gen(7700)
+    k_pages, v_pages, table = paged(lens, Bt, page, hkv, d, g, wide=wide)
+    k_pages.normal_(generator=g["generator"])
+    v_pages.normal_(generator=g["generator"])
+    prefix = torch.randn((max(prompts, 1), hkv, N, d), **g).bfloat16(), torch.randn((max(prompts, 1), hkv, N, d), **g).bfloat16(), N
+    q = torch.randn((n, hq, Bt, d), **g).bfloat16()
+    need = kd.branch_workspace_bytes(n, hq, hkv, d, Bt, prompts)
+    work = torch.full((need + (1 << 22),), 0xAB, dtype=torch.uint8, device="cuda")
+    kd.branch_attention(q, k_pages, v_pages, table, ints(lens), prefix=prefix if prompts else None, n_new=None if n_new is None else ints(n_new),
+                        workspace=work[:need])
+    assert bool((work[need:] == 0xAB).all())
+
+
+def test_captured_steps_follow_rows_that_move_to_other_pages(wide):  # noqa: F811
+    # between replays pages are exchanged for others, which the rows move to; the pages they leave hold NaN
+    hq, hkv, d, N, page, n, Bt, steps = 8, 2, 64, 150, 16, 4, 2, 7
+    g = gen(7800)
+    k_pages, v_pages, table = paged([60] * n, Bt * steps, page, hkv, d, g, spare=3, wide=wide)
+    first = [0, 13, 60, 31]
+    for s, L in enumerate(first):
+        if L:
+            put_rows(k_pages, table, s, torch.randn((hkv, L, d), **g).bfloat16())
+            put_rows(v_pages, table, s, torch.randn((hkv, L, d), **g).bfloat16())
+    used = set(table[table >= 0].tolist())
+    free = [p for p in range(k_pages.shape[0]) if p not in used]
+    assert len(free) == 3
+    kp, vp = torch.randn((1, hkv, N, d), **g).bfloat16(), torch.randn((1, hkv, N, d), **g).bfloat16()
+    x = torch.randn((n, hq + 2 * hkv, Bt, d), **g).bfloat16()
+    lens, taken, (cos, sin) = ints(first), ints([2, 2, 2, 2]), tables(400, d)
+    pos0 = ints([200] * n)
+    out = torch.full((n, hq, Bt, d), 3.0, dtype=torch.bfloat16, device="cuda")
+    q_out = torch.full_like(out, 4.0)
+    work = torch.empty(kd.branch_workspace_bytes(n, hq, hkv, d, Bt, 1), dtype=torch.uint8, device="cuda")
+
+    def step(kpool, vpool, q_to, to, workspace):
+        kd.branch_append(x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], kpool, vpool, table, lens, n_new=taken, pos0=pos0, cos=cos, sin=sin, q_out=q_to)
+        kd.branch_attention(q_to, kpool, vpool, table, lens, prefix=(kp, vp, N), n_new=taken, out=to, workspace=workspace)
+
+    graphs, eager = (k_pages, v_pages, q_out, out), (k_pages.clone(), v_pages.clone(), q_out.clone(), out.clone())
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            step(*graphs, work)
+    torch.cuda.current_stream().wait_stream(side)
+    for i in range(steps):
+        x.copy_(torch.randn(x.shape, **g).bfloat16())
+        taken.copy_(ints([[2, 1, 0, 2], [1, 2, 2, 0]][i % 2]))
+        graph.replay()
+        torch.cuda.synchronize()
+        step(*eager, None)
+        for a, b, what in zip(graphs, eager, ("keys", "values", "queries", "outputs")):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16)), f"replay {i}: {what}"
+        for s in range(n):   # ... which are those of the definition
+            m, L = taken[s].item(), lens[s].item()
+            if m:
+                own = rows_of(k_pages, table, s, L + m), rows_of(v_pages, table, s, L + m)
+                want, bound = attention_reference(q_out[s, :, :m], (kp[0].double(), vp[0].double()), N, own, lambda j: L + j + 1, d ** -0.5)
+                close(out[s, :, :m], want, bound, f"replay {i}, sequence {s}")
+        lens += taken
+        s, c, to = i % n, (i // 2) % 3, free.pop(0)
+        old = table[s, c].item()
+        for pool in graphs[:2] + eager[:2]:
+            pool[to] = pool[old]
+            pool[old] = float("nan")
+        table[s, c] = to
+        free.append(old)
