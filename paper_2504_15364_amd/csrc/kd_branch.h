@@ -58,8 +58,8 @@ hipError_t launch_norm_rope_layers(const NormRopeLayers &p, hipStream_t s);
 
 // ------------------------------------------------------------------ attention of sequences that share a prompt's cache
 // Quotients of numbers below 2^31 by a number that the host knows (three instructions; the compiler's division, some forty that wait for one
-// another, eleven of them ahead of a launch's first loads, took 1.5 us).  With s the bits of d - 1 and mul = 2^32 (2^s - d) / d + 1 rounded down,
-// n / d = (n mul / 2^32 + n) / 2^s.
+// another, eleven of them ahead of a launch's first loads, took 1.5 us).  Division by an invariant number as by Granlund and Montgomery: with s
+// the bits of d - 1 and mul = 2^32 (2^s - d) / d + 1 rounded down, n / d = (n mul / 2^32 + n) / 2^s, whose sum stays below 2^32.
 struct Divisor {
     uint32_t mul, shift;
     void set(uint32_t d)
@@ -68,11 +68,10 @@ struct Divisor {
         while ((1ull << shift) < d) ++shift;
         mul = (uint32_t)((((1ull << shift) - d) << 32) / d + 1);
     }
-#ifdef __HIP_DEVICE_COMPILE__
-    __device__ __forceinline__ int divide(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
-#else
-    int divide(int n) const { return (int)((uint32_t)(((uint64_t)(uint32_t)n * mul) >> 32) + (uint32_t)n) >> shift; }
-#endif
+    __host__ __device__ __forceinline__ int divide(int n) const
+    {
+        return (int)(((uint32_t)(((uint64_t)(uint32_t)n * mul) >> 32) + (uint32_t)n) >> shift);
+    }
 };
 struct BranchParams {
     Rows q;
