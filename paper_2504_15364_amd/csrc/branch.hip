@@ -288,10 +288,10 @@ __device__ __forceinline__ void join_waves(const float *outs, const float2 (&ml_
 }
 
 // The shared part in blocks of 16 query rows: a workgroup its piece of a segment, every wave tiles of its own
-template <int D, int CB>
+template <int D>
 __device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned char *smem)
 {
-    constexpr int NC = D / 32, NDB = D / 16, UPR = D / 8, ROWB = D * 2, RPL = 64 / UPR, NV = TK / RPL, R = 16 * CB;
+    constexpr int NC = D / 32, NDB = D / 16, UPR = D / 8, ROWB = D * 2, RPL = 64 / UPR, NV = TK / RPL, R = 16;
     __shared__ float2 ml_s[NW][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c16 = lane & 15, g = lane >> 4;
@@ -302,7 +302,7 @@ __device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned cha
         const Segment sg = segment_of(p, task);
         const int ch = sg.ch, mb = sg.mb, c = sg.c, h = sg.h, stride = plan.splits * NW;
         const uint16_t *kh = p.k_prefix + (size_t)ch * p.prefix_cap * D, *vh = p.v_prefix + (size_t)ch * p.prefix_cap * D;
-        State<D, CB> st;
+        State<D, 1> st;
         st.reset();
         u32x4 kr[2][NC], vr[NV];
         // rows past the last repeat it: finite data whose weights are masked to zero.  (Offsets of 32 bits from the head's first row.)
@@ -324,17 +324,14 @@ __device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned cha
         int t = sg.k * NW + wave;
         load_k(t);   // (a tile behind the last repeats rows that exist)
         load_v(t);
+        const int m = min(mb * R + c16, M - 1);
+        const int f = p.by_Mt.divide(m);
+        const uint16_t *qr = query_row(p, c * p.fan + f, h, m - f * Mt) + 8 * g;
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            const int m = min(mb * R + 16 * cb + c16, M - 1);
-            const int f = p.by_Mt.divide(m);
-            const uint16_t *qr = query_row(p, c * p.fan + f, h, m - f * Mt) + 8 * g;
-#pragma unroll
-            for (int cc = 0; cc < NC; ++cc) st.q[cb][cc] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qr + cc * 32));
-        }
+        for (int cc = 0; cc < NC; ++cc) st.q[0][cc] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qr + cc * 32));
         for (; t < nt; t += stride) {
             store_v<D>(vt, vr, lane);
-            tile_step<D, CB>(
+            tile_step<D, 1>(
                 st, vt, p.scale_log2e, lane, [&](int kg, int cc) { return __builtin_bit_cast(bf16x8, kr[kg][cc]); },
                 [&]() {
                     if (t + stride < nt) {
@@ -342,27 +339,23 @@ __device__ void shared_few(const BranchParams &p, const Plan &plan, unsigned cha
                         load_v(t + stride);
                     }
                 },
-                [&](f32x4 (&s)[CB][2]) {
-                    if ((t + 1) * TK > p.prefix_len) hide_from<CB>(s, p.prefix_len - t * TK, g);   // uniform
+                [&](f32x4 (&s)[1][2]) {
+                    if ((t + 1) * TK > p.prefix_len) hide_from<1>(s, p.prefix_len - t * TK, g);   // uniform
                 });
         }
-        // the eight results become one, a block of 16 rows at a time
+        // the eight results become one
         const size_t slot = task;
+        const float l = sum_over_rows(st.l[0]);
+        __syncthreads();
+        float *ow = outs + (size_t)wave * 16 * OUT_PITCH<D>;
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            const float l = sum_over_rows(st.l[cb]);
-            __syncthreads();
-            float *ow = outs + (size_t)wave * 16 * OUT_PITCH<D>;
-#pragma unroll
-            for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(ow + c16 * OUT_PITCH<D> + 16 * db + 4 * g) = st.o[cb][db];
-            if (g == 0) ml_s[wave][c16] = make_float2(st.m[cb], l);
-            __syncthreads();
-            const int rows = min(16, M - mb * R - 16 * cb);
-            join_waves<D>(outs, ml_s, rows, tid, [&](int m, int d0, f32x4 acc, float mx, float L) {
-                *reinterpret_cast<f32x4 *>(p.part_o + (slot * R + 16 * cb + m) * D + d0) = acc;
-                if (d0 == 0) p.part_ml[slot * R + 16 * cb + m] = piece_ml(mx, L);
-            });
-        }
+        for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(ow + c16 * OUT_PITCH<D> + 16 * db + 4 * g) = st.o[0][db];
+        if (g == 0) ml_s[wave][c16] = make_float2(st.m[0], l);
+        __syncthreads();
+        join_waves<D>(outs, ml_s, min(16, M - mb * R), tid, [&](int row, int d0, f32x4 acc, float mx, float L) {
+            *reinterpret_cast<f32x4 *>(p.part_o + (slot * R + row) * D + d0) = acc;
+            if (d0 == 0) p.part_ml[slot * R + row] = piece_ml(mx, L);
+        });
         __syncthreads();   // the outputs are read before the next segment's V tiles overwrite them
     }
 }
@@ -881,7 +874,7 @@ __global__ __launch_bounds__(64 * NW) void branch_main_kernel(BranchParams p)
     }
     if ((int)blockIdx.x < plan.shared_wgs) {
         if constexpr (RS > 32) shared_many<D, RS / 32>(p, plan, smem);
-        else shared_few<D, RS / 16>(p, plan, smem);
+        else shared_few<D>(p, plan, smem);
     } else {
         const size_t rows = shared_slots(p.n_prefixes, p.fan, p.hkv, Mt, RS, wgs) * RS;
         own_part<D, RO / 16>(p, plan, ((int)blockIdx.x - plan.shared_wgs) * NW + wave, len0, rows0, p.part_o + rows * D, p.part_ml + rows,
