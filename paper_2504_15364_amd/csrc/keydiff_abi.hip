@@ -1299,12 +1299,16 @@ int check_prefixes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, 
 
 // The workspace is large enough, and what the call writes, `out` and the workspace, is nothing that it reads, but for `out` in the place of
 // the queries: a row is stored by the workgroup that has read it, or behind the launch that has.
+struct BranchWork {   // where the parts of a call's workspace begin, for a chip of `cus` compute units
+    size_t off_ml, off_plan;
+    int32_t cus;
+};
 int check_buffers(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix,
-                  int32_t n_prefixes, int64_t prefix_cap, const void *out, const void *workspace, size_t workspace_bytes)
+                  int32_t n_prefixes, int64_t prefix_cap, const void *out, const void *workspace, size_t workspace_bytes, BranchWork *work)
 {
     const int32_t hq = b->n_q_heads, D = b->head_dim;
-    size_t off_ml = 0, off_plan = 0;
-    const size_t need = kd::branch_workspace(b->n_seqs, n_prefixes, b->n_kv_heads, hq / b->n_kv_heads, Bt, D, std::max(compute_units(), 2), &off_ml, &off_plan);
+    work->cus = std::max(compute_units(), 2);
+    const size_t need = kd::branch_workspace(b->n_seqs, n_prefixes, b->n_kv_heads, hq / b->n_kv_heads, Bt, D, work->cus, &work->off_ml, &work->off_plan);
     if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
     const size_t rows = (size_t)b->n_seqs * hq * Bt * D * 2, pool = (size_t)b->n_pages * b->n_kv_heads * b->page_rows * D * 2;
     const size_t prefix = k_prefix ? (size_t)n_prefixes * b->n_kv_heads * prefix_cap * D * 2 : 0;
@@ -1326,7 +1330,8 @@ int check_buffers(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t 
 }
 
 int branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix,
-                     int32_t n_prefixes, int32_t prefix_len, int64_t prefix_cap, float scale_log2e, void *out, void *workspace, hipStream_t s)
+                     int32_t n_prefixes, int32_t prefix_len, int64_t prefix_cap, float scale_log2e, void *out, void *workspace,
+                     const BranchWork &work, hipStream_t s)
 {
     kd::BranchParams p{};
     p.q = rows_of(*q);
@@ -1343,14 +1348,12 @@ int branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32
     p.D = b->head_dim;
     p.prefix_len = n_prefixes > 0 ? prefix_len : 0;
     p.prefix_cap = prefix_cap;
-    p.cus = std::max(compute_units(), 2);
+    p.cus = work.cus;
     p.scale_log2e = scale_log2e;
-    size_t off_ml = 0, off_plan = 0;
-    kd::branch_workspace(p.n_seqs, n_prefixes, p.hkv, p.G, Bt, p.D, p.cus, &off_ml, &off_plan);
     unsigned char *w = static_cast<unsigned char *>(workspace);
     p.part_o = reinterpret_cast<float *>(w);
-    p.part_ml = reinterpret_cast<float2 *>(w + off_ml);
-    p.plan = reinterpret_cast<int32_t *>(w + off_plan);
+    p.part_ml = reinterpret_cast<float2 *>(w + work.off_ml);
+    p.plan = reinterpret_cast<int32_t *>(w + work.off_plan);
     KD_LAUNCH(kd::launch_branch_attention(p, s), "branch attention kernels");
     return KEYDIFF_OK;
 }
@@ -1484,10 +1487,12 @@ int keydiff_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *
         if (prefix_cap < prefix_len) return fail(KEYDIFF_ESHAPE, "prefix_cap must be at least prefix_len");
     }
     const bool shared = n_prefixes > 0 && prefix_len > 0;
-    if (int rc = check_buffers(b, q, Bt, shared ? k_prefix : nullptr, v_prefix, n_prefixes, prefix_cap, out, workspace, workspace_bytes)) return rc;
+    BranchWork work;
+    if (int rc = check_buffers(b, q, Bt, shared ? k_prefix : nullptr, v_prefix, n_prefixes, prefix_cap, out, workspace, workspace_bytes, &work))
+        return rc;
     const double scale = softmax_scale > 0.f ? (double)softmax_scale : 1.0 / std::sqrt((double)b->head_dim);
     return branch_attention(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, (float)(scale * 1.4426950408889634), out,
-                            workspace, static_cast<hipStream_t>(stream));
+                            workspace, work, static_cast<hipStream_t>(stream));
 }
 
 int keydiff_cache_branch_attention(keydiff_cache_t *c, const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, void *out,
@@ -1501,13 +1506,14 @@ int keydiff_cache_branch_attention(keydiff_cache_t *c, const keydiff_branches_t 
     // (a pending eviction leaves the budget's rows)
     const int32_t rows = c->len;
     if (int rc = check_prefixes(b, Bt, c->cfg.batch, rows)) return rc;
-    if (int rc = check_buffers(b, q, Bt, c->k, c->v, c->cfg.batch, c->L.cap, out, workspace, workspace_bytes)) return rc;
+    BranchWork work;
+    if (int rc = check_buffers(b, q, Bt, c->k, c->v, c->cfg.batch, c->L.cap, out, workspace, workspace_bytes, &work)) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     if ((c->pending || c->shift_pending) && hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone)
         return fail(KEYDIFF_ESTATE, "the cache has a pending eviction, which every replay would repeat: keydiff_finish it ahead of the capture");
     if (int rc = finish_pending(c, s)) return rc;
-    return branch_attention(b, q, Bt, c->k, c->v, c->cfg.batch, c->len, c->L.cap, c->scale_log2e, out, workspace, s);
+    return branch_attention(b, q, Bt, c->k, c->v, c->cfg.batch, c->len, c->L.cap, c->scale_log2e, out, workspace, work, s);
 }
 
 int keydiff_finish(keydiff_cache_t *c, void *stream)
