@@ -1133,7 +1133,8 @@ SharedBlock shared_block(int64_t rows, int heads, int prefix_len, int cus)
 }
 
 // Whether one launch with a workgroup a segment (branch_short_kernel) takes the call: its time, with as many own rows as the tables can name
-// (the lengths themselves are on the device: tables laid out for long answers take two launches from the first token on), against the two launches' with the prompts' part alone, whose pieces are dealt to all workgroups.
+// (the lengths themselves are on the device: tables laid out for long answers take two launches from the first token on), against the two
+// launches' with the prompts' part alone, whose pieces are dealt to all workgroups.
 // Lines through the times of 345 sizes, of which the choice is as fast as the better on average (two launches always: 36 % slower).  Measured, one
 // launch against two (D 128, 8 KV heads of 4 query heads): one sequence, 40 shared and 10 own rows 4.5 us against 9.1, 200 and 100 6.8
 // and 9.8, 1000 and 300 15.6 and 10.4; 32 sequences, 200 and 100 7.2 and 14.8, 1000 and 100 13.7 and 16.7, 2000 and 100 22.5 and 18.6;

@@ -1297,21 +1297,22 @@ int check_prefixes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, 
     return KEYDIFF_OK;
 }
 
-// The workspace is large enough, and what the call writes, `out` and the workspace, is nothing that it reads, but for `out` in the place of
-// the queries: a row is stored by the workgroup that has read it, or behind the launch that has.
 struct BranchWork {   // where the parts of a call's workspace begin, for a chip of `cus` compute units
     size_t off_ml, off_plan;
     int32_t cus;
 };
-int check_buffers(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix,
-                  int32_t n_prefixes, int64_t prefix_cap, const void *out, const void *workspace, size_t workspace_bytes, BranchWork *work)
+// The workspace is large enough, and what the call writes, `out` and the workspace, is nothing that it reads, but for `out` in the place of
+// the queries: a row is stored by the workgroup that has read it, or behind the launch that has.
+int check_buffers(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix, int32_t n_prefixes,
+                  int32_t prefix_len, int64_t prefix_cap, const void *out, const void *workspace, size_t workspace_bytes, BranchWork *work)
 {
     const int32_t hq = b->n_q_heads, D = b->head_dim;
     work->cus = std::max(compute_units(), 2);
     const size_t need = kd::branch_workspace(b->n_seqs, n_prefixes, b->n_kv_heads, hq / b->n_kv_heads, Bt, D, work->cus, &work->off_ml, &work->off_plan);
     if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
     const size_t rows = (size_t)b->n_seqs * hq * Bt * D * 2, pool = (size_t)b->n_pages * b->n_kv_heads * b->page_rows * D * 2;
-    const size_t prefix = k_prefix ? (size_t)n_prefixes * b->n_kv_heads * prefix_cap * D * 2 : 0;
+    const bool shared = n_prefixes > 0 && prefix_len > 0;   // (of the last head, no row behind prefix_len need exist)
+    const size_t prefix = shared ? (((size_t)n_prefixes * b->n_kv_heads - 1) * prefix_cap + prefix_len) * D * 2 : 0;
     const struct {
         const void *at;
         size_t bytes;
@@ -1486,9 +1487,8 @@ int keydiff_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *
         if (misaligned(k_prefix) || misaligned(v_prefix)) return fail(KEYDIFF_EINVAL, "tensors must be 16-byte aligned");
         if (prefix_cap < prefix_len) return fail(KEYDIFF_ESHAPE, "prefix_cap must be at least prefix_len");
     }
-    const bool shared = n_prefixes > 0 && prefix_len > 0;
     BranchWork work;
-    if (int rc = check_buffers(b, q, Bt, shared ? k_prefix : nullptr, v_prefix, n_prefixes, prefix_cap, out, workspace, workspace_bytes, &work))
+    if (int rc = check_buffers(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, out, workspace, workspace_bytes, &work))
         return rc;
     const double scale = softmax_scale > 0.f ? (double)softmax_scale : 1.0 / std::sqrt((double)b->head_dim);
     return branch_attention(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, (float)(scale * 1.4426950408889634), out,
@@ -1507,7 +1507,7 @@ int keydiff_cache_branch_attention(keydiff_cache_t *c, const keydiff_branches_t 
     const int32_t rows = c->len;
     if (int rc = check_prefixes(b, Bt, c->cfg.batch, rows)) return rc;
     BranchWork work;
-    if (int rc = check_buffers(b, q, Bt, c->k, c->v, c->cfg.batch, c->L.cap, out, workspace, workspace_bytes, &work)) return rc;
+    if (int rc = check_buffers(b, q, Bt, c->k, c->v, c->cfg.batch, (int32_t)c->L.cap, c->L.cap, out, workspace, workspace_bytes, &work)) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     if ((c->pending || c->shift_pending) && hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone)

@@ -107,6 +107,28 @@ def test_outputs_in_the_place_of_the_queries_and_next_to_what_is_read(fan, N, Bt
         kd.branch_attention(both[0], k_pages, v_pages, table, ints(lens), prefix=prefix, out=both.view(-1)[d:d + q.numel()].view(q.shape))
 
 
+def test_rows_behind_the_last_head_of_a_prefix_need_not_exist():
+    # one head: the distance to the next one is never used, and a large one is no overlap
+    import ctypes as C
+    from paper_2504_15364_amd import binding
+    hq, d, N, n = 4, 64, 300, 3
+    g = gen(7350)
+    k_pages, v_pages, table = paged([20] * n, 1, 16, 1, d, g)
+    for s in range(n):
+        put_rows(k_pages, table, s, torch.randn((1, 21, d), **g).bfloat16())
+        put_rows(v_pages, table, s, torch.randn((1, 21, d), **g).bfloat16())
+    kp, vp = torch.randn((1, 1, N, d), **g).bfloat16(), torch.randn((1, 1, N, d), **g).bfloat16()
+    q, lens = torch.randn((n, hq, 1, d), **g).bfloat16(), ints([20] * n)
+    want = kd.branch_attention(q, k_pages, v_pages, table, lens, prefix=(kp, vp, N))
+    out, work = torch.zeros_like(q), torch.empty(kd.branch_workspace_bytes(n, hq, 1, d, 1, 1), dtype=torch.uint8, device="cuda")
+    b = binding._Branches(k_pages=k_pages.data_ptr(), v_pages=v_pages.data_ptr(), table=table.data_ptr(), lens=lens.data_ptr(), n_seqs=n, n_q_heads=hq,
+                          n_kv_heads=1, head_dim=d, page_rows=16, n_pages=k_pages.shape[0], table_width=table.shape[1])
+    rc = binding.load_library().keydiff_branch_attention(C.byref(b), C.byref(binding._Rows(q.data_ptr(), hq * d, d, 0)), 1, kp.data_ptr(), vp.data_ptr(), 1, N,
+                                                         1 << 40, 0.0, out.data_ptr(), work.data_ptr(), work.numel(),
+                                                         torch.cuda.current_stream().cuda_stream)
+    assert rc == 0 and torch.equal(out, want)
+
+
 # ------------------------------------------------------------------------------------------------ positions at the end of 64 bits
 def test_blocks_whose_positions_do_not_fit_are_refused():
     hq, hkv, d, B = 4, 2, 64, 16
