@@ -328,6 +328,60 @@ KEYDIFF_API int keydiff_branch_attention(const keydiff_branches_t *b, const keyd
 KEYDIFF_API int keydiff_cache_branch_attention(keydiff_cache_t *prompt, const keydiff_branches_t *b, const keydiff_rows_t *q,
                                    int32_t Bt, void *out, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Attention of pieces of many tokens (a tool's answer, the next turn of a dialogue, a prompt in pages of its own): what keydiff_branch_attention
+ * computes, bounded by the matrix cores instead of by the reads of own rows, and the logarithms of the weight sums besides.
+ *   out   [n_seqs][n_q_heads][Bt][head_dim], as there
+ *   lse   device, float [n_seqs][n_q_heads][Bt]: log sum_i exp(softmax_scale q.k_i) over the keys that the query sees; -inf where it sees none
+ * Rows of both behind a sequence's n_new, and those of a sequence that is not in use, are left as they were; no work is spent on them.  Any Bt; where
+ * a sequence has at most 32 query rows per KV head, the kernels are those of keydiff_branch_attention.
+ * The workspace (keydiff_branch_chunk_workspace_bytes), overlaps, limits of values and sizes are as there; KEYDIFF_ESHAPE also if the blocks of
+ * 32 query rows of all KV heads exceed 2^23.  A weight goes into the product with the values as one bf16 number.                             */
+KEYDIFF_API int keydiff_branch_chunk_workspace_bytes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, size_t *bytes);
+KEYDIFF_API int keydiff_branch_chunk_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt,
+                             const void *k_prefix, const void *v_prefix, int32_t n_prefixes, int32_t prefix_len,
+                             int64_t prefix_cap, float softmax_scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                             void *stream);
+/* ... with the rows and the softmax scale of a KeyDiff cache, as keydiff_cache_branch_attention. */
+KEYDIFF_API int keydiff_cache_branch_chunk_attention(keydiff_cache_t *prompt, const keydiff_branches_t *b, const keydiff_rows_t *q,
+                                   int32_t Bt, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The attention weight that the own rows of a sequence gather, for an eviction that goes by it.  With
+ *   p(r) = sum exp(softmax_scale q.k_r - lse) over the query heads of row r's KV head and over the last `observe` tokens that the sequence takes
+ *          in this step (0: all of them) and that see row r,
+ * w(r) becomes decay w(r) + p(r) for a row that the sequence held before the step, p(r) for a new one.
+ *   q, b        as given to the attention (v_pages is not read and may be null); b->lens and b->n_new too: the rows before the step
+ *   lse         device, float [n_seqs][n_q_heads][Bt], from the attention of the same tokens (a part of each query's weight is that of the
+ *               prompt's rows, which are not weighed); -inf: the query gives no weight
+ *   w_pages     device, float [n_pages][n_kv_heads][page_rows], 16-byte aligned: the weights, in pages beside the rows.  Nothing in them has to be
+ *               initialised.  With decay 0 what they hold is not used
+ * Sequences that take no token keep their weights, and so do rows of pages that do not exist.  A page that this call writes weights of must belong to one
+ * sequence alone.  Sums are kept in float, in an order that depends on sizes alone; a
+ * weight below 2^-126 counts as zero.  Inputs of rows and queries that take part must be
+ * finite.  EINVAL if decay is not in [0, 1] or softmax_scale not finite; ESHAPE for sizes that keydiff_branch_chunk_attention refuses too.
+ *   workspace   as for the attention, of keydiff_branch_weights_workspace_bytes                                                              */
+KEYDIFF_API int keydiff_branch_weights_workspace_bytes(const keydiff_branches_t *b, int32_t Bt, int32_t observe, size_t *bytes);
+KEYDIFF_API int keydiff_branch_weights(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const float *lse, float *w_pages,
+                             int32_t observe, float decay, float softmax_scale, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Eviction of own rows (Eq. 6 by attention weight instead of key similarity).  With n = lens[s] + the tokens that the sequence takes in this step: if
+ * n <= budget nothing is evicted; else every KV head keeps `budget` of its n rows: those of the latest `window` positions (from
+ * pos0[s] + n - window on) ahead of all others, then those of the largest weights (NaN counts as -inf), of equal ones those of the lower position, of equal
+ * positions the lower row.  Kept rows at [budget, n) move to the places of evicted ones in [0, budget), both in ascending order: key, value, weight and
+ * position.  Rows behind the budget stay as they are and mean nothing any more.
+ *   b           as given to the attention: the rows before the step
+ *   w_pages     as above
+ *   p_pages     device, int32 [n_pages][n_kv_heads][page_rows], 16-byte aligned: the position of every row.  The call writes those of the new tokens, pos0[s] +
+ *               lens[s] + j as in keydiff_branch_append; nothing has to be initialised
+ *   pos0        device int32 [n_seqs], null: zeros
+ *   status      device int32, nullable: KEYDIFF_LEFT_OUT_ROW is set in it, and nothing cleared, if a sequence has more than `budget` rows, of which some lie
+ *               outside its table or on a page outside the pool: it is left as it was but for the positions of the new rows
+ * lens and pos0 are not changed: all layers of a step read the same ones.  Behind the last layer the caller sets lens[s] to min(n, budget) and adds the
+ * n - lens[s] rows evicted to pos0[s], so that the next token's position, pos0[s] + lens[s], goes on.
+ * Pages of sequences that may evict must belong to them alone.  KEYDIFF_ESHAPE unless 0 <= window < budget.                                   */
+KEYDIFF_API int keydiff_branch_evict_workspace_bytes(const keydiff_branches_t *b, int32_t budget, size_t *bytes);
+KEYDIFF_API int keydiff_branch_evict(const keydiff_branches_t *b, int32_t Bt, float *w_pages, int32_t *p_pages, const int32_t *pos0, int32_t budget,
+                           int32_t window, int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Enqueue the pending eviction of `cache` on `stream`, if it has one (else a no-op). */
 KEYDIFF_API int keydiff_finish(keydiff_cache_t *cache, void *stream);
 

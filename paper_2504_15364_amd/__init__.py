@@ -17,6 +17,12 @@ from .binding import (  # noqa: F401
     KeyDiffError,
     branch_append,
     branch_attention,
+    branch_chunk_attention,
+    branch_chunk_workspace_bytes,
+    branch_evict,
+    branch_evict_workspace_bytes,
+    branch_weights,
+    branch_weights_workspace_bytes,
     branch_workspace_bytes,
     load_library,
     norm_rope,

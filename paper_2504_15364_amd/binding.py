@@ -24,6 +24,8 @@ EXPORTS = (
     "keydiff_prefill_block_layers", "keydiff_prefill_block_rope", "keydiff_prefill_block_layers_rope", "keydiff_finish", "keydiff_decode_step",
     "keydiff_prefill_block_norm_rope", "keydiff_prefill_block_layers_norm_rope", "keydiff_norm_rope", "keydiff_branch_append",
     "keydiff_branch_workspace_bytes", "keydiff_branch_attention", "keydiff_cache_branch_attention",
+    "keydiff_branch_chunk_workspace_bytes", "keydiff_branch_chunk_attention", "keydiff_cache_branch_chunk_attention",
+    "keydiff_branch_weights_workspace_bytes", "keydiff_branch_weights", "keydiff_branch_evict_workspace_bytes", "keydiff_branch_evict",
     "keydiff_scores", "keydiff_cache_len", "keydiff_cache_plan", "keydiff_cache_positions", "keydiff_cache_load",
     "keydiff_cache_status", "keydiff_profile_enable", "keydiff_profile_read", "keydiff_destroy_cache",
     "keydiff_last_error", "keydiff_version",
@@ -107,6 +109,13 @@ def load_library() -> C.CDLL:
     L.keydiff_branch_workspace_bytes.argtypes = [bp, i32, i32, szp]
     L.keydiff_branch_attention.argtypes = [bp, rp, i32, vp, vp, i32, i32, i64, C.c_float, vp, vp, C.c_size_t, vp]
     L.keydiff_cache_branch_attention.argtypes = [vp, bp, rp, i32, vp, vp, C.c_size_t, vp]
+    L.keydiff_branch_chunk_workspace_bytes.argtypes = [bp, i32, i32, szp]
+    L.keydiff_branch_chunk_attention.argtypes = [bp, rp, i32, vp, vp, i32, i32, i64, C.c_float, vp, vp, vp, C.c_size_t, vp]
+    L.keydiff_cache_branch_chunk_attention.argtypes = [vp, bp, rp, i32, vp, vp, vp, C.c_size_t, vp]
+    L.keydiff_branch_weights_workspace_bytes.argtypes = [bp, i32, i32, szp]
+    L.keydiff_branch_weights.argtypes = [bp, rp, i32, vp, vp, i32, C.c_float, C.c_float, vp, C.c_size_t, vp]
+    L.keydiff_branch_evict_workspace_bytes.argtypes = [bp, i32, szp]
+    L.keydiff_branch_evict.argtypes = [bp, i32, vp, vp, vp, i32, i32, vp, vp, C.c_size_t, vp]
     L.keydiff_finish.argtypes = [vp, vp]
     L.keydiff_decode_step.argtypes = [vp, vp, vp, vp, i64, vp, vp]
     L.keydiff_scores.argtypes = [vp, vp, vp]
@@ -265,7 +274,10 @@ def _native():
             raise ImportError(f"{e}: build it first (python -m paper_2504_15364_amd.build)") from e
         address = lambda f: C.cast(f, C.c_void_p).value  # noqa: E731
         m.bind(*(address(f) for f in (L.keydiff_norm_rope, L.keydiff_branch_append, L.keydiff_branch_workspace_bytes,
-                                      L.keydiff_branch_attention, L.keydiff_cache_branch_attention)),
+                                      L.keydiff_branch_attention, L.keydiff_cache_branch_attention, L.keydiff_branch_chunk_workspace_bytes,
+                                      L.keydiff_branch_chunk_attention, L.keydiff_cache_branch_chunk_attention,
+                                      L.keydiff_branch_weights_workspace_bytes, L.keydiff_branch_weights,
+                                      L.keydiff_branch_evict_workspace_bytes, L.keydiff_branch_evict)),
                _C._cuda_getCurrentRawStream)
         _calls = m
     return _calls
@@ -336,15 +348,84 @@ def branch_attention(q, k_pages, v_pages, table, lens, prefix=None, n_new=None, 
     out may be q itself where q is contiguous, and must else overlap nothing that the call reads.
     Returns out [n_seqs][Hq][Bt][d]; rows behind a sequence's n_new, and those of a sequence with lens < 0, are left as they were
     (they hold anything where out is None)."""
-    handle = batch = keys = values = rows = None
+    return _call("branch_attention", q.device, stream, q, k_pages, v_pages, table, lens, n_new, *_prefix(prefix, q), softmax_scale, out, workspace)
+
+
+def _prefix(prefix, q):
+    """Handle and batch of a cache, or keys, values and their rows."""
     if isinstance(prefix, KeyDiffCache):
-        handle, batch = prefix._h.value if prefix._h else 0, prefix.cfg.batch
         if prefix.device != q.device:
             raise ValueError(f"the cache lives on {prefix.device}, the queries on {q.device}")
-    elif prefix is not None:
-        keys, values, rows = prefix
-    return _call("branch_attention", q.device, stream, q, k_pages, v_pages, table, lens, n_new, handle, batch, keys, values, rows,
-                 softmax_scale, out, workspace)
+        return prefix._h.value if prefix._h else 0, prefix.cfg.batch, None, None, None
+    return None, None, *(prefix if prefix is not None else (None, None, None))
+
+
+def branch_chunk_workspace_bytes(n_seqs, n_q_heads, n_kv_heads, head_dim, Bt, n_prefixes=0):
+    """Bytes of the workspace that branch_chunk_attention needs for calls of these sizes on the current device."""
+    b = _Branches(n_seqs=n_seqs, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim)
+    size = C.c_size_t()
+    _check(load_library().keydiff_branch_chunk_workspace_bytes(C.byref(b), Bt, n_prefixes, C.byref(size)))
+    return size.value
+
+
+def branch_chunk_attention(q, k_pages, v_pages, table, lens, prefix=None, n_new=None, softmax_scale: float = 0.0, out=None, lse=None,
+                           workspace=None, stream=None):
+    """branch_attention for pieces of many tokens (a tool's answer, the next turn, a prompt in pages of its own): the same arguments and outputs,
+    bounded by the matrix cores, and the logarithms of the weight sums, which branch_weights asks for.  Any number of tokens.
+    lse: float32 [n_seqs][Hq][Bt], log sum_i exp(softmax_scale q.k_i) over the keys that a query sees, -inf where it sees none.
+    workspace: as for branch_attention, of at least branch_chunk_workspace_bytes.
+    Returns (out, lse); rows of both behind a sequence's n_new, and those of a sequence with lens < 0, are left as they were."""
+    return _call("branch_chunk_attention", q.device, stream, q, k_pages, v_pages, table, lens, n_new, *_prefix(prefix, q), softmax_scale, out,
+                 workspace, lse)
+
+
+def branch_weights_workspace_bytes(n_seqs, n_q_heads, n_kv_heads, head_dim, Bt=1, observe=0):
+    """Bytes of the workspace that branch_weights needs for calls of these sizes on the current device."""
+    b = _Branches(n_seqs=n_seqs, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim)
+    size = C.c_size_t()
+    _check(load_library().keydiff_branch_weights_workspace_bytes(C.byref(b), Bt, observe, C.byref(size)))
+    return size.value
+
+
+def branch_weights(q, k_pages, w_pages, table, lens, lse, n_new=None, observe: int = 0, decay: float = 1.0, softmax_scale: float = 0.0,
+                   workspace=None, stream=None):
+    """The attention weight that the tokens of a step give to the own rows of their sequences, added to what these have gathered: with
+    p = sum exp(softmax_scale q.k - lse) over a row's query heads and the last `observe` tokens that see it (0: all), w becomes
+    decay * w + p for rows that the sequence held before the step, p for new ones.
+    q, k_pages, table, lens, n_new: as given to branch_chunk_attention, whose lse this is.
+    w_pages: float32 [pages][Hkv][page_rows], updated; nothing in it has to be initialised.  A page whose weights change must belong to one
+    sequence alone.  decay 1 adds up all there was, 0 leaves the weight of these tokens alone.
+    softmax_scale <= 0: 1/sqrt(d).  (With a cache as the attention's prefix: the cache's scale.)
+    workspace: a uint8 tensor of at least branch_weights_workspace_bytes that no other call in flight uses (None: allocated for the call)."""
+    _call("branch_weights", q.device, stream, q, k_pages, w_pages, table, lens, lse, n_new, observe, decay, softmax_scale, workspace)
+
+
+def branch_evict_workspace_bytes(n_seqs, n_kv_heads, table_rows, budget):
+    """Bytes of the workspace that branch_evict needs for calls of these sizes (table_rows: rows that a sequence's table can name)."""
+    b = _Branches(n_seqs=n_seqs, n_q_heads=n_kv_heads, n_kv_heads=n_kv_heads, page_rows=1, table_width=table_rows)
+    size = C.c_size_t()
+    _check(load_library().keydiff_branch_evict_workspace_bytes(C.byref(b), budget, C.byref(size)))
+    return size.value
+
+
+def branch_evict(k_pages, v_pages, w_pages, p_pages, table, lens, budget: int, Bt: int = 1, n_new=None, pos0=None, window: int = 0, workspace=None,
+                 stream=None, status=None):
+    """Eviction of own rows by the weight they have gathered.  A sequence that holds n = lens[s] + its new tokens (Bt, or n_new[s] of them) keeps, in
+    every KV head, `budget` of its n rows: those of the latest `window` positions first, then those of the largest weights, of equal ones the lower
+    position.  Rows behind the budget that are kept move to the places of evicted ones, with their weights and positions.
+    w_pages: from branch_weights.  p_pages: int32 [pages][Hkv][page_rows], the positions of the rows; those of new tokens (pos0[s] + lens[s] + j)
+    are written by this call, nothing has to be initialised.  Pages of sequences that may evict must belong to them alone.
+    lens and pos0 are not changed.  Behind the last layer of a step:
+
+        n = lens + n_new                       # (or Bt; of sequences in use)
+        kept = n.clamp(max=budget)
+        pos0 += n - kept                       # positions go on
+        lens.copy_(kept)
+
+    status: an int32 tensor of one element, in which LEFT_OUT_ROW is set, and nothing cleared, if a sequence that would have to evict has rows outside
+    its table or on pages outside the pool; its rows are left as they were.
+    workspace: a uint8 tensor of at least branch_evict_workspace_bytes that no other call in flight uses (None: allocated for the call)."""
+    _call("branch_evict", k_pages.device, stream, k_pages, v_pages, w_pages, p_pages, table, lens, budget, Bt, n_new, pos0, window, status, workspace)
 
 
 class KeyDiffCache:

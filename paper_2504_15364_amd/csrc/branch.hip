@@ -63,6 +63,8 @@ __device__ __forceinline__ float sum_over_rows(float x)
 // What a piece of a row leaves for the join: its reference and weight sum.  A reference of -inf stands for a piece without a key, which the join
 // skips; one whose logits are all NaN has none either, and its NaN must not be lost.
 __device__ __forceinline__ float2 piece_ml(float m, float L) { return make_float2(L == L ? m : 0.f, L); }
+// Natural logarithm of a row's weight sum, -inf where it has seen no key
+__device__ __forceinline__ float log_sum(float m, float L) { return L == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(L)) * 0.6931471805599453f; }
 // New tokens of a sequence that holds `len` rows, and rows that are keys of theirs (its own and the new ones); 0 where it has nothing to do
 __device__ __forceinline__ int new_of(const BranchParams &p, int len, int asked) { return len < 0 ? 0 : max(0, min(asked, p.Bt)); }
 __device__ __forceinline__ int own_rows(const BranchParams &p, int len, int asked)
@@ -957,6 +959,7 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
         if (group != 0) return;
         float top = -INFINITY;
         for (int k = 0; k < groups; ++k) top = fmaxf(top, ml_s[unit + k].x);
+        mx = top;
         acc = f32x4{0.f, 0.f, 0.f, 0.f};
         L = 0.f;
         for (int k = 0; k < groups; ++k) {
@@ -972,6 +975,7 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = (__bf16)(acc[i] * inv);
     *reinterpret_cast<bf16x4 *>(p.out + (((size_t)s * p.hkv + h) * Mt + m) * D + d0) = o;
+    if (p.lse && d0 == 0) p.lse[((size_t)s * p.hkv + h) * Mt + m] = log_sum(mx, L);
 }
 
 // Few rows: one launch, a workgroup for every (sequence, head, block of rows), whose waves take tiles of the prompt's and of the own rows in
@@ -1081,13 +1085,14 @@ __global__ __launch_bounds__(64 * NW) void branch_short_kernel(BranchParams p)
         for (int db = 0; db < NDB; ++db) *reinterpret_cast<f32x4 *>(ow + c16 * OUT_PITCH<D> + 16 * db + 4 * g) = st.o[cb][db];
         if (g == 0) ml_s[wave][c16] = make_float2(st.m[cb], l);
         __syncthreads();
-        join_waves<D>(outs, ml_s, min(16, Mt - m0 - 16 * cb), tid, [&](int row, int d0, f32x4 acc, float, float) {
+        join_waves<D>(outs, ml_s, min(16, Mt - m0 - 16 * cb), tid, [&](int row, int d0, f32x4 acc, float mx, float L) {
             const int m = m0 + 16 * cb + row;
             if (m - p.by_Bt.divide(m) * p.Bt >= fresh) return;
             bf16x4 o;
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = (__bf16)acc[i];
             *reinterpret_cast<bf16x4 *>(p.out + ((size_t)sh * Mt + m) * D + d0) = o;
+            if (p.lse && d0 == 0) p.lse[(size_t)sh * Mt + m] = log_sum(mx, L);
         });
     }
 }

@@ -1,0 +1,684 @@
+// branch_chunk_attention: pieces of many new tokens attend to the rows of their prompt's cache and to the rows in their sequence's pages.
+//
+//   o = sum_i p_i v_i,  p_i = 2^(a_i - lse2),  a_i = scale log2(e) q.k_i,  lse2 = log2 sum_i 2^a_i,  i over the N rows of the prompt and the
+//   sequence's own rows up to the token itself; the running reference m of a row and sum of 2^(a_i - m) go along with the output, and
+//   pieces of a row's keys join by them: o = sum_w l_w 2^(m_w - m) o_w / sum_w l_w 2^(m_w - m).
+//
+// The query rows of a (sequence, KV head), token after token with the group's heads side by side, are cut into blocks of 256; a segment is
+// a block with all tiles of 64 keys that its last token sees.  What bounds it is the matrix pipe (4 D operations a pair of a
+// query row and a key), so the work is cut by tiles: the segments of all heads form one list of tiles, of which every workgroup, one per compute
+// unit, takes an equal and contiguous part (chunk_plan).  A segment that lies inside one part is written at once; of one that is cut every part leaves a
+// partial, and a second launch joins them.  Ragged lengths and the triangle of the causal mask cost nothing that way, and one
+// sequence's block of 128 tokens fills the chip as 24 pieces of 300 do.  Heads are the outermost in the list and workgroups of one XCD take
+// neighbouring parts of it, so an XCD's L2 serves the blocks that read the same rows.
+#include <algorithm>
+#include <type_traits>
+
+#include "kd_device.h"
+#include "kd_pages.h"
+#include "kd_select.h"
+
+namespace kd {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int NW = 8;                 // waves of a workgroup, 32 query rows each
+constexpr int R = 32 * NW;            // query rows of a block
+constexpr int TK = 64;                // keys of a tile
+constexpr int STAGES = 4;             // tiles in LDS: t and t + 1 in use, two on their way
+// The reference of a row's weights is put 2^LIFT above the largest logit seen and moves when one exceeds it by 2^SLACK: moving it costs a pass
+// over the outputs.  A weight is 2^SLACK at most, so sums over 2^24 rows stay below 2^127 with values of 2^100.
+constexpr float LIFT = 13.f, SLACK = 3.f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+__device__ const u32x4 zeros[64] = {};   // what rows of pages that do not exist are read from
+
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+// Lane i and lane i ^ 32 hold the two halves of a query's keys
+__device__ __forceinline__ float max_halves(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_halves(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+template <int N>
+__device__ __forceinline__ void wait_copies()   // at most N of this wave's copies still in flight
+{
+    static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+}
+
+// A block of query rows of a sequence: slot s * blocks + qb
+struct Block {
+    int s, m0, M;        // sequence; first row, and rows of the sequence in all
+    int len, last;       // rows held before the step; the last own row that a row of the block sees
+    int tiles;           // of the prompt and of own rows; 0: no row
+};
+__device__ __forceinline__ Block block_of(const ChunkParams &p, int slot)
+{
+    Block b{};
+    b.s = p.by_blocks.divide(slot);
+    b.m0 = (slot - b.s * p.blocks) * R;
+    const int len = table_entry(p.pages.lens, b.s), fresh = new_rows(len, asked_rows(p.pages, p.Bt, b.s), p.Bt);
+    b.M = fresh * p.G;
+    if (b.m0 >= b.M) return b;
+    const int n = rows_with(p.pages, len, fresh);
+    b.len = min(len, n);
+    const int j = p.by_G.divide(min(b.m0 + R, b.M) - 1);
+    b.last = (int64_t)len + j < n ? len + j : n - 1;
+    b.tiles = (p.prefix_len + TK - 1) / TK + b.last / TK + 1;
+    return b;
+}
+
+// How the list is cut: heads outermost, then the slots.  Part w of `parts` is [w total / parts, (w + 1) total / parts).
+struct Plan {
+    int per_head;        // tiles of one head's segments
+    int parts;
+};
+__device__ __forceinline__ int64_t part_begin(const ChunkParams &p, const Plan &plan, int w) { return (int64_t)w * plan.per_head * p.hkv / plan.parts; }
+__device__ __forceinline__ int part_of(const ChunkParams &p, const Plan &plan, int64_t x) { return (int)(((x + 1) * plan.parts - 1) / ((int64_t)plan.per_head * p.hkv)); }
+// As many parts as there are workgroups, but whole segments where these are about alike and fewer than the workgroups, and at
+// least MIN_TILES tiles a part: a part costs 5 us around its tiles, of which one takes 1.5.
+constexpr int MIN_TILES = 4;
+__device__ __forceinline__ int parts_of(int64_t segments, int64_t total, int wgs)
+{
+    int64_t parts = segments > 0 && segments <= wgs ? segments * (wgs / segments) : wgs;
+    if (parts > segments) parts = total / MIN_TILES < parts ? (total / MIN_TILES > segments ? total / MIN_TILES : segments) : parts;
+    return (int)parts;
+}
+
+// One segment, or a part of one: the tiles [t0, t1) of block b and KV head h.  slot < 0: all of them, the outputs are written; else the partial `slot`.
+template <int D>
+__device__ void attend(const ChunkParams &p, unsigned char *smem, const Block &b, const int h, const int t0, const int t1, const int slot)
+{
+    constexpr int NT = 64 * NW;
+    constexpr int UPR = D / 8;                // 16-byte units of a row
+    constexpr int NC = D / 16;                // chunks of the first product
+    constexpr int NDB = D / 32;               // 32-wide blocks of the output
+    constexpr int ROWB = D * 2, TILE_B = TK * ROWB;
+    constexpr int RPL = 64 / UPR;             // rows of a copy (64 lanes x 16 bytes)
+    constexpr int CPT = TK / RPL, CPW = CPT / NW, LPW = 2 * CPW;   // copies of a K tile, of a wave's share of it, and of K and V
+    constexpr int CSTEP = NW * RPL;           // rows from one copy of a wave to the next
+    constexpr int VSW = UPR / 4;
+    static_assert(CPW * NW == CPT && 2 * LPW < 64 && CSTEP % UPR == 0, "copies are dealt evenly, and their swizzles are alike");
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));   // (what follows from it is worked out here, not kept in registers across segments)
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, hh = lane >> 5;
+    const int np = (p.prefix_len + TK - 1) / TK, prefix_full = p.prefix_len / TK;
+    const int shift = p.pages.page_shift, page_mask = (1 << shift) - 1;
+    const int32_t *table = p.pages.table + (int64_t)b.s * p.pages.width;
+    const int64_t prompt = p.prefix_len > 0 ? ((int64_t)p.by_fan.divide(b.s) * p.hkv + h) * p.prefix_cap * D : 0;
+    const int ntl = t1 - t0;
+    const bool active = b.m0 + 32 * wave < b.M;   // uniform in the wave: else it only copies
+    const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
+
+    // ---- copies.  Wave w fills rows RPL w + CSTEP i of a tile; lane: row lane / UPR of these, the unit that the swizzle puts in its place.
+    const int lrow = lane / UPR, trow = RPL * wave + lrow;
+    const uint32_t koff = (uint32_t)(lrow * ROWB + ((lane % UPR) ^ (trow & (UPR - 1))) * 16);
+    const uint32_t voff = (uint32_t)(lrow * ROWB + ((lane % UPR) ^ (VSW * (trow & 3))) * 16);
+    // The page of each copy's rows, looked up a tile ahead (scalar loads); rows behind the last one stand for it
+    int page[CPW];
+    auto look_up = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < CPW; ++i) {
+            const int row = (t - np) * TK + RPL * wave + CSTEP * i;
+            page[i] = table_entry(table, t < np ? 0 : min(row, b.last) >> shift);
+        }
+    };
+    struct Source {
+        const uint16_t *k, *v;   // first row of the copy
+        bool there;
+    };
+    auto source = [&](int t, int i) {
+        Source r;
+        const int in_tile = RPL * wave + CSTEP * i;
+        if (t < np) {
+            const int64_t off = prompt + (int64_t)min(t * TK + in_tile, p.prefix_len - 1) * D;
+            r.k = p.k_prefix + off;
+            r.v = p.v_prefix + off;
+            r.there = true;
+        } else {
+            const int row = min((t - np) * TK + in_tile, b.last);
+            r.there = (uint32_t)page[i] < (uint32_t)p.pages.n_pages;
+            const int64_t off = ((((int64_t)(r.there ? page[i] : 0) * p.hkv + h) << shift) + (row & page_mask)) * D;
+            r.k = p.pages.k + off;
+            r.v = p.pages.v + off;
+        }
+        return r;
+    };
+    auto lds_of = [&](int t, int i) { return lds0 + (uint32_t)((t % STAGES) * 2 * TILE_B) + 1024u * (wave + NW * i); };
+    // copy c of tile t: c < CPW of K, else of V.  `whole`: all rows of the tile exist
+    auto copy_whole = [&](int t, int c, const Source (&src)[CPW]) {
+        const bool isv = c >= CPW;
+        const int i = isv ? c - CPW : c;
+        lds_copy16(lds_of(t, i) + (isv ? TILE_B : 0), isv ? src[i].v : src[i].k, isv ? voff : koff);
+    };
+    auto copy_any = [&](int t, int c, const Source (&src)[CPW]) {
+        const bool isv = c >= CPW;
+        const int i = isv ? c - CPW : c;
+        const int row0 = (t < np ? t : t - np) * TK + RPL * wave + CSTEP * i, last = t < np ? p.prefix_len - 1 : b.last;
+        const uint32_t unit = isv ? (lane % UPR) ^ (VSW * (trow & 3)) : (lane % UPR) ^ (trow & (UPR - 1));
+        const int ahead = max(min(row0 + lrow, last) - row0, 0);   // (rows behind the last one stand for it: finite data, masked)
+        const char *at = reinterpret_cast<const char *>(isv ? src[i].v : src[i].k) + ahead * ROWB + unit * 16;
+        if (!src[i].there) at = reinterpret_cast<const char *>(zeros) + unit * 16;   // uniform
+        lds_copy16(lds_of(t, i) + (isv ? TILE_B : 0), at);
+    };
+    auto issue_tile = [&](int t) {   // (tiles are issued in order: the pages of the next are requested behind)
+        Source src[CPW];
+#pragma unroll
+        for (int i = 0; i < CPW; ++i) src[i] = source(t, i);
+        look_up(t + 1);
+#pragma unroll
+        for (int c = 0; c < LPW; ++c) copy_any(t, c, src);
+    };
+
+    __syncthreads();   // nobody reads what the segment before has left in LDS
+    look_up(t0);
+
+    // ---- queries: whole rows, through the two buffers that tiles t0 + 2 and t0 + 3 use later, into registers
+    const int qj0 = p.by_G.divide(min(b.m0 + 32 * wave + l32, b.M - 1));
+    const int vis = ((int64_t)b.len + qj0 < b.last ? b.len + qj0 : b.last) + 1;   // own rows [0, vis) are seen
+    constexpr int QBYTES = 32 * ROWB;
+    static_assert(NW * QBYTES <= 2 * 2 * TILE_B && (2 * TILE_B) % QBYTES == 0, "the queries take two buffers");
+    const int qoff = wave * QBYTES, qhalf = qoff / (2 * TILE_B);
+    unsigned char *qwave = smem + (size_t)((t0 + 2 + qhalf) % STAGES) * 2 * TILE_B + (qoff - qhalf * 2 * TILE_B);
+#pragma unroll
+    for (int i = 0; i < QBYTES / 1024; ++i) {
+        const int r = RPL * i + lrow, m = min(b.m0 + 32 * wave + r, b.M - 1), j = p.by_G.divide(m);
+        const uint16_t *at = p.q.p + (int64_t)b.s * p.q.seq + (int64_t)(h * p.G + m - j * p.G) * p.q.head + (int64_t)j * p.q.token;
+        lds_copy16((uint32_t)(uintptr_t)qwave + 1024u * i, reinterpret_cast<const char *>(at) + (((lane % UPR) ^ (r & (UPR - 1))) * 16));
+    }
+    issue_tile(t0);
+    if (ntl > 1) issue_tile(t0 + 1);
+
+    // ---- whether all pages of the part exist
+    bool absent = false;
+    {
+        const int first = max(t0 - np, 0) * TK, end = min((t1 - np) * TK - 1, b.last);
+        if (end >= first)
+            for (int e = (first >> shift) + tid; e <= end >> shift; e += NT) absent |= (uint32_t)table[e] >= (uint32_t)p.pages.n_pages;
+    }
+    absent = __builtin_amdgcn_readfirstlane(__syncthreads_or(absent)) != 0;
+
+    if (ntl > 1) wait_copies<LPW>();   // (the queries and the first tile)
+    else wait_copies<0>();
+    bf16x8 qreg[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+        qreg[c] = as_bf16x8(*reinterpret_cast<const u32x4 *>(qwave + l32 * ROWB + (((2 * c + hh) ^ (l32 & (UPR - 1))) * 16)));
+    f32x16 oacc[NDB];
+    float mref = -INFINITY, lacc[2] = {0.f, 0.f};
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) oacc[db][e] = 0.f;
+
+    // ---- operands in LDS, as in the block step's attention: K rows as they are, V by transposing reads in the order of the accumulators
+    const int kof0 = l32 * ROWB + (hh ^ (l32 & (UPR - 1))) * 16;
+    const int i16 = lane & 15, vrow = 4 * hh + (i16 >> 2);
+    const int vof0 = vrow * ROWB + (((2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) ^ (VSW * (vrow & 3))) * 16) + (i16 & 1) * 8;
+    auto read_k = [&](const unsigned char *tK, int i) {   // operand i: keys 32 (i % 2) .., chunk i / 2
+        return as_bf16x8(*reinterpret_cast<const u32x4 *>(tK + ((kof0 ^ (i / 2 * 32)) + i % 2 * 32 * ROWB)));
+    };
+    auto read_v = [&](const unsigned char *tV, int j) {   // operand j: keys 16 (j / NDB) .., columns 32 (j % NDB) ..
+        const unsigned char *ap = tV + ((vof0 ^ (j % NDB * 64)) + j / NDB * 16 * ROWB);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)(ap));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3))) *)(ap + 8 * ROWB));
+        return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    // Tiles that every row of the block sees whole: those of the prompt but for a last one that ends early, and own ones up to the first token's row
+    const int own_full = absent ? 0 : (__builtin_amdgcn_readfirstlane((int64_t)b.len + p.by_G.divide(b.m0) < b.last ? b.len + p.by_G.divide(b.m0) : b.last) + 1) / TK;
+    auto plain = [&](int t) { return t < np ? t < prefix_full : t < np + own_full; };
+    auto plain_end = [&](int t) {   // the end of the run of such tiles that t is part of (t itself if it is none)
+        if (t < prefix_full && prefix_full < np) return prefix_full;
+        return t < prefix_full || t >= np ? max(np + own_full, t) : t;
+    };
+    // Logits that a row does not see: element e of s[kg] is key 32 kg + 8 (e / 4) + 4 hh + e % 4
+    auto mask_tile = [&](f32x16 (&s)[2], int t) {
+        uint32_t gone = 0;   // bit i: the rows 8 i .. of the tile lie on a page that does not exist
+        if (absent && t >= np) {
+#pragma unroll
+            for (int i = 0; i < TK / 8; ++i)
+                if ((uint32_t)table_entry(table, min((t - np) * TK + 8 * i, b.last) >> shift) >= (uint32_t)p.pages.n_pages) gone |= 1u << i;
+        }
+        const int lim = (t < np ? p.prefix_len - t * TK : vis - (t - np) * TK) - 4 * hh;
+#pragma unroll
+        for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                s[kg][e] = 32 * kg + 8 * (e >> 2) + (e & 3) < lim && !(gone >> (4 * kg + (e >> 2)) & 1) ? s[kg][e] : -INFINITY;
+    };
+    float mloc = -INFINITY;   // the lane's largest logit of the tile whose weights come next
+    auto new_reference = [&]() {
+        const float mtile = max_halves(mloc) * p.scale_log2e;
+        if (__builtin_amdgcn_ballot_w64(mtile > mref + SLACK) != 0) {   // rare.  (Every row whose maximum has grown moves along)
+            const float up = fmaxf(mref, mtile + LIFT);
+            const float alpha = up == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mref - up);
+            mref = up;
+            lacc[0] *= alpha;
+            lacc[1] *= alpha;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) oacc[db][e] *= alpha;
+        }
+    };
+    // The 32 exponentials of a lane and tile, in slices of two that go through three steps one beat apart: scale and shift, exponential,
+    // rounding to bf16 and sum.  The weights are rounded to one bf16 number (half a step of 2^-8 each, independent of one another: less than the
+    // rounding of the output in all but rows of very few keys), their sum is that of the floats: the logarithm that the call returns is exact to float.
+    auto slice_F = [&](const f32x16 (&s)[2], int i, float (&arg)[2]) {
+        const float nm = mref == -INFINITY ? 0.f : -mref;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            arg[r] = __builtin_fmaf(s[i >> 3][2 * (i & 7) + r], p.scale_log2e, nm);
+            asm volatile("" : "+v"(arg[r]));   // computed here, not where the optimiser finds its use
+        }
+    };
+    auto slice_E = [&](const float (&arg)[2], float (&ex)[2]) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            ex[r] = __builtin_amdgcn_exp2f(arg[r]);
+            asm volatile("" : "+v"(ex[r]));
+        }
+    };
+    auto slice_C = [&](const float (&ex)[2], int i, bf16x8 (&pk)[4]) {
+        pk[i >> 2][2 * (i & 3)] = (__bf16)ex[0];
+        pk[i >> 2][2 * (i & 3) + 1] = (__bf16)ex[1];
+        lacc[0] += ex[0];
+        lacc[1] += ex[1];
+    };
+
+    f32x16 s[2], s2[2];
+    __syncthreads();   // every wave has its queries and its part of tile t0 is in LDS; the buffers of the queries are free
+    if (ntl > 2) issue_tile(t0 + 2);
+    if (active) {
+        const unsigned char *tK = smem + (size_t)(t0 % STAGES) * 2 * TILE_B;
+#pragma unroll
+        for (int i = 0; i < 2 * NC; ++i)
+            s[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_k(tK, i), qreg[i / 2], i < 2 ? zero : s[i % 2], 0, 0, 0);
+        if (!plain(t0)) mask_tile(s, t0);
+        mloc = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mloc = max3(mloc, s[0][e], s[1][e]);
+    }
+    // ---- the loop, software pipelined by hand as the block step's: iteration t forms the logits of tile t + 1 beside the weights of tile t (stage
+    // A), then the outputs of tile t beside the rest of its weights and the maxima of tile t + 1 (stage B).  Two waves share a
+    // SIMD and little else hides a latency; the scheduling barriers pin the order.
+    auto open_step = [&](int t) {   // tile t + 1 has landed, and every wave is through with tile t - 1
+        if (t + 2 < t1) wait_copies<LPW>();
+        else wait_copies<0>();
+        __syncthreads();
+    };
+    // NEXT: there is a tile t + 1; PLAIN: tiles t + 1 and t + 3 exist and are plain
+    auto step = [&](int t, f32x16 (&sc)[2], f32x16 (&sn)[2], auto next_tag, auto plain_tag) {
+        constexpr bool NEXT = decltype(next_tag)::value, PLAIN = decltype(plain_tag)::value;
+        constexpr int NA = 2 * NC, NB = 4 * NDB;
+        static_assert((NA == 16 && NB == 16) || (NA == 8 && NB == 8), "the slices below are dealt to this many products");
+        constexpr int REF = NEXT ? NA * 3 / 16 : 0;   // products of stage A ahead of the reference of tile t
+        constexpr int NS = 16;                        // slices of a tile
+        constexpr int SLOTS = NEXT ? NA + NB * 3 / 4 : NA + NB / 2;
+        constexpr int SPG = NS > SLOTS ? 2 : 1, NG = NS / SPG;
+        auto slot_of = [](int g) { return REF + g * (SLOTS - REF) / NG; };
+        auto beat = [&](int g, float (&arg)[2][SPG][2], float (&ex)[2][SPG][2], bf16x8 (&pk)[4]) {
+            if (g < NG) {
+#pragma unroll
+                for (int e = 0; e < SPG; ++e) slice_E(arg[g & 1][e], ex[g & 1][e]);
+            }
+            if (g > 0) {
+#pragma unroll
+                for (int e = 0; e < SPG; ++e) slice_C(ex[(g - 1) & 1][e], SPG * (g - 1) + e, pk);
+            }
+            if (g + 1 < NG) {
+#pragma unroll
+                for (int e = 0; e < SPG; ++e) slice_F(sc, SPG * (g + 1) + e, arg[(g + 1) & 1][e]);
+            }
+        };
+        constexpr int KAHEAD = 2, VAHEAD = 2;   // operands are read this many products ahead
+        const unsigned char *tV = smem + (size_t)(t % STAGES) * 2 * TILE_B + TILE_B;
+        const unsigned char *tK = smem + (size_t)((t + 1) % STAGES) * 2 * TILE_B;
+        bf16x8 pk[4], kf[KAHEAD + 1], vf[VAHEAD + 1];
+        float arg[2][SPG][2], ex[2][SPG][2];
+        Source src[CPW];
+        const bool fetch = PLAIN || (NEXT && t + STAGES - 1 < t1);
+        if (NEXT) {
+            open_step(t);
+            if (fetch) {
+#pragma unroll
+                for (int i = 0; i < CPW; ++i) src[i] = source(t + STAGES - 1, i);
+                look_up(t + STAGES);
+            }
+#pragma unroll
+            for (int i = 0; i < KAHEAD; ++i) kf[i] = read_k(tK, i);
+        }
+        auto first_arguments = [&]() {
+            new_reference();
+#pragma unroll
+            for (int e = 0; e < SPG; ++e) slice_F(sc, e, arg[0][e]);
+        };
+        if (!NEXT) first_arguments();
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            if (NEXT) {
+                if (i + KAHEAD < NA) kf[(i + KAHEAD) % (KAHEAD + 1)] = read_k(tK, i + KAHEAD);
+                sn[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % (KAHEAD + 1)], qreg[i / 2], i < 2 ? zero : sn[i % 2], 0, 0, 0);
+            }
+            if (i >= NA - VAHEAD) vf[i - (NA - VAHEAD)] = read_v(tV, i - (NA - VAHEAD));
+            if (NEXT) {
+#pragma unroll
+                for (int c = i * LPW / NA; c < (i + 1) * LPW / NA; ++c) {
+                    if (PLAIN) copy_whole(t + STAGES - 1, c, src);
+                    else if (fetch) copy_any(t + STAGES - 1, c, src);
+                }
+            }
+            if (NEXT && i == REF - 1) first_arguments();
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+                if (slot_of(g) == i) beat(g, arg, ex, pk);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (NEXT && !PLAIN && !plain(t + 1)) mask_tile(sn, t + 1);   // uniform
+        float mch[2];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            if (j + VAHEAD < NB) vf[(j + VAHEAD) % (VAHEAD + 1)] = read_v(tV, j + VAHEAD);
+#pragma unroll
+            for (int g = 0; g <= NG; ++g)
+                if ((g < NG ? slot_of(g) : slot_of(NG - 1) + 1) == NA + j) beat(g, arg, ex, pk);
+            oacc[j % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j % (VAHEAD + 1)], pk[j / NDB], oacc[j % NDB], 0, 0, 0);
+            if (NEXT) {
+                constexpr int PER = 16 / NB;
+#pragma unroll
+                for (int r = 0; r < PER; ++r) {
+                    const int e = PER * j + r;
+                    mch[e & 1] = e < 2 ? fmaxf(sn[0][e], sn[1][e]) : max3(mch[e & 1], sn[0][e], sn[1][e]);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (NEXT) {
+            mloc = fmaxf(mch[0], mch[1]);
+            asm volatile("" : "+v"(mloc));   // (here, and not where its result is used)
+        }
+    };
+    using T_ = std::true_type;
+    using F_ = std::false_type;
+    int t = t0;
+    if (!active) {   // a wave without query rows: its share of the copies
+        for (; t + 1 < t1; ++t) {
+            open_step(t);
+            if (t + STAGES - 1 < t1) issue_tile(t + STAGES - 1);
+        }
+    } else {
+        while (t + 1 < t1) {
+            const int lim = min(plain_end(t + 1), t1);
+            for (; t + STAGES < lim; t += 2) {
+                step(t, s, s2, T_{}, T_{});
+                step(t + 1, s2, s, T_{}, T_{});
+            }
+            if (t + 1 < t1) {
+                step(t, s, s2, T_{}, F_{});
+                s[0] = s2[0];
+                s[1] = s2[1];
+                ++t;
+            }
+        }
+        step(t, s, s2, F_{}, F_{});
+    }
+
+    // ---- results.  A lane holds the sum of its own keys: the other half is with lane ^ 32
+    const float L = sum_halves(lacc[0] + lacc[1]), inv = L > 0.f ? 1.f / L : 0.f;   // (a row may see no key at all: zero)
+    const int64_t head = (int64_t)b.s * p.hkv * p.G + h * p.G;
+    if (slot >= 0) {
+        // In the accumulators' own layout, whole kilobytes a store; the join reads them in the same order.
+        if (active) {
+            float *base = p.part_o + (((int64_t)slot * (p.part_rows / 32) + wave) * (D / 8) * 64 + lane) * 4;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int jj = 0; jj < 4; ++jj) {
+                    f32x4 o;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[r] = oacc[db][4 * jj + r] * inv;
+                    *reinterpret_cast<f32x4 *>(base + (size_t)(4 * db + jj) * 64 * 4) = o;
+                }
+            // (a piece without a key has the reference -inf; one whose logits are all NaN has none either, and its NaN must not be lost)
+            if (hh == 0) p.part_ml[(int64_t)slot * p.part_rows + 32 * wave + l32] = make_float2(L == L ? mref : 0.f, L);
+        }
+        return;
+    }
+    // A wave turns its rows in LDS and stores them whole.  (Buffers that no tile has occupied since the last barrier: all waves are past tile t1 - 2,
+    // and tiles t1 - 1 and t1 - 2 occupy the other two.)
+    if (!active) return;
+    auto stage = [&](int off) {
+        const int half = off / (2 * TILE_B);
+        return smem + (size_t)((t1 + 1 - half + STAGES) % STAGES) * 2 * TILE_B + (off - half * 2 * TILE_B);
+    };
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) {
+            bf16x4 o;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = (__bf16)(oacc[db][4 * jj + r] * inv);
+            *reinterpret_cast<bf16x4 *>(stage(wave * QBYTES + l32 * ROWB + (((4 * db + jj) ^ (l32 & (UPR - 1))) * 16) + 8 * hh)) = o;
+        }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int i = 0; i < QBYTES / 1024; ++i) {
+        const int r = RPL * i + lrow, m = b.m0 + 32 * wave + r, j = p.by_G.divide(min(m, b.M - 1));
+        const u32x4 val = *reinterpret_cast<const u32x4 *>(stage(wave * QBYTES + r * ROWB + (((lane % UPR) ^ (r & (UPR - 1))) * 16)));
+        if (m < b.M) *reinterpret_cast<u32x4 *>(p.out + ((head + m - j * p.G) * p.Bt + j) * D + lane % UPR * 8) = val;
+    }
+    const int m = b.m0 + 32 * wave + l32, j = p.by_G.divide(min(m, b.M - 1));
+    if (hh == 0 && m < b.M) p.lse[(head + m - j * p.G) * p.Bt + j] = L == 0.f ? -INFINITY : (mref + __builtin_amdgcn_logf(L)) * LN2;
+}
+
+template <int D>
+constexpr int lds_bytes() { return STAGES * 2 * TK * D * 2; }
+
+// One launch, a workgroup a segment: where no segment can have many tiles
+template <int D>
+__global__ __launch_bounds__(64 * NW) void chunk_whole_kernel(ChunkParams)
+{
+    warm_arguments<sizeof(ChunkParams)>();
+    const ChunkParams &p = argument_at<ChunkParams>(0);   // (read where it is needed)
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[lds_bytes<D>()];
+    const int h = p.by_slots.divide(blockIdx.x), slot = (int)blockIdx.x - h * p.slots;
+    const Block b = block_of(p, slot);
+    if (b.tiles == 0) return;   // uniform
+    attend<D>(p, smem, b, h, 0, b.tiles, -1);
+}
+
+// Where a part goes on: tile t of (KV head, slot), `left` tiles, second: it has been at another segment before
+struct Place {
+    int h, slot, t, left, second;
+};
+// The list of tiles cut into parts
+template <int D>
+__global__ __launch_bounds__(64 * NW) void chunk_parts_kernel(ChunkParams)
+{
+    warm_arguments<sizeof(ChunkParams)>();
+    const ChunkParams &p = argument_at<ChunkParams>(0);   // (read where it is needed)
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[lds_bytes<D>()];
+    __shared__ int wave_tiles[NW], wave_used[NW];
+    __shared__ Place place;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wgs = (int)gridDim.x;
+    // workgroups go round the XCDs: those of one XCD take neighbouring parts
+    const int w = wgs % 8 == 0 ? (int)blockIdx.x % 8 * (wgs / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;
+    // every thread the tiles of `each` slots, then sums over the threads
+    const int each = (p.slots + 64 * NW - 1) / (64 * NW), first = tid * each;
+    int mine = 0, used = 0;
+    for (int i = 0; i < each; ++i)
+        if (first + i < p.slots) {
+            const int tiles = block_of(p, first + i).tiles;
+            mine += tiles;
+            used += tiles > 0;
+        }
+    const int upto = (int)wave_inclusive_scan((uint32_t)mine), used_upto = (int)wave_inclusive_scan((uint32_t)used);
+    if (lane == 63) {
+        wave_tiles[wave] = upto;
+        wave_used[wave] = used_upto;
+    }
+    __syncthreads();
+    int before = upto - mine, segments = 0;
+    Plan plan{0, 1};
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+        if (i < wave) before += wave_tiles[i];
+        plan.per_head += wave_tiles[i];
+        segments += wave_used[i];
+    }
+    if (plan.per_head == 0) return;   // uniform: the join finds nothing either
+    plan.parts = parts_of((int64_t)segments * p.hkv, (int64_t)plan.per_head * p.hkv, wgs);
+    if (blockIdx.x == 0) {   // for the join
+        if (tid == 0) {
+            p.plan[0] = plan.per_head;
+            p.plan[1] = plan.parts;
+        }
+        int at = before;
+        for (int i = 0; i < each; ++i)
+            if (first + i < p.slots) {
+                p.plan[CHUNK_PLAN_WORDS + first + i] = at;
+                at += block_of(p, first + i).tiles;
+            }
+    }
+    if (w >= plan.parts) return;
+    {
+        const int64_t begin = part_begin(p, plan, w);
+        const int h = (int)(begin / plan.per_head), from = (int)(begin - (int64_t)h * plan.per_head);
+        if (from >= before && from < before + mine) {   // one thread's
+            int at = before, slot = first;
+            for (;; ++slot) {
+                const int tiles = block_of(p, slot).tiles;
+                if (from < at + tiles) break;
+                at += tiles;
+            }
+            place = Place{h, slot, from - at, (int)(part_begin(p, plan, w + 1) - begin), 0};
+        }
+    }
+    __syncthreads();
+    for (;;) {   // (where the part goes on is kept in LDS: the loop over the tiles has no scalar registers to spare)
+        const int h = __builtin_amdgcn_readfirstlane(place.h), slot = __builtin_amdgcn_readfirstlane(place.slot), t = __builtin_amdgcn_readfirstlane(place.t);
+        const int left = __builtin_amdgcn_readfirstlane(place.left), second = __builtin_amdgcn_readfirstlane(place.second);
+        if (left == 0) return;   // uniform
+        const Block b = block_of(p, slot);
+        const int take = min(b.tiles - t, left);
+        __syncthreads();
+        if (tid == 0) place = slot + 1 == p.slots ? Place{h + 1, 0, 0, left - take, second | (take > 0)} : Place{h, slot + 1, 0, left - take, second | (take > 0)};
+        if (take > 0) attend<D>(p, smem, b, h, t, t + take, take == b.tiles ? -1 : 2 * w + second);
+        __syncthreads();
+    }
+}
+
+// Joins the partials of the segments that were cut: a workgroup 32 rows of one
+template <int D>
+__global__ __launch_bounds__(256) void chunk_join_kernel(ChunkParams p)
+{
+    const int per = p.part_rows / 32, id = (int)blockIdx.x / per, wave = (int)blockIdx.x - id * per;
+    const int h = p.by_slots.divide(id), slot = id - h * p.slots;
+    const Block b = block_of(p, slot);
+    if (b.tiles == 0 || b.m0 + 32 * wave >= b.M) return;
+    const Plan plan{p.plan[0], p.plan[1]};
+    const int64_t x0 = (int64_t)h * plan.per_head + p.plan[CHUNK_PLAN_WORDS + slot], x1 = x0 + b.tiles;
+    const int w0 = part_of(p, plan, x0), w1 = part_of(p, plan, x1 - 1);
+    if (w0 == w1) return;
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5, group = threadIdx.x >> 6;
+    const int64_t first = 2 * (int64_t)w0 + (part_begin(p, plan, w0) != x0);
+    auto slot_at = [&](int w) { return w == w0 ? first : 2 * (int64_t)w; };
+    float top = -INFINITY, L = 0.f;
+    for (int w = w0; w <= w1; ++w) top = fmaxf(top, p.part_ml[slot_at(w) * p.part_rows + 32 * wave + l32].x);
+    constexpr int SLABS = D / 8, MINE = SLABS / 4;
+    f32x4 acc[MINE];
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int w = w0; w <= w1; ++w) {
+        const float2 ml = p.part_ml[slot_at(w) * p.part_rows + 32 * wave + l32];
+        const float f = ml.x == -INFINITY ? 0.f : ml.y * __builtin_amdgcn_exp2f(ml.x - top);
+        const float *base = p.part_o + ((slot_at(w) * per + wave) * SLABS * 64 + lane) * 4;
+        L += f;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) acc[i] += f * *reinterpret_cast<const f32x4 *>(base + (size_t)(group + 4 * i) * 64 * 4);
+    }
+    const int m = b.m0 + 32 * wave + l32;
+    if (m >= b.M) return;
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+    const int j = p.by_G.divide(m), g = m - j * p.G;
+    const int64_t row = ((int64_t)b.s * p.hkv * p.G + h * p.G + g) * p.Bt + j;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+        bf16x4 o;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] = (__bf16)(acc[i][r] * inv);
+        *reinterpret_cast<bf16x4 *>(p.out + row * D + 8 * (group + 4 * i) + 4 * hh) = o;
+    }
+    if (group == 0 && hh == 0) p.lse[row] = L == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(L)) * LN2;
+}
+
+// Tiles that a segment can have at most
+int64_t most_tiles(int prefix_len, int64_t table_rows) { return (prefix_len + TK - 1) / TK + (table_rows + TK - 1) / TK; }
+
+}  // namespace
+
+int chunk_block_rows() { return R; }
+
+// Cut segments leave two partials a workgroup
+size_t chunk_workspace(int n_seqs, int hkv, int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_plan)
+{
+    const int64_t rows = std::min<int64_t>(R, ((int64_t)G * Bt + 31) / 32 * 32), blocks = ((int64_t)G * Bt + R - 1) / R;
+    size_t off = (size_t)2 * cus * rows * D * 4;
+    *off_ml = off;
+    off += ((size_t)2 * cus * rows * 8 + 255) & ~(size_t)255;
+    *off_plan = off;
+    off += ((size_t)(CHUNK_PLAN_WORDS + n_seqs * blocks) * 4 + 255) & ~(size_t)255;
+    return off;
+}
+
+namespace {
+
+template <int D>
+hipError_t launch(const ChunkParams &p, hipStream_t s)
+{
+    const int64_t segments = (int64_t)p.slots * p.hkv;
+    if (most_tiles(p.prefix_len, (int64_t)p.pages.width << p.pages.page_shift) <= 2 * MIN_TILES) {
+        hipLaunchKernelGGL((chunk_whole_kernel<D>), dim3((unsigned)segments), dim3(64 * NW), 0, s, p);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((chunk_parts_kernel<D>), dim3(p.cus), dim3(64 * NW), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((chunk_join_kernel<D>), dim3((unsigned)(segments * (p.part_rows / 32))), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_branch_chunk(ChunkParams p, hipStream_t s)
+{
+    const int64_t M = (int64_t)p.G * p.Bt;
+    p.blocks = (int32_t)((M + R - 1) / R);
+    p.slots = p.n_seqs * p.blocks;
+    p.part_rows = (int32_t)std::min<int64_t>(R, (M + 31) / 32 * 32);
+    p.by_blocks.set((uint32_t)p.blocks);
+    p.by_slots.set((uint32_t)p.slots);
+    p.by_G.set((uint32_t)p.G);
+    p.by_fan.set((uint32_t)std::max(p.fan, 1));
+    return p.D == 128 ? launch<128>(p, s) : p.D == 64 ? launch<64>(p, s) : hipErrorInvalidValue;
+}
+
+}  // namespace kd

@@ -1,4 +1,4 @@
-// Python's side of norm_rope, branch_append and branch_attention: checks of the tensors, allocation of what the caller does not give, and the
+// Python's side of norm_rope, branch_append, branch_attention and of the calls that go with them: checks of the tensors, allocation of what the caller does not give, and the
 // call of the C ABI (include/keydiff.h), whose entry points the package hands over once (`bind`).  No arithmetic lives here.  A function returns
 // its tensors, or the error code of the C ABI as a number.
 //
@@ -12,6 +12,7 @@
 
 #include <stdexcept>
 #include <string>
+#include <type_traits>
 
 #include "../../include/keydiff.h"
 
@@ -22,6 +23,13 @@ decltype(&keydiff_branch_append) append_abi;
 decltype(&keydiff_branch_workspace_bytes) workspace_abi;
 decltype(&keydiff_branch_attention) attention_abi;
 decltype(&keydiff_cache_branch_attention) cache_attention_abi;
+decltype(&keydiff_branch_chunk_workspace_bytes) chunk_workspace_abi;
+decltype(&keydiff_branch_chunk_attention) chunk_abi;
+decltype(&keydiff_cache_branch_chunk_attention) cache_chunk_abi;
+decltype(&keydiff_branch_weights_workspace_bytes) weights_workspace_abi;
+decltype(&keydiff_branch_weights) weights_abi;
+decltype(&keydiff_branch_evict_workspace_bytes) evict_workspace_abi;
+decltype(&keydiff_branch_evict) evict_abi;
 PyObject *current_stream;   // torch's function: device index -> handle of the current stream
 
 struct Refused : std::runtime_error {   // becomes a ValueError
@@ -122,7 +130,7 @@ struct Checked {
         if (table.size(1) > INT32_MAX) throw Refused("table is too large: " + what_is(table));
         keydiff_branches_t b{};
         b.k_pages = dense("k_pages", pages, pages.sizes(), at::kBFloat16);
-        b.v_pages = dense("v_pages", tensor_of(v_pages, "v_pages"), pages.sizes(), at::kBFloat16);
+        if (v_pages) b.v_pages = dense("v_pages", tensor_of(v_pages, "v_pages"), pages.sizes(), at::kBFloat16);
         b.table = static_cast<const int32_t *>(dense("table", table, {n, table.size(1)}, at::kInt));
         b.lens = static_cast<const int32_t *>(dense("lens", tensor_of(lens, "lens"), {n}, at::kInt));
         b.n_new = static_cast<const int32_t *>(dense_or_null("n_new", n_new, {n}, at::kInt));
@@ -250,12 +258,55 @@ PyObject *branch_append(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     KD_END
 }
 
-// q, k_pages, v_pages, table, lens, n_new, the handle of the prefix's cache (None: no cache), its batch, prefix keys and values (None: no rows), rows,
-// softmax_scale, out, workspace
-PyObject *branch_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+// The rows that sequences share: those of a cache (its handle and batch), or tensors
+struct Prefix {
+    bool cached;
+    const void *k = nullptr, *v = nullptr;
+    int64_t prompts, rows = 0, cap = 0;
+
+    // a: handle (None: no cache), batch, keys and values (None: no rows), rows
+    Prefix(const Checked &on, PyObject *const *a, int64_t hkv, int64_t d) : cached(a[0] != Py_None), prompts(cached ? whole(a[1]) : 0)
+    {
+        if (a[2] == Py_None) return;
+        const at::Tensor &keys = tensor_of(a[2], "prefix keys");
+        four("prefix keys", keys);
+        prompts = keys.size(0);
+        cap = keys.size(2);
+        rows = whole(a[4]);
+        if (rows < 0 || rows > cap) throw Refused("the prefix has " + std::to_string(cap) + " rows a head, " + std::to_string(rows) + " are to be read");
+        k = on.dense("prefix keys", keys, {prompts, hkv, cap, d}, at::kBFloat16);
+        v = on.dense("prefix values", tensor_of(a[3], "prefix values"), {prompts, hkv, cap, d}, at::kBFloat16);
+    }
+};
+
+double number(PyObject *o)
 {
-    KD_TRY
-    arguments(n_args, 14);
+    const double x = PyFloat_AsDouble(o);
+    if (PyErr_Occurred()) throw python_error();
+    return x;
+}
+
+int32_t small(const char *name, PyObject *o)
+{
+    const int64_t v = whole(o);
+    if (v < INT32_MIN || v > INT32_MAX) throw Refused(std::string(name) + " is too large: " + std::to_string(v));
+    return (int32_t)v;
+}
+
+// The caller's workspace, or a new one
+at::Tensor workspace_of(const Checked &on, PyObject *o, size_t need, const at::Tensor &like)
+{
+    if (o == Py_None) return at::empty({(int64_t)need}, like.options().dtype(at::kByte));
+    const at::Tensor &work = tensor_of(o, "workspace");
+    if (work.scalar_type() != at::kByte || !work.is_contiguous() || (size_t)work.numel() < need || work.device() != on.device)
+        throw Refused("workspace must be a contiguous uint8 tensor of at least " + std::to_string(need) + " elements on " + on.device.str());
+    return work;
+}
+
+// q, k_pages, v_pages, table, lens, n_new, the handle of the prefix's cache (None: no cache), its batch, prefix keys and values (None: no rows), rows,
+// softmax_scale, out, workspace; chunk: and lse
+PyObject *attention(PyObject *const *a, bool chunk)
+{
     const at::Tensor &q = tensor_of(a[0], "q"), &pages = tensor_of(a[1], "k_pages");
     four("q", q);
     four("k_pages", pages);
@@ -264,59 +315,127 @@ PyObject *branch_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     const keydiff_rows_t rq = on.rows("q", q, n, hq, Bt, d);
     const keydiff_branches_t b = on.branches(n, hq, hkv, d, a[1], a[2], a[3], a[4], a[5]);
     void *out = on.dense_or_null("out", a[12], {n, hq, Bt, d}, at::kBFloat16);
-    const bool cached = a[6] != Py_None;
-    const void *kp = nullptr, *vp = nullptr;
-    int64_t prompts = cached ? whole(a[7]) : 0, rows = 0, cap = 0;
-    if (a[8] != Py_None) {
-        const at::Tensor &keys = tensor_of(a[8], "prefix keys");
-        four("prefix keys", keys);
-        prompts = keys.size(0);
-        cap = keys.size(2);
-        rows = whole(a[10]);
-        if (rows < 0 || rows > cap) throw Refused("the prefix has " + std::to_string(cap) + " rows a head, " + std::to_string(rows) + " are to be read");
-        kp = on.dense("prefix keys", keys, {prompts, hkv, cap, d}, at::kBFloat16);
-        vp = on.dense("prefix values", tensor_of(a[9], "prefix values"), {prompts, hkv, cap, d}, at::kBFloat16);
-    }
-    const double scale = PyFloat_AsDouble(a[11]);
-    if (PyErr_Occurred()) throw python_error();
-    if (cached && !(scale <= 0)) throw Refused("softmax_scale is the cache's");
+    float *lse = chunk ? static_cast<float *>(on.dense_or_null("lse", a[14], {n, hq, Bt}, at::kFloat)) : nullptr;
+    const Prefix prefix(on, a + 6, hkv, d);
+    const double scale = number(a[11]);
+    if (prefix.cached && !(scale <= 0)) throw Refused("softmax_scale is the cache's");
     on.on_gpu();
     const c10::DeviceGuard guard(on.device);
     size_t need = 0;
-    if (const int rc = workspace_abi(&b, (int32_t)Bt, (int32_t)prompts, &need)) return PyLong_FromLong(rc);
-    at::Tensor work, made;
-    if (a[13] == Py_None) {
-        work = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
-    } else {
-        work = tensor_of(a[13], "workspace");
-        if (work.scalar_type() != at::kByte || !work.is_contiguous() || (size_t)work.numel() < need || work.device() != on.device)
-            throw Refused("workspace must be a contiguous uint8 tensor of at least " + std::to_string(need) + " elements on " + on.device.str());
-    }
+    if (const int rc = (chunk ? chunk_workspace_abi : workspace_abi)(&b, (int32_t)Bt, (int32_t)prefix.prompts, &need)) return PyLong_FromLong(rc);
+    const at::Tensor work = workspace_of(on, a[13], need, q);
+    at::Tensor made, made_lse;
     if (!out) out = (made = at::empty({n, hq, Bt, d}, q.options())).data_ptr();
-    void *stream = on.stream();
-    const int rc = cached ? cache_attention_abi(static_cast<keydiff_cache_t *>(PyLong_AsVoidPtr(a[6])), &b, &rq, (int32_t)Bt, out, work.data_ptr(),
-                                                (size_t)work.numel(), stream)
-                          : attention_abi(&b, &rq, (int32_t)Bt, kp, vp, (int32_t)prompts, (int32_t)rows, cap, (float)scale, out, work.data_ptr(),
-                                          (size_t)work.numel(), stream);
+    if (chunk && !lse) lse = static_cast<float *>((made_lse = at::empty({n, hq, Bt}, q.options().dtype(at::kFloat))).data_ptr());
+    void *stream = on.stream(), *ws = work.data_ptr();
+    const size_t bytes = (size_t)work.numel();
+    keydiff_cache_t *cache = prefix.cached ? static_cast<keydiff_cache_t *>(PyLong_AsVoidPtr(a[6])) : nullptr;
+    const int32_t T = (int32_t)Bt, prompts = (int32_t)prefix.prompts, rows = (int32_t)prefix.rows;
+    int rc;
+    if (chunk)
+        rc = prefix.cached ? cache_chunk_abi(cache, &b, &rq, T, out, lse, ws, bytes, stream)
+                           : chunk_abi(&b, &rq, T, prefix.k, prefix.v, prompts, rows, prefix.cap, (float)scale, out, lse, ws, bytes, stream);
+    else
+        rc = prefix.cached ? cache_attention_abi(cache, &b, &rq, T, out, ws, bytes, stream)
+                           : attention_abi(&b, &rq, T, prefix.k, prefix.v, prompts, rows, prefix.cap, (float)scale, out, ws, bytes, stream);
     if (rc != KEYDIFF_OK) return PyLong_FromLong(rc);
-    return given_or(a[12], made);
+    if (!chunk) return given_or(a[12], made);
+    PyObject *x = given_or(a[12], made), *y = given_or(a[14], made_lse), *both = x && y ? PyTuple_Pack(2, x, y) : nullptr;
+    Py_XDECREF(x);
+    Py_XDECREF(y);
+    return both;
+}
+
+PyObject *branch_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    KD_TRY
+    arguments(n_args, 14);
+    return attention(a, false);
     KD_END
 }
 
-// Addresses of keydiff_norm_rope, _branch_append, _branch_workspace_bytes, _branch_attention, _cache_branch_attention; torch's current-stream function
+PyObject *branch_chunk_attention(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    KD_TRY
+    arguments(n_args, 15);
+    return attention(a, true);
+    KD_END
+}
+
+// q, k_pages, w_pages, table, lens, lse, n_new, observe, decay, softmax_scale, workspace
+PyObject *branch_weights(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    KD_TRY
+    arguments(n_args, 11);
+    const at::Tensor &q = tensor_of(a[0], "q"), &pages = tensor_of(a[1], "k_pages");
+    four("q", q);
+    four("k_pages", pages);
+    const int64_t n = q.size(0), hq = q.size(1), Bt = q.size(2), d = q.size(3), hkv = pages.size(1);
+    const Checked on{q.device()};
+    const keydiff_rows_t rq = on.rows("q", q, n, hq, Bt, d);
+    const keydiff_branches_t b = on.branches(n, hq, hkv, d, a[1], nullptr, a[3], a[4], a[6]);
+    float *w = static_cast<float *>(on.dense("w_pages", tensor_of(a[2], "w_pages"), {pages.size(0), hkv, pages.size(2)}, at::kFloat));
+    const float *lse = static_cast<const float *>(on.dense("lse", tensor_of(a[5], "lse"), {n, hq, Bt}, at::kFloat));
+    const int32_t observe = small("observe", a[7]);
+    const double decay = number(a[8]), scale = number(a[9]);
+    on.on_gpu();
+    const c10::DeviceGuard guard(on.device);
+    size_t need = 0;
+    if (const int rc = weights_workspace_abi(&b, (int32_t)Bt, observe, &need)) return PyLong_FromLong(rc);
+    const at::Tensor work = workspace_of(on, a[10], need, q);
+    return PyLong_FromLong(weights_abi(&b, &rq, (int32_t)Bt, lse, w, observe, (float)decay, (float)scale, work.data_ptr(), (size_t)work.numel(), on.stream()));
+    KD_END
+}
+
+// k_pages, v_pages, w_pages, p_pages, table, lens, budget, Bt, n_new, pos0, window, status, workspace
+PyObject *branch_evict(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    KD_TRY
+    arguments(n_args, 13);
+    const at::Tensor &pages = tensor_of(a[0], "k_pages"), &table = tensor_of(a[4], "table");
+    four("k_pages", pages);
+    if (table.dim() != 2) throw Refused("table must be [sequences][width], got " + what_is(table));
+    if (table.size(0) > INT32_MAX) throw Refused("table is too large: " + what_is(table));
+    const int64_t n = table.size(0), hkv = pages.size(1);
+    const Checked on{pages.device()};
+    const keydiff_branches_t b = on.branches(n, hkv, hkv, pages.size(3), a[0], a[1], a[4], a[5], a[8]);
+    float *w = static_cast<float *>(on.dense("w_pages", tensor_of(a[2], "w_pages"), {pages.size(0), hkv, pages.size(2)}, at::kFloat));
+    int32_t *positions = static_cast<int32_t *>(on.dense("p_pages", tensor_of(a[3], "p_pages"), {pages.size(0), hkv, pages.size(2)}, at::kInt));
+    const int32_t budget = small("budget", a[6]), Bt = small("Bt", a[7]), window = small("window", a[10]);
+    const int32_t *pos0 = static_cast<const int32_t *>(on.dense_or_null("pos0", a[9], {n}, at::kInt));
+    int32_t *status = static_cast<int32_t *>(on.dense_or_null("status", a[11], {1}, at::kInt));
+    on.on_gpu();
+    const c10::DeviceGuard guard(on.device);
+    size_t need = 0;
+    if (const int rc = evict_workspace_abi(&b, budget, &need)) return PyLong_FromLong(rc);
+    const at::Tensor work = workspace_of(on, a[12], need, pages);
+    return PyLong_FromLong(evict_abi(&b, Bt, w, positions, pos0, budget, window, status, work.data_ptr(), (size_t)work.numel(), on.stream()));
+    KD_END
+}
+
+// Addresses of the entry points in the order of their declaration above; torch's current-stream function
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     KD_TRY
-    arguments(n, 6);
-    norm_rope_abi = reinterpret_cast<decltype(norm_rope_abi)>(PyLong_AsVoidPtr(a[0]));
-    append_abi = reinterpret_cast<decltype(append_abi)>(PyLong_AsVoidPtr(a[1]));
-    workspace_abi = reinterpret_cast<decltype(workspace_abi)>(PyLong_AsVoidPtr(a[2]));
-    attention_abi = reinterpret_cast<decltype(attention_abi)>(PyLong_AsVoidPtr(a[3]));
-    cache_attention_abi = reinterpret_cast<decltype(cache_attention_abi)>(PyLong_AsVoidPtr(a[4]));
+    arguments(n, 13);
+    int i = 0;
+    auto take = [&](auto &f) { f = reinterpret_cast<std::decay_t<decltype(f)>>(PyLong_AsVoidPtr(a[i++])); };
+    take(norm_rope_abi);
+    take(append_abi);
+    take(workspace_abi);
+    take(attention_abi);
+    take(cache_attention_abi);
+    take(chunk_workspace_abi);
+    take(chunk_abi);
+    take(cache_chunk_abi);
+    take(weights_workspace_abi);
+    take(weights_abi);
+    take(evict_workspace_abi);
+    take(evict_abi);
     if (PyErr_Occurred()) throw python_error();
-    Py_INCREF(a[5]);
+    Py_INCREF(a[i]);
     Py_XDECREF(current_stream);
-    current_stream = a[5];
+    current_stream = a[i];
     Py_RETURN_NONE;
     KD_END
 }
@@ -333,7 +452,9 @@ PyObject *row_form(PyObject *, PyObject *const *a, Py_ssize_t n)
 }
 
 #define KD_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {KD_METHOD(bind), KD_METHOD(row_form), KD_METHOD(norm_rope), KD_METHOD(branch_append), KD_METHOD(branch_attention), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {KD_METHOD(bind), KD_METHOD(row_form), KD_METHOD(norm_rope), KD_METHOD(branch_append),
+                         KD_METHOD(branch_attention),
+                         KD_METHOD(branch_chunk_attention), KD_METHOD(branch_weights), KD_METHOD(branch_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

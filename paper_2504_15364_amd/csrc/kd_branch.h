@@ -76,6 +76,7 @@ struct Divisor {
 struct BranchParams {
     Rows q;
     uint16_t *out;                        // [n_seqs][hq][Bt][D]
+    float *lse;                           // nullable, [n_seqs][hq][Bt]: logarithms of the weight sums
     const uint16_t *k_prefix, *v_prefix;  // [n_prefixes][hkv][prefix_cap][D]
     Pages pages;
     float *part_o;                        // partial outputs, each normalised by its weight sum: slot by slot
@@ -92,5 +93,57 @@ struct BranchParams {
 constexpr int BRANCH_PLAN_WORDS = 8;
 size_t branch_workspace(int n_seqs, int n_prefixes, int hkv, int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_plan);
 hipError_t launch_branch_attention(const BranchParams &p, hipStream_t s);   // (it fills in segments and divisors)
+
+// ------------------------------------------------------------------ pieces of many new tokens over the same rows
+struct ChunkParams {
+    Rows q;
+    uint16_t *out;                        // [n_seqs][hq][Bt][D]
+    float *lse;                           // [n_seqs][hq][Bt]
+    const uint16_t *k_prefix, *v_prefix;  // [n_prefixes][hkv][prefix_cap][D]
+    Pages pages;
+    float *part_o;                        // partial outputs, each normalised by its weight sum: two slots a workgroup
+    float2 *part_ml;                      // (reference in log2 units, weight sum) of every row of a slot
+    int32_t *plan;                        // [CHUNK_PLAN_WORDS + slots]: how the launch cut the work, for the join
+    int32_t n_seqs, fan, hkv, G, Bt, D;
+    int32_t prefix_len;
+    int64_t prefix_cap;
+    int32_t cus;
+    float scale_log2e;
+    int32_t blocks, slots, part_rows;     // blocks of query rows of a sequence and head; n_seqs times that; rows of a partial
+    Divisor by_blocks, by_slots, by_G, by_fan;
+};
+constexpr int CHUNK_PLAN_WORDS = 8;
+size_t chunk_workspace(int n_seqs, int hkv, int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_plan);
+hipError_t launch_branch_chunk(ChunkParams p, hipStream_t s);   // (it fills in the last two lines)
+
+// ------------------------------------------------------------------ the attention weight that own rows gather
+struct WeightsParams {
+    Rows q;
+    const float *lse;                     // [n_seqs][hq][Bt]
+    float *w;                             // [n_pages][hkv][page_rows]
+    Pages pages;                          // (v: not used)
+    float *part;                          // partial sums of blocks of rows that were cut: two a workgroup
+    int32_t *plan;                        // [WEIGHTS_PLAN_WORDS + n_seqs + 1]
+    int32_t n_seqs, hkv, G, Bt, D, observe, cus;
+    float scale_log2e, decay;
+    Divisor by_G, by_hkv;
+};
+constexpr int WEIGHTS_PLAN_WORDS = 8;
+size_t weights_workspace(int n_seqs, int G, int Bt, int observe, int cus, size_t *off_plan);
+hipError_t launch_branch_weights(WeightsParams p, hipStream_t s);   // (it fills in the divisors)
+
+// ------------------------------------------------------------------ eviction of own rows
+struct BranchEvictParams {
+    Pages pages;
+    float *w;                             // [n_pages][hkv][page_rows]
+    int32_t *positions;                   // [n_pages][hkv][page_rows]
+    const int32_t *pos0;                  // nullable [n_seqs]
+    int32_t *status;                      // nullable
+    int32_t *moves;                       // per (sequence, head): the number of moves, then from and to of each
+    int32_t n_seqs, hkv, Bt, D, budget, window, most_moves;
+    Divisor by_hkv;
+};
+size_t branch_evict_workspace(int n_seqs, int hkv, int64_t table_rows, int budget, int *most_moves);
+hipError_t launch_branch_evict(BranchEvictParams p, hipStream_t s);   // (it fills in the divisor)
 
 }  // namespace kd

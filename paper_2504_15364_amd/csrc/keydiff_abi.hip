@@ -1258,11 +1258,12 @@ int check_rows(const keydiff_rows_t *r, const char *name)
 
 kd::Rows rows_of(const keydiff_rows_t &r) { return {static_cast<const uint16_t *>(r.data), r.seq_stride, r.head_stride, r.token_stride}; }
 
-int check_branches(const keydiff_branches_t *b, int32_t Bt)
+// values: whether the call reads or writes the values' pages
+int check_branches(const keydiff_branches_t *b, int32_t Bt, bool values = true)
 {
-    if (!b || !b->k_pages || !b->v_pages || !b->table || !b->lens) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (!b || !b->k_pages || (values && !b->v_pages) || !b->table || !b->lens) return fail(KEYDIFF_EINVAL, "null pointer");
     if (int rc = check_heads(b->n_seqs, b->n_q_heads, b->n_kv_heads, b->head_dim, Bt)) return rc;
-    if (misaligned(b->k_pages) || misaligned(b->v_pages)) return fail(KEYDIFF_EINVAL, "pages must be 16-byte aligned");
+    if (misaligned(b->k_pages) || (values && misaligned(b->v_pages))) return fail(KEYDIFF_EINVAL, "pages must be 16-byte aligned");
     if (b->page_rows < 8 || b->page_rows > 1024 || (b->page_rows & (b->page_rows - 1)))
         return fail(KEYDIFF_ESHAPE, "page_rows must be a power of two from 8 to 1024, got %d", b->page_rows);
     if (b->n_pages < 1 || b->table_width < 1) return fail(KEYDIFF_ESHAPE, "n_pages and table_width must be positive");
@@ -1298,17 +1299,23 @@ int check_prefixes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, 
 }
 
 struct BranchWork {   // where the parts of a call's workspace begin, for a chip of `cus` compute units
-    size_t off_ml, off_plan;
+    size_t need, off_ml, off_plan;
     int32_t cus;
 };
+BranchWork branch_work(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes)
+{
+    BranchWork w;
+    w.cus = std::max(compute_units(), 2);
+    w.need = kd::branch_workspace(b->n_seqs, n_prefixes, b->n_kv_heads, b->n_q_heads / b->n_kv_heads, Bt, b->head_dim, w.cus, &w.off_ml, &w.off_plan);
+    return w;
+}
 // The workspace is large enough, and what the call writes, `out` and the workspace, is nothing that it reads, but for `out` in the place of
 // the queries: a row is stored by the workgroup that has read it, or behind the launch that has.
 int check_buffers(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix, int32_t n_prefixes,
-                  int32_t prefix_len, int64_t prefix_cap, const void *out, const void *workspace, size_t workspace_bytes, BranchWork *work)
+                  int32_t prefix_len, int64_t prefix_cap, const void *out, const void *workspace, size_t workspace_bytes, const BranchWork *work)
 {
     const int32_t hq = b->n_q_heads, D = b->head_dim;
-    work->cus = std::max(compute_units(), 2);
-    const size_t need = kd::branch_workspace(b->n_seqs, n_prefixes, b->n_kv_heads, hq / b->n_kv_heads, Bt, D, work->cus, &work->off_ml, &work->off_plan);
+    const size_t need = work->need;
     if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
     const size_t rows = (size_t)b->n_seqs * hq * Bt * D * 2, pool = (size_t)b->n_pages * b->n_kv_heads * b->page_rows * D * 2;
     const bool shared = n_prefixes > 0 && prefix_len > 0;   // (of the last head, no row behind prefix_len need exist)
@@ -1331,12 +1338,13 @@ int check_buffers(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t 
 }
 
 int branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix,
-                     int32_t n_prefixes, int32_t prefix_len, int64_t prefix_cap, float scale_log2e, void *out, void *workspace,
+                     int32_t n_prefixes, int32_t prefix_len, int64_t prefix_cap, float scale_log2e, void *out, float *lse, void *workspace,
                      const BranchWork &work, hipStream_t s)
 {
     kd::BranchParams p{};
     p.q = rows_of(*q);
     p.out = static_cast<uint16_t *>(out);
+    p.lse = lse;
     p.k_prefix = static_cast<const uint16_t *>(k_prefix);
     p.v_prefix = static_cast<const uint16_t *>(v_prefix);
     p.pages = pages_of(b);
@@ -1359,6 +1367,24 @@ int branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32
     return KEYDIFF_OK;
 }
 
+float scale_log2e(float softmax_scale, int32_t head_dim)
+{
+    return (float)((softmax_scale > 0.f ? (double)softmax_scale : 1.0 / std::sqrt((double)head_dim)) * 1.4426950408889634);
+}
+
+int check_prefix_rows(const keydiff_branches_t *b, int32_t Bt, const void *k_prefix, const void *v_prefix, int32_t n_prefixes, int32_t prefix_len,
+                      int64_t prefix_cap, float softmax_scale)
+{
+    if (!std::isfinite(softmax_scale)) return fail(KEYDIFF_EINVAL, "softmax_scale must be finite");
+    if (int rc = check_prefixes(b, Bt, n_prefixes, prefix_len)) return rc;
+    if (n_prefixes > 0 && prefix_len > 0) {
+        if (!k_prefix || !v_prefix) return fail(KEYDIFF_EINVAL, "null pointer: prefix rows");
+        if (misaligned(k_prefix) || misaligned(v_prefix)) return fail(KEYDIFF_EINVAL, "tensors must be 16-byte aligned");
+        if (prefix_cap < prefix_len) return fail(KEYDIFF_ESHAPE, "prefix_cap must be at least prefix_len");
+    }
+    return KEYDIFF_OK;
+}
+
 int check_query_rows(const keydiff_branches_t *b, int32_t Bt)
 {
     if ((int64_t)b->n_seqs * Bt * b->n_q_heads > (1 << 26)) return fail(KEYDIFF_ESHAPE, "sequences * Bt * n_q_heads must not exceed 2^26");
@@ -1375,6 +1401,104 @@ int check_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *q,
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(KEYDIFF_EINVAL, "the workspace must be 256-byte aligned");
     return KEYDIFF_OK;
 }
+
+int check_prompt_cache(const keydiff_cache_t *c, const keydiff_branches_t *b, int32_t Bt)
+{
+    if (b->n_q_heads != c->cfg.n_q_heads || b->n_kv_heads != c->cfg.n_kv_heads || b->head_dim != c->cfg.head_dim)
+        return fail(KEYDIFF_ESHAPE, "the cache holds %d / %d heads of %d, the continuations have %d / %d of %d", c->cfg.n_q_heads,
+                    c->cfg.n_kv_heads, c->cfg.head_dim, b->n_q_heads, b->n_kv_heads, b->head_dim);
+    return check_prefixes(b, Bt, c->cfg.batch, c->len);   // (a pending eviction leaves the budget's rows)
+}
+
+int finish_prompt_cache(keydiff_cache_t *c, hipStream_t s)
+{
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if ((c->pending || c->shift_pending) && hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone)
+        return fail(KEYDIFF_ESTATE, "the cache has a pending eviction, which every replay would repeat: keydiff_finish it ahead of the capture");
+    return finish_pending(c, s);
+}
+
+// ------------------------------------------------------------------ pieces of many tokens, weights of own rows, their eviction
+constexpr int kFewRows = 32;   // query rows of a sequence and KV head up to which the kernels of branch_attention take a piece
+
+bool few_rows(const keydiff_branches_t *b, int32_t Bt) { return (int64_t)b->n_q_heads / b->n_kv_heads * Bt <= kFewRows; }
+
+BranchWork chunk_work(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes)
+{
+    if (few_rows(b, Bt)) return branch_work(b, Bt, n_prefixes);
+    BranchWork w;
+    w.cus = std::max(compute_units(), 2);
+    w.need = kd::chunk_workspace(b->n_seqs, b->n_kv_heads, b->n_q_heads / b->n_kv_heads, Bt, b->head_dim, w.cus, &w.off_ml, &w.off_plan);
+    return w;
+}
+
+int check_chunk_rows(const keydiff_branches_t *b, int32_t Bt)
+{
+    if (int rc = check_query_rows(b, Bt)) return rc;
+    const int64_t Mt = (int64_t)b->n_q_heads / b->n_kv_heads * Bt;
+    if (!few_rows(b, Bt) && (int64_t)b->n_seqs * b->n_kv_heads * ((Mt + 31) / 32) > (1 << 23))   // (a launch counts its threads in 32 bits)
+        return fail(KEYDIFF_ESHAPE, "the blocks of 32 query rows of all sequences and KV heads must not exceed 2^23");
+    return KEYDIFF_OK;
+}
+
+// ... and `lse` is nothing that the call reads or writes else
+int check_lse(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix, int32_t n_prefixes,
+              int32_t prefix_len, int64_t prefix_cap, const void *out, const float *lse, const void *workspace, const BranchWork &work)
+{
+    const size_t rows = (size_t)b->n_seqs * b->n_q_heads * Bt, pool = (size_t)b->n_pages * b->n_kv_heads * b->page_rows * b->head_dim * 2;
+    const size_t prefix = n_prefixes > 0 && prefix_len > 0 ? (((size_t)n_prefixes * b->n_kv_heads - 1) * prefix_cap + prefix_len) * b->head_dim * 2 : 0;
+    const struct {
+        const void *at;
+        size_t bytes;
+    } other[] = {{b->k_pages, pool}, {b->v_pages, pool}, {k_prefix, prefix}, {v_prefix, prefix}, {b->lens, (size_t)b->n_seqs * 4},
+                 {b->table, (size_t)b->n_seqs * b->table_width * 4}, {b->n_new, b->n_new ? (size_t)b->n_seqs * 4 : 0}, {out, rows * b->head_dim * 2},
+                 {workspace, work.need}, {q->data, 2 * span(*q, b->n_seqs, b->n_q_heads, Bt, b->head_dim)}};
+    for (const auto &o : other)
+        if (o.bytes && overlap(lse, rows * 4, o.at, o.bytes))
+            return fail(KEYDIFF_EINVAL, "lse must not overlap the inputs, out or the workspace");
+    return KEYDIFF_OK;
+}
+
+int check_chunk(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *out, const float *lse, const void *workspace)
+{
+    if (int rc = check_branch_attention(b, q, Bt, out, workspace)) return rc;
+    if (!lse) return fail(KEYDIFF_EINVAL, "null pointer: lse");
+    if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(KEYDIFF_EINVAL, "lse must be 4-byte aligned");
+    return check_chunk_rows(b, Bt);
+}
+
+int branch_chunk(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix, int32_t n_prefixes,
+                 int32_t prefix_len, int64_t prefix_cap, float scale, void *out, float *lse, void *workspace, const BranchWork &work, hipStream_t s)
+{
+    if (few_rows(b, Bt))
+        return branch_attention(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, scale, out, lse, workspace, work, s);
+    kd::ChunkParams p{};
+    p.q = rows_of(*q);
+    p.out = static_cast<uint16_t *>(out);
+    p.lse = lse;
+    p.k_prefix = static_cast<const uint16_t *>(k_prefix);
+    p.v_prefix = static_cast<const uint16_t *>(v_prefix);
+    p.pages = pages_of(b);
+    p.n_seqs = b->n_seqs;
+    p.fan = n_prefixes > 0 ? b->n_seqs / n_prefixes : 1;
+    p.hkv = b->n_kv_heads;
+    p.G = b->n_q_heads / b->n_kv_heads;
+    p.Bt = Bt;
+    p.D = b->head_dim;
+    p.prefix_len = n_prefixes > 0 ? prefix_len : 0;
+    p.prefix_cap = prefix_cap;
+    p.cus = work.cus;
+    p.scale_log2e = scale;
+    unsigned char *w = static_cast<unsigned char *>(workspace);
+    p.part_o = reinterpret_cast<float *>(w);
+    p.part_ml = reinterpret_cast<float2 *>(w + work.off_ml);
+    p.plan = reinterpret_cast<int32_t *>(w + work.off_plan);
+    KD_LAUNCH(kd::launch_branch_chunk(p, s), "chunk attention kernels");
+    return KEYDIFF_OK;
+}
+
+// Weights and positions in pages: float and int32 [n_pages][n_kv_heads][page_rows]
+size_t words_of_pages(const keydiff_branches_t *b) { return (size_t)b->n_pages * b->n_kv_heads * b->page_rows * 4; }
 
 }  // namespace
 
@@ -1469,9 +1593,7 @@ int keydiff_branch_workspace_bytes(const keydiff_branches_t *b, int32_t Bt, int3
     if (int rc = check_query_rows(b, Bt)) return rc;
     if (n_prefixes < 0 || (n_prefixes > 0 && b->n_seqs % n_prefixes))
         return fail(KEYDIFF_ESHAPE, "n_prefixes must divide the %d sequences, got %d", b->n_seqs, n_prefixes);
-    size_t off_ml = 0, off_plan = 0;
-    *bytes = kd::branch_workspace(b->n_seqs, n_prefixes, b->n_kv_heads, b->n_q_heads / b->n_kv_heads, Bt, b->head_dim,
-                                  std::max(compute_units(), 2), &off_ml, &off_plan);
+    *bytes = branch_work(b, Bt, n_prefixes).need;
     return KEYDIFF_OK;
 }
 
@@ -1480,18 +1602,11 @@ int keydiff_branch_attention(const keydiff_branches_t *b, const keydiff_rows_t *
                              void *workspace, size_t workspace_bytes, void *stream)
 {
     if (int rc = check_branch_attention(b, q, Bt, out, workspace)) return rc;
-    if (!std::isfinite(softmax_scale)) return fail(KEYDIFF_EINVAL, "softmax_scale must be finite");
-    if (int rc = check_prefixes(b, Bt, n_prefixes, prefix_len)) return rc;
-    if (n_prefixes > 0 && prefix_len > 0) {
-        if (!k_prefix || !v_prefix) return fail(KEYDIFF_EINVAL, "null pointer: prefix rows");
-        if (misaligned(k_prefix) || misaligned(v_prefix)) return fail(KEYDIFF_EINVAL, "tensors must be 16-byte aligned");
-        if (prefix_cap < prefix_len) return fail(KEYDIFF_ESHAPE, "prefix_cap must be at least prefix_len");
-    }
-    BranchWork work;
+    if (int rc = check_prefix_rows(b, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, softmax_scale)) return rc;
+    const BranchWork work = branch_work(b, Bt, n_prefixes);
     if (int rc = check_buffers(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, out, workspace, workspace_bytes, &work))
         return rc;
-    const double scale = softmax_scale > 0.f ? (double)softmax_scale : 1.0 / std::sqrt((double)b->head_dim);
-    return branch_attention(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, (float)(scale * 1.4426950408889634), out,
+    return branch_attention(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, scale_log2e(softmax_scale, b->head_dim), out, nullptr,
                             workspace, work, static_cast<hipStream_t>(stream));
 }
 
@@ -1500,20 +1615,174 @@ int keydiff_cache_branch_attention(keydiff_cache_t *c, const keydiff_branches_t 
 {
     if (!c) return fail(KEYDIFF_EINVAL, "null pointer");
     if (int rc = check_branch_attention(b, q, Bt, out, workspace)) return rc;
-    if (b->n_q_heads != c->cfg.n_q_heads || b->n_kv_heads != c->cfg.n_kv_heads || b->head_dim != c->cfg.head_dim)
-        return fail(KEYDIFF_ESHAPE, "the cache holds %d / %d heads of %d, the continuations have %d / %d of %d", c->cfg.n_q_heads,
-                    c->cfg.n_kv_heads, c->cfg.head_dim, b->n_q_heads, b->n_kv_heads, b->head_dim);
-    // (a pending eviction leaves the budget's rows)
-    const int32_t rows = c->len;
-    if (int rc = check_prefixes(b, Bt, c->cfg.batch, rows)) return rc;
-    BranchWork work;
+    if (int rc = check_prompt_cache(c, b, Bt)) return rc;
+    const BranchWork work = branch_work(b, Bt, c->cfg.batch);
     if (int rc = check_buffers(b, q, Bt, c->k, c->v, c->cfg.batch, (int32_t)c->L.cap, c->L.cap, out, workspace, workspace_bytes, &work)) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    if ((c->pending || c->shift_pending) && hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone)
-        return fail(KEYDIFF_ESTATE, "the cache has a pending eviction, which every replay would repeat: keydiff_finish it ahead of the capture");
-    if (int rc = finish_pending(c, s)) return rc;
-    return branch_attention(b, q, Bt, c->k, c->v, c->cfg.batch, c->len, c->L.cap, c->scale_log2e, out, workspace, work, s);
+    if (int rc = finish_prompt_cache(c, s)) return rc;
+    return branch_attention(b, q, Bt, c->k, c->v, c->cfg.batch, c->len, c->L.cap, c->scale_log2e, out, nullptr, workspace, work, s);
+}
+
+int keydiff_branch_chunk_workspace_bytes(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes, size_t *bytes)
+{
+    if (!b || !bytes) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (int rc = check_heads(b->n_seqs, b->n_q_heads, b->n_kv_heads, b->head_dim, Bt)) return rc;
+    if (int rc = check_chunk_rows(b, Bt)) return rc;
+    if (n_prefixes < 0 || (n_prefixes > 0 && b->n_seqs % n_prefixes))
+        return fail(KEYDIFF_ESHAPE, "n_prefixes must divide the %d sequences, got %d", b->n_seqs, n_prefixes);
+    *bytes = chunk_work(b, Bt, n_prefixes).need;
+    return KEYDIFF_OK;
+}
+
+int keydiff_branch_chunk_attention(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix,
+                                   int32_t n_prefixes, int32_t prefix_len, int64_t prefix_cap, float softmax_scale, void *out, float *lse,
+                                   void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_chunk(b, q, Bt, out, lse, workspace)) return rc;
+    if (int rc = check_prefix_rows(b, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, softmax_scale)) return rc;
+    const BranchWork work = chunk_work(b, Bt, n_prefixes);
+    if (int rc = check_buffers(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, out, workspace, workspace_bytes, &work)) return rc;
+    if (int rc = check_lse(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, out, lse, workspace, work)) return rc;
+    return branch_chunk(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, scale_log2e(softmax_scale, b->head_dim), out, lse, workspace,
+                        work, static_cast<hipStream_t>(stream));
+}
+
+int keydiff_cache_branch_chunk_attention(keydiff_cache_t *c, const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, void *out, float *lse,
+                                         void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!c) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (int rc = check_chunk(b, q, Bt, out, lse, workspace)) return rc;
+    if (int rc = check_prompt_cache(c, b, Bt)) return rc;
+    const BranchWork work = chunk_work(b, Bt, c->cfg.batch);
+    const int32_t cap = (int32_t)c->L.cap;
+    if (int rc = check_buffers(b, q, Bt, c->k, c->v, c->cfg.batch, cap, cap, out, workspace, workspace_bytes, &work)) return rc;
+    if (int rc = check_lse(b, q, Bt, c->k, c->v, c->cfg.batch, cap, cap, out, lse, workspace, work)) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (int rc = finish_prompt_cache(c, s)) return rc;
+    return branch_chunk(b, q, Bt, c->k, c->v, c->cfg.batch, c->len, c->L.cap, c->scale_log2e, out, lse, workspace, work, s);
+}
+
+int keydiff_branch_weights_workspace_bytes(const keydiff_branches_t *b, int32_t Bt, int32_t observe, size_t *bytes)
+{
+    if (!b || !bytes) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (int rc = check_heads(b->n_seqs, b->n_q_heads, b->n_kv_heads, b->head_dim, Bt)) return rc;
+    if (int rc = check_chunk_rows(b, Bt)) return rc;
+    if (observe < 0) return fail(KEYDIFF_ESHAPE, "observe must not be negative, got %d", observe);
+    size_t off_plan = 0;
+    *bytes = kd::weights_workspace(b->n_seqs, b->n_q_heads / b->n_kv_heads, Bt, observe, std::max(compute_units(), 2), &off_plan);
+    return KEYDIFF_OK;
+}
+
+int keydiff_branch_weights(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const float *lse, float *w_pages, int32_t observe,
+                           float decay, float softmax_scale, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_branches(b, Bt, false)) return rc;
+    if (int rc = check_chunk_rows(b, Bt)) return rc;
+    if (int rc = check_rows(q, "q")) return rc;
+    if (!lse || !w_pages || !workspace) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (misaligned(w_pages)) return fail(KEYDIFF_EINVAL, "pages must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(lse) & 3) return fail(KEYDIFF_EINVAL, "lse must be 4-byte aligned");
+    if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(KEYDIFF_EINVAL, "the workspace must be 256-byte aligned");
+    if (observe < 0) return fail(KEYDIFF_ESHAPE, "observe must not be negative, got %d", observe);
+    if (!(decay >= 0.f && decay <= 1.f)) return fail(KEYDIFF_EINVAL, "decay must lie in [0, 1], got %g", (double)decay);
+    if (!std::isfinite(softmax_scale)) return fail(KEYDIFF_EINVAL, "softmax_scale must be finite");
+    if (int rc = check_prefixes(b, Bt, 0, 0)) return rc;
+    const int32_t cus = std::max(compute_units(), 2), G = b->n_q_heads / b->n_kv_heads;
+    size_t off_plan = 0;
+    const size_t need = kd::weights_workspace(b->n_seqs, G, Bt, observe, cus, &off_plan);
+    if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
+    const struct {
+        const void *at;
+        size_t bytes;
+    } read[] = {{b->k_pages, words_of_pages(b) / 2 * b->head_dim}, {b->lens, (size_t)b->n_seqs * 4}, {b->table, (size_t)b->n_seqs * b->table_width * 4},
+                {b->n_new, b->n_new ? (size_t)b->n_seqs * 4 : 0}, {lse, (size_t)b->n_seqs * b->n_q_heads * Bt * 4},
+                {q->data, 2 * span(*q, b->n_seqs, b->n_q_heads, Bt, b->head_dim)}};
+    for (const auto &r : read)
+        if (r.bytes && (overlap(w_pages, words_of_pages(b), r.at, r.bytes) || overlap(workspace, need, r.at, r.bytes)))
+            return fail(KEYDIFF_EINVAL, "w_pages and the workspace must not overlap the inputs");
+    if (overlap(w_pages, words_of_pages(b), workspace, need)) return fail(KEYDIFF_EINVAL, "w_pages and the workspace must not overlap");
+    kd::WeightsParams p{};
+    p.q = rows_of(*q);
+    p.lse = lse;
+    p.w = w_pages;
+    p.pages = pages_of(b);
+    p.part = static_cast<float *>(workspace);
+    p.plan = reinterpret_cast<int32_t *>(static_cast<unsigned char *>(workspace) + off_plan);
+    p.n_seqs = b->n_seqs;
+    p.hkv = b->n_kv_heads;
+    p.G = G;
+    p.Bt = Bt;
+    p.D = b->head_dim;
+    p.observe = observe > 0 && observe < Bt ? observe : Bt;
+    p.cus = cus;
+    p.scale_log2e = scale_log2e(softmax_scale, b->head_dim);
+    p.decay = decay;
+    KD_LAUNCH(kd::launch_branch_weights(p, static_cast<hipStream_t>(stream)), "attention weight kernels");
+    return KEYDIFF_OK;
+}
+
+namespace {
+
+int check_evict(const keydiff_branches_t *b, int32_t budget)
+{
+    if (b->n_seqs < 1 || b->n_kv_heads < 1) return fail(KEYDIFF_ESHAPE, "sequences and head counts must be positive");
+    if (b->page_rows < 1 || b->table_width < 1 || (int64_t)b->table_width * b->page_rows > 0x3fffffff)
+        return fail(KEYDIFF_ESHAPE, "table_width * page_rows must lie in [1, 2^30]");
+    if (budget < 1) return fail(KEYDIFF_ESHAPE, "budget must be positive, got %d", budget);
+    if ((int64_t)b->n_seqs * b->n_kv_heads > (1 << 22)) return fail(KEYDIFF_ESHAPE, "sequences * n_kv_heads must not exceed 2^22");
+    return KEYDIFF_OK;
+}
+
+}  // namespace
+
+int keydiff_branch_evict_workspace_bytes(const keydiff_branches_t *b, int32_t budget, size_t *bytes)
+{
+    if (!b || !bytes) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (int rc = check_evict(b, budget)) return rc;
+    int most = 0;
+    *bytes = kd::branch_evict_workspace(b->n_seqs, b->n_kv_heads, (int64_t)b->table_width * b->page_rows, budget, &most);
+    return KEYDIFF_OK;
+}
+
+int keydiff_branch_evict(const keydiff_branches_t *b, int32_t Bt, float *w_pages, int32_t *p_pages, const int32_t *pos0, int32_t budget, int32_t window,
+                         int32_t *status, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_branches(b, Bt)) return rc;
+    if (int rc = check_evict(b, budget)) return rc;
+    if (!w_pages || !p_pages || !workspace) return fail(KEYDIFF_EINVAL, "null pointer");
+    if (misaligned(w_pages) || misaligned(p_pages)) return fail(KEYDIFF_EINVAL, "pages must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(status) & 3) return fail(KEYDIFF_EINVAL, "status must be 4-byte aligned");
+    if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(KEYDIFF_EINVAL, "the workspace must be 256-byte aligned");
+    if (window < 0 || window >= budget) return fail(KEYDIFF_ESHAPE, "window must lie in [0, budget), got %d of %d", window, budget);
+    int most = 0;
+    const size_t need = kd::branch_evict_workspace(b->n_seqs, b->n_kv_heads, (int64_t)b->table_width * b->page_rows, budget, &most);
+    if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
+    const size_t words = words_of_pages(b), pool = words / 2 * b->head_dim, per_seq = (size_t)b->n_seqs * 4;
+    const struct {
+        const void *at;
+        size_t bytes;
+    } all[] = {{b->k_pages, pool}, {b->v_pages, pool}, {w_pages, words}, {p_pages, words}, {workspace, need}, {status, status ? (size_t)4 : 0},
+               {b->lens, per_seq}, {b->table, per_seq * b->table_width}, {b->n_new, b->n_new ? per_seq : 0}, {pos0, pos0 ? per_seq : 0}};
+    for (int i = 0; i < 6; ++i)   // (what the call writes, against all others)
+        for (int j = i + 1; j < 10; ++j)
+            if (all[i].bytes && all[j].bytes && overlap(all[i].at, all[i].bytes, all[j].at, all[j].bytes))
+                return fail(KEYDIFF_EINVAL, "the pages, the workspace, status, the table and the lengths must not overlap one another");
+    kd::BranchEvictParams p{};
+    p.pages = pages_of(b);
+    p.w = w_pages;
+    p.positions = p_pages;
+    p.pos0 = pos0;
+    p.status = status;
+    p.moves = static_cast<int32_t *>(workspace);
+    p.n_seqs = b->n_seqs;
+    p.hkv = b->n_kv_heads;
+    p.Bt = Bt;
+    p.D = b->head_dim;
+    p.budget = budget;
+    p.window = window;
+    p.most_moves = most;
+    KD_LAUNCH(kd::launch_branch_evict(p, static_cast<hipStream_t>(stream)), "branch eviction kernels");
+    return KEYDIFF_OK;
 }
 
 int keydiff_finish(keydiff_cache_t *c, void *stream)
