@@ -26,6 +26,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -83,26 +84,34 @@ __device__ __forceinline__ Block block_of(const ChunkParams &p, int slot)
     return b;
 }
 
-// How the list is cut: heads outermost, then the slots.  Part w of `parts` is [w total / parts, (w + 1) total / parts).
-struct Plan {
-    int per_head;        // tiles of one head's segments
-    int parts;
-};
-__device__ __forceinline__ int64_t part_begin(const ChunkParams &p, const Plan &plan, int w) { return (int64_t)w * plan.per_head * p.hkv / plan.parts; }
-__device__ __forceinline__ int part_of(const ChunkParams &p, const Plan &plan, int64_t x) { return (int)(((x + 1) * plan.parts - 1) / ((int64_t)plan.per_head * p.hkv)); }
-// As many parts as there are workgroups, but whole segments where these are about alike and fewer than the workgroups, and at
-// least MIN_TILES tiles a part: a part costs 5 us around its tiles, of which one takes 1.5.
-constexpr int MIN_TILES = 4;
-__device__ __forceinline__ int parts_of(int64_t segments, int64_t total, int wgs)
+// What a segment costs, in units of 0.2 us: START around its tiles, and a tile by its waves of query rows.  Measured, heads of 128, keys in the L2: 1.05 to
+// 1.15 us up to four waves, one a SIMD; five to eight 1.49, 1.55, 1.67 and 1.81.  (Heads of 64: three fifths of that, in the same proportion.)
+constexpr int START = 30;
+__device__ __forceinline__ int tile_cost(const Block &b)
 {
-    int64_t parts = segments > 0 && segments <= wgs ? segments * (wgs / segments) : wgs;
-    if (parts > segments) parts = total / MIN_TILES < parts ? (total / MIN_TILES > segments ? total / MIN_TILES : segments) : parts;
-    return (int)parts;
+    const int rows = b.M - b.m0;
+    return rows <= R / 2 ? 6 : rows <= R * 3 / 4 ? 8 : 9;
+}
+__device__ __forceinline__ int cost_of(const Block &b) { return b.tiles ? START + b.tiles * tile_cost(b) : 0; }
+// The tile at which a border `at` units behind a segment's start cuts it: where no more than SLIVER tiles would be left on one side, none are
+constexpr int SLIVER = 2;
+__device__ __forceinline__ int cut_at(const Block &b, int at)
+{
+    const int t = (max(at - START, 0) + tile_cost(b) - 1) / tile_cost(b);
+    return t <= SLIVER ? 0 : t >= b.tiles - SLIVER ? b.tiles : t;
 }
 
+constexpr int LEAST = START + 36;   // units of a part at least
+// What partials and their join cost a launch, in the same units
+constexpr int JOIN = 40;
+
+// What the end of a segment asks for, kept in LDS meanwhile: the loop over the tiles has no scalar registers to spare
+struct Kept {
+    int s, m0, M, slot;
+};
 // One segment, or a part of one: the tiles [t0, t1) of block b and KV head h.  slot < 0: all of them, the outputs are written; else the partial `slot`.
 template <int D>
-__device__ void attend(const ChunkParams &p, unsigned char *smem, const Block &b, const int h, const int t0, const int t1, const int slot)
+__device__ void attend(const ChunkParams &p, unsigned char *smem, Kept &kept, const Block &b, const int h, const int t0, const int t1, const int part)
 {
     constexpr int NT = 64 * NW;
     constexpr int UPR = D / 8;                // 16-byte units of a row
@@ -119,9 +128,9 @@ __device__ void attend(const ChunkParams &p, unsigned char *smem, const Block &b
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, hh = lane >> 5;
     const int np = (p.prefix_len + TK - 1) / TK, prefix_full = p.prefix_len / TK;
-    const int shift = p.pages.page_shift, page_mask = (1 << shift) - 1;
+    const int shift = p.pages.page_shift;
     const int32_t *table = p.pages.table + (int64_t)b.s * p.pages.width;
-    const int64_t prompt = p.prefix_len > 0 ? ((int64_t)p.by_fan.divide(b.s) * p.hkv + h) * p.prefix_cap * D : 0;
+    const int64_t prompt = p.prefix_len > 0 ? ((int64_t)p.by_fan.divide(b.s) * p.hkv + h) * p.prefix_cap : 0;   // the first row of the prompt's head
     const int ntl = t1 - t0;
     const bool active = b.m0 + 32 * wave < b.M;   // uniform in the wave: else it only copies
     const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
@@ -147,14 +156,14 @@ __device__ void attend(const ChunkParams &p, unsigned char *smem, const Block &b
         Source r;
         const int in_tile = RPL * wave + CSTEP * i;
         if (t < np) {
-            const int64_t off = prompt + (int64_t)min(t * TK + in_tile, p.prefix_len - 1) * D;
+            const int64_t off = (prompt + min(t * TK + in_tile, p.prefix_len - 1)) * D;
             r.k = p.k_prefix + off;
             r.v = p.v_prefix + off;
             r.there = true;
         } else {
             const int row = min((t - np) * TK + in_tile, b.last);
             r.there = (uint32_t)page[i] < (uint32_t)p.pages.n_pages;
-            const int64_t off = ((((int64_t)(r.there ? page[i] : 0) * p.hkv + h) << shift) + (row & page_mask)) * D;
+            const int64_t off = ((((int64_t)(r.there ? page[i] : 0) * p.hkv + h) << shift) + (row & ((1 << shift) - 1))) * D;
             r.k = p.pages.k + off;
             r.v = p.pages.v + off;
         }
@@ -187,6 +196,7 @@ __device__ void attend(const ChunkParams &p, unsigned char *smem, const Block &b
     };
 
     __syncthreads();   // nobody reads what the segment before has left in LDS
+    if (tid == 0) kept = Kept{b.s, b.m0, b.M, part};
     look_up(t0);
 
     // ---- queries: whole rows, through the two buffers that tiles t0 + 2 and t0 + 3 use later, into registers
@@ -442,22 +452,32 @@ __device__ void attend(const ChunkParams &p, unsigned char *smem, const Block &b
 
     // ---- results.  A lane holds the sum of its own keys: the other half is with lane ^ 32
     const float L = sum_halves(lacc[0] + lacc[1]), inv = L > 0.f ? 1.f / L : 0.f;   // (a row may see no key at all: zero)
-    const int64_t head = (int64_t)b.s * p.hkv * p.G + h * p.G;
+    const int seq = __builtin_amdgcn_readfirstlane(kept.s), m0 = __builtin_amdgcn_readfirstlane(kept.m0), M = __builtin_amdgcn_readfirstlane(kept.M);
+    const int slot = __builtin_amdgcn_readfirstlane(kept.slot);
+    const int64_t head = (int64_t)seq * p.hkv * p.G + h * p.G;
     if (slot >= 0) {
-        // In the accumulators' own layout, whole kilobytes a store; the join reads them in the same order.
+        // In the accumulators' own layout, whole kilobytes a store; the join reads them in the same order.  As fp16 with a power of two for each row, which
+        // puts its largest value at 2^14: 11 bits, an eighth of the output's rounding, and half the bytes of floats.
         if (active) {
-            float *base = p.part_o + (((int64_t)slot * (p.part_rows / 32) + wave) * (D / 8) * 64 + lane) * 4;
+            float most = 0.f;
 #pragma unroll
             for (int db = 0; db < NDB; ++db)
 #pragma unroll
-                for (int jj = 0; jj < 4; ++jj) {
-                    f32x4 o;
+                for (int e = 0; e < 16; e += 2) most = max3(most, __builtin_fabsf(oacc[db][e]), __builtin_fabsf(oacc[db][e + 1]));
+            most = max_halves(most) * inv;
+            const int power = most > 0.f ? __builtin_amdgcn_frexp_expf(most) : -126;
+            _Float16 *base = p.part_o + (((int64_t)slot * (p.part_rows / 32) + wave) * (D / 16) * 64 + lane) * 8;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) o[r] = oacc[db][4 * jj + r] * inv;
-                    *reinterpret_cast<f32x4 *>(base + (size_t)(4 * db + jj) * 64 * 4) = o;
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int jj = 0; jj < 2; ++jj) {
+                    f16x8 o;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) o[r] = (_Float16)__builtin_amdgcn_ldexpf(oacc[db][8 * jj + r] * inv, 14 - power);
+                    *reinterpret_cast<f16x8 *>(base + (size_t)(2 * db + jj) * 64 * 8) = o;
                 }
             // (a piece without a key has the reference -inf; one whose logits are all NaN has none either, and its NaN must not be lost)
-            if (hh == 0) p.part_ml[(int64_t)slot * p.part_rows + 32 * wave + l32] = make_float2(L == L ? mref : 0.f, L);
+            if (hh == 0) p.part_ml[(int64_t)slot * p.part_rows + 32 * wave + l32] = f32x4{L == L ? mref : 0.f, L, __int_as_float(power), 0.f};
         }
         return;
     }
@@ -480,12 +500,12 @@ __device__ void attend(const ChunkParams &p, unsigned char *smem, const Block &b
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int i = 0; i < QBYTES / 1024; ++i) {
-        const int r = RPL * i + lrow, m = b.m0 + 32 * wave + r, j = p.by_G.divide(min(m, b.M - 1));
+        const int r = RPL * i + lrow, m = m0 + 32 * wave + r, j = p.by_G.divide(min(m, M - 1));
         const u32x4 val = *reinterpret_cast<const u32x4 *>(stage(wave * QBYTES + r * ROWB + (((lane % UPR) ^ (r & (UPR - 1))) * 16)));
-        if (m < b.M) *reinterpret_cast<u32x4 *>(p.out + ((head + m - j * p.G) * p.Bt + j) * D + lane % UPR * 8) = val;
+        if (m < M) *reinterpret_cast<u32x4 *>(p.out + ((head + m - j * p.G) * p.Bt + j) * D + lane % UPR * 8) = val;
     }
-    const int m = b.m0 + 32 * wave + l32, j = p.by_G.divide(min(m, b.M - 1));
-    if (hh == 0 && m < b.M) p.lse[(head + m - j * p.G) * p.Bt + j] = L == 0.f ? -INFINITY : (mref + __builtin_amdgcn_logf(L)) * LN2;
+    const int m = m0 + 32 * wave + l32, j = p.by_G.divide(min(m, M - 1));
+    if (hh == 0 && m < M) p.lse[(head + m - j * p.G) * p.Bt + j] = L == 0.f ? -INFINITY : (mref + __builtin_amdgcn_logf(L)) * LN2;
 }
 
 template <int D>
@@ -498,155 +518,218 @@ __global__ __launch_bounds__(64 * NW) void chunk_whole_kernel(ChunkParams)
     warm_arguments<sizeof(ChunkParams)>();
     const ChunkParams &p = argument_at<ChunkParams>(0);   // (read where it is needed)
     __shared__ __attribute__((aligned(1024))) unsigned char smem[lds_bytes<D>()];
+    __shared__ Kept kept;
     const int h = p.by_slots.divide(blockIdx.x), slot = (int)blockIdx.x - h * p.slots;
     const Block b = block_of(p, slot);
     if (b.tiles == 0) return;   // uniform
-    attend<D>(p, smem, b, h, 0, b.tiles, -1);
+    attend<D>(p, smem, kept, b, h, 0, b.tiles, -1);
 }
 
-// Where a part goes on: tile t of (KV head, slot), `left` tiles, second: it has been at another segment before
+// Where a workgroup goes on: `at` units behind the start of (KV head, slot), `left` units of its part (0: it is done); turn: segments that it has been at
 struct Place {
-    int h, slot, t, left, second;
+    int h, slot, at, left, turn;
 };
-// The list of tiles cut into parts
+// Segments dealt to the workgroups.  Where whole ones can be dealt evenly enough they are: sorted by what they cost, dealt out and back again in
+// turn.  Else the list is cut into equal parts.
 template <int D>
 __global__ __launch_bounds__(64 * NW) void chunk_parts_kernel(ChunkParams)
 {
     warm_arguments<sizeof(ChunkParams)>();
     const ChunkParams &p = argument_at<ChunkParams>(0);   // (read where it is needed)
+    constexpr int NT = 64 * NW;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[lds_bytes<D>()];
-    __shared__ int wave_tiles[NW], wave_used[NW];
+    __shared__ int tot[2][NW];
+    __shared__ int16_t slot_r[NT];   // the slots by rank, where segments stay whole
+    __shared__ int worst, segments_s;
     __shared__ Place place;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wgs = (int)gridDim.x;
-    // workgroups go round the XCDs: those of one XCD take neighbouring parts
-    const int w = wgs % 8 == 0 ? (int)blockIdx.x % 8 * (wgs / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;
-    // every thread the tiles of `each` slots, then sums over the threads
-    const int each = (p.slots + 64 * NW - 1) / (64 * NW), first = tid * each;
-    int mine = 0, used = 0;
-    for (int i = 0; i < each; ++i)
-        if (first + i < p.slots) {
-            const int tiles = block_of(p, first + i).tiles;
-            mine += tiles;
-            used += tiles > 0;
-        }
-    const int upto = (int)wave_inclusive_scan((uint32_t)mine), used_upto = (int)wave_inclusive_scan((uint32_t)used);
-    if (lane == 63) {
-        wave_tiles[wave] = upto;
-        wave_used[wave] = used_upto;
-    }
-    __syncthreads();
-    int before = upto - mine, segments = 0;
-    Plan plan{0, 1};
-#pragma unroll
-    for (int i = 0; i < NW; ++i) {
-        if (i < wave) before += wave_tiles[i];
-        plan.per_head += wave_tiles[i];
-        segments += wave_used[i];
-    }
-    if (plan.per_head == 0) return;   // uniform: the join finds nothing either
-    plan.parts = parts_of((int64_t)segments * p.hkv, (int64_t)plan.per_head * p.hkv, wgs);
-    if (blockIdx.x == 0) {   // for the join
-        if (tid == 0) {
-            p.plan[0] = plan.per_head;
-            p.plan[1] = plan.parts;
-        }
-        int at = before;
+    __shared__ Cut plan_s;
+    __shared__ Kept kept;
+    {
+        const int tid = threadIdx.x, wgs = (int)gridDim.x;
+        // every thread the cost of `each` slots, then sums over the threads
+        const int each = (p.slots + NT - 1) / NT, first = tid * each;
+        int mine = 0, used = 0;
         for (int i = 0; i < each; ++i)
             if (first + i < p.slots) {
-                p.plan[CHUNK_PLAN_WORDS + first + i] = at;
-                at += block_of(p, first + i).tiles;
+                const int cost = cost_of(block_of(p, first + i));
+                mine += cost;
+                used += cost > 0;
             }
-    }
-    if (w >= plan.parts) return;
-    {
-        const int64_t begin = part_begin(p, plan, w);
-        const int h = (int)(begin / plan.per_head), from = (int)(begin - (int64_t)h * plan.per_head);
-        if (from >= before && from < before + mine) {   // one thread's
-            int at = before, slot = first;
-            for (;; ++slot) {
-                const int tiles = block_of(p, slot).tiles;
-                if (from < at + tiles) break;
-                at += tiles;
+        if (tid == 0) worst = 0;
+        int *cost_s = reinterpret_cast<int *>(smem), *cost_r = cost_s + NT;
+        cost_s[tid] = mine;
+        const Sums sum = sums_over_threads<NW>(mine, used, tot);
+        const int segments = sum.entries, before = sum.cost_before;
+        Cut plan{sum.cost, segments ? parts_of(segments * p.hkv, sum.cost * p.hkv, wgs, LEAST) : 1, 0, 0};
+        plan.set(sum.cost * p.hkv);
+        // whole segments: heads side by side, `groups` workgroups each, so that an XCD's L2 serves few of them
+        const int groups = wgs / p.hkv;
+        bool whole = segments == 0;
+        if (each == 1 && groups > 0) {
+            if (mine > 0) {
+                const int rank = rank_by_cost(cost_s, p.slots, tid);
+                slot_r[rank] = (int16_t)tid;
+                cost_r[rank] = mine;
             }
-            place = Place{h, slot, from - at, (int)(part_begin(p, plan, w + 1) - begin), 0};
+            __syncthreads();
+            whole = whole || dealt_worst(cost_r, segments, groups, &worst) <= plan.wide + START + JOIN;
         }
+        if (tid == 0) p.cuts[part_number()].pieces = 0;   // (the join's; written again where a segment is cut)
+        if (whole) {
+            const int g = (int)blockIdx.x / p.hkv;
+            if (tid == 0) {
+                segments_s = segments;
+                place = Place{(int)blockIdx.x % p.hkv, g < groups && g < segments ? slot_r[g] : 0, 0, g < groups && g < segments ? INT32_MAX : 0, 0};
+            }
+        } else {
+            const int w = part_number();
+            if (w >= plan.parts) return;
+            const int begin = plan.begin(w), h = begin / plan.per_head, from = begin - h * plan.per_head;
+            if (tid == 0) {
+                segments_s = 0;
+                plan_s = plan;
+            }
+            if (from >= before && from < before + mine) {   // one thread's
+                int at = before, slot = first;
+                for (;; ++slot) {
+                    const int cost = cost_of(block_of(p, slot));
+                    if (from < at + cost) break;
+                    at += cost;
+                }
+                place = Place{h, slot, from - at, plan.begin(w + 1) - begin, 0};
+            }
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    for (;;) {   // (where the part goes on is kept in LDS: the loop over the tiles has no scalar registers to spare)
-        const int h = __builtin_amdgcn_readfirstlane(place.h), slot = __builtin_amdgcn_readfirstlane(place.slot), t = __builtin_amdgcn_readfirstlane(place.t);
-        const int left = __builtin_amdgcn_readfirstlane(place.left), second = __builtin_amdgcn_readfirstlane(place.second);
+    for (;;) {   // (where the workgroup goes on is kept in LDS: the loop over the tiles has no registers to spare)
+        const int h = __builtin_amdgcn_readfirstlane(place.h), slot = __builtin_amdgcn_readfirstlane(place.slot), at = __builtin_amdgcn_readfirstlane(place.at);
+        const int left = __builtin_amdgcn_readfirstlane(place.left), turn = __builtin_amdgcn_readfirstlane(place.turn);
         if (left == 0) return;   // uniform
         const Block b = block_of(p, slot);
-        const int take = min(b.tiles - t, left);
+        const int cost = cost_of(b), take = min(cost - at, left);
         __syncthreads();
-        if (tid == 0) place = slot + 1 == p.slots ? Place{h + 1, 0, 0, left - take, second | (take > 0)} : Place{h, slot + 1, 0, left - take, second | (take > 0)};
-        if (take > 0) attend<D>(p, smem, b, h, t, t + take, take == b.tiles ? -1 : 2 * w + second);
+        if (threadIdx.x == 0) {
+            const int segments = segments_s;
+            if (segments > 0) {
+                const int groups = (int)gridDim.x / p.hkv, g = (int)blockIdx.x / p.hkv, k = turn + 1, r = dealt_rank(k, g, groups);
+                place = Place{h, r < segments ? slot_r[r] : 0, 0, r < segments ? INT32_MAX : 0, k};
+            } else {
+                if (at == 0 && cost > left) {   // the segment begins here and is cut by the end of the part: what the join has to know of it
+                    const Cut plan = plan_s;
+                    const int w = part_number(), x0 = plan.begin(w + 1) - left;
+                    int w0 = w, w1 = plan.part_of(x0 + cost - 1);
+                    while (w0 < w1 && cut_at(b, plan.begin(w0 + 1) - x0) == 0) ++w0;   // (of the first and the last part perhaps no tile)
+                    while (w0 < w1 && cut_at(b, plan.begin(w1) - x0) == b.tiles) --w1;
+                    p.cuts[w] = ChunkCut{b.s, h, b.m0, b.M, 2 * w0 + (plan.begin(w0) < x0), w1 - w0 + 1};
+                }
+                place = slot + 1 == p.slots ? Place{h + 1, 0, 0, left - take, turn | (cost > 0)} : Place{h, slot + 1, 0, left - take, turn | (cost > 0)};
+            }
+        }
+        if (take > 0) {
+            const int w = part_number();
+            const int t0 = cut_at(b, at), t1 = at + take == cost ? b.tiles : cut_at(b, at + take);
+            if (t0 < t1) attend<D>(p, smem, kept, b, h, t0, t1, t1 - t0 == b.tiles ? -1 : 2 * w + turn);
+        }
         __syncthreads();
     }
 }
 
-// Joins the partials of the segments that were cut: a workgroup 32 rows of one
+// Joins the partials of the segments that were cut: a workgroup 32 rows of the one that the end of a part has cut first, if it has, each of its waves a
+// quarter of the columns
 template <int D>
 __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkParams p)
 {
-    const int per = p.part_rows / 32, id = (int)blockIdx.x / per, wave = (int)blockIdx.x - id * per;
-    const int h = p.by_slots.divide(id), slot = id - h * p.slots;
-    const Block b = block_of(p, slot);
-    if (b.tiles == 0 || b.m0 + 32 * wave >= b.M) return;
-    const Plan plan{p.plan[0], p.plan[1]};
-    const int64_t x0 = (int64_t)h * plan.per_head + p.plan[CHUNK_PLAN_WORDS + slot], x1 = x0 + b.tiles;
-    const int w0 = part_of(p, plan, x0), w1 = part_of(p, plan, x1 - 1);
-    if (w0 == w1) return;
-    const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5, group = threadIdx.x >> 6;
-    const int64_t first = 2 * (int64_t)w0 + (part_begin(p, plan, w0) != x0);
-    auto slot_at = [&](int w) { return w == w0 ? first : 2 * (int64_t)w; };
+    const int per = p.part_rows / 32, border = (int)blockIdx.x / per, wave = (int)blockIdx.x - border * per;
+    const ChunkCut cut = p.cuts[border];
+    if (cut.pieces <= 1 || cut.m0 + 32 * wave >= cut.M) return;   // uniform
+    const int pieces = cut.pieces, first = cut.first;
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5, quarter = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int SLABS = D / 16, MINE = SLABS / 4, BATCH = 8;
     float top = -INFINITY, L = 0.f;
-    for (int w = w0; w <= w1; ++w) top = fmaxf(top, p.part_ml[slot_at(w) * p.part_rows + 32 * wave + l32].x);
-    constexpr int SLABS = D / 8, MINE = SLABS / 4;
-    f32x4 acc[MINE];
+    int power = -126;   // of the sums so far; of a piece's rows it is the third number beside the reference and the weight sum
+    float acc[MINE][8] = {};
+    for (int k0 = 0; k0 < pieces; k0 += BATCH) {
+        f32x4 ml[BATCH];
+        f16x8 o[BATCH][MINE];
 #pragma unroll
-    for (int i = 0; i < MINE; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int w = w0; w <= w1; ++w) {
-        const float2 ml = p.part_ml[slot_at(w) * p.part_rows + 32 * wave + l32];
-        const float f = ml.x == -INFINITY ? 0.f : ml.y * __builtin_amdgcn_exp2f(ml.x - top);
-        const float *base = p.part_o + ((slot_at(w) * per + wave) * SLABS * 64 + lane) * 4;
-        L += f;
+        for (int k = 0; k < BATCH; ++k) {
+            ml[k] = f32x4{-INFINITY, 0.f, __int_as_float(-126), 0.f};
 #pragma unroll
-        for (int i = 0; i < MINE; ++i) acc[i] += f * *reinterpret_cast<const f32x4 *>(base + (size_t)(group + 4 * i) * 64 * 4);
+            for (int c = 0; c < MINE; ++c) o[k][c] = f16x8{};
+            if (k0 + k < pieces) {   // uniform
+                const int64_t at = k0 + k == 0 ? first : (first & ~1) + 2 * (int64_t)(k0 + k);
+                ml[k] = p.part_ml[at * p.part_rows + 32 * wave + l32];
+#pragma unroll
+                for (int c = 0; c < MINE; ++c)
+                    o[k][c] = *reinterpret_cast<const f16x8 *>(p.part_o + (((at * per + wave) * SLABS + quarter * MINE + c) * 64 + lane) * 8);
+            }
+        }
+        float high = top;
+        int most = power;
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            high = fmaxf(high, ml[k][0]);
+            most = max(most, __float_as_int(ml[k][2]));
+        }
+        if (k0 > 0) {
+            const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - high), g = __builtin_amdgcn_ldexpf(old, power - most);
+            L *= old;
+#pragma unroll
+            for (int c = 0; c < MINE; ++c)
+#pragma unroll
+                for (int r = 0; r < 8; ++r) acc[c][r] *= g;
+        }
+        top = high;
+        power = most;
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const float f = ml[k][0] == -INFINITY ? 0.f : ml[k][1] * __builtin_amdgcn_exp2f(ml[k][0] - top);
+            const float g = __builtin_amdgcn_ldexpf(f, __float_as_int(ml[k][2]) - power);
+            L += f;
+#pragma unroll
+            for (int c = 0; c < MINE; ++c)
+#pragma unroll
+                for (int r = 0; r < 8; ++r) acc[c][r] += g * (float)o[k][c][r];
+        }
     }
-    const int m = b.m0 + 32 * wave + l32;
-    if (m >= b.M) return;
+    const int m = cut.m0 + 32 * wave + l32;
+    if (m >= cut.M) return;
     const float inv = L > 0.f ? 1.f / L : 0.f;
     const int j = p.by_G.divide(m), g = m - j * p.G;
-    const int64_t row = ((int64_t)b.s * p.hkv * p.G + h * p.G + g) * p.Bt + j;
+    const int64_t row = ((int64_t)cut.s * p.hkv * p.G + cut.h * p.G + g) * p.Bt + j;
 #pragma unroll
-    for (int i = 0; i < MINE; ++i) {
-        bf16x4 o;
+    for (int i = 0; i < MINE; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[r] = (__bf16)(acc[i][r] * inv);
-        *reinterpret_cast<bf16x4 *>(p.out + row * D + 8 * (group + 4 * i) + 4 * hh) = o;
-    }
-    if (group == 0 && hh == 0) p.lse[row] = L == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(L)) * LN2;
+        for (int jj = 0; jj < 2; ++jj) {   // slab 2 db + half: columns 32 db + 16 half + 8 jj + 4 hh ..
+            bf16x4 o;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = (__bf16)__builtin_amdgcn_ldexpf(acc[i][4 * jj + r] * inv, power - 14);
+            *reinterpret_cast<bf16x4 *>(p.out + row * D + 16 * (quarter * MINE + i) + 8 * jj + 4 * hh) = o;
+        }
+    if (quarter == 0 && hh == 0) p.lse[row] = L == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(L)) * LN2;
 }
 
-// Tiles that a segment can have at most
+// Tiles that a segment can have at most, and how many of them are not worth a plan
+constexpr int SHORT = 4;
 int64_t most_tiles(int prefix_len, int64_t table_rows) { return (prefix_len + TK - 1) / TK + (table_rows + TK - 1) / TK; }
 
 }  // namespace
 
-int chunk_block_rows() { return R; }
+bool chunk_fits(int n_seqs, int hkv, int G, int Bt, int prefix_len, int64_t table_rows)
+{
+    const int64_t blocks = ((int64_t)G * Bt + R - 1) / R;
+    return (double)n_seqs * hkv * blocks * (START + 9.0 * (double)most_tiles(prefix_len, table_rows)) < 2147483647.0;
+}
 
 // Cut segments leave two partials a workgroup
-size_t chunk_workspace(int n_seqs, int hkv, int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_plan)
+size_t chunk_workspace(int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_cuts)
 {
-    const int64_t rows = std::min<int64_t>(R, ((int64_t)G * Bt + 31) / 32 * 32), blocks = ((int64_t)G * Bt + R - 1) / R;
-    size_t off = (size_t)2 * cus * rows * D * 4;
+    const int64_t rows = std::min<int64_t>(R, ((int64_t)G * Bt + 31) / 32 * 32);
+    size_t off = (size_t)2 * cus * rows * D * 2;
     *off_ml = off;
-    off += ((size_t)2 * cus * rows * 8 + 255) & ~(size_t)255;
-    *off_plan = off;
-    off += ((size_t)(CHUNK_PLAN_WORDS + n_seqs * blocks) * 4 + 255) & ~(size_t)255;
-    return off;
+    off += (size_t)2 * cus * rows * 16;
+    *off_cuts = off;
+    return off + (((size_t)cus * sizeof(ChunkCut) + 255) & ~(size_t)255);
 }
 
 namespace {
@@ -655,14 +738,14 @@ template <int D>
 hipError_t launch(const ChunkParams &p, hipStream_t s)
 {
     const int64_t segments = (int64_t)p.slots * p.hkv;
-    if (most_tiles(p.prefix_len, (int64_t)p.pages.width << p.pages.page_shift) <= 2 * MIN_TILES) {
+    if (most_tiles(p.prefix_len, (int64_t)p.pages.width << p.pages.page_shift) <= SHORT * 2) {
         hipLaunchKernelGGL((chunk_whole_kernel<D>), dim3((unsigned)segments), dim3(64 * NW), 0, s, p);
         return hipGetLastError();
     }
     hipLaunchKernelGGL((chunk_parts_kernel<D>), dim3(p.cus), dim3(64 * NW), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((chunk_join_kernel<D>), dim3((unsigned)(segments * (p.part_rows / 32))), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((chunk_join_kernel<D>), dim3((unsigned)((p.cus - 1) * (p.part_rows / 32))), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 

@@ -11,6 +11,7 @@
 //         joined by a second launch, in order.
 // No atomics: every sum has one order.
 #include <algorithm>
+#include <type_traits>
 
 #include "kd_device.h"
 #include "kd_pages.h"
@@ -190,10 +191,19 @@ constexpr int QT = 64;             // query rows of a tile
 constexpr int STAGES = 5;          // tiles of query rows in LDS.  (At the start the second half of the keys occupies the first four.)
 constexpr int SUM_PITCH = 33;
 
+// What a block costs, in units of 0.6 us: START around its tiles (its keys, and the turn of its sums at the end), TILE a tile of query rows
+constexpr int START = 8, TILE = 3;
+// The tile at which a border `at` units behind a block's start cuts it; blocks of few tiles stay whole
+constexpr int FEW_TILES = 4;
+__device__ __forceinline__ int cut_at(int tiles, int at)
+{
+    if (tiles <= FEW_TILES) return 2 * at < START + tiles * TILE ? 0 : tiles;
+    return (max(at - START, 0) + TILE - 1) / TILE;
+}
 // The blocks of a sequence: block k of KB keys is seen by the tiles from seen_from(k) on
 struct Blocks {
     Seq q;
-    int tiles, full, count, cost;   // tiles of query rows; blocks that all tiles see; blocks in all; pairs of both that see one another
+    int tiles, full, count, cost;   // tiles of query rows; blocks that all tiles see; blocks in all; what they cost
 };
 __device__ __forceinline__ int seen_from(const WeightsParams &p, const Seq &q, int k) { return max(k * KB - q.len - q.j0, 0) * p.G / QT; }
 __device__ __forceinline__ Blocks blocks_of(const WeightsParams &p, int s)
@@ -203,21 +213,22 @@ __device__ __forceinline__ Blocks blocks_of(const WeightsParams &p, int s)
     b.tiles = (b.q.rows + QT - 1) / QT;
     b.count = (b.q.n + KB - 1) / KB;
     b.full = min((b.q.len + b.q.j0) / KB + 1, b.count);
-    b.cost = b.full * b.tiles;
-    for (int k = b.full; k < b.count; ++k) b.cost += b.tiles - seen_from(p, b.q, k);
+    b.cost = b.count * START + b.full * b.tiles * TILE;
+    for (int k = b.full; k < b.count; ++k) b.cost += (b.tiles - seen_from(p, b.q, k)) * TILE;
     return b;
 }
-// Block and offset in it of pair `at` of a sequence
+// Block, and offset in it, `at` units behind the start of a sequence
 __device__ __forceinline__ int block_at(const WeightsParams &p, const Blocks &b, int at, int *offset)
 {
-    if (at < b.full * b.tiles) {
-        const int k = at / b.tiles;
-        *offset = at - k * b.tiles;
+    const int whole = START + b.tiles * TILE;
+    if (at < b.full * whole) {
+        const int k = at / whole;
+        *offset = at - k * whole;
         return k;
     }
-    at -= b.full * b.tiles;
+    at -= b.full * whole;
     for (int k = b.full;; ++k) {
-        const int cost = b.tiles - seen_from(p, b.q, k);
+        const int cost = START + (b.tiles - seen_from(p, b.q, k)) * TILE;
         if (at < cost) {
             *offset = at;
             return k;
@@ -226,23 +237,14 @@ __device__ __forceinline__ int block_at(const WeightsParams &p, const Blocks &b,
     }
 }
 
-struct Plan {
-    int per_head, parts;
-};
-__device__ __forceinline__ int64_t part_begin(const WeightsParams &p, const Plan &plan, int w) { return (int64_t)w * plan.per_head * p.hkv / plan.parts; }
-__device__ __forceinline__ int part_of(const WeightsParams &p, const Plan &plan, int64_t x) { return (int)(((x + 1) * plan.parts - 1) / ((int64_t)plan.per_head * p.hkv)); }
-constexpr int MIN_TILES = 4;   // tiles a part at least, where there are more parts than blocks
-__device__ __forceinline__ int parts_of(int64_t segments, int64_t total, int wgs)
-{
-    int64_t parts = segments <= wgs ? segments * (wgs / segments) : wgs;
-    if (parts > segments) parts = total / MIN_TILES < parts ? (total / MIN_TILES > segments ? total / MIN_TILES : segments) : parts;
-    return (int)parts;
-}
+constexpr int LEAST = START + 4 * TILE;   // units of a part at least
+// What cut blocks cost a launch: their second START, and the join
+constexpr int JOIN = START + 6;
 
 template <int D>
 struct Lds {
     static constexpr int ROWB = 2 * D, HALF = 32 * NW * ROWB, STAGE = QT * ROWB;
-    static constexpr int RING = HALF, LSE = RING + STAGES * STAGE, BYTES = LSE + STAGES * QT * 4;
+    static constexpr int RING = HALF, LSE = RING + STAGES * STAGE, OLD = LSE + STAGES * QT * 4, BYTES = OLD + KB * 8;   // OLD: place and weight of each row
     static_assert(HALF <= (STAGES - 1) * STAGE && NW * 64 * SUM_PITCH * 4 <= LSE, "");
 };
 
@@ -275,35 +277,66 @@ __device__ void weigh(const WeightsParams &p, unsigned char *smem, const Seq &sq
     const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
     const int ntl = q1 - q0;
     auto stage = [&](int i) { return (i + STAGES - 1) % STAGES; };   // of the i-th tile
-    // tile q0 + i of query rows; rows behind the last one stand for it
+    // Tile q0 + i of query rows; rows behind the last one stand for it.  Where the heads of a group divide a tile, a lane's rows lie as far behind the
+    // first one in every tile, and a copy takes a scalar address and an offset (worked out anew for each row it was a third of the loop's instructions).
+    const bool alike = QT % p.G == 0 && ((uint64_t)p.G * p.q.head + (uint64_t)QT * p.q.token) * 2 < (1u << 31) && (uint64_t)p.G * p.Bt * 4 < (1u << 31);
+    uint32_t off[CPW + 1];
+#pragma unroll
+    for (int c = 0; c <= CPW; ++c) {
+        const int row = c < CPW ? (wave + NW * c) * RPL + lane / UPR : wave * (QT / NW) + (lane & (QT / NW - 1)), j = p.by_G.divide(row), g = row - j * p.G;
+        off[c] = c < CPW ? (uint32_t)(g * p.q.head + j * p.q.token) * 2 + ((lane % UPR) ^ (row & (UPR - 1))) * 16 : (uint32_t)(g * p.Bt + j) * 4;
+    }
+    const uint16_t *qh = p.q.p + (int64_t)s * p.q.seq + (int64_t)h * p.G * p.q.head + (int64_t)sq.j0 * p.q.token;
+    const float *lh = p.lse + (int64_t)(s * p.hkv + h) * p.G * p.Bt + sq.j0;
     auto issue = [&](int i) {
-        const uint32_t to = lds0 + L::RING + stage(i) * L::STAGE;
+        const uint32_t to = lds0 + L::RING + stage(i) * L::STAGE, to_lse = lds0 + L::LSE + stage(i) * QT * 4 + wave * (QT / NW) * 4;
+        if (alike && (q0 + i + 1) * QT <= sq.rows) {   // uniform
+            const int j = p.by_G.divide((q0 + i) * QT);
+#pragma unroll
+            for (int c = 0; c < CPW; ++c) lds_copy16(to + 1024u * (wave + NW * c), qh + (int64_t)j * p.q.token, off[c]);
+            if (lane < QT / NW) lds_copy4(to_lse, reinterpret_cast<const char *>(lh + j) + off[CPW]);
+            return;
+        }
+        int ln = lane;
+        asm volatile("" : "+v"(ln));   // (what follows from it is worked out here, not kept in registers)
 #pragma unroll
         for (int c = 0; c < CPW; ++c) {
-            const int row = (wave + NW * c) * RPL + lane / UPR, m = min((q0 + i) * QT + row, sq.rows - 1), jr = p.by_G.divide(m);
-            const uint16_t *at = p.q.p + (int64_t)s * p.q.seq + (int64_t)(h * p.G + m - jr * p.G) * p.q.head + (int64_t)(sq.j0 + jr) * p.q.token;
-            lds_copy16(to + 1024u * (wave + NW * c), reinterpret_cast<const char *>(at) + ((lane % UPR) ^ (row & (UPR - 1))) * 16);
+            const int row = (wave + NW * c) * RPL + ln / UPR, m = min((q0 + i) * QT + row, sq.rows - 1), j = p.by_G.divide(m);
+            const uint16_t *at = qh + (int64_t)(m - j * p.G) * p.q.head + (int64_t)j * p.q.token;
+            lds_copy16(to + 1024u * (wave + NW * c), reinterpret_cast<const char *>(at) + ((ln % UPR) ^ (row & (UPR - 1))) * 16);
         }
-        if (lane < QT / NW) {
-            const int row = wave * (QT / NW) + lane, m = min((q0 + i) * QT + row, sq.rows - 1), jr = p.by_G.divide(m);
-            lds_copy4(lds0 + L::LSE + stage(i) * QT * 4 + wave * (QT / NW) * 4, p.lse + ((int64_t)(s * p.hkv + h) * p.G + m - jr * p.G) * p.Bt + sq.j0 + jr);
+        if (ln < QT / NW) {
+            const int m = min((q0 + i) * QT + wave * (QT / NW) + ln, sq.rows - 1), j = p.by_G.divide(m);
+            lds_copy4(to_lse, lh + (int64_t)(m - j * p.G) * p.Bt + j);
         }
     };
     __syncthreads();   // nobody reads what the block before has left in LDS
-    // the keys: rows of the wave, half in the place of four stages
+    // the keys: rows of the wave, half in the place of four stages.  (The pages of all 64 rows are looked up at once, a lane each.)
+    const int pages = table_entry(table, min(key0 + lane, last) >> shift);
 #pragma unroll
     for (int kg = 0; kg < 2; ++kg)
 #pragma unroll
         for (int i = 0; i < 32 / RPL; ++i) {
-            const int in = RPL * i, row0 = min(key0 + 32 * kg + in, last & ~7), row = min(key0 + 32 * kg + in + lane / UPR, last);
-            const int page = table_entry(table, min(key0 + 32 * kg + in, last) >> shift);
+            const int in = RPL * i, row = min(key0 + 32 * kg + in + lane / UPR, last);   // (rows behind the last one stand for it)
+            const int page = __builtin_amdgcn_readlane(pages, 32 * kg + in);
             const int64_t off = ((((int64_t)page * p.hkv + h) << shift) + (row & ((1 << shift) - 1))) * D;
             const char *at = (uint32_t)page < (uint32_t)p.pages.n_pages ? reinterpret_cast<const char *>(p.pages.k + off) : reinterpret_cast<const char *>(zeros);
-            (void)row0;
             lds_copy16(lds0 + (kg ? L::RING : 0) + wave * 32 * ROWB + 1024u * i, at + ((lane % UPR) ^ ((in + lane / UPR) & (UPR - 1))) * 16);
         }
     issue(0);
-    wait_copies<CPT>();
+    // where the weight of row key0 + lane goes, and what it has gathered so far: asked for now, kept in LDS
+    struct Old {
+        int page;   // negative: nowhere
+        float w;
+    };
+    Old *old = reinterpret_cast<Old *>(smem + L::OLD) + 64 * wave + lane;
+    {
+        const int r = key0 + lane;
+        Old o{r <= last && (uint32_t)pages < (uint32_t)p.pages.n_pages ? pages : -1, 0.f};
+        if (!part && o.page >= 0 && r < sq.len && p.decay != 0.f) o.w = p.decay * p.w[(((int64_t)pages * p.hkv + h) << shift) + (r & ((1 << shift) - 1))];
+        wait_copies<CPT>();
+        *old = o;
+    }
     bf16x8 kreg[2][NC];
 #pragma unroll
     for (int kg = 0; kg < 2; ++kg)
@@ -322,41 +355,128 @@ __device__ void weigh(const WeightsParams &p, unsigned char *smem, const Seq &sq
     __syncthreads();
     if (ntl > 1) issue(1);
     if (ntl > 2) issue(2);
+    if (ntl > 3) issue(3);
+    // Half a tile, 32 query rows, at a time: the products of one beside the exponentials of the one before, in an order that the scheduling barriers pin.
+    // A lane's 32 exponentials go in slices of two through three steps one beat apart: scale and shift, exponential, sum.
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < ntl; ++i) {
+    auto tile_at = [&](int i) { return smem + L::RING + stage(i) * L::STAGE; };
+    const int qof0 = l32 * ROWB + (hh ^ (l32 & (UPR - 1))) * 16;   // chunk c of a row: unit 2 c + hh, swizzled by the row
+    auto read_q = [&](const unsigned char *tq, int c) { return as_bf16x8(*reinterpret_cast<const u32x4 *>(tq + (qof0 ^ (32 * c)))); };
+    // of the lane's query row: what the call was given, and in log2 units, +inf where the row gives no weight
+    auto read_lse = [&](int i, int half) { return (reinterpret_cast<const float *>(smem + L::LSE) + stage(i) * QT)[32 * half + l32]; };
+    auto logarithm = [&](float x, int i, int half) { return (q0 + i) * QT + 32 * half + l32 < sq.rows ? in_log2(x) : INFINITY; };
+    auto mask = [&](f32x16 (&sc)[2], int i, int half) {   // rows that not every query of the half tile sees (uniform)
+        const int m0 = (q0 + i) * QT + 32 * half;
+        if (key0 + 63 <= sq.len + sq.j0 + p.by_G.divide(min(m0, sq.rows - 1))) return;
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const int lim = sq.len + sq.j0 + p.by_G.divide(min(m0 + (ln & 31), sq.rows - 1)) - key0 - 4 * (ln >> 5);
+#pragma unroll
+        for (int kg = 0; kg < 2; ++kg)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[kg][e] = 32 * kg + 8 * (e >> 2) + (e & 3) <= lim ? sc[kg][e] : -INFINITY;
+    };
+    // sc, lse2: logits of the half tile to be weighed; sn: those of the next one, formed beside them (NEXT) from its rows at tq, the first AHEAD operands of
+    // which are in qn already; those of the one behind it, at tn, are requested at the end (MORE)
+    constexpr int AHEAD = 2;
+    bf16x8 qn[AHEAD];
+    auto request = [&](const unsigned char *tq) {
+#pragma unroll
+        for (int c = 0; c < AHEAD; ++c) qn[c] = read_q(tq, c);
+    };
+    auto step = [&](const f32x16 (&sc)[2], float lse2, f32x16 (&sn)[2], const unsigned char *tq, const unsigned char *tn, auto next_tag, auto more_tag) {
+        constexpr bool NEXT = decltype(next_tag)::value, MORE = decltype(more_tag)::value;
+        constexpr int NP = 2 * NC, NS = 16, SPB = NS / NP > 0 ? NS / NP : 1;   // products, slices, slices a beat
+        bf16x8 qf[AHEAD + 1];
+        float arg[2][SPB][2], ex[2][SPB][2];
+        auto F = [&](int sl, float (&x)[2]) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                x[r] = __builtin_fmaf(sc[sl >> 3][2 * (sl & 7) + r], p.scale_log2e, -lse2);
+                asm volatile("" : "+v"(x[r]));   // (here, and not where it is used)
+            }
+        };
+        if (NEXT) {
+#pragma unroll
+            for (int c = 0; c < AHEAD; ++c) qf[c] = qn[c];
+        }
+#pragma unroll
+        for (int e = 0; e < SPB; ++e) F(e, arg[0][e]);
+        constexpr int BEATS = NS / SPB;
+#pragma unroll
+        for (int b = 0; b <= BEATS; ++b) {
+            if (NEXT && b < NP) {
+                if (b % 2 == 0 && b / 2 + AHEAD < NC) qf[(b / 2 + AHEAD) % (AHEAD + 1)] = read_q(tq, b / 2 + AHEAD);
+                sn[b % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kreg[b % 2][b / 2], qf[b / 2 % (AHEAD + 1)], b < 2 ? zero : sn[b % 2], 0, 0, 0);
+                if (MORE && b == NP - 4) request(tn);
+            }
+            if (b < BEATS) {
+#pragma unroll
+                for (int e = 0; e < SPB; ++e)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        ex[b & 1][e][r] = __builtin_amdgcn_exp2f(arg[b & 1][e][r]);
+                        asm volatile("" : "+v"(ex[b & 1][e][r]));
+                    }
+            }
+            if (b > 0) {
+#pragma unroll
+                for (int e = 0; e < SPB; ++e) {
+                    const int sl = SPB * (b - 1) + e;
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        acc[sl >> 3][2 * (sl & 7) + r] += ex[(b - 1) & 1][e][r];
+                        asm volatile("" : "+v"(acc[sl >> 3][2 * (sl & 7) + r]));
+                    }
+                }
+            }
+            if (b + 1 < BEATS) {
+#pragma unroll
+                for (int e = 0; e < SPB; ++e) F(SPB * (b + 1) + e, arg[(b + 1) & 1][e]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto open = [&](int i) {   // tile i has landed
         if (i + 2 < ntl) wait_copies<2 * CPT>();
         else if (i + 1 < ntl) wait_copies<CPT>();
         else wait_copies<0>();
-        __syncthreads();   // tile i is there, and every wave is through with tile i - 1
-        if (i + 3 < ntl) issue(i + 3);
-        const unsigned char *tq = smem + L::RING + stage(i) * L::STAGE;
-        const float *tl = reinterpret_cast<const float *>(smem + L::LSE) + stage(i) * QT;
+        __syncthreads();   // ... every wave's part of it, and every wave is through with tile i - 2
+    };
+    using T_ = std::true_type;
+    using F_ = std::false_type;
+    constexpr int HALF = 32 * ROWB;
+    f32x16 s0[2], s1[2];
+    if (ntl > 3) wait_copies<3 * CPT>();   // tile 0
+    else if (ntl > 2) wait_copies<2 * CPT>();
+    else if (ntl > 1) wait_copies<CPT>();
+    else wait_copies<0>();
+    __syncthreads();
+    {
+        const unsigned char *tq = tile_at(0);
 #pragma unroll
-        for (int half = 0; half < QT / 32; ++half) {
-            const int m = (q0 + i) * QT + 32 * half + l32;
-            const float lse2 = m < sq.rows ? in_log2(tl[32 * half + l32]) : INFINITY;
-            f32x16 sc[2];
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const bf16x8 qf = as_bf16x8(*reinterpret_cast<const u32x4 *>(tq + (32 * half + l32) * ROWB + (((2 * c + hh) ^ (l32 & (UPR - 1))) * 16)));
-#pragma unroll
-                for (int kg = 0; kg < 2; ++kg) sc[kg] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kreg[kg][c], qf, c == 0 ? zero : sc[kg], 0, 0, 0);
-            }
-            // rows that not every query of the tile sees (uniform)
-            const int seen = sq.len + sq.j0 + p.by_G.divide(min((q0 + i) * QT + 32 * half, sq.rows - 1));
-            if (key0 + 63 > seen) {
-                const int lim = sq.len + sq.j0 + p.by_G.divide(min(m, sq.rows - 1)) - key0 - 4 * hh;
-#pragma unroll
-                for (int kg = 0; kg < 2; ++kg)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) sc[kg][e] = 32 * kg + 8 * (e >> 2) + (e & 3) <= lim ? sc[kg][e] : -INFINITY;
-            }
-#pragma unroll
-            for (int kg = 0; kg < 2; ++kg)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[kg][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kg][e], p.scale_log2e, -lse2));
-        }
+        for (int b = 0; b < 2 * NC; ++b)
+            s0[b % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kreg[b % 2][b / 2], read_q(tq, b / 2), b < 2 ? zero : s0[b % 2], 0, 0, 0);
+        mask(s0, 0, 0);
+        request(tq + HALF);
     }
+    float x0 = read_lse(0, 0), x1 = read_lse(0, 1);
+    for (int i = 0; i + 1 < ntl; ++i) {
+        open(i + 1);
+        if (i + 4 < ntl) issue(i + 4);
+        const unsigned char *tq = tile_at(i), *tn = tile_at(i + 1);
+        const float l0 = logarithm(x0, i, 0), l1 = logarithm(x1, i, 1);
+        x0 = read_lse(i + 1, 0);
+        x1 = read_lse(i + 1, 1);
+        step(s0, l0, s1, tq + HALF, tn, T_{}, T_{});
+        mask(s1, i, 1);
+        step(s1, l1, s0, tn, tn + HALF, T_{}, T_{});
+        mask(s0, i + 1, 0);
+    }
+    const float l1 = logarithm(x1, ntl - 1, 1);
+    step(s0, logarithm(x0, ntl - 1, 0), s1, tile_at(ntl - 1) + HALF, nullptr, T_{}, F_{});
+    mask(s1, ntl - 1, 1);
+    step(s1, l1, s0, nullptr, nullptr, F_{}, F_{});
     // the sums over the lanes of a row of keys, turned in LDS: lane i gets key i
     __syncthreads();
     float *turn = reinterpret_cast<float *>(smem) + wave * 64 * SUM_PITCH;
@@ -375,81 +495,135 @@ __device__ void weigh(const WeightsParams &p, unsigned char *smem, const Seq &sq
         part[64 * wave + lane] = sum;
         return;
     }
-    const int r = key0 + lane;
-    if (r > last) return;
-    const int page = table_entry(table, r >> shift);
-    if ((uint32_t)page >= (uint32_t)p.pages.n_pages) return;
-    float *w = p.w + (((int64_t)page * p.hkv + h) << shift) + (r & ((1 << shift) - 1));
-    *w = (r < sq.len && p.decay != 0.f ? p.decay * *w : 0.f) + sum;
+    const Old o = *old;
+    if (o.page >= 0) p.w[(((int64_t)o.page * p.hkv + h) << shift) + ((key0 + lane) & ((1 << shift) - 1))] = o.w + sum;
 }
 
+// Where a workgroup goes on: `at` units behind the start of block k of sequence s; `left` units of its part (0: it is done); turn: blocks that it has been at
 struct Place {
-    int h, s, k, t, left, second;   // tile t (of those that see it) of block k of sequence s; `left` pairs; second: the part has been at another block before
+    int h, s, k, at, left, turn;
 };
 
+// Blocks dealt to the workgroups.  Where whole ones can be dealt evenly enough they are: sorted by what they cost, dealt out and back again in turn.  Else the
+// list of what they cost is cut into equal parts.
 template <int D>
 __global__ __launch_bounds__(64 * NW) void weights_many_kernel(WeightsParams)
 {
     const WeightsParams &p = argument_at<WeightsParams>(0);   // (read where it is needed)
+    constexpr int NT = 64 * NW;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[Lds<D>::BYTES];
-    __shared__ uint32_t wave_tot[2][NW];
+    __shared__ int tot[2][NW];
+    __shared__ int seq_r[NT];      // sequence and block by rank, where blocks stay whole
+    __shared__ int16_t block_r[NT];
+    __shared__ int worst, blocks_s;
     __shared__ Place place;
-    const int tid = threadIdx.x, wgs = (int)gridDim.x;
-    const int wg = wgs % 8 == 0 ? (int)blockIdx.x % 8 * (wgs / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;   // neighbouring parts on one XCD
-    const int each = (p.n_seqs + 64 * NW - 1) / (64 * NW), first = tid * each;
-    int mine = 0, used = 0;
-    for (int i = 0; i < each; ++i)
-        if (first + i < p.n_seqs) {
-            const Blocks b = blocks_of(p, first + i);
-            mine += b.cost;
-            used += b.count;
-        }
-    uint32_t total, segments;
-    const int before = (int)block_exclusive_scan_t<64 * NW, uint32_t>((uint32_t)mine, wave_tot[0], &total);
-    (void)block_exclusive_scan_t<64 * NW, uint32_t>((uint32_t)used, wave_tot[1], &segments);
-    if (blockIdx.x == 0) {   // for the join
-        int at = before;
+    const int tid = threadIdx.x, wgs = (int)gridDim.x, wg = part_number();
+    {
+        const int each = (p.n_seqs + NT - 1) / NT, first = tid * each;
+        int mine = 0, used = 0;
+        Blocks own{};
         for (int i = 0; i < each; ++i)
             if (first + i < p.n_seqs) {
-                p.plan[WEIGHTS_PLAN_WORDS + first + i] = at;
-                at += blocks_of(p, first + i).cost;
+                own = blocks_of(p, first + i);
+                mine += own.cost;
+                used += own.count;
             }
-    }
-    Plan plan{(int)total, 1};
-    if (total) plan.parts = parts_of((int64_t)segments * p.hkv, (int64_t)total * p.hkv, wgs);
-    if (blockIdx.x == 0 && tid == 0) {
-        p.plan[0] = plan.per_head;
-        p.plan[1] = plan.parts;
-    }
-    if (wg >= plan.parts || total == 0) return;
-    {
-        const int64_t begin = part_begin(p, plan, wg);
-        const int h = (int)(begin / plan.per_head), from = (int)(begin - (int64_t)h * plan.per_head);
-        if (from >= before && from < before + mine) {   // one thread's
-            int at = before, s = first, t;
-            Blocks b = blocks_of(p, s);
-            while (from >= at + b.cost) {
-                at += b.cost;
-                b = blocks_of(p, ++s);
-            }
-            const int k = block_at(p, b, from - at, &t);
-            place = Place{h, s, k, t, (int)(part_begin(p, plan, wg + 1) - begin), 0};
+        if (tid == 0) worst = 0;
+        const Sums sum = sums_over_threads<NW>(mine, used, tot);
+        const int total = sum.cost, segments = sum.entries, before = sum.cost_before;
+        if (total == 0) {   // uniform
+            if (blockIdx.x == 0 && tid == 0) p.plan[1] = 0;
+            return;
         }
+        Cut plan{total, parts_of(segments * p.hkv, total * p.hkv, wgs, LEAST), 0, 0};
+        plan.set(total * p.hkv);
+        // whole blocks: heads side by side, `groups` workgroups each, so that an XCD's L2 serves few of them
+        const int groups = wgs / p.hkv;
+        bool whole = false;
+        if (each == 1 && segments <= NT && groups > 0) {
+            // the sequences' first blocks, then every thread a block
+            Seq *seq_s = reinterpret_cast<Seq *>(smem);
+            int *first_s = reinterpret_cast<int *>(seq_s + NT), *cost_s = first_s + NT, *cost_r = cost_s + NT;
+            seq_s[tid] = own.q;
+            first_s[tid] = sum.entries_before;
+            cost_s[tid] = 0;
+            __syncthreads();
+            int s = 0, k = 0;
+            if (tid < segments) {
+                for (int step = NT / 2; step > 0; step /= 2)   // the last sequence that begins at or before block tid
+                    if (s + step < p.n_seqs && first_s[s + step] <= tid) s += step;
+                k = tid - first_s[s];
+                const Seq q = seq_s[s];
+                cost_s[tid] = START + ((q.rows + QT - 1) / QT - seen_from(p, q, k)) * TILE;
+            }
+            __syncthreads();
+            if (tid < segments) {
+                const int rank = segments <= groups ? tid : rank_by_cost(cost_s, segments, tid);   // (one each: the order is of no consequence)
+                seq_r[rank] = s;
+                block_r[rank] = (int16_t)k;
+                cost_r[rank] = cost_s[tid];
+            }
+            __syncthreads();
+            whole = dealt_worst(cost_r, segments, groups, &worst) <= plan.wide + JOIN;
+        }
+        if (blockIdx.x == 0) {   // for the join
+            if (tid == 0) {
+                p.plan[0] = plan.per_head;
+                p.plan[1] = whole ? 0 : plan.parts;
+            }
+            for (int i = 0, at = before; i < each && !whole; ++i)
+                if (first + i < p.n_seqs) {
+                    p.plan[WEIGHTS_PLAN_WORDS + first + i] = at;
+                    at += blocks_of(p, first + i).cost;
+                }
+        }
+        if (whole) {
+            const int g = (int)blockIdx.x / p.hkv;
+            if (g >= groups || g >= segments) return;
+            if (tid == 0) {
+                blocks_s = segments;
+                place = Place{(int)blockIdx.x % p.hkv, seq_r[g], block_r[g], 0, INT32_MAX, 0};
+            }
+        } else {
+            if (wg >= plan.parts) return;
+            const int begin = plan.begin(wg), h = begin / plan.per_head, from = begin - h * plan.per_head;
+            if (tid == 0) blocks_s = 0;
+            if (from >= before && from < before + mine) {   // one thread's
+                int at = before, s = first, off;
+                Blocks b = blocks_of(p, s);
+                while (from >= at + b.cost) {
+                    at += b.cost;
+                    b = blocks_of(p, ++s);
+                }
+                const int k = block_at(p, b, from - at, &off);
+                place = Place{h, s, k, off, plan.begin(wg + 1) - begin, 0};
+            }
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    for (;;) {   // (where the part goes on is kept in LDS, not in scalar registers)
+    for (;;) {   // (where the workgroup goes on is kept in LDS, not in scalar registers)
         const int h = __builtin_amdgcn_readfirstlane(place.h), s = __builtin_amdgcn_readfirstlane(place.s), k = __builtin_amdgcn_readfirstlane(place.k);
-        const int t = __builtin_amdgcn_readfirstlane(place.t), left = __builtin_amdgcn_readfirstlane(place.left), second = __builtin_amdgcn_readfirstlane(place.second);
+        const int at = __builtin_amdgcn_readfirstlane(place.at), left = __builtin_amdgcn_readfirstlane(place.left), turn = __builtin_amdgcn_readfirstlane(place.turn);
         if (left == 0) return;   // uniform
         const Seq sq = sequence(p, s);
-        const int from = sq.n ? seen_from(p, sq, k) : 0, cost = sq.n ? (sq.rows + QT - 1) / QT - from : 0, take = min(cost - t, left);
+        const int from = sq.n ? seen_from(p, sq, k) : 0, tiles = sq.n ? (sq.rows + QT - 1) / QT - from : 0, cost = sq.n ? START + tiles * TILE : 0;
+        const int take = min(cost - at, left);
         __syncthreads();
-        if (tid == 0) {
-            Place next{h, s, k + 1, 0, left - take, second | (take > 0)};
-            if ((int64_t)(k + 1) * KB >= sq.n) next = s + 1 == p.n_seqs ? Place{h + 1, 0, 0, 0, next.left, next.second} : Place{h, s + 1, 0, 0, next.left, next.second};
-            place = next;
+        if (threadIdx.x == 0) {
+            const int blocks = blocks_s;
+            if (blocks > 0) {
+                const int groups = (int)gridDim.x / p.hkv, g = (int)blockIdx.x / p.hkv, n = turn + 1, r = dealt_rank(n, g, groups);
+                place = r < blocks ? Place{h, seq_r[r], block_r[r], 0, INT32_MAX, n} : Place{0, 0, 0, 0, 0, 0};
+            } else {
+                Place next{h, s, k + 1, 0, left - take, turn | (cost > 0)};
+                if ((int64_t)(k + 1) * KB >= sq.n) next = s + 1 == p.n_seqs ? Place{h + 1, 0, 0, 0, next.left, next.turn} : Place{h, s + 1, 0, 0, next.left, next.turn};
+                place = next;
+            }
         }
-        if (take > 0) weigh<D>(p, smem, sq, s, h, k, from + t, from + t + take, take == cost ? nullptr : p.part + (int64_t)(2 * wg + second) * KB);
+        if (take > 0) {
+            const int t0 = at == 0 ? 0 : cut_at(tiles, at), t1 = at + take == cost ? tiles : cut_at(tiles, at + take);
+            if (t0 < t1) weigh<D>(p, smem, sq, s, h, k, from + t0, from + t1, t1 - t0 == tiles ? nullptr : p.part + (int64_t)(2 * wg + turn) * KB);
+        }
         __syncthreads();
     }
 }
@@ -458,11 +632,11 @@ __global__ __launch_bounds__(64 * NW) void weights_many_kernel(WeightsParams)
 __global__ __launch_bounds__(KB) void weights_join_kernel(WeightsParams p)
 {
     __shared__ int where[3];
-    const Plan plan{p.plan[0], p.plan[1]};
+    Cut plan{p.plan[0], p.plan[1], 0, 0};
     const int w = (int)blockIdx.x + 1;
     if (w >= plan.parts) return;
-    const int64_t x = part_begin(p, plan, w);
-    const int h = (int)(x / plan.per_head), from = (int)(x - (int64_t)h * plan.per_head);
+    plan.set(plan.per_head * p.hkv);
+    const int x = plan.begin(w), h = x / plan.per_head, from = x - h * plan.per_head;
     for (int s = threadIdx.x; s < p.n_seqs; s += KB) {
         const int at = p.plan[WEIGHTS_PLAN_WORDS + s];
         if (from < at) continue;
@@ -474,13 +648,17 @@ __global__ __launch_bounds__(KB) void weights_join_kernel(WeightsParams p)
     }
     __syncthreads();
     const int s = __builtin_amdgcn_readfirstlane(where[0]), k = __builtin_amdgcn_readfirstlane(where[1]), off = __builtin_amdgcn_readfirstlane(where[2]);
-    const int64_t x0 = x - off, before = part_begin(p, plan, w - 1);
-    if (off == 0 || before > x0) return;   // no block is cut here, or an earlier border inside it is the first
+    const int x0 = x - off;
+    if (off == 0 || plan.begin(w - 1) > x0) return;   // no block is cut here, or an earlier border inside it is the first
     const Seq sq = sequence(p, s);
-    const int cost = (sq.rows + QT - 1) / QT - seen_from(p, sq, k), end = part_of(p, plan, x0 + cost - 1), r = k * KB + (int)threadIdx.x;
+    const int tiles = (sq.rows + QT - 1) / QT - seen_from(p, sq, k), r = k * KB + (int)threadIdx.x;
+    int first = w - 1, end = plan.part_of(x0 + START + tiles * TILE - 1);
+    while (first < end && cut_at(tiles, plan.begin(first + 1) - x0) == 0) ++first;    // (of the first and the last part perhaps no tile)
+    while (first < end && cut_at(tiles, plan.begin(end) - x0) == tiles) --end;
+    if (first == end) return;   // it was not cut
     if (r >= sq.n) return;
-    float sum = p.part[(int64_t)(2 * (w - 1) + (before != x0)) * KB + threadIdx.x];
-    for (int i = w; i <= end; ++i) sum += p.part[(int64_t)2 * i * KB + threadIdx.x];
+    float sum = p.part[(int64_t)(2 * first + (plan.begin(first) < x0)) * KB + threadIdx.x];
+    for (int i = first + 1; i <= end; ++i) sum += p.part[(int64_t)2 * i * KB + threadIdx.x];
     const int page = table_entry(p.pages.table + (int64_t)s * p.pages.width, r >> p.pages.page_shift);
     if ((uint32_t)page >= (uint32_t)p.pages.n_pages) return;
     float *wp = p.w + (((int64_t)page * p.hkv + h) << p.pages.page_shift) + (r & ((1 << p.pages.page_shift) - 1));
@@ -500,7 +678,7 @@ hipError_t launch(const WeightsParams &p, hipStream_t s)
     }
     hipLaunchKernelGGL((weights_many_kernel<D>), dim3(p.cus), dim3(64 * NW), 0, s, p);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || (int64_t)p.G * p.observe <= FEW_TILES * QT) return e;   // (no block is cut)
     hipLaunchKernelGGL(weights_join_kernel, dim3(p.cus - 1), dim3(KB), 0, s, p);
     return hipGetLastError();
 }

@@ -95,15 +95,18 @@ size_t branch_workspace(int n_seqs, int n_prefixes, int hkv, int G, int Bt, int 
 hipError_t launch_branch_attention(const BranchParams &p, hipStream_t s);   // (it fills in segments and divisors)
 
 // ------------------------------------------------------------------ pieces of many new tokens over the same rows
+struct ChunkCut {   // a block of query rows whose keys were cut: sequence, KV head, first row, rows of the sequence; its first partial, and how many
+    int32_t s, h, m0, M, first, pieces;
+};
 struct ChunkParams {
     Rows q;
     uint16_t *out;                        // [n_seqs][hq][Bt][D]
     float *lse;                           // [n_seqs][hq][Bt]
     const uint16_t *k_prefix, *v_prefix;  // [n_prefixes][hkv][prefix_cap][D]
     Pages pages;
-    float *part_o;                        // partial outputs, each normalised by its weight sum: two slots a workgroup
-    float2 *part_ml;                      // (reference in log2 units, weight sum) of every row of a slot
-    int32_t *plan;                        // [CHUNK_PLAN_WORDS + slots]: how the launch cut the work, for the join
+    _Float16 *part_o;                     // partial outputs, each normalised by its weight sum and scaled row by row: two slots a workgroup
+    float __attribute__((ext_vector_type(4))) *part_ml;   // (reference in log2 units, weight sum, power of two) of every row of a slot
+    ChunkCut *cuts;                       // one a workgroup: the segment that the end of its part cuts first
     int32_t n_seqs, fan, hkv, G, Bt, D;
     int32_t prefix_len;
     int64_t prefix_cap;
@@ -112,8 +115,8 @@ struct ChunkParams {
     int32_t blocks, slots, part_rows;     // blocks of query rows of a sequence and head; n_seqs times that; rows of a partial
     Divisor by_blocks, by_slots, by_G, by_fan;
 };
-constexpr int CHUNK_PLAN_WORDS = 8;
-size_t chunk_workspace(int n_seqs, int hkv, int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_plan);
+size_t chunk_workspace(int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_cuts);
+bool chunk_fits(int n_seqs, int hkv, int G, int Bt, int prefix_len, int64_t table_rows);   // what a launch counts fits in int32
 hipError_t launch_branch_chunk(ChunkParams p, hipStream_t s);   // (it fills in the last two lines)
 
 // ------------------------------------------------------------------ the attention weight that own rows gather
@@ -133,17 +136,21 @@ size_t weights_workspace(int n_seqs, int G, int Bt, int observe, int cus, size_t
 hipError_t launch_branch_weights(WeightsParams p, hipStream_t s);   // (it fills in the divisors)
 
 // ------------------------------------------------------------------ eviction of own rows
+struct BranchMove {
+    int64_t from, to;                     // rows of the pools, heads among them
+};
 struct BranchEvictParams {
     Pages pages;
     float *w;                             // [n_pages][hkv][page_rows]
     int32_t *positions;                   // [n_pages][hkv][page_rows]
     const int32_t *pos0;                  // nullable [n_seqs]
     int32_t *status;                      // nullable
-    int32_t *moves;                       // per (sequence, head): the number of moves, then from and to of each
+    int32_t *counts;                      // [n_seqs][hkv]: moves that are left to the second launch
+    BranchMove *moves;                    // [n_seqs][hkv][most_moves]
     int32_t n_seqs, hkv, Bt, D, budget, window, most_moves;
     Divisor by_hkv;
 };
-size_t branch_evict_workspace(int n_seqs, int hkv, int64_t table_rows, int budget, int *most_moves);
+size_t branch_evict_workspace(int n_seqs, int hkv, int64_t table_rows, int budget, int *most_moves, size_t *off_moves);
 hipError_t launch_branch_evict(BranchEvictParams p, hipStream_t s);   // (it fills in the divisor)
 
 }  // namespace kd

@@ -1,6 +1,7 @@
 // Device helpers of the kernels that read the own rows of sequences in pages: how many rows there are, and where they lie.
 #pragma once
 #include "kd_branch.h"
+#include "kd_select.h"
 
 namespace kd {
 
@@ -19,4 +20,85 @@ __device__ __forceinline__ int rows_with(const Pages &pages, int len, int fresh)
     const int64_t n = (int64_t)len + fresh, most = (int64_t)pages.width << pages.page_shift;
     return (int)(n < most ? n : most);
 }
+
+// What each thread's share of a list costs and how many entries it has, summed over the workgroup: in all, and over the threads before this one
+struct Sums {
+    int cost, entries, cost_before, entries_before;
+};
+template <int WAVES>
+__device__ __forceinline__ Sums sums_over_threads(int cost, int entries, int (&tot)[2][WAVES])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c = (int)wave_inclusive_scan((uint32_t)cost), e = (int)wave_inclusive_scan((uint32_t)entries);
+    if (lane == 63) {
+        tot[0][wave] = c;
+        tot[1][wave] = e;
+    }
+    __syncthreads();
+    Sums s{0, 0, c - cost, e - entries};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        const int x = tot[0][w], y = tot[1][w];
+        s.cost += x;
+        s.entries += y;
+        s.cost_before += w < wave ? x : 0;
+        s.entries_before += w < wave ? y : 0;
+    }
+    return s;
+}
+
+// Entries of a list sorted by what they cost, dealt to `groups` workgroups out and back again in turn: the rank of the entry that workgroup g takes in
+// round k, and the most that one of them gets (cost_r: what they cost by rank; worst: a word in LDS that is zero)
+__device__ __forceinline__ int dealt_rank(int k, int g, int groups) { return k * groups + (k & 1 ? groups - 1 - g : g); }
+__device__ __forceinline__ int dealt_worst(const int *cost_r, int entries, int groups, int *worst)
+{
+    if ((int)threadIdx.x < groups) {
+        int load = 0;
+        for (int k = 0; k * groups < entries; ++k) {
+            const int r = dealt_rank(k, threadIdx.x, groups);
+            if (r < entries) load += cost_r[r];
+        }
+        atomicMax(worst, load);   // (of integers: the order is of no consequence)
+    }
+    __syncthreads();
+    return *worst;
+}
+// The rank of entry `mine`, the most expensive first, of equal ones the first (cost_s: 16-byte aligned, entries behind the last cost nothing)
+__device__ __forceinline__ int rank_by_cost(const int *cost_s, int entries, int mine)
+{
+    typedef int int4_ __attribute__((ext_vector_type(4)));
+    const int own = cost_s[mine];
+    int rank = 0;
+    for (int i = 0; i < entries; i += 4) {
+        const int4_ c = *reinterpret_cast<const int4_ *>(cost_s + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) rank += c[k] > own || (c[k] == own && i + k < mine);
+    }
+    return rank;
+}
+
+// A list of what entries cost, cut into parts: part w begins at w * wide + min(w, longer), the first `longer` parts are a unit longer
+struct Cut {
+    int per_head, parts, wide, longer;   // per_head: units of one head's entries; heads are the outermost in the list
+    __device__ __forceinline__ void set(int total)
+    {
+        wide = total / parts;
+        longer = total - wide * parts;
+    }
+    __device__ __forceinline__ int begin(int w) const { return w * wide + min(w, longer); }
+    __device__ __forceinline__ int part_of(int x) const { return x < longer * (wide + 1) ? x / (wide + 1) : longer + (x - longer * (wide + 1)) / wide; }
+};
+// As many parts as there are workgroups, but whole entries a part where there are fewer of them, and `least` units a part
+__device__ __forceinline__ int parts_of(int entries, int total, int wgs, int least)
+{
+    const int parts = entries <= wgs ? entries * (wgs / entries) : wgs;
+    return parts > entries ? max(min(parts, total / least), entries) : parts;
+}
+// Workgroups go round the XCDs: those of one XCD take neighbouring parts
+__device__ __forceinline__ int part_number()
+{
+    const int wgs = (int)gridDim.x, id = (int)blockIdx.x;
+    return wgs % 8 == 0 ? id % 8 * (wgs / 8) + id / 8 : id;
+}
+
 }  // namespace kd

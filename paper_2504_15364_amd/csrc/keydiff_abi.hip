@@ -1428,7 +1428,7 @@ BranchWork chunk_work(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixe
     if (few_rows(b, Bt)) return branch_work(b, Bt, n_prefixes);
     BranchWork w;
     w.cus = std::max(compute_units(), 2);
-    w.need = kd::chunk_workspace(b->n_seqs, b->n_kv_heads, b->n_q_heads / b->n_kv_heads, Bt, b->head_dim, w.cus, &w.off_ml, &w.off_plan);
+    w.need = kd::chunk_workspace(b->n_q_heads / b->n_kv_heads, Bt, b->head_dim, w.cus, &w.off_ml, &w.off_plan);
     return w;
 }
 
@@ -1467,6 +1467,13 @@ int check_chunk(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt
     return check_chunk_rows(b, Bt);
 }
 
+int check_chunk_tiles(const keydiff_branches_t *b, int32_t Bt, int32_t prefix_len)
+{
+    if (!few_rows(b, Bt) && !kd::chunk_fits(b->n_seqs, b->n_kv_heads, b->n_q_heads / b->n_kv_heads, Bt, prefix_len, (int64_t)b->table_width * b->page_rows))
+        return fail(KEYDIFF_ESHAPE, "too many rows for one call: what the tiles of 64 keys and 256 query rows cost must fit in int32");
+    return KEYDIFF_OK;
+}
+
 int branch_chunk(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t Bt, const void *k_prefix, const void *v_prefix, int32_t n_prefixes,
                  int32_t prefix_len, int64_t prefix_cap, float scale, void *out, float *lse, void *workspace, const BranchWork &work, hipStream_t s)
 {
@@ -1490,9 +1497,9 @@ int branch_chunk(const keydiff_branches_t *b, const keydiff_rows_t *q, int32_t B
     p.cus = work.cus;
     p.scale_log2e = scale;
     unsigned char *w = static_cast<unsigned char *>(workspace);
-    p.part_o = reinterpret_cast<float *>(w);
-    p.part_ml = reinterpret_cast<float2 *>(w + work.off_ml);
-    p.plan = reinterpret_cast<int32_t *>(w + work.off_plan);
+    p.part_o = reinterpret_cast<_Float16 *>(w);
+    p.part_ml = reinterpret_cast<decltype(p.part_ml)>(w + work.off_ml);
+    p.cuts = reinterpret_cast<kd::ChunkCut *>(w + work.off_plan);
     KD_LAUNCH(kd::launch_branch_chunk(p, s), "chunk attention kernels");
     return KEYDIFF_OK;
 }
@@ -1640,6 +1647,7 @@ int keydiff_branch_chunk_attention(const keydiff_branches_t *b, const keydiff_ro
 {
     if (int rc = check_chunk(b, q, Bt, out, lse, workspace)) return rc;
     if (int rc = check_prefix_rows(b, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, softmax_scale)) return rc;
+    if (int rc = check_chunk_tiles(b, Bt, prefix_len)) return rc;
     const BranchWork work = chunk_work(b, Bt, n_prefixes);
     if (int rc = check_buffers(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, out, workspace, workspace_bytes, &work)) return rc;
     if (int rc = check_lse(b, q, Bt, k_prefix, v_prefix, n_prefixes, prefix_len, prefix_cap, out, lse, workspace, work)) return rc;
@@ -1653,6 +1661,7 @@ int keydiff_cache_branch_chunk_attention(keydiff_cache_t *c, const keydiff_branc
     if (!c) return fail(KEYDIFF_EINVAL, "null pointer");
     if (int rc = check_chunk(b, q, Bt, out, lse, workspace)) return rc;
     if (int rc = check_prompt_cache(c, b, Bt)) return rc;
+    if (int rc = check_chunk_tiles(b, Bt, c->len)) return rc;
     const BranchWork work = chunk_work(b, Bt, c->cfg.batch);
     const int32_t cap = (int32_t)c->L.cap;
     if (int rc = check_buffers(b, q, Bt, c->k, c->v, c->cfg.batch, cap, cap, out, workspace, workspace_bytes, &work)) return rc;
@@ -1740,7 +1749,8 @@ int keydiff_branch_evict_workspace_bytes(const keydiff_branches_t *b, int32_t bu
     if (!b || !bytes) return fail(KEYDIFF_EINVAL, "null pointer");
     if (int rc = check_evict(b, budget)) return rc;
     int most = 0;
-    *bytes = kd::branch_evict_workspace(b->n_seqs, b->n_kv_heads, (int64_t)b->table_width * b->page_rows, budget, &most);
+    size_t off_moves = 0;
+    *bytes = kd::branch_evict_workspace(b->n_seqs, b->n_kv_heads, (int64_t)b->table_width * b->page_rows, budget, &most, &off_moves);
     return KEYDIFF_OK;
 }
 
@@ -1755,7 +1765,8 @@ int keydiff_branch_evict(const keydiff_branches_t *b, int32_t Bt, float *w_pages
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(KEYDIFF_EINVAL, "the workspace must be 256-byte aligned");
     if (window < 0 || window >= budget) return fail(KEYDIFF_ESHAPE, "window must lie in [0, budget), got %d of %d", window, budget);
     int most = 0;
-    const size_t need = kd::branch_evict_workspace(b->n_seqs, b->n_kv_heads, (int64_t)b->table_width * b->page_rows, budget, &most);
+    size_t off_moves = 0;
+    const size_t need = kd::branch_evict_workspace(b->n_seqs, b->n_kv_heads, (int64_t)b->table_width * b->page_rows, budget, &most, &off_moves);
     if (workspace_bytes < need) return fail(KEYDIFF_ESHAPE, "the workspace holds %zu bytes, this call needs %zu", workspace_bytes, need);
     const size_t words = words_of_pages(b), pool = words / 2 * b->head_dim, per_seq = (size_t)b->n_seqs * 4;
     const struct {
@@ -1773,7 +1784,8 @@ int keydiff_branch_evict(const keydiff_branches_t *b, int32_t Bt, float *w_pages
     p.positions = p_pages;
     p.pos0 = pos0;
     p.status = status;
-    p.moves = static_cast<int32_t *>(workspace);
+    p.counts = static_cast<int32_t *>(workspace);
+    p.moves = reinterpret_cast<kd::BranchMove *>(static_cast<unsigned char *>(workspace) + off_moves);
     p.n_seqs = b->n_seqs;
     p.hkv = b->n_kv_heads;
     p.Bt = Bt;

@@ -181,6 +181,7 @@ WEIGHT_KINDS = {
     "zero": lambda shape, g: torch.where(torch.rand(shape, **g) < 0.5, -0.0, 0.0),                # both zeros are one weight
     "odd": lambda shape, g: torch.where(torch.rand(shape, **g) < 0.1, float("nan"), torch.where(torch.rand(shape, **g) < 0.1, float("inf"), torch.where(
         torch.rand(shape, **g) < 0.1, float("-inf"), torch.randn(shape, **g)))),
+    "alike": lambda shape, g: torch.full(shape, 0.5, device="cuda"),                               # positions decide
     "close": lambda shape, g: 1.0 + 2.0 ** -23 * torch.randint(0, 40, shape, **g).float(),        # borders in the last bits
 }
 EVICT = [
@@ -194,6 +195,10 @@ EVICT = [
     (1, 128, 1024, 9, [20000], [9], 9000, 100),                                 # more rows than are kept in LDS
     (2, 64, 64, 1, [40000], [1], 39999, 0),
     (3, 64, 16, 2, [33] * 100, [2, 1] * 50, 33, 4),
+    (2, 128, 64, 1, [4000, 3999, 1], [1, 1, 1], 4000, 0),                       # up to 4096 rows in registers; one too many, none, none
+    (2, 64, 32, 700, [3000, 2500], [700, 64], 1100, 100),                       # more moves than the workgroup makes itself
+    (1, 128, 64, 30, [16000], [30], 15999, 500),                                # up to 16384 rows
+    (2, 64, 64, 1, [12000, 5000], [1, 0], 6000, 0),                             # half of the rows at once
 ]
 
 
@@ -220,6 +225,34 @@ def test_eviction_without_new_counts_and_positions():
     want = after_eviction((k, v, w, p), table, lens, [20] * 3, [0] * 3, budget, 0)
     kd.branch_evict(k, v, w, p, table, ints(lens), budget, Bt=20)
     same((k, v, w, p), want)
+
+
+@pytest.mark.parametrize("L", [300, 3000, 9000, 20000])
+def test_rows_that_are_alike_go_from_the_last_one(L):
+    # weights and positions of a few kinds each: whole classes of rows of one rank, cut by the budget
+    hkv, d, page = 2, 64, 8
+    g = gen(75)
+    k, v, w, p, table = evict_case(hkv, d, page, [L], [1], 0, g, WEIGHT_KINDS["ties"], [0])
+    for budget in (L, L - 40, L // 3, 1):
+        put_rows(p, table, 0, torch.randint(0, 2, (hkv, L), **g).to(torch.int32))
+        if budget == 1:
+            put_rows(w, table, 0, torch.zeros((hkv, L + 1), device="cuda"))
+            put_rows(p, table, 0, torch.full((hkv, L), L, dtype=torch.int32, device="cuda"))
+        want = after_eviction((k, v, w, p), table, [L], [1], [0], budget, 0)
+        kd.branch_evict(k, v, w, p, table, ints([L]), budget)
+        same((k, v, w, p), want)
+
+
+def test_evicting_again_from_what_is_there_already():
+    # rows behind the budget are still there: the same call once more, many times, while copies of rows take over
+    hkv, d, page, L, Bt, budget = 2, 64, 16, 500, 200, 450
+    g = gen(76)
+    pools = evict_case(hkv, d, page, [L], [Bt], budget, g, spread, [0])
+    k, v, w, p, table = pools
+    for _ in range(12):
+        want = after_eviction((k, v, w, p), table, [L], [Bt], [0], budget, 30)
+        kd.branch_evict(k, v, w, p, table, ints([L]), budget, Bt=Bt, window=30)
+        same((k, v, w, p), want)
 
 
 def test_positions_that_make_no_sense_do_no_harm():

@@ -181,14 +181,14 @@ def test_chunk_attention_of_queries_in_a_projections_output_and_in_place(wide): 
     assert torch.equal(got, out)
 
 
-@pytest.mark.parametrize("power", [-90, 90])
+@pytest.mark.parametrize("power", [-115, -90, 90])
 @pytest.mark.parametrize("Bt", [6, 80])
 def test_chunk_attention_values_of_extreme_size(power, Bt, wide):  # noqa: F811
     hq, hkv, d, N = 8, 2, 128, 700
     g = gen(300 + power + Bt)
     lens = [0, 33, 500]
     k_pages, v_pages, table = paged(lens, Bt, 16, hkv, d, g, wide=wide)
-    size = 2.0 ** (power + torch.randint(-10, 11, (hkv, 1, 1), **g).float())
+    size = 2.0 ** (power + torch.randint(-10, 10, (hkv, 1, 1), **g).float())
     for s, L in enumerate(lens):
         put_rows(k_pages, table, s, torch.randn((hkv, L + Bt, d), **g).bfloat16())
         put_rows(v_pages, table, s, (torch.randn((hkv, L + Bt, d), **g) * size).bfloat16())
@@ -198,8 +198,12 @@ def test_chunk_attention_values_of_extreme_size(power, Bt, wide):  # noqa: F811
     for s, L in enumerate(lens):
         own = rows_of(k_pages, table, s, L + Bt), rows_of(v_pages, table, s, L + Bt)
         o, bound, log_sum, e_lse, _ = reference(q[s], (kp[0].double(), vp[0].double()), own, L, d ** -0.5)
-        close(out[s], o, bound, f"sequence {s}")
+        # (near the smallest normal number, 2^-126, sums of such values lose at most it for each key, and an output that lies below it)
+        close(out[s], o, bound + (2.0 ** -126 * (N + L + Bt) if power == -115 else 0.0), f"sequence {s}")
         close(lse[s], log_sum, e_lse, f"sequence {s}, log sums")
+    # no values at all
+    out, _ = kd.branch_chunk_attention(q, k_pages, torch.zeros_like(v_pages), table, ints(lens), prefix=(kp, torch.zeros_like(kp), N))
+    assert bool((out == 0).all())
 
 
 def test_chunk_attention_logits_that_rise_and_fall(wide):  # noqa: F811
