@@ -3,8 +3,10 @@
 // A row's rank is (latest positions first, weight, lower position, lower row); of n rows those of the n - budget lowest ranks are evicted.  One
 // workgroup a (sequence, KV head) finds them and pairs the evicted rows below the budget with the kept ones behind it, both in ascending order.
 // What bounds it: a chain of look-ups (length, page, weight) and barriers where few rows are evicted, the moves where many are.
-//   up to 16384 rows in the table   weights and positions in registers.  One row too many, a generated token's case: the lowest rank by one reduction.  Else
-//                          histograms of 2048 bins over the range of what is left narrow the border down to candidates that are ranked in pairs
+//   up to 16384 rows in the table   weights and positions in LDS.  One row too many, a generated token's case: the lowest rank by one reduction.  Else
+//                          histograms of 2048 bins over the range of what is left narrow the border down to candidates that are ranked in pairs.  Loops
+//                          over LDS and not rows in registers: with 16 of them a thread, every pass unrolled, the code of each was run once and
+//                          waited for from memory (16 heads of 16384 rows 51 us)
 //   more                   a radix select that reads weights and positions again in every pass
 // Few moves are made by the workgroup itself (a second launch took 4 us for one row of each of 512 heads), many by a second launch over the whole chip.
 #include <algorithm>
@@ -42,11 +44,12 @@ __device__ __forceinline__ uint32_t ordered(float x)
 }
 
 // Rows of one head from one place to another, 16 bytes a thread and turn: thread `tid` of `threads`
-__device__ __forceinline__ void move_rows(const BranchEvictParams &p, const Move *moves, int count, int64_t tid, int64_t threads)
+template <class Moves>
+__device__ __forceinline__ void move_rows(const BranchEvictParams &p, Moves move, int count, int64_t tid, int64_t threads)
 {
     const int units = p.D / 8, shift = units == 16 ? 5 : 4;   // of a row of K, then of V
     for (int64_t i = tid; i < (int64_t)count << shift; i += threads) {
-        const Move m = moves[i >> shift];
+        const Move m = move(i >> shift);
         const int u = (int)i & (2 * units - 1);
         u32x4 *rows = reinterpret_cast<u32x4 *>(u < units ? p.pages.k : p.pages.v);
         const int at = u & (units - 1);
@@ -60,142 +63,147 @@ __device__ __forceinline__ void move_rows(const BranchEvictParams &p, const Move
     }
 }
 
-constexpr int OWN_MOVES = 128;   // moves that the workgroup of a head makes itself
-constexpr int BINS = 2048, CANDIDATES = 512;
+// The largest of a wave's numbers, in every lane
+__device__ __forceinline__ uint32_t wave_max(uint32_t x)
+{
+    x = max(x, dpp_fetch<0x111, 0xF>(x));
+    x = max(x, dpp_fetch<0x112, 0xF>(x));
+    x = max(x, dpp_fetch<0x114, 0xF>(x));
+    x = max(x, dpp_fetch<0x118, 0xF>(x));
+    x = max(x, dpp_fetch<0x142, 0xA>(x));
+    x = max(x, dpp_fetch<0x143, 0xC>(x));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
 
-template <int NT, int RPT>
+constexpr int OWN_MOVES = 128;   // moves that the workgroup of a head makes itself
+constexpr int BINS = 2048, CANDIDATES = 128;
+
+template <int NT, int ROWS>
 __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
 {
-    constexpr int WAVES = NT / 64, WORDS = WAVES * RPT;   // words of 64 rows
-    __shared__ uint32_t hist[BINS], wave_tot[WAVES], bits[WORDS * 2], words[WORDS + 1], cand_key[CANDIDATES], cand_low[CANDIDATES], found[4], counted;
+    constexpr int WAVES = NT / 64, WORDS = ROWS / 64;   // words of 64 rows
+    // of every row: it goes ahead of another if its key is lower, or its `low` at equal keys, or its row higher at equal both
+    __shared__ uint32_t key_s[ROWS], low_s[ROWS];
+    __shared__ uint32_t hist[BINS], wave_tot[WAVES], words[WORDS + 1], cand_key[CANDIDATES], cand_low[CANDIDATES], found[4], counted, best[3][WAVES];
+    __shared__ uint64_t out_s[WORDS];   // a bit for every row that goes
     __shared__ int cand_row[CANDIDATES];
-    __shared__ uint32_t low_s[3][WAVES];
     __shared__ Move list[OWN_MOVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int s = p.by_hkv.divide(blockIdx.x), h = (int)blockIdx.x - s * p.hkv;
     const int len = table_entry(p.pages.lens, s), fresh = new_rows(len, asked_rows(p.pages, p.Bt, s), p.Bt), pos0 = p.pos0 ? table_entry(p.pos0, s) : 0;
     const int n = len < 0 ? 0 : rows_with(p.pages, len, fresh);
     const int64_t all = (int64_t)len + fresh;
-    const bool evicts = len >= 0 && all > p.budget;   // uniform
-    if (tid == 0) p.counts[blockIdx.x] = 0;
-    // what the thread's rows tid + NT i hold.  (A sequence that does not evict: the new rows' positions alone.)
     const Head head{p.pages.table + (int64_t)s * p.pages.width, p.pages.page_shift, p.hkv, h};
-    int page[RPT];
-    bool absent = all > n;
-#pragma unroll
-    for (int i = 0; i < RPT; ++i) {
-        page[i] = -1;
-        if (NT * i < n && (evicts || NT * (i + 1) > len)) {   // uniform
-            const int e = table_entry(head.table, min(tid + NT * i, n - 1) >> head.shift);
-            page[i] = (uint32_t)e < (uint32_t)p.pages.n_pages ? e : -1;
-            absent = absent || page[i] < 0;
-        }
+    if (tid == 0) p.counts[blockIdx.x] = 0;
+    if (len < 0 || all <= p.budget) {   // uniform: nothing to evict, the new rows' positions alone
+        for (int r = len + tid; len >= 0 && r < n; r += NT)
+            if ((uint32_t)table_entry(head.table, r >> head.shift) < (uint32_t)p.pages.n_pages) p.positions[head.at(r)] = (int32_t)((uint32_t)pos0 + (uint32_t)r);
+        return;
     }
-    auto place = [&](int i) { return (((int64_t)max(page[i], 0) * head.hkv + h) << head.shift) + ((tid + NT * i) & ((1 << head.shift) - 1)); };
-    uint32_t key[RPT], low[RPT];   // a row goes ahead of another if its key is lower, or its `low` at equal keys, or its row higher at equal both
+    int need = n - p.budget;
     const int64_t late = (int64_t)pos0 + n - p.window;   // positions from here on are kept ahead of all others
+    bool absent = all > n;
+    uint32_t lo = 0xFFFFFFFFu, hi = 0;   // the range of the keys
+    uint32_t k_first = 0xFFFFFFFFu, l_first = 0xFFFFFFFFu;   // the thread's row that goes ahead of its others
+    int r_first = -1;
+    constexpr int AT_ONCE = 4;           // rows of a thread that are asked for together
+    for (int base = 0; base < n; base += NT * AT_ONCE) {
+        int page[AT_ONCE];
+        int64_t at[AT_ONCE];
+        float w[AT_ONCE];
+        int32_t before[AT_ONCE];
 #pragma unroll
-    for (int i = 0; i < RPT; ++i) {
-        const int r = tid + NT * i;
-        key[i] = low[i] = 0xFFFFFFFFu;
-        if (NT * i < n && (evicts || NT * (i + 1) > len)) {   // uniform
-            int32_t position = (int32_t)((uint32_t)pos0 + (uint32_t)r);
-            if (evicts) {
-                const int32_t before = p.positions[place(i)];
-                const float w = p.w[place(i)];
-                position = r < len ? before : position;
-                if (r < n) {
-                    key[i] = p.window > 0 && position >= late ? 0xFFFFFFFFu : ordered(w);
-                    low[i] = ~((uint32_t)position ^ 0x80000000u);
-                }
+        for (int i = 0; i < AT_ONCE; ++i) page[i] = table_entry(head.table, min(base + NT * i + tid, n - 1) >> head.shift);
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int r = min(base + NT * i + tid, n - 1);
+            const bool there = (uint32_t)page[i] < (uint32_t)p.pages.n_pages;
+            absent = absent || !there;
+            at[i] = (((int64_t)(there ? page[i] : 0) * head.hkv + h) << head.shift) + (r & ((1 << head.shift) - 1));
+            w[i] = p.w[at[i]];
+            before[i] = p.positions[at[i]];
+            if (!there) at[i] = -1;
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int r = base + NT * i + tid;
+            if (r >= n) continue;
+            const int32_t position = r < len ? before[i] : (int32_t)((uint32_t)pos0 + (uint32_t)r);
+            if (r >= len && at[i] >= 0) p.positions[at[i]] = position;
+            const uint32_t key = p.window > 0 && position >= late ? 0xFFFFFFFFu : ordered(w[i]), low = ~((uint32_t)position ^ 0x80000000u);
+            key_s[r] = key;
+            low_s[r] = low;
+            lo = min(lo, key);
+            hi = max(hi, key);
+            if (r_first < 0 || key < k_first || (key == k_first && low <= l_first)) {   // (of equal ones the higher row, which comes later)
+                k_first = key;
+                l_first = low;
+                r_first = r;
             }
-            if (r >= len && r < n && page[i] >= 0) p.positions[place(i)] = position;
         }
     }
-    if (!evicts) return;
     if (__syncthreads_or(absent)) {
         if (tid == 0 && p.status) atomicOr(p.status, LEFT_OUT_ROW);
         return;
     }
-    int need = n - p.budget;
     if (need == 1) {
-        // the row that goes ahead of all others
-        uint32_t k = 0xFFFFFFFFu, l = 0xFFFFFFFFu;
-        int row = -1;
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-            const int r = tid + NT * i;
-            if (r < n && (row < 0 || key[i] < k || (key[i] == k && low[i] <= l))) {   // (of equal ones the higher row, which comes later)
-                k = key[i];
-                l = low[i];
-                row = r;
-            }
-        }
-        auto first = [&](uint32_t &k0, uint32_t &l0, int &r0, uint32_t k1, uint32_t l1, int r1) {
-            const bool take = r1 >= 0 && (r0 < 0 || k1 < k0 || (k1 == k0 && (l1 < l0 || (l1 == l0 && r1 > r0))));
-            k0 = take ? k1 : k0;
-            l0 = take ? l1 : l0;
-            r0 = take ? r1 : r0;
+        auto first = [&](uint32_t k1, uint32_t l1, int r1) {
+            const bool take = r1 >= 0 && (r_first < 0 || k1 < k_first || (k1 == k_first && (l1 < l_first || (l1 == l_first && r1 > r_first))));
+            k_first = take ? k1 : k_first;
+            l_first = take ? l1 : l_first;
+            r_first = take ? r1 : r_first;
         };
 #pragma unroll
-        for (int m = 1; m < 64; m *= 2) first(k, l, row, __shfl_xor(k, m), __shfl_xor(l, m), __shfl_xor(row, m));
+        for (int m = 1; m < 64; m *= 2) first(__shfl_xor(k_first, m), __shfl_xor(l_first, m), __shfl_xor(r_first, m));
         if (lane == 0) {
-            low_s[0][wave] = k;
-            low_s[1][wave] = l;
-            low_s[2][wave] = (uint32_t)row;
+            best[0][wave] = k_first;
+            best[1][wave] = l_first;
+            best[2][wave] = (uint32_t)r_first;
         }
         __syncthreads();
-        k = low_s[0][lane % WAVES];
-        l = low_s[1][lane % WAVES];
-        row = (int)low_s[2][lane % WAVES];
+        if (wave > 0) return;
+        k_first = best[0][lane % WAVES];
+        l_first = best[1][lane % WAVES];
+        r_first = (int)best[2][lane % WAVES];
 #pragma unroll
-        for (int m = 1; m < WAVES; m *= 2) first(k, l, row, __shfl_xor(k, m), __shfl_xor(l, m), __shfl_xor(row, m));
-        row = __builtin_amdgcn_readfirstlane(row);
+        for (int m = 1; m < WAVES; m *= 2) first(__shfl_xor(k_first, m), __shfl_xor(l_first, m), __shfl_xor(r_first, m));
+        const int row = __builtin_amdgcn_readfirstlane(r_first);
         if (row >= p.budget) return;   // the last row: it lies behind the budget
         if (tid < p.D / 4) {
-            list[0] = Move{head.at(p.budget), head.at(row)};   // (every thread its own copy of the same)
-            move_rows(p, list, 1, tid, p.D / 4);
+            const Move m{head.at(p.budget), head.at(row)};
+            move_rows(p, [&](int64_t) { return m; }, 1, tid, p.D / 4);
         }
         return;
     }
-    // the range of the keys
-    uint32_t lo = 0xFFFFFFFFu, hi = 0;
-#pragma unroll
-    for (int i = 0; i < RPT; ++i)
-        if (tid + NT * i < n) {
-            lo = min(lo, key[i]);
-            hi = max(hi, key[i]);
-        }
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        lo = min(lo, (uint32_t)__shfl_xor(lo, m));
-        hi = max(hi, (uint32_t)__shfl_xor(hi, m));
-    }
+    lo = ~wave_max(~lo);
+    hi = wave_max(hi);
     if (lane == 0) {
-        low_s[0][wave] = lo;
-        low_s[1][wave] = hi;
+        best[0][wave] = lo;
+        best[1][wave] = hi;
     }
     for (int i = tid; i < BINS; i += NT) hist[i] = 0;
-    for (int i = tid; i < WORDS * 2; i += NT) bits[i] = 0;
+    for (int i = tid; i < WORDS; i += NT) words[i] = 0;
     if (tid == 0) counted = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-        lo = min(lo, low_s[0][w]);
-        hi = max(hi, low_s[1][w]);
+        lo = min(lo, best[0][w]);
+        hi = max(hi, best[1][w]);
     }
     // Narrow down: of the rows whose value (the key; later, among those of key `equal`, low) lies in [lo, hi] the `need` first ones go; those below lo go, those
     // above hi stay
     bool by_low = false;
     uint32_t equal = 0, count = 0;
+    auto inside = [&](int r) {
+        const uint32_t v = by_low ? low_s[r] : key_s[r];
+        return v >= lo && v <= hi && (!by_low || key_s[r] == equal);
+    };
     for (;;) {
         const uint32_t span = hi - lo;
         const int down = span < BINS ? 0 : 32 - 11 - __builtin_clz(span);
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-            const uint32_t v = by_low ? low[i] : key[i];
-            if (tid + NT * i < n && v >= lo && v <= hi && (!by_low || key[i] == equal)) atomicAdd(&hist[(v - lo) >> down], 1u);
-        }
+#pragma unroll 4
+        for (int r = tid; r < n; r += NT)
+            if (inside(r)) atomicAdd(&hist[((by_low ? low_s[r] : key_s[r]) - lo) >> down], 1u);
         __syncthreads();
         constexpr int PER = BINS / NT;
         uint32_t mine[PER], sum = 0, total;
@@ -231,10 +239,7 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
         }
         __syncthreads();
     }
-    auto value = [&](int i) { return by_low ? low[i] : key[i]; };
-    auto below = [&](int i) { return by_low ? key[i] < equal || (key[i] == equal && low[i] < lo) : key[i] < lo; };
-    auto inside = [&](int i) { return value(i) >= lo && value(i) <= hi && (!by_low || key[i] == equal); };
-    const bool whole = count == (uint32_t)need, ranked = !whole && count <= CANDIDATES;   // uniform
+    const bool whole = count == (uint32_t)need;   // uniform
     // numbers in `words` become those of all words before, the last one their sum
     auto add_up = [&]() {
         __syncthreads();
@@ -256,71 +261,80 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
         }
         __syncthreads();
     };
+    const bool ranked = !whole && count <= CANDIDATES;
+    auto goes_first = [&](int r) { return by_low ? key_s[r] < equal || (key_s[r] == equal && low_s[r] < lo) : key_s[r] < lo; };
+    for (int base = 0; base < n; base += NT) {
+        const int r = base + tid;
+        const bool in = r < n && inside(r);
+        const uint64_t out = __builtin_amdgcn_ballot_w64(r < n && (goes_first(r) || (whole && in)));
+        if (lane == 0) out_s[(base >> 6) + wave] = out;
+        if (ranked && in) {   // a candidate (their order is of no consequence)
+            const uint32_t c = atomicAdd(&counted, 1u);
+            cand_key[c] = key_s[r];
+            cand_low[c] = low_s[r];
+            cand_row[c] = r;
+        }
+        if (!whole && !ranked) {
+            const uint64_t same = __builtin_amdgcn_ballot_w64(in);
+            if (lane == 0) words[(base >> 6) + wave] = (uint32_t)__popcll(same);
+        }
+    }
+    auto goes = [&](int r) { atomicOr(reinterpret_cast<uint32_t *>(out_s) + (r >> 5), 1u << (r & 31)); };
     if (ranked) {
-        // the candidates, and which of them go
-#pragma unroll
-        for (int i = 0; i < RPT; ++i)
-            if (tid + NT * i < n && inside(i)) {
-                const uint32_t c = atomicAdd(&counted, 1u);   // (their order is of no consequence)
-                cand_key[c] = key[i];
-                cand_low[c] = low[i];
-                cand_row[c] = tid + NT * i;
-            }
         __syncthreads();
-        for (int c = tid; c < (int)count; c += NT) {
+        for (int c = wave; c < (int)count; c += WAVES) {   // a wave a candidate, against 64 others at a time
             const uint32_t k = cand_key[c], l = cand_low[c];
             const int r = cand_row[c];
             int rank = 0;
-            for (int o = 0; o < (int)count; ++o) {
+            for (int o0 = 0; o0 < (int)count; o0 += 64) {
+                const int o = min(o0 + lane, CANDIDATES - 1);
                 const uint32_t ko = cand_key[o], lw = cand_low[o];
-                rank += ko < k || (ko == k && (lw < l || (lw == l && cand_row[o] > r)));
+                const int ro = cand_row[o];
+                rank += __popcll(__builtin_amdgcn_ballot_w64(o0 + lane < (int)count && (ko < k || (ko == k && (lw < l || (lw == l && ro > r))))));
             }
-            if (rank < need) atomicOr(&bits[r >> 5], 1u << (r & 31));
+            if (lane == 0 && rank < need) goes(r);
         }
-        __syncthreads();
     } else if (!whole) {
         // alike in all but their rows: the last `need` of them
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-            const uint64_t same = __builtin_amdgcn_ballot_w64(tid + NT * i < n && inside(i));
-            if (lane == 0) words[i * WAVES + wave] = (uint32_t)__popcll(same);
-        }
         add_up();
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-            const uint64_t same = __builtin_amdgcn_ballot_w64(tid + NT * i < n && inside(i));
-            const int ahead = (int)words[i * WAVES + wave] + __popcll(same & ((1ull << lane) - 1)), r = tid + NT * i;
-            if ((same >> lane & 1) && ahead >= (int)count - need) atomicOr(&bits[r >> 5], 1u << (r & 31));
+        for (int base = 0; base < n; base += NT) {
+            const int r = base + tid;
+            const uint64_t same = __builtin_amdgcn_ballot_w64(r < n && inside(r));
+            const int ahead = (int)words[(base >> 6) + wave] + __popcll(same & ((1ull << lane) - 1));
+            if ((same >> lane & 1) && ahead >= (int)count - need) goes(r);
         }
-        __syncthreads();
     }
-    // evicted rows below the budget and kept ones behind it: a word of 64 rows each wave and turn, their numbers added up in the order of the rows
-    uint64_t holes[RPT], movers[RPT];
-#pragma unroll
-    for (int i = 0; i < RPT; ++i) {
-        const int r = tid + NT * i;
-        const bool out = r < n && (below(i) || (inside(i) && (whole || (bits[r >> 5] >> (r & 31) & 1))));
-        holes[i] = __builtin_amdgcn_ballot_w64(out && r < p.budget);
-        movers[i] = __builtin_amdgcn_ballot_w64(r < n && !out && r >= p.budget);
-        if (lane == 0) words[i * WAVES + wave] = (uint32_t)__popcll(holes[i]) << 16 | (uint32_t)__popcll(movers[i]);
-    }
+    __syncthreads();
+    // evicted rows below the budget and kept ones behind it, counted in the order of the rows, a word of 64 a thread
+    auto first_bits = [](int bits) { return bits <= 0 ? 0ull : bits >= 64 ? ~0ull : (1ull << bits) - 1; };
+    auto holes_of = [&](int word) { return out_s[word] & first_bits(p.budget - 64 * word); };
+    auto movers_of = [&](int word) { return ~out_s[word] & first_bits(n - 64 * word) & ~first_bits(p.budget - 64 * word); };
+    for (int i = tid; i < WORDS; i += NT) words[i] = 64 * i < n ? (uint32_t)__popcll(holes_of(i)) << 16 | (uint32_t)__popcll(movers_of(i)) : 0u;
     add_up();
     const int count_moves = (int)(words[WORDS] & 0xFFFFu);
     const bool own = count_moves <= OWN_MOVES;   // uniform
     Move *to = own ? list : p.moves + (int64_t)blockIdx.x * p.most_moves;
+    for (int base = 0; base < n; base += NT * AT_ONCE) {
+        int page[AT_ONCE];
 #pragma unroll
-    for (int i = 0; i < RPT; ++i) {
-        const uint32_t before = words[i * WAVES + wave];
-        const uint64_t ahead = (1ull << lane) - 1;
-        if (holes[i] >> lane & 1) to[(before >> 16) + __popcll(holes[i] & ahead)].to = place(i);
-        if (movers[i] >> lane & 1) to[(before & 0xFFFFu) + __popcll(movers[i] & ahead)].from = place(i);
+        for (int i = 0; i < AT_ONCE; ++i) page[i] = table_entry(head.table, min(base + NT * i + tid, n - 1) >> head.shift);
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int r = base + NT * i + tid, word = ((base + NT * i) >> 6) + wave;
+            if (64 * word >= n) break;   // uniform in the wave
+            const uint64_t holes = holes_of(word), movers = movers_of(word), ahead = (1ull << lane) - 1;
+            const uint32_t before = words[word];
+            const int64_t at = (((int64_t)page[i] * head.hkv + h) << head.shift) + (r & ((1 << head.shift) - 1));
+            if (holes >> lane & 1) to[(before >> 16) + __popcll(holes & ahead)].to = at;
+            if (movers >> lane & 1) to[(before & 0xFFFFu) + __popcll(movers & ahead)].from = at;
+        }
     }
     if (!own) {
         if (tid == 0) p.counts[blockIdx.x] = count_moves;
         return;
     }
     __syncthreads();
-    move_rows(p, list, count_moves, tid, NT);
+    move_rows(p, [&](int64_t i) { return list[i]; }, count_moves, tid, NT);
 }
 
 __global__ __launch_bounds__(LNT) void evict_select_long_kernel(BranchEvictParams p)
@@ -425,7 +439,8 @@ __global__ __launch_bounds__(LNT) void evict_select_long_kernel(BranchEvictParam
 __global__ __launch_bounds__(256) void evict_move_kernel(BranchEvictParams p)
 {
     const int count = p.counts[blockIdx.x];
-    move_rows(p, p.moves + (int64_t)blockIdx.x * p.most_moves, count, (int64_t)blockIdx.y * 256 + threadIdx.x, (int64_t)gridDim.y * 256);
+    const Move *moves = p.moves + (int64_t)blockIdx.x * p.most_moves;
+    move_rows(p, [&](int64_t i) { return moves[i]; }, count, (int64_t)blockIdx.y * 256 + threadIdx.x, (int64_t)gridDim.y * 256);
 }
 
 }  // namespace
@@ -443,13 +458,13 @@ hipError_t launch_branch_evict(BranchEvictParams p, hipStream_t s)
     p.by_hkv.set((uint32_t)p.hkv);
     const unsigned heads = (unsigned)(p.n_seqs * p.hkv);
     const int64_t rows = (int64_t)p.pages.width << p.pages.page_shift;
-    const bool registers = rows <= 16384;
-    if (rows <= 1024) hipLaunchKernelGGL((evict_select_kernel<256, 4>), dim3(heads), dim3(256), 0, s, p);
-    else if (rows <= 4096) hipLaunchKernelGGL((evict_select_kernel<512, 8>), dim3(heads), dim3(512), 0, s, p);
-    else if (registers) hipLaunchKernelGGL((evict_select_kernel<1024, 16>), dim3(heads), dim3(1024), 0, s, p);
+    const bool in_lds = rows <= 16384;
+    if (rows <= 1024) hipLaunchKernelGGL((evict_select_kernel<256, 1024>), dim3(heads), dim3(256), 0, s, p);
+    else if (rows <= 4096) hipLaunchKernelGGL((evict_select_kernel<512, 4096>), dim3(heads), dim3(512), 0, s, p);
+    else if (in_lds) hipLaunchKernelGGL((evict_select_kernel<1024, 16384>), dim3(heads), dim3(1024), 0, s, p);
     else hipLaunchKernelGGL(evict_select_long_kernel, dim3(heads), dim3(LNT), 0, s, p);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.most_moves == 0 || (registers && p.most_moves <= OWN_MOVES)) return e;
+    if (e != hipSuccess || p.most_moves == 0 || (in_lds && p.most_moves <= OWN_MOVES)) return e;
     const unsigned parts = (unsigned)std::max<int64_t>(1, std::min<int64_t>(2048 / heads, ((int64_t)p.most_moves * (p.D / 4) + 255) / 256));
     hipLaunchKernelGGL(evict_move_kernel, dim3(heads, parts), dim3(256), 0, s, p);
     return hipGetLastError();
