@@ -538,7 +538,7 @@ __global__ __launch_bounds__(64 * NW) void chunk_parts_kernel(ChunkParams)
     const ChunkParams &p = argument_at<ChunkParams>(0);   // (read where it is needed)
     constexpr int NT = 64 * NW;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[lds_bytes<D>()];
-    __shared__ int tot[2][NW];
+    __shared__ int tot[3][NW];
     __shared__ int16_t slot_r[NT];   // the slots by rank, where segments stay whole
     __shared__ int worst, segments_s;
     __shared__ Place place;
@@ -548,24 +548,29 @@ __global__ __launch_bounds__(64 * NW) void chunk_parts_kernel(ChunkParams)
         const int tid = threadIdx.x, wgs = (int)gridDim.x;
         // every thread the cost of `each` slots, then sums over the threads
         const int each = (p.slots + NT - 1) / NT, first = tid * each;
-        int mine = 0, used = 0;
+        int mine = 0, used = 0, most = 0;
         for (int i = 0; i < each; ++i)
             if (first + i < p.slots) {
                 const int cost = cost_of(block_of(p, first + i));
                 mine += cost;
                 used += cost > 0;
+                most = max(most, cost);
             }
         if (tid == 0) worst = 0;
         int *cost_s = reinterpret_cast<int *>(smem), *cost_r = cost_s + NT;
         cost_s[tid] = mine;
-        const Sums sum = sums_over_threads<NW>(mine, used, tot);
+        const Sums sum = sums_over_threads<NW>(mine, used, most, tot);
         const int segments = sum.entries, before = sum.cost_before;
         Cut plan{sum.cost, segments ? parts_of(segments * p.hkv, sum.cost * p.hkv, wgs, LEAST) : 1, 0, 0};
         plan.set(sum.cost * p.hkv);
         // whole segments: heads side by side, `groups` workgroups each, so that an XCD's L2 serves few of them
         const int groups = wgs / p.hkv;
         bool whole = segments == 0;
-        if (each == 1 && groups > 0) {
+        if (each == 1 && segments <= groups) {   // (one each, in any order)
+            if (mine > 0) slot_r[sum.entries_before] = (int16_t)tid;
+            __syncthreads();
+            whole = whole || sum.most <= plan.wide + START + JOIN;
+        } else if (each == 1 && groups > 0) {
             if (mine > 0) {
                 const int rank = rank_by_cost(cost_s, p.slots, tid);
                 slot_r[rank] = (int16_t)tid;

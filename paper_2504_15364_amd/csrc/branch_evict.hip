@@ -63,18 +63,6 @@ __device__ __forceinline__ void move_rows(const BranchEvictParams &p, Moves move
     }
 }
 
-// The largest of a wave's numbers, in every lane
-__device__ __forceinline__ uint32_t wave_max(uint32_t x)
-{
-    x = max(x, dpp_fetch<0x111, 0xF>(x));
-    x = max(x, dpp_fetch<0x112, 0xF>(x));
-    x = max(x, dpp_fetch<0x114, 0xF>(x));
-    x = max(x, dpp_fetch<0x118, 0xF>(x));
-    x = max(x, dpp_fetch<0x142, 0xA>(x));
-    x = max(x, dpp_fetch<0x143, 0xC>(x));
-    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
-}
-
 constexpr int OWN_MOVES = 128;   // moves that the workgroup of a head makes itself
 constexpr int BINS = 2048, CANDIDATES = 128;
 
@@ -84,7 +72,7 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
     constexpr int WAVES = NT / 64, WORDS = ROWS / 64;   // words of 64 rows
     // of every row: it goes ahead of another if its key is lower, or its `low` at equal keys, or its row higher at equal both
     __shared__ uint32_t key_s[ROWS], low_s[ROWS];
-    __shared__ uint32_t hist[BINS], wave_tot[WAVES], words[WORDS + 1], cand_key[CANDIDATES], cand_low[CANDIDATES], found[4], counted, best[3][WAVES];
+    __shared__ uint32_t hist[BINS], wave_tot[WAVES], words[WORDS + 1], cand_key[CANDIDATES], cand_low[CANDIDATES], found[4], counted, best[3][WAVES], range_s[3][2][WAVES];
     __shared__ uint64_t out_s[WORDS];   // a bit for every row that goes
     __shared__ int cand_row[CANDIDATES];
     __shared__ Move list[OWN_MOVES];
@@ -103,7 +91,7 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
     int need = n - p.budget;
     const int64_t late = (int64_t)pos0 + n - p.window;   // positions from here on are kept ahead of all others
     bool absent = all > n;
-    uint32_t lo = 0xFFFFFFFFu, hi = 0;   // the range of the keys
+    uint32_t lo = 0xFFFFFFFFu, hi = 0, low_lo = 0xFFFFFFFFu, low_hi = 0;   // the range of the keys, and of `low`
     uint32_t k_first = 0xFFFFFFFFu, l_first = 0xFFFFFFFFu;   // the thread's row that goes ahead of its others
     int r_first = -1;
     constexpr int AT_ONCE = 4;           // rows of a thread that are asked for together
@@ -135,6 +123,8 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
             low_s[r] = low;
             lo = min(lo, key);
             hi = max(hi, key);
+            low_lo = min(low_lo, low);
+            low_hi = max(low_hi, low);
             if (r_first < 0 || key < k_first || (key == k_first && low <= l_first)) {   // (of equal ones the higher row, which comes later)
                 k_first = key;
                 l_first = low;
@@ -175,21 +165,26 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
         }
         return;
     }
-    lo = ~wave_max(~lo);
-    hi = wave_max(hi);
-    if (lane == 0) {
-        best[0][wave] = lo;
-        best[1][wave] = hi;
-    }
+    // the lowest and the highest over the workgroup
+    auto range_of = [&](uint32_t &a, uint32_t &b, uint32_t (&of_waves)[2][WAVES]) {
+        a = ~wave_max(~a);
+        b = wave_max(b);
+        if (lane == 0) {
+            of_waves[0][wave] = a;
+            of_waves[1][wave] = b;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            a = min(a, of_waves[0][w]);
+            b = max(b, of_waves[1][w]);
+        }
+    };
     for (int i = tid; i < BINS; i += NT) hist[i] = 0;
     for (int i = tid; i < WORDS; i += NT) words[i] = 0;
     if (tid == 0) counted = 0;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        lo = min(lo, best[0][w]);
-        hi = max(hi, best[1][w]);
-    }
+    range_of(lo, hi, range_s[0]);
+    range_of(low_lo, low_hi, range_s[1]);
     // Narrow down: of the rows whose value (the key; later, among those of key `equal`, low) lies in [lo, hi] the `need` first ones go; those below lo go, those
     // above hi stay
     bool by_low = false;
@@ -230,12 +225,22 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
         need = (int)found[1];
         count = found[2];
         if (count == (uint32_t)need || count <= CANDIDATES) break;
+        // many rows in one bin, often because they are alike: the range of what they hold
+        uint32_t a = 0xFFFFFFFFu, b = 0;
+        for (int r = tid; r < n; r += NT)
+            if (inside(r)) {
+                a = min(a, by_low ? low_s[r] : key_s[r]);
+                b = max(b, by_low ? low_s[r] : key_s[r]);
+            }
+        range_of(a, b, range_s[2]);
+        lo = a;
+        hi = b;
         if (lo == hi) {
             if (by_low) break;   // alike in all but their rows
             by_low = true;
             equal = lo;
-            lo = 0;
-            hi = 0xFFFFFFFFu;
+            lo = low_lo;
+            hi = low_hi;
         }
         __syncthreads();
     }

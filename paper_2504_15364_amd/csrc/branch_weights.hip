@@ -512,7 +512,7 @@ __global__ __launch_bounds__(64 * NW) void weights_many_kernel(WeightsParams)
     const WeightsParams &p = argument_at<WeightsParams>(0);   // (read where it is needed)
     constexpr int NT = 64 * NW;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[Lds<D>::BYTES];
-    __shared__ int tot[2][NW];
+    __shared__ int tot[3][NW];
     __shared__ int seq_r[NT];      // sequence and block by rank, where blocks stay whole
     __shared__ int16_t block_r[NT];
     __shared__ int worst, blocks_s;
@@ -520,16 +520,17 @@ __global__ __launch_bounds__(64 * NW) void weights_many_kernel(WeightsParams)
     const int tid = threadIdx.x, wgs = (int)gridDim.x, wg = part_number();
     {
         const int each = (p.n_seqs + NT - 1) / NT, first = tid * each;
-        int mine = 0, used = 0;
+        int mine = 0, used = 0, most = 0;
         Blocks own{};
         for (int i = 0; i < each; ++i)
             if (first + i < p.n_seqs) {
                 own = blocks_of(p, first + i);
                 mine += own.cost;
                 used += own.count;
+                most = max(most, own.count ? START + own.tiles * TILE : 0);
             }
         if (tid == 0) worst = 0;
-        const Sums sum = sums_over_threads<NW>(mine, used, tot);
+        const Sums sum = sums_over_threads<NW>(mine, used, most, tot);
         const int total = sum.cost, segments = sum.entries, before = sum.cost_before;
         if (total == 0) {   // uniform
             if (blockIdx.x == 0 && tid == 0) p.plan[1] = 0;
@@ -540,7 +541,14 @@ __global__ __launch_bounds__(64 * NW) void weights_many_kernel(WeightsParams)
         // whole blocks: heads side by side, `groups` workgroups each, so that an XCD's L2 serves few of them
         const int groups = wgs / p.hkv;
         bool whole = false;
-        if (each == 1 && segments <= NT && groups > 0) {
+        if (each == 1 && segments <= groups) {   // (one each, in any order)
+            for (int k = 0; k < own.count; ++k) {
+                seq_r[sum.entries_before + k] = tid;
+                block_r[sum.entries_before + k] = (int16_t)k;
+            }
+            __syncthreads();
+            whole = sum.most <= plan.wide + JOIN;
+        } else if (each == 1 && segments <= NT && groups > 0) {
             // the sequences' first blocks, then every thread a block
             Seq *seq_s = reinterpret_cast<Seq *>(smem);
             int *first_s = reinterpret_cast<int *>(seq_s + NT), *cost_s = first_s + NT, *cost_r = cost_s + NT;
@@ -558,7 +566,7 @@ __global__ __launch_bounds__(64 * NW) void weights_many_kernel(WeightsParams)
             }
             __syncthreads();
             if (tid < segments) {
-                const int rank = segments <= groups ? tid : rank_by_cost(cost_s, segments, tid);   // (one each: the order is of no consequence)
+                const int rank = rank_by_cost(cost_s, segments, tid);
                 seq_r[rank] = s;
                 block_r[rank] = (int16_t)k;
                 cost_r[rank] = cost_s[tid];

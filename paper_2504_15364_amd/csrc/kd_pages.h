@@ -21,26 +21,42 @@ __device__ __forceinline__ int rows_with(const Pages &pages, int len, int fresh)
     return (int)(n < most ? n : most);
 }
 
-// What each thread's share of a list costs and how many entries it has, summed over the workgroup: in all, and over the threads before this one
+// The largest of a wave's numbers, in every lane
+__device__ __forceinline__ uint32_t wave_max(uint32_t x)
+{
+    x = max(x, dpp_fetch<0x111, 0xF>(x));
+    x = max(x, dpp_fetch<0x112, 0xF>(x));
+    x = max(x, dpp_fetch<0x114, 0xF>(x));
+    x = max(x, dpp_fetch<0x118, 0xF>(x));
+    x = max(x, dpp_fetch<0x142, 0xA>(x));
+    x = max(x, dpp_fetch<0x143, 0xC>(x));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
+// What each thread's share of a list costs, how many entries it has and what the most expensive one costs, summed over the workgroup: in all, and over the
+// threads before this one
 struct Sums {
-    int cost, entries, cost_before, entries_before;
+    int cost, entries, most, cost_before, entries_before;
 };
 template <int WAVES>
-__device__ __forceinline__ Sums sums_over_threads(int cost, int entries, int (&tot)[2][WAVES])
+__device__ __forceinline__ Sums sums_over_threads(int cost, int entries, int most, int (&tot)[3][WAVES])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int c = (int)wave_inclusive_scan((uint32_t)cost), e = (int)wave_inclusive_scan((uint32_t)entries);
+    most = (int)wave_max((uint32_t)most);
     if (lane == 63) {
         tot[0][wave] = c;
         tot[1][wave] = e;
+        tot[2][wave] = most;
     }
     __syncthreads();
-    Sums s{0, 0, c - cost, e - entries};
+    Sums s{0, 0, 0, c - cost, e - entries};
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
         const int x = tot[0][w], y = tot[1][w];
         s.cost += x;
         s.entries += y;
+        s.most = max(s.most, tot[2][w]);
         s.cost_before += w < wave ? x : 0;
         s.entries_before += w < wave ? y : 0;
     }
