@@ -1419,9 +1419,19 @@ int finish_prompt_cache(keydiff_cache_t *c, hipStream_t s)
 }
 
 // ------------------------------------------------------------------ pieces of many tokens, weights of own rows, their eviction
-constexpr int kFewRows = 32;   // query rows of a sequence and KV head up to which the kernels of branch_attention take a piece
+// A piece goes to the kernels of branch_attention with up to kFewRows query rows of a sequence and KV head, and with up to twice as many where
+// few groups share the device: theirs split every run of rows over waves and workgroups, where a tile of branch_chunk.hip has room for 256 query
+// rows and is slower to start.  Measured, 8 KV heads, d 128 (us, chunk | branch): 32 query rows, 1 sequence of 1000 rows 26.7 | 16.9, 64 of 1000
+// 56.7 | 58.4, 64 of 50 rows behind a prompt of 4096 144 | 72; 36 query rows, 64 sequences of 1000 rows 56 | 68, of 50 behind 4096 155 | 75, 2 of
+// 2000 28.7 | 23.1, 2 of 100 behind 4096 28.6 | 19.2; 64 query rows, 1 of 1000 26.9 | 19.6, 1 of 8192 28.2 | 27.9, 2 of 2000 28.4 | 24.2, 4 of 8000
+// 36.2 | 55.3, 8 of 2000 29.3 | 38.2, 64 of 1000 57.5 | 79.0, of 50 behind 4096 156 | 172; 128 query rows, 1 of 1000 29.5 | 23.6, 1 of 8192
+// 29.9 | 36.6, 8 of 2000 32.7 | 55.3.
+constexpr int kFewRows = 32, kFewGroups = 16;
 
-bool few_rows(const keydiff_branches_t *b, int32_t Bt) { return (int64_t)b->n_q_heads / b->n_kv_heads * Bt <= kFewRows; }
+bool few_rows(const keydiff_branches_t *b, int32_t Bt)
+{
+    return (int64_t)b->n_q_heads / b->n_kv_heads * Bt <= ((int64_t)b->n_seqs * b->n_kv_heads <= kFewGroups ? 2 * kFewRows : kFewRows);
+}
 
 BranchWork chunk_work(const keydiff_branches_t *b, int32_t Bt, int32_t n_prefixes)
 {
