@@ -2,11 +2,12 @@
 //
 // A row's rank is (latest positions first, weight, lower position, lower row); of n rows those of the n - budget lowest ranks are evicted.  One
 // workgroup a (sequence, KV head) finds them and pairs the evicted rows below the budget with the kept ones behind it, both in ascending order.
-// What bounds it: a chain of look-ups (length, page, weight) and barriers where few rows are evicted, the moves where many are.
-//   up to 16384 rows in the table   weights and positions in LDS.  One row too many, a generated token's case: the lowest rank by one reduction.  Else
-//                          histograms of 2048 bins over the range of what is left narrow the border down to candidates that are ranked in pairs.  Loops
-//                          over LDS and not rows in registers: with 16 of them a thread, every pass unrolled, the code of each was run once and
-//                          waited for from memory (16 heads of 16384 rows 51 us)
+// What bounds it: a chain of look-ups (length, page, weight) and barriers where few rows are evicted; where many are, the passes of a workgroup over its
+// rows, 64 of them an instruction of 4 cycles, four waves a SIMD (an instruction more in a pass over 16384 rows is 0.1 us), and then the moves.
+//   up to 16384 rows in the table   weights and positions in LDS, in kernels of 1024, 4096, 8192 and 16384 rows.  One row too many, a generated token's
+//                          case: the lowest rank by one reduction (512 heads of 4097 rows 5.9 us, launch and all).  Else a histogram of 2048 bins over
+//                          the range of what is left, once more if needed, narrows the border down to 128 candidates that are ranked in pairs
+//                          (16 heads of 16384 rows: 4 us to load them, 4 to the border, 5 for the bits of what goes and the ranks, 3 for the list)
 //   more                   a radix select that reads weights and positions again in every pass
 // Few moves are made by the workgroup itself (a second launch took 4 us for one row of each of 512 heads), many by a second launch over the whole chip.
 #include <algorithm>
@@ -40,31 +41,44 @@ using Move = BranchMove;
 __device__ __forceinline__ uint32_t ordered(float x)
 {
     const uint32_t u = __float_as_uint(x != x ? -INFINITY : x + 0.f);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
-// Rows of one head from one place to another, 16 bytes a thread and turn: thread `tid` of `threads`
-template <class Moves>
-__device__ __forceinline__ void move_rows(const BranchEvictParams &p, Moves move, int count, int64_t tid, int64_t threads)
+// Rows of one head from one place to another, 16 bytes a thread and turn: thread `tid` of `threads`.  move(i), i < most, may be read ahead of the count
+template <int AT_ONCE, class Moves>
+__device__ __forceinline__ void move_rows(const BranchEvictParams &p, Moves move, int count, int most, int64_t tid, int64_t threads)
 {
     const int units = p.D / 8, shift = units == 16 ? 5 : 4;   // of a row of K, then of V
-    for (int64_t i = tid; i < (int64_t)count << shift; i += threads) {
-        const Move m = move(i >> shift);
-        const int u = (int)i & (2 * units - 1);
-        u32x4 *rows = reinterpret_cast<u32x4 *>(u < units ? p.pages.k : p.pages.v);
-        const int at = u & (units - 1);
-        if (u == 0) {
-            const float w = p.w[m.from];
-            const int32_t position = p.positions[m.from];
-            p.w[m.to] = w;
-            p.positions[m.to] = position;
+    const int u = (int)tid & (2 * units - 1);                 // (`threads` is a multiple of the units)
+    u32x4 *const rows = reinterpret_cast<u32x4 *>(u < units ? p.pages.k : p.pages.v) + (u & (units - 1));
+    for (int64_t i = tid; i < (int64_t)most << shift; i += threads * AT_ONCE) {
+        Move m[AT_ONCE];
+        u32x4 x[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) m[k] = move(min((i + threads * k) >> shift, (int64_t)most - 1));
+        if (i >> shift >= count) return;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if ((i + threads * k) >> shift >= count) m[k] = m[0];   // (loaded once more, not stored)
+            x[k] = rows[m[k].from * units];
         }
-        rows[m.to * units + at] = rows[m.from * units + at];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if ((i + threads * k) >> shift >= count) continue;
+            rows[m[k].to * units] = x[k];
+            if (u == 0) {
+                const float w = p.w[m[k].from];
+                const int32_t position = p.positions[m[k].from];
+                p.w[m[k].to] = w;
+                p.positions[m[k].to] = position;
+            }
+        }
     }
 }
 
 constexpr int OWN_MOVES = 128;   // moves that the workgroup of a head makes itself
 constexpr int BINS = 2048, CANDIDATES = 128;
+constexpr uint32_t ZERO = 0x80000000u;   // ordered(0)
 
 template <int NT, int ROWS>
 __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
@@ -72,9 +86,10 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
     constexpr int WAVES = NT / 64, WORDS = ROWS / 64;   // words of 64 rows
     // of every row: it goes ahead of another if its key is lower, or its `low` at equal keys, or its row higher at equal both
     __shared__ uint32_t key_s[ROWS], low_s[ROWS];
-    __shared__ uint32_t hist[BINS], wave_tot[WAVES], words[WORDS + 1], cand_key[CANDIDATES], cand_low[CANDIDATES], found[4], counted, best[3][WAVES], range_s[3][2][WAVES];
+    __shared__ uint32_t hist[BINS], wave_tot[WAVES], words[WORDS + 1], found[4], counted, best[4][WAVES], range_s[2][WAVES];
     __shared__ uint64_t out_s[WORDS];   // a bit for every row that goes
-    __shared__ int cand_row[CANDIDATES];
+    __shared__ uint64_t cand[CANDIDATES];
+    __shared__ int cand_row[CANDIDATES], cand_rank[CANDIDATES], page_s[ROWS / 8];
     __shared__ Move list[OWN_MOVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int s = p.by_hkv.divide(blockIdx.x), h = (int)blockIdx.x - s * p.hkv;
@@ -89,69 +104,86 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
         return;
     }
     int need = n - p.budget;
-    const int64_t late = (int64_t)pos0 + n - p.window;   // positions from here on are kept ahead of all others
+    // positions from `late` on are kept ahead of all others
+    const int64_t late64 = (int64_t)pos0 + n - p.window;
+    const bool window = p.window > 0 && late64 <= INT32_MAX;
+    const int32_t late = (int32_t)(late64 < INT32_MIN ? INT32_MIN : late64);
+    const int in_page = (1 << head.shift) - 1;
+    const uint32_t of_page = (uint32_t)p.hkv << head.shift, of_head = (uint32_t)h << head.shift;
     bool absent = all > n;
-    uint32_t lo = 0xFFFFFFFFu, hi = 0, low_lo = 0xFFFFFFFFu, low_hi = 0;   // the range of the keys, and of `low`
-    uint32_t k_first = 0xFFFFFFFFu, l_first = 0xFFFFFFFFu;   // the thread's row that goes ahead of its others
-    int r_first = -1;
+    uint32_t above_lo = 0xFFFFFFFFu;     // the range of the keys of positive weights, less the lowest such key
+    int32_t above_hi = -1;
     constexpr int AT_ONCE = 4;           // rows of a thread that are asked for together
-    for (int base = 0; base < n; base += NT * AT_ONCE) {
-        int page[AT_ONCE];
-        int64_t at[AT_ONCE];
-        float w[AT_ONCE];
-        int32_t before[AT_ONCE];
+    int page[AT_ONCE];                   // asked for one turn ahead
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) page[i] = table_entry(head.table, min(base + NT * i + tid, n - 1) >> head.shift);
+    for (int i = 0; i < AT_ONCE; ++i) page[i] = table_entry(head.table, min(NT * i + tid, n - 1) >> head.shift);
+    for (int base = 0; base < n; base += NT * AT_ONCE) {
+        uint64_t at[AT_ONCE];
+        float w[AT_ONCE];
+        int32_t position[AT_ONCE];
+        bool there[AT_ONCE];
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
             const int r = min(base + NT * i + tid, n - 1);
-            const bool there = (uint32_t)page[i] < (uint32_t)p.pages.n_pages;
-            absent = absent || !there;
-            at[i] = (((int64_t)(there ? page[i] : 0) * head.hkv + h) << head.shift) + (r & ((1 << head.shift) - 1));
+            there[i] = (uint32_t)page[i] < (uint32_t)p.pages.n_pages;
+            absent = absent || !there[i];
+            at[i] = (uint64_t)(uint32_t)(there[i] ? page[i] : 0) * of_page + (of_head + (uint32_t)(r & in_page));
             w[i] = p.w[at[i]];
-            before[i] = p.positions[at[i]];
-            if (!there) at[i] = -1;
+            position[i] = p.positions[at[i]];
+        }
+        if (base + NT * AT_ONCE < n) {
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) page[i] = table_entry(head.table, min(base + NT * (AT_ONCE + i) + tid, n - 1) >> head.shift);
+        }
+        if (base + NT * AT_ONCE > len) {   // uniform: new rows
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int r = base + NT * i + tid;
+                if (r < len || r >= n) continue;
+                position[i] = (int32_t)((uint32_t)pos0 + (uint32_t)r);
+                if (there[i]) p.positions[at[i]] = position[i];
+            }
         }
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
             const int r = base + NT * i + tid;
             if (r >= n) continue;
-            const int32_t position = r < len ? before[i] : (int32_t)((uint32_t)pos0 + (uint32_t)r);
-            if (r >= len && at[i] >= 0) p.positions[at[i]] = position;
-            const uint32_t key = p.window > 0 && position >= late ? 0xFFFFFFFFu : ordered(w[i]), low = ~((uint32_t)position ^ 0x80000000u);
-            key_s[r] = key;
-            low_s[r] = low;
-            lo = min(lo, key);
-            hi = max(hi, key);
-            low_lo = min(low_lo, low);
-            low_hi = max(low_hi, low);
-            if (r_first < 0 || key < k_first || (key == k_first && low <= l_first)) {   // (of equal ones the higher row, which comes later)
-                k_first = key;
-                l_first = low;
-                r_first = r;
-            }
+            const uint32_t key = ordered(w[i]), above = key - (ZERO + 1);
+            above_lo = min(above_lo, above);   // (keys of zeros and negative weights wrap around to the upper half)
+            above_hi = max(above_hi, (int32_t)above);
+            key_s[r] = window && position[i] >= late ? 0xFFFFFFFFu : key;
+            low_s[r] = (uint32_t)position[i] ^ 0x7FFFFFFFu;
         }
     }
-    if (__syncthreads_or(absent)) {
-        if (tid == 0 && p.status) atomicOr(p.status, LEFT_OUT_ROW);
-        return;
-    }
+    absent = __builtin_amdgcn_ballot_w64(absent) != 0;
     if (need == 1) {
+        uint32_t k_first = 0xFFFFFFFFu, l_first = 0xFFFFFFFFu;   // the row that goes ahead of all others
+        int r_first = -1;
         auto first = [&](uint32_t k1, uint32_t l1, int r1) {
             const bool take = r1 >= 0 && (r_first < 0 || k1 < k_first || (k1 == k_first && (l1 < l_first || (l1 == l_first && r1 > r_first))));
             k_first = take ? k1 : k_first;
             l_first = take ? l1 : l_first;
             r_first = take ? r1 : r_first;
         };
+#pragma unroll 1
+        for (int r = tid; r < n; r += NT) {   // (its own rows: no barrier)
+            const uint32_t k1 = key_s[r];
+            if (k1 <= k_first) first(k1, low_s[r], r);
+        }
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) first(__shfl_xor(k_first, m), __shfl_xor(l_first, m), __shfl_xor(r_first, m));
         if (lane == 0) {
             best[0][wave] = k_first;
             best[1][wave] = l_first;
             best[2][wave] = (uint32_t)r_first;
+            best[3][wave] = absent;
         }
         __syncthreads();
         if (wave > 0) return;
+        if (__builtin_amdgcn_ballot_w64(best[3][lane % WAVES] != 0)) {
+            if (tid == 0 && p.status) atomicOr(p.status, LEFT_OUT_ROW);
+            return;
+        }
         k_first = best[0][lane % WAVES];
         l_first = best[1][lane % WAVES];
         r_first = (int)best[2][lane % WAVES];
@@ -161,44 +193,68 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
         if (row >= p.budget) return;   // the last row: it lies behind the budget
         if (tid < p.D / 4) {
             const Move m{head.at(p.budget), head.at(row)};
-            move_rows(p, [&](int64_t) { return m; }, 1, tid, p.D / 4);
+            move_rows<1>(p, [&](int64_t) { return m; }, 1, 1, tid, p.D / 4);
         }
         return;
     }
     // the lowest and the highest over the workgroup
-    auto range_of = [&](uint32_t &a, uint32_t &b, uint32_t (&of_waves)[2][WAVES]) {
+    auto range_of = [&](uint32_t &a, uint32_t &b) {
         a = ~wave_max(~a);
         b = wave_max(b);
         if (lane == 0) {
-            of_waves[0][wave] = a;
-            of_waves[1][wave] = b;
+            range_s[0][wave] = a;
+            range_s[1][wave] = b;
         }
         __syncthreads();
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            a = min(a, of_waves[0][w]);
-            b = max(b, of_waves[1][w]);
-        }
+        a = ~wave_max(~range_s[0][lane % WAVES]);
+        b = wave_max(range_s[1][lane % WAVES]);
     };
     for (int i = tid; i < BINS; i += NT) hist[i] = 0;
     for (int i = tid; i < WORDS; i += NT) words[i] = 0;
+    for (int i = tid; i < CANDIDATES; i += NT) {   // (places without a candidate go behind all)
+        cand[i] = ~0ull;
+        cand_row[i] = -1;
+        cand_rank[i] = 0;
+    }
     if (tid == 0) counted = 0;
-    range_of(lo, hi, range_s[0]);
-    range_of(low_lo, low_hi, range_s[1]);
+    if (lane == 0) best[3][wave] = absent;
+    uint32_t inner_lo = above_lo, inner_hi = (uint32_t)max(above_hi, 0);
+    for (int i = tid; i <= (n - 1) >> head.shift; i += NT) page_s[i] = table_entry(head.table, i);
+    range_of(inner_lo, inner_hi);
+    if (__builtin_amdgcn_ballot_w64(best[3][lane % WAVES] != 0)) {   // uniform: every wave reads all flags
+        if (tid == 0 && p.status) atomicOr(p.status, LEFT_OUT_ROW);
+        return;
+    }
+    if (inner_lo > inner_hi) inner_lo = inner_hi = 0;
+    inner_lo += ZERO + 1;
+    inner_hi += ZERO + 1;
     // Narrow down: of the rows whose value (the key; later, among those of key `equal`, low) lies in [lo, hi] the `need` first ones go; those below lo go, those
-    // above hi stay
+    // above hi stay.  What lies outside of the inner range, rows without a weight and those of the window, which would else stretch the bins over twenty times the
+    // range that the weights have, goes into the first bin and into the last one in use
+    uint32_t lo = 0, hi = 0xFFFFFFFFu;
     bool by_low = false;
     uint32_t equal = 0, count = 0;
+    auto value = [&](int r) { return by_low ? low_s[r] : key_s[r]; };
     auto inside = [&](int r) {
-        const uint32_t v = by_low ? low_s[r] : key_s[r];
+        const uint32_t v = value(r);
         return v >= lo && v <= hi && (!by_low || key_s[r] == equal);
     };
-    for (;;) {
-        const uint32_t span = hi - lo;
-        const int down = span < BINS ? 0 : 32 - 11 - __builtin_clz(span);
+    for (bool all_of_them = true;; all_of_them = false) {
+        const uint32_t span = inner_hi - inner_lo;
+        int down = span < BINS ? 0 : 32 - 11 - __builtin_clz(span);
+        if (span >> down > BINS - 2) ++down;
+        if (all_of_them) {   // (inner_lo exceeds ZERO: neither difference wraps)
+            const uint32_t least = inner_lo - 1, offset = inner_lo - (1u << down);
+            auto count_in = [&](int r) { atomicAdd(&hist[(min(max(key_s[r], least), inner_hi) - offset) >> down], 1u); };
+            int r = tid;
 #pragma unroll 4
-        for (int r = tid; r < n; r += NT)
-            if (inside(r)) atomicAdd(&hist[((by_low ? low_s[r] : key_s[r]) - lo) >> down], 1u);
+            for (int base = NT; base <= n; base += NT, r += NT) count_in(r);
+            if (r < n) count_in(r);
+        } else {             // nothing lies outside
+#pragma unroll 1
+            for (int r = tid; r < n; r += NT)
+                if (inside(r)) atomicAdd(&hist[((value(r) - inner_lo) >> down) + 1], 1u);
+        }
         __syncthreads();
         constexpr int PER = BINS / NT;
         uint32_t mine[PER], sum = 0, total;
@@ -219,30 +275,36 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
             hist[tid * PER + b] = 0;   // for the next turn
         }
         __syncthreads();
-        const uint32_t from = lo + (found[0] << down);
-        hi = hi - from >= 1u << down ? from + ((1u << down) - 1) : hi;
-        lo = from;
+        const uint32_t bin = found[0], from = inner_lo + ((bin - 1) << down);
         need = (int)found[1];
         count = found[2];
+        if (bin == 0) hi = inner_lo - 1;
+        else {
+            lo = from;
+            if (inner_hi - from >= 1u << down) hi = from + ((1u << down) - 1);
+        }
         if (count == (uint32_t)need || count <= CANDIDATES) break;
         // many rows in one bin, often because they are alike: the range of what they hold
-        uint32_t a = 0xFFFFFFFFu, b = 0;
-        for (int r = tid; r < n; r += NT)
-            if (inside(r)) {
-                a = min(a, by_low ? low_s[r] : key_s[r]);
-                b = max(b, by_low ? low_s[r] : key_s[r]);
-            }
-        range_of(a, b, range_s[2]);
-        lo = a;
-        hi = b;
-        if (lo == hi) {
-            if (by_low) break;   // alike in all but their rows
+        for (;;) {
+            uint32_t a = 0xFFFFFFFFu, b = 0;
+            for (int r = tid; r < n; r += NT)
+                if (inside(r)) {
+                    a = min(a, value(r));
+                    b = max(b, value(r));
+                }
+            range_of(a, b);
+            __syncthreads();
+            lo = a;
+            hi = b;
+            if (lo < hi || by_low) break;
             by_low = true;
             equal = lo;
-            lo = low_lo;
-            hi = low_hi;
+            lo = 0;
+            hi = 0xFFFFFFFFu;
         }
-        __syncthreads();
+        if (lo == hi) break;   // alike in all but their rows
+        inner_lo = lo;
+        inner_hi = hi;
     }
     const bool whole = count == (uint32_t)need;   // uniform
     // numbers in `words` become those of all words before, the last one their sum
@@ -267,38 +329,55 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
         __syncthreads();
     };
     const bool ranked = !whole && count <= CANDIDATES;
-    auto goes_first = [&](int r) { return by_low ? key_s[r] < equal || (key_s[r] == equal && low_s[r] < lo) : key_s[r] < lo; };
-    for (int base = 0; base < n; base += NT) {
-        const int r = base + tid;
-        const bool in = r < n && inside(r);
-        const uint64_t out = __builtin_amdgcn_ballot_w64(r < n && (goes_first(r) || (whole && in)));
-        if (lane == 0) out_s[(base >> 6) + wave] = out;
-        if (ranked && in) {   // a candidate (their order is of no consequence)
-            const uint32_t c = atomicAdd(&counted, 1u);
-            cand_key[c] = key_s[r];
-            cand_low[c] = low_s[r];
-            cand_row[c] = r;
+    auto rank_of = [&](int r) { return (uint64_t)key_s[r] << 32 | low_s[r]; };
+    // a word of 64 rows a wave and turn: those below lo go, those in [lo, hi] go too, are candidates or are counted
+    auto place = [&](int base, bool out, bool in) {
+        const uint64_t of_wave = __builtin_amdgcn_ballot_w64(out), some = __builtin_amdgcn_ballot_w64(in);
+        if (lane == 0) out_s[(base >> 6) + wave] = of_wave;
+        if (ranked) {
+            if (in) {   // a candidate (their order is of no consequence)
+                const uint32_t c = atomicAdd(&counted, 1u);
+                cand[c] = rank_of(base + tid);
+                cand_row[c] = base + tid;
+            }
+        } else if (!whole && lane == 0) words[(base >> 6) + wave] = (uint32_t)__popcll(some);
+    };
+    if (!by_low) {   // uniform
+        const uint32_t bound = whole ? hi + 1 : lo;   // (hi + 1 does not wrap: the highest rows of all stay, a budget is 1 at least)
+        int base = 0;
+#pragma unroll 1
+        for (; base + NT <= n; base += NT) {
+            const uint32_t k = key_s[base + tid];
+            place(base, k < bound, k - lo <= hi - lo);
         }
-        if (!whole && !ranked) {
-            const uint64_t same = __builtin_amdgcn_ballot_w64(in);
-            if (lane == 0) words[(base >> 6) + wave] = (uint32_t)__popcll(same);
+        if (base < n) {
+            const bool there = base + tid < n;
+            const uint32_t k = there ? key_s[base + tid] : 0u;
+            place(base, there && k < bound, there && k - lo <= hi - lo);
         }
-    }
+    } else
+#pragma unroll 1
+        for (int base = 0; base < n; base += NT) {
+            const int r = base + tid;
+            const bool in = r < n && inside(r), out = r < n && rank_of(r) < ((uint64_t)equal << 32 | lo);
+            place(base, out || (whole && in), in);
+        }
     auto goes = [&](int r) { atomicOr(reinterpret_cast<uint32_t *>(out_s) + (r >> 5), 1u << (r & 31)); };
     if (ranked) {
         __syncthreads();
-        for (int c = wave; c < (int)count; c += WAVES) {   // a wave a candidate, against 64 others at a time
-            const uint32_t k = cand_key[c], l = cand_low[c];
-            const int r = cand_row[c];
-            int rank = 0;
-            for (int o0 = 0; o0 < (int)count; o0 += 64) {
-                const int o = min(o0 + lane, CANDIDATES - 1);
-                const uint32_t ko = cand_key[o], lw = cand_low[o];
-                const int ro = cand_row[o];
-                rank += __popcll(__builtin_amdgcn_ballot_w64(o0 + lane < (int)count && (ko < k || (ko == k && (lw < l || (lw == l && ro > r))))));
-            }
-            if (lane == 0 && rank < need) goes(r);
+        // a candidate against a part of the others a thread: the others' words come to all lanes of a wave at once
+        constexpr int PARTS = NT / CANDIDATES, OTHERS = CANDIDATES / PARTS;
+        const int c = tid % CANDIDATES, first = tid / CANDIDATES * OTHERS;
+        const uint64_t own = cand[c];
+        const int r = cand_row[c];
+        int rank = 0;
+        if (first < (int)count) {   // uniform in the wave
+#pragma unroll 8
+            for (int o = first; o < first + OTHERS; ++o) rank += cand[o] < own || (cand[o] == own && cand_row[o] > r);
         }
+        if (rank > 0) atomicAdd(&cand_rank[c], rank);
+        __syncthreads();
+        if (tid < (int)count && cand_rank[tid] < need) goes(cand_row[tid]);
     } else if (!whole) {
         // alike in all but their rows: the last `need` of them
         add_up();
@@ -319,27 +398,25 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
     const int count_moves = (int)(words[WORDS] & 0xFFFFu);
     const bool own = count_moves <= OWN_MOVES;   // uniform
     Move *to = own ? list : p.moves + (int64_t)blockIdx.x * p.most_moves;
-    for (int base = 0; base < n; base += NT * AT_ONCE) {
-        int page[AT_ONCE];
-#pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) page[i] = table_entry(head.table, min(base + NT * i + tid, n - 1) >> head.shift);
-#pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) {
-            const int r = base + NT * i + tid, word = ((base + NT * i) >> 6) + wave;
-            if (64 * word >= n) break;   // uniform in the wave
-            const uint64_t holes = holes_of(word), movers = movers_of(word), ahead = (1ull << lane) - 1;
-            const uint32_t before = words[word];
-            const int64_t at = (((int64_t)page[i] * head.hkv + h) << head.shift) + (r & ((1 << head.shift) - 1));
-            if (holes >> lane & 1) to[(before >> 16) + __popcll(holes & ahead)].to = at;
-            if (movers >> lane & 1) to[(before & 0xFFFFu) + __popcll(movers & ahead)].from = at;
-        }
+#pragma unroll 1
+    for (int word = wave; 64 * word < n; word += WAVES) {
+        const uint64_t word_s = out_s[word];
+        const uint64_t out = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(word_s >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)word_s);
+        const uint64_t kept = first_bits(p.budget - 64 * word), holes = out & kept, movers = ~out & first_bits(n - 64 * word) & ~kept;
+        if (!(holes | movers)) continue;
+        const uint32_t before = (uint32_t)__builtin_amdgcn_readfirstlane((int)words[word]);
+        auto ahead = [](uint64_t m) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u)); };
+        const int r = 64 * word + lane;
+        const int64_t at = (int64_t)((uint64_t)(uint32_t)page_s[min(r, n - 1) >> head.shift] * of_page + (of_head + (uint32_t)(r & in_page)));
+        if (__builtin_amdgcn_inverse_ballot_w64(holes)) to[(before >> 16) + ahead(holes)].to = at;
+        if (__builtin_amdgcn_inverse_ballot_w64(movers)) to[(before & 0xFFFFu) + ahead(movers)].from = at;
     }
     if (!own) {
         if (tid == 0) p.counts[blockIdx.x] = count_moves;
         return;
     }
     __syncthreads();
-    move_rows(p, [&](int64_t i) { return list[i]; }, count_moves, tid, NT);
+    move_rows<2>(p, [&](int64_t i) { return list[i]; }, count_moves, count_moves, tid, NT);
 }
 
 __global__ __launch_bounds__(LNT) void evict_select_long_kernel(BranchEvictParams p)
@@ -445,7 +522,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(BranchEvictParams p)
 {
     const int count = p.counts[blockIdx.x];
     const Move *moves = p.moves + (int64_t)blockIdx.x * p.most_moves;
-    move_rows(p, [&](int64_t i) { return moves[i]; }, count, (int64_t)blockIdx.y * 256 + threadIdx.x, (int64_t)gridDim.y * 256);
+    move_rows<4>(p, [&](int64_t i) { return moves[i]; }, count, p.most_moves, (int64_t)blockIdx.y * 256 + threadIdx.x, (int64_t)gridDim.y * 256);
 }
 
 }  // namespace
@@ -466,6 +543,7 @@ hipError_t launch_branch_evict(BranchEvictParams p, hipStream_t s)
     const bool in_lds = rows <= 16384;
     if (rows <= 1024) hipLaunchKernelGGL((evict_select_kernel<256, 1024>), dim3(heads), dim3(256), 0, s, p);
     else if (rows <= 4096) hipLaunchKernelGGL((evict_select_kernel<512, 4096>), dim3(heads), dim3(512), 0, s, p);
+    else if (rows <= 8192) hipLaunchKernelGGL((evict_select_kernel<1024, 8192>), dim3(heads), dim3(1024), 0, s, p);
     else if (in_lds) hipLaunchKernelGGL((evict_select_kernel<1024, 16384>), dim3(heads), dim3(1024), 0, s, p);
     else hipLaunchKernelGGL(evict_select_long_kernel, dim3(heads), dim3(LNT), 0, s, p);
     const hipError_t e = hipGetLastError();

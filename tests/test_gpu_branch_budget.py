@@ -243,6 +243,24 @@ def test_rows_that_are_alike_go_from_the_last_one(L):
         same((k, v, w, p), want)
 
 
+@pytest.mark.parametrize("weight", [0.0, -0.0, 0.5, -3.0, float("inf"), float("-inf"), float("nan"), None])
+@pytest.mark.parametrize("L", [900, 5000, 12000])
+def test_rows_of_equal_weight_go_by_positions_of_the_whole_range(L, weight):
+    # no weight, one weight, or two of them, and positions from one end of int32 to the other, its ends among them many times
+    hkv, d, page = 2, 64, 16
+    g = gen(77)
+    k, v, w, p, table = evict_case(hkv, d, page, [L], [5], 0, g, spread, [0])
+    for budget in (L + 5 - 2, L - 200, L // 2, 3):
+        at = torch.randint(-2 ** 31, 2 ** 31, (hkv, L), **g)
+        at = torch.where(torch.rand((hkv, L), **g) < 0.1, -2 ** 31, torch.where(torch.rand((hkv, L), **g) < 0.1, 2 ** 31 - 1, at))
+        put_rows(p, table, 0, at.to(torch.int32))
+        flat = torch.full((hkv, L + 5), weight, device="cuda") if weight is not None else (torch.rand((hkv, L + 5), **g) < 0.5).float() - 0.5
+        put_rows(w, table, 0, flat)
+        want = after_eviction((k, v, w, p), table, [L], [5], [0], budget, -(1 << 40))   # (no row is late)
+        kd.branch_evict(k, v, w, p, table, ints([L]), budget, Bt=5)
+        same((k, v, w, p), want)
+
+
 def test_evicting_again_from_what_is_there_already():
     # rows behind the budget are still there: the same call once more, many times, while copies of rows take over
     hkv, d, page, L, Bt, budget = 2, 64, 16, 500, 200, 450
