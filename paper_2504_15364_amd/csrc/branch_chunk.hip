@@ -64,21 +64,22 @@ __device__ __forceinline__ void wait_copies()   // at most N of this wave's copi
 
 // A block of query rows of a sequence: slot s * blocks + qb
 struct Block {
-    int s, m0, M;        // sequence; first row, and rows of the sequence in all
+    int s, m0, M;        // sequence; first row, and the one behind the last
     int len, last;       // rows held before the step; the last own row that a row of the block sees
     int tiles;           // of the prompt and of own rows; 0: no row
 };
-__device__ __forceinline__ Block block_of(const ChunkParams &p, int slot)
+// half: -1, or the half of the block that is meant
+__device__ __forceinline__ Block block_of(const ChunkParams &p, int slot, int half)
 {
     Block b{};
     b.s = p.by_blocks.divide(slot);
-    b.m0 = (slot - b.s * p.blocks) * R;
+    b.m0 = (slot - b.s * p.blocks) * R + (half > 0 ? R / 2 : 0);
     const int len = table_entry(p.pages.lens, b.s), fresh = new_rows(len, asked_rows(p.pages, p.Bt, b.s), p.Bt);
-    b.M = fresh * p.G;
+    b.M = min(b.m0 + (half < 0 ? R : R / 2), fresh * p.G);
     if (b.m0 >= b.M) return b;
     const int n = rows_with(p.pages, len, fresh);
     b.len = min(len, n);
-    const int j = p.by_G.divide(min(b.m0 + R, b.M) - 1);
+    const int j = p.by_G.divide(b.M - 1);
     b.last = (int64_t)len + j < n ? len + j : n - 1;
     b.tiles = (p.prefix_len + TK - 1) / TK + b.last / TK + 1;
     return b;
@@ -520,7 +521,7 @@ __global__ __launch_bounds__(64 * NW) void chunk_whole_kernel(ChunkParams)
     __shared__ __attribute__((aligned(1024))) unsigned char smem[lds_bytes<D>()];
     __shared__ Kept kept;
     const int h = p.by_slots.divide(blockIdx.x), slot = (int)blockIdx.x - h * p.slots;
-    const Block b = block_of(p, slot);
+    const Block b = block_of(p, slot, gridDim.y > 1 ? (int)blockIdx.y : -1);
     if (b.tiles == 0) return;   // uniform
     attend<D>(p, smem, kept, b, h, 0, b.tiles, -1);
 }
@@ -530,7 +531,8 @@ struct Place {
     int h, slot, at, left, turn;
 };
 // Segments dealt to the workgroups.  Where whole ones can be dealt evenly enough they are: sorted by what they cost, dealt out and back again in
-// turn.  Else the list is cut into equal parts.
+// turn.  Where there are at most half as many as workgroups, each goes to two in halves of 128 query rows, which take a tile in three fifths of the time (7
+// pieces of 233 tokens, 6 heads on 2, 32 to 26 us).  Else the list is cut into equal parts.
 template <int D>
 __global__ __launch_bounds__(64 * NW) void chunk_parts_kernel(ChunkParams)
 {
@@ -540,7 +542,7 @@ __global__ __launch_bounds__(64 * NW) void chunk_parts_kernel(ChunkParams)
     __shared__ __attribute__((aligned(1024))) unsigned char smem[lds_bytes<D>()];
     __shared__ int tot[3][NW];
     __shared__ int16_t slot_r[NT];   // the slots by rank, where segments stay whole
-    __shared__ int worst, segments_s;
+    __shared__ int worst, segments_s, halves_s;
     __shared__ Place place;
     __shared__ Cut plan_s;
     __shared__ Kept kept;
@@ -548,31 +550,42 @@ __global__ __launch_bounds__(64 * NW) void chunk_parts_kernel(ChunkParams)
         const int tid = threadIdx.x, wgs = (int)gridDim.x;
         // every thread the cost of `each` slots, then sums over the threads
         const int each = (p.slots + NT - 1) / NT, first = tid * each;
-        int mine = 0, used = 0, most = 0;
+        int mine = 0, used = 0, most = 0, rows = 0;
         for (int i = 0; i < each; ++i)
             if (first + i < p.slots) {
-                const int cost = cost_of(block_of(p, first + i));
+                const Block b = block_of(p, first + i, -1);
+                const int cost = cost_of(b);
                 mine += cost;
                 used += cost > 0;
-                most = max(most, cost);
+                most = max(most, b.tiles);
+                rows = b.M - b.m0;
             }
+        const int my_halves = mine == 0 ? 0 : rows > R / 2 ? 2 : 1;
+        if (each == 1) used |= my_halves << 16;   // (512 of them at most)
         if (tid == 0) worst = 0;
         int *cost_s = reinterpret_cast<int *>(smem), *cost_r = cost_s + NT;
-        cost_s[tid] = mine;
+        cost_s[tid] = each == 1 ? cost_key(mine, tid) : 0;
         const Sums sum = sums_over_threads<NW>(mine, used, most, tot);
-        const int segments = sum.entries, before = sum.cost_before;
+        const int segments = each == 1 ? sum.entries & 0xFFFF : sum.entries, halves = sum.entries >> 16, before = sum.cost_before;
+        int dealt = segments;
         Cut plan{sum.cost, segments ? parts_of(segments * p.hkv, sum.cost * p.hkv, wgs, LEAST) : 1, 0, 0};
         plan.set(sum.cost * p.hkv);
         // whole segments: heads side by side, `groups` workgroups each, so that an XCD's L2 serves few of them
         const int groups = wgs / p.hkv;
         bool whole = segments == 0;
-        if (each == 1 && segments <= groups) {   // (one each, in any order)
-            if (mine > 0) slot_r[sum.entries_before] = (int16_t)tid;
+        if (each == 1 && halves <= groups) {   // (half a block each, in any order: a tile takes four waves three fifths of the time of eight)
+            if (mine > 0) slot_r[sum.entries_before >> 16] = (int16_t)(2 * tid);
+            if (my_halves > 1) slot_r[(sum.entries_before >> 16) + 1] = (int16_t)(2 * tid + 1);
             __syncthreads();
-            whole = whole || sum.most <= plan.wide + START + JOIN;
+            whole = whole || START + 6 * sum.most <= plan.wide + START + JOIN;
+            dealt = halves;
+        } else if (each == 1 && segments <= groups) {   // (one each, in any order)
+            if (mine > 0) slot_r[sum.entries_before & 0xFFFF] = (int16_t)tid;
+            __syncthreads();
+            whole = whole || START + 9 * sum.most <= plan.wide + START + JOIN;
         } else if (each == 1 && groups > 0) {
             if (mine > 0) {
-                const int rank = rank_by_cost(cost_s, p.slots, tid);
+                const int rank = rank_by_cost(cost_s, p.slots, cost_key(mine, tid));
                 slot_r[rank] = (int16_t)tid;
                 cost_r[rank] = mine;
             }
@@ -583,8 +596,9 @@ __global__ __launch_bounds__(64 * NW) void chunk_parts_kernel(ChunkParams)
         if (whole) {
             const int g = (int)blockIdx.x / p.hkv;
             if (tid == 0) {
-                segments_s = segments;
-                place = Place{(int)blockIdx.x % p.hkv, g < groups && g < segments ? slot_r[g] : 0, 0, g < groups && g < segments ? INT32_MAX : 0, 0};
+                segments_s = dealt;
+                halves_s = dealt > 0 && halves <= groups && each == 1;
+                place = Place{(int)blockIdx.x % p.hkv, g < groups && g < dealt ? slot_r[g] : 0, 0, g < groups && g < dealt ? INT32_MAX : 0, 0};
             }
         } else {
             const int w = part_number();
@@ -592,12 +606,13 @@ __global__ __launch_bounds__(64 * NW) void chunk_parts_kernel(ChunkParams)
             const int begin = plan.begin(w), h = begin / plan.per_head, from = begin - h * plan.per_head;
             if (tid == 0) {
                 segments_s = 0;
+                halves_s = 0;
                 plan_s = plan;
             }
             if (from >= before && from < before + mine) {   // one thread's
                 int at = before, slot = first;
                 for (;; ++slot) {
-                    const int cost = cost_of(block_of(p, slot));
+                    const int cost = cost_of(block_of(p, slot, -1));
                     if (from < at + cost) break;
                     at += cost;
                 }
@@ -610,7 +625,8 @@ __global__ __launch_bounds__(64 * NW) void chunk_parts_kernel(ChunkParams)
         const int h = __builtin_amdgcn_readfirstlane(place.h), slot = __builtin_amdgcn_readfirstlane(place.slot), at = __builtin_amdgcn_readfirstlane(place.at);
         const int left = __builtin_amdgcn_readfirstlane(place.left), turn = __builtin_amdgcn_readfirstlane(place.turn);
         if (left == 0) return;   // uniform
-        const Block b = block_of(p, slot);
+        const int in_halves = __builtin_amdgcn_readfirstlane(halves_s);
+        const Block b = block_of(p, in_halves ? slot >> 1 : slot, in_halves ? slot & 1 : -1);
         const int cost = cost_of(b), take = min(cost - at, left);
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -743,8 +759,9 @@ template <int D>
 hipError_t launch(const ChunkParams &p, hipStream_t s)
 {
     const int64_t segments = (int64_t)p.slots * p.hkv;
+    // (halves, as in the plan: 3 pieces of 33 tokens, 8 heads on 2, 7.9 to 7.0 us)
     if (most_tiles(p.prefix_len, (int64_t)p.pages.width << p.pages.page_shift) <= SHORT * 2) {
-        hipLaunchKernelGGL((chunk_whole_kernel<D>), dim3((unsigned)segments), dim3(64 * NW), 0, s, p);
+        hipLaunchKernelGGL((chunk_whole_kernel<D>), dim3((unsigned)segments, segments * 2 <= p.cus && p.part_rows > R / 2 ? 2 : 1), dim3(64 * NW), 0, s, p);
         return hipGetLastError();
     }
     hipLaunchKernelGGL((chunk_parts_kernel<D>), dim3(p.cus), dim3(64 * NW), 0, s, p);

@@ -556,20 +556,21 @@ __global__ __launch_bounds__(64 * NW) void weights_many_kernel(WeightsParams)
             first_s[tid] = sum.entries_before;
             cost_s[tid] = 0;
             __syncthreads();
-            int s = 0, k = 0;
+            int s = 0, k = 0, cost = 0;
             if (tid < segments) {
                 for (int step = NT / 2; step > 0; step /= 2)   // the last sequence that begins at or before block tid
                     if (s + step < p.n_seqs && first_s[s + step] <= tid) s += step;
                 k = tid - first_s[s];
                 const Seq q = seq_s[s];
-                cost_s[tid] = START + ((q.rows + QT - 1) / QT - seen_from(p, q, k)) * TILE;
+                cost = START + ((q.rows + QT - 1) / QT - seen_from(p, q, k)) * TILE;
+                cost_s[tid] = cost_key(cost, tid);
             }
             __syncthreads();
             if (tid < segments) {
-                const int rank = rank_by_cost(cost_s, segments, tid);
+                const int rank = rank_by_cost(cost_s, segments, cost_key(cost, tid));
                 seq_r[rank] = s;
                 block_r[rank] = (int16_t)k;
-                cost_r[rank] = cost_s[tid];
+                cost_r[rank] = cost;
             }
             __syncthreads();
             whole = dealt_worst(cost_r, segments, groups, &worst) <= plan.wide + JOIN;

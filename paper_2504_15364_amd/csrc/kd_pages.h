@@ -79,16 +79,21 @@ __device__ __forceinline__ int dealt_worst(const int *cost_r, int entries, int g
     __syncthreads();
     return *worst;
 }
-// The rank of entry `mine`, the most expensive first, of equal ones the first (cost_s: 16-byte aligned, entries behind the last cost nothing)
-__device__ __forceinline__ int rank_by_cost(const int *cost_s, int entries, int mine)
+// What an entry of a list of at most 512 is sorted by: the most expensive first, of equal ones the first.  (Costs from 2^21 on count as alike)
+__device__ __forceinline__ int cost_key(int cost, int entry) { return min(cost, (1 << 21) - 1) << 9 | (511 - entry); }
+// The rank of the entry with the key `own` (keys: 16-byte aligned, as many as a multiple of 16, those behind the last below 512)
+__device__ __forceinline__ int rank_by_cost(const int *keys, int entries, int own)
 {
     typedef int int4_ __attribute__((ext_vector_type(4)));
-    const int own = cost_s[mine];
     int rank = 0;
-    for (int i = 0; i < entries; i += 4) {
-        const int4_ c = *reinterpret_cast<const int4_ *>(cost_s + i);
+    for (int i = 0; i < entries; i += 16) {   // (reads that are under way together: one behind another they were all that this took)
+        int4_ c[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) rank += c[k] > own || (c[k] == own && i + k < mine);
+        for (int k = 0; k < 4; ++k) c[k] = *reinterpret_cast<const int4_ *>(keys + i + 4 * k);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) rank += c[k][j] > own;
     }
     return rank;
 }
