@@ -9,7 +9,7 @@
 //                          the range of what is left, once more if needed, narrows the border down to 128 candidates that are ranked in pairs
 //                          (16 heads of 16384 rows: 4 us to load them, 4 to the border, 5 for the bits of what goes and the ranks, 3 for the list)
 //   more                   a radix select that reads weights and positions again in every pass
-// Few moves are made by the workgroup itself (a second launch took 4 us for one row of each of 512 heads), many by a second launch over the whole chip.
+// Few moves are made by the workgroup itself (see OWN_MOVES), many by a second launch over the whole chip.
 #include <algorithm>
 
 #include "kd_device.h"
@@ -76,7 +76,9 @@ __device__ __forceinline__ void move_rows(const BranchEvictParams &p, Moves move
     }
 }
 
-constexpr int OWN_MOVES = 128;   // moves that the workgroup of a head makes itself
+// Moves that the workgroup of a head makes itself: a launch that finds none takes 2 us, one that makes a few 4 (8 heads of 3000 rows: 32 moves 10.7 | 13.3,
+// 100 12.3 | 13.1, 300 14.1 | 13.7, 500 16.9 | 13.9; 512 heads: 100 17.8 | 21.6, 500 30.2 | 33.7)
+constexpr int OWN_MOVES = 256;
 constexpr int BINS = 2048, CANDIDATES = 128;
 constexpr uint32_t ZERO = 0x80000000u;   // ordered(0)
 
@@ -86,11 +88,15 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
     constexpr int WAVES = NT / 64, WORDS = ROWS / 64;   // words of 64 rows
     // of every row: it goes ahead of another if its key is lower, or its `low` at equal keys, or its row higher at equal both
     __shared__ uint32_t key_s[ROWS], low_s[ROWS];
-    __shared__ uint32_t hist[BINS], wave_tot[WAVES], words[WORDS + 1], found[4], counted, best[4][WAVES], range_s[2][WAVES];
+    __shared__ __attribute__((aligned(16))) uint32_t hist[BINS];
+    __shared__ uint32_t wave_tot[WAVES], words[WORDS + 1], found[4], counted, best[4][WAVES], range_s[2][WAVES];
     __shared__ uint64_t out_s[WORDS];   // a bit for every row that goes
-    __shared__ uint64_t cand[CANDIDATES];
-    __shared__ int cand_row[CANDIDATES], cand_rank[CANDIDATES], page_s[ROWS / 8];
-    __shared__ Move list[OWN_MOVES];
+    __shared__ int page_s[ROWS / 8];
+    // in the place of the histogram once the border is found (two workgroups of 8192 rows share a compute unit that way)
+    Move *const list = reinterpret_cast<Move *>(hist);
+    uint64_t *const cand = reinterpret_cast<uint64_t *>(list + OWN_MOVES);
+    int *const cand_row = reinterpret_cast<int *>(cand + CANDIDATES), *const cand_rank = cand_row + CANDIDATES;
+    static_assert(OWN_MOVES * sizeof(Move) + CANDIDATES * 16 <= sizeof hist, "");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int s = p.by_hkv.divide(blockIdx.x), h = (int)blockIdx.x - s * p.hkv;
     const int len = table_entry(p.pages.lens, s), fresh = new_rows(len, asked_rows(p.pages, p.Bt, s), p.Bt), pos0 = p.pos0 ? table_entry(p.pos0, s) : 0;
@@ -211,11 +217,6 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
     };
     for (int i = tid; i < BINS; i += NT) hist[i] = 0;
     for (int i = tid; i < WORDS; i += NT) words[i] = 0;
-    for (int i = tid; i < CANDIDATES; i += NT) {   // (places without a candidate go behind all)
-        cand[i] = ~0ull;
-        cand_row[i] = -1;
-        cand_rank[i] = 0;
-    }
     if (tid == 0) counted = 0;
     if (lane == 0) best[3][wave] = absent;
     uint32_t inner_lo = above_lo, inner_hi = (uint32_t)max(above_hi, 0);
@@ -306,6 +307,12 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
         inner_lo = lo;
         inner_hi = hi;
     }
+    for (int i = tid; i < CANDIDATES; i += NT) {   // (places without a candidate go behind all)
+        cand[i] = ~0ull;
+        cand_row[i] = -1;
+        cand_rank[i] = 0;
+    }
+    __syncthreads();
     const bool whole = count == (uint32_t)need;   // uniform
     // numbers in `words` become those of all words before, the last one their sum
     auto add_up = [&]() {
@@ -541,6 +548,8 @@ hipError_t launch_branch_evict(BranchEvictParams p, hipStream_t s)
     const unsigned heads = (unsigned)(p.n_seqs * p.hkv);
     const int64_t rows = (int64_t)p.pages.width << p.pages.page_shift;
     const bool in_lds = rows <= 16384;
+    // (the LDS and the threads of a workgroup by the rows that a table can name: one row of each of 512 heads of 1000 rows goes in 5.1 us by the first kernel,
+    // 7.8, 10.9 and 12.1 by the others; of 4000 rows in 7.5 by the second, 12.1 and 13.6; of 8000 in 13.0 and 16.5)
     if (rows <= 1024) hipLaunchKernelGGL((evict_select_kernel<256, 1024>), dim3(heads), dim3(256), 0, s, p);
     else if (rows <= 4096) hipLaunchKernelGGL((evict_select_kernel<512, 4096>), dim3(heads), dim3(512), 0, s, p);
     else if (rows <= 8192) hipLaunchKernelGGL((evict_select_kernel<1024, 8192>), dim3(heads), dim3(1024), 0, s, p);

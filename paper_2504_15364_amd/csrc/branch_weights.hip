@@ -674,6 +674,8 @@ __global__ __launch_bounds__(KB) void weights_join_kernel(WeightsParams p)
     *wp = (r < sq.len && p.decay != 0.f ? p.decay * *wp : 0.f) + sum;
 }
 
+// (8 KV heads of 128, us, few | many: 32 query rows, 1 sequence of 8000 rows 6.6 | 9.7, 8 of 4000 16.3 | 23.6, 64 of 4000 110 | 154; 4 query rows 5.6 | 9.9,
+// 14.4 | 24.3 and 107 | 157)
 bool few(int G, int observe) { return (int64_t)G * observe <= 32; }
 
 template <int D>
