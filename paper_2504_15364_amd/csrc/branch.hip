@@ -886,8 +886,9 @@ __global__ __launch_bounds__(64 * NW) void branch_main_kernel(BranchParams p)
 
 // The join of a row's pieces: `groups` groups of D / 4 threads take a row's pieces in turn, four at a time, and join what they have
 // in LDS.  (Groups: where there are few rows and many pieces, the pieces requested one behind another were all the time this took: one
-// sequence, 8192 shared rows, 17.7 us with one group a row.)
-template <int D, int RS, int RO>
+// sequence, 8192 shared rows, 17.7 us with one group a row.)  LSE: the logarithms of the weight sums too (a test of the pointer in the kernel alone took
+// 0.3 us of the calls without)
+template <int D, int RS, int RO, bool LSE>
 __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int wgs, int groups)
 {
     constexpr int TPR = D / 4, BATCH = 4;
@@ -959,7 +960,7 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
         if (group != 0) return;
         float top = -INFINITY;
         for (int k = 0; k < groups; ++k) top = fmaxf(top, ml_s[unit + k].x);
-        mx = top;
+        if (LSE) mx = top;
         acc = f32x4{0.f, 0.f, 0.f, 0.f};
         L = 0.f;
         for (int k = 0; k < groups; ++k) {
@@ -975,12 +976,12 @@ __global__ __launch_bounds__(256) void branch_merge_kernel(BranchParams p, int w
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = (__bf16)(acc[i] * inv);
     *reinterpret_cast<bf16x4 *>(p.out + (((size_t)s * p.hkv + h) * Mt + m) * D + d0) = o;
-    if (p.lse && d0 == 0) p.lse[((size_t)s * p.hkv + h) * Mt + m] = log_sum(mx, L);
+    if (LSE && d0 == 0) p.lse[((size_t)s * p.hkv + h) * Mt + m] = log_sum(mx, L);
 }
 
 // Few rows: one launch, a workgroup for every (sequence, head, block of rows), whose waves take tiles of the prompt's and of the own rows in
 // turn and join their results in LDS; no partials, no plan and no second launch.
-template <int D, int RO>
+template <int D, int RO, bool LSE>
 __global__ __launch_bounds__(64 * NW) void branch_short_kernel(BranchParams p)
 {
     constexpr int CB = RO / 16, NC = D / 32, NDB = D / 16, UPR = D / 8, ROWB = D * 2, RPL = 64 / UPR, NV = TK / RPL;
@@ -1092,7 +1093,7 @@ __global__ __launch_bounds__(64 * NW) void branch_short_kernel(BranchParams p)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = (__bf16)acc[i];
             *reinterpret_cast<bf16x4 *>(p.out + ((size_t)sh * Mt + m) * D + d0) = o;
-            if (p.lse && d0 == 0) p.lse[(size_t)sh * Mt + m] = log_sum(mx, L);
+            if (LSE && d0 == 0) p.lse[(size_t)sh * Mt + m] = log_sum(mx, L);
         });
     }
 }
@@ -1190,7 +1191,9 @@ hipError_t launch_both(const BranchParams &p, hipStream_t s)
     hipLaunchKernelGGL((branch_main_kernel<D, RS, RO>), dim3(wgs), dim3(64 * NW), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((branch_merge_kernel<D, RS, RO>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, s, p, wgs, groups);
+    const dim3 grid((unsigned)((rows + per - 1) / per));
+    if (p.lse) hipLaunchKernelGGL((branch_merge_kernel<D, RS, RO, true>), grid, dim3(256), 0, s, p, wgs, groups);
+    else hipLaunchKernelGGL((branch_merge_kernel<D, RS, RO, false>), grid, dim3(256), 0, s, p, wgs, groups);
     return hipGetLastError();
 }
 
@@ -1209,7 +1212,9 @@ hipError_t launch(BranchParams p, hipStream_t s)
     p.by_fan.set(std::max(p.fan, 1));
     p.by_own_blocks.set((uint32_t)blocks);
     if (one_launch<D, RO>(p, block)) {
-        hipLaunchKernelGGL((branch_short_kernel<D, RO>), dim3((unsigned)(p.n_seqs * p.hkv * blocks)), dim3(64 * NW), 0, s, p);
+        const dim3 grid((unsigned)(p.n_seqs * p.hkv * blocks));
+        if (p.lse) hipLaunchKernelGGL((branch_short_kernel<D, RO, true>), grid, dim3(64 * NW), 0, s, p);
+        else hipLaunchKernelGGL((branch_short_kernel<D, RO, false>), grid, dim3(64 * NW), 0, s, p);
         return hipGetLastError();
     }
     switch (block.rows) {

@@ -76,7 +76,6 @@ struct Divisor {
 struct BranchParams {
     Rows q;
     uint16_t *out;                        // [n_seqs][hq][Bt][D]
-    float *lse;                           // nullable, [n_seqs][hq][Bt]: logarithms of the weight sums
     const uint16_t *k_prefix, *v_prefix;  // [n_prefixes][hkv][prefix_cap][D]
     Pages pages;
     float *part_o;                        // partial outputs, each normalised by its weight sum: slot by slot
@@ -89,6 +88,7 @@ struct BranchParams {
     float scale_log2e;
     int32_t shared_segs;                  // (prompt, head, block of rows) segments of the shared part; 0: there is none
     Divisor by_segs, by_heads, by_hkv, by_Mt, by_Bt, by_fan, by_own_blocks;   // heads: n_prefixes hkv; Mt: G Bt
+    float *lse;                           // nullable, [n_seqs][hq][Bt]: logarithms of the weight sums
 };
 constexpr int BRANCH_PLAN_WORDS = 8;
 size_t branch_workspace(int n_seqs, int n_prefixes, int hkv, int G, int Bt, int D, int cus, size_t *off_ml, size_t *off_plan);
