@@ -105,7 +105,7 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(BranchEvictParams p)
     const Head head{p.pages.table + (int64_t)s * p.pages.width, p.pages.page_shift, p.hkv, h};
     if (tid == 0) p.counts[blockIdx.x] = 0;
     if (len < 0 || all <= p.budget) {   // uniform: nothing to evict, the new rows' positions alone
-        for (int r = len + tid; len >= 0 && r < n; r += NT)
+        for (int r = len >= 0 && len < n ? len + tid : n; r < n; r += NT)   // (a length from far behind the table on would wrap)
             if ((uint32_t)table_entry(head.table, r >> head.shift) < (uint32_t)p.pages.n_pages) p.positions[head.at(r)] = (int32_t)((uint32_t)pos0 + (uint32_t)r);
         return;
     }
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(LNT) void evict_select_long_kernel(BranchEvictParam
     const int n = rows_with(p.pages, len, fresh), pos0 = p.pos0 ? table_entry(p.pos0, s) : 0;
     const Head head{p.pages.table + (int64_t)s * p.pages.width, p.pages.page_shift, p.hkv, h};
     auto exists = [&](int r) { return (uint32_t)table_entry(head.table, r >> head.shift) < (uint32_t)p.pages.n_pages; };
-    for (int r = len + tid; r < n; r += LNT)
+    for (int r = len < n ? len + tid : n; r < n; r += LNT)   // (a length from far behind the table on would wrap)
         if (exists(r)) p.positions[head.at(r)] = (int32_t)((uint32_t)pos0 + (uint32_t)r);
     if (all <= p.budget) return;   // uniform, as all that follows
     bool absent = all > n;

@@ -298,6 +298,28 @@ def test_positions_that_make_no_sense_do_no_harm():
         same((k, v, w, p), want)
 
 
+@pytest.mark.parametrize("L", [900, 20000])
+@pytest.mark.parametrize("length", [2 ** 31 - 1, 2 ** 31 - 100, 2 ** 30])
+def test_lengths_far_behind_the_table(L, length):
+    # rows that no table can name: the sequence is left as it was, whether its length is within the budget or not
+    hkv, d, page = 2, 64, 16
+    g = gen(79)
+    k, v, w, p, table = evict_case(hkv, d, page, [L], [5], 0, g, spread, [0])
+    before = [x.clone() for x in (k, v, w, p)]
+    for budget, bits in ((2 ** 31 - 1, kd.LEFT_OUT_ROW if length + 5 > 2 ** 31 - 1 else 0), (700, kd.LEFT_OUT_ROW)):
+        status = ints([0])
+        kd.branch_evict(k, v, w, p, table, ints([length]), budget, Bt=5, status=status)
+        assert status.tolist() == [bits]
+        same((k, v, w, p), before)
+        gathered = w.clone()
+        kd.branch_weights(torch.zeros((1, hkv, 5, d), dtype=torch.bfloat16, device="cuda"), k, gathered, table, ints([length]),
+                          torch.full((1, hkv, 5), float("-inf"), device="cuda"))
+        same((gathered,), (w,))
+    q = torch.randn((1, 4, 90, d), **g).bfloat16()   # ... and it sees all rows of the table
+    got, want = (kd.branch_chunk_attention(q, k, v, table, ints([x])) for x in (length, table.shape[1] * page))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and bool(torch.isfinite(want[1]).all())
+
+
 def test_sequences_with_rows_on_absent_pages_are_left_out():
     hkv, d, page, budget = 2, 64, 8, 60
     lens = [100, 100, 100, 20]
