@@ -666,25 +666,32 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkParams p)
     const int pieces = cut.pieces, first = cut.first;
     const int lane = threadIdx.x & 63, l32 = lane & 31, hh = lane >> 5, quarter = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     constexpr int SLABS = D / 16, MINE = SLABS / 4, BATCH = 8;
+    __shared__ f32x4 ml_s[BATCH][32];   // what is known of the rows of a batch's pieces: a wave asks for two of them
     float top = -INFINITY, L = 0.f;
     int power = -126;   // of the sums so far; of a piece's rows it is the third number beside the reference and the weight sum
     float acc[MINE][8] = {};
     for (int k0 = 0; k0 < pieces; k0 += BATCH) {
-        f32x4 ml[BATCH];
+        auto slot_of = [&](int k) { return k == 0 ? (int64_t)first : (first & ~1) + 2 * (int64_t)k; };
+        f32x4 ml[BATCH], two = {-INFINITY, 0.f, __int_as_float(-126), 0.f};
+        const int own = k0 + 2 * quarter + hh;
+        if (own < pieces) two = p.part_ml[slot_of(own) * p.part_rows + 32 * wave + l32];
         f16x8 o[BATCH][MINE];
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
-            ml[k] = f32x4{-INFINITY, 0.f, __int_as_float(-126), 0.f};
 #pragma unroll
             for (int c = 0; c < MINE; ++c) o[k][c] = f16x8{};
             if (k0 + k < pieces) {   // uniform
-                const int64_t at = k0 + k == 0 ? first : (first & ~1) + 2 * (int64_t)(k0 + k);
-                ml[k] = p.part_ml[at * p.part_rows + 32 * wave + l32];
+                const int64_t at = slot_of(k0 + k);
 #pragma unroll
                 for (int c = 0; c < MINE; ++c)
                     o[k][c] = *reinterpret_cast<const f16x8 *>(p.part_o + (((at * per + wave) * SLABS + quarter * MINE + c) * 64 + lane) * 8);
             }
         }
+        if (k0 > 0) __syncthreads();
+        ml_s[2 * quarter + hh][l32] = two;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) ml[k] = ml_s[k][l32];
         float high = top;
         int most = power;
 #pragma unroll
