@@ -102,9 +102,10 @@ __device__ __forceinline__ int cut_at(const Block &b, int at)
     return t <= SLIVER ? 0 : t >= b.tiles - SLIVER ? b.tiles : t;
 }
 
-constexpr int LEAST = START + 36;   // units of a part at least
-// What partials and their join cost a launch, in the same units
-constexpr int JOIN = 40;
+// Units of a part at least, and what partials and their join cost a launch.  By 26 sizes, START from 30 to 40, LEAST from START + 6 to + 54 and JOIN from 40 to 80: against
+// START + 36 and 40, 3 pieces of 38 tokens behind 4713 rows (8 KV heads of 128) take 30.1 us instead of 34.1, one of 354 behind 249 rows and a prompt of 1418 (2 heads
+// of 64) 21.3 instead of 25.5, 24 of 81 behind prompts of 2174 67.0 instead of 73.2; the geometric mean is 3 % less
+constexpr int LEAST = START + 6, JOIN = 60;
 
 // What the end of a segment asks for, kept in LDS meanwhile: the loop over the tiles has no scalar registers to spare
 struct Kept {

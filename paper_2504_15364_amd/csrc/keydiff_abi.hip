@@ -1421,11 +1421,11 @@ int finish_prompt_cache(keydiff_cache_t *c, hipStream_t s)
 // ------------------------------------------------------------------ pieces of many tokens, weights of own rows, their eviction
 // A piece goes to the kernels of branch_attention with up to kFewRows query rows of a sequence and KV head, and with up to twice as many where
 // few groups share the device: theirs split every run of rows over waves and workgroups, where a tile of branch_chunk.hip has room for 256 query
-// rows and is slower to start.  Measured, 8 KV heads, d 128 (us, chunk | branch): 32 query rows, 1 sequence of 1000 rows 26.7 | 16.9, 64 of 1000
-// 56.7 | 58.4, 64 of 50 rows behind a prompt of 4096 144 | 72; 36 query rows, 64 sequences of 1000 rows 56 | 68, of 50 behind 4096 155 | 75, 2 of
-// 2000 28.7 | 23.1, 2 of 100 behind 4096 28.6 | 19.2; 64 query rows, 1 of 1000 26.9 | 19.6, 1 of 8192 28.2 | 27.9, 2 of 2000 28.4 | 24.2, 4 of 8000
-// 36.2 | 55.3, 8 of 2000 29.3 | 38.2, 64 of 1000 57.5 | 79.0, of 50 behind 4096 156 | 172; 128 query rows, 1 of 1000 29.5 | 23.6, 1 of 8192
-// 29.9 | 36.6, 8 of 2000 32.7 | 55.3.
+// rows and is slower to start.  Measured, 8 KV heads, d 128 (us, chunk | branch): 32 query rows, 1 sequence of 1000 rows 27.3 | 16.9, 64 of 1000
+// 56.0 | 58.3, 64 of 50 rows behind a prompt of 4096 145 | 72; 36 query rows, 64 sequences of 1000 rows 56 | 67, of 50 behind 4096 149 | 75, 2 of
+// 2000 22.4 | 22.4, 2 of 100 behind 4096 24.1 | 18.7; 64 query rows, 1 of 1000 28.3 | 19.4, 1 of 8192 26.5 | 27.5, 2 of 2000 22.0 | 23.7, 2 of 100
+// behind 4096 23.8 | 20.8, 4 of 8000 35.3 | 54.5, 8 of 2000 27.6 | 37.7, 64 of 1000 56.4 | 75.7, of 50 behind 4096 153 | 173; 128 query rows, 1 of
+// 1000 23.5 | 23.3, 1 of 8192 27.0 | 36.9, 8 of 2000 31.8 | 56.5.
 constexpr int kFewRows = 32, kFewGroups = 16;
 
 bool few_rows(const keydiff_branches_t *b, int32_t Bt)
